@@ -67,7 +67,8 @@ typedef enum {
   CADDTREE_E_HIP = 5           /* a HIP runtime call or kernel launch failed */
 } caddtree_status_t;
 
-typedef enum { CADDTREE_F32 = 0, CADDTREE_BF16 = 1 } caddtree_dtype_t;
+/* Logits are F32 or BF16; the attention operators below take BF16 or F16. */
+typedef enum { CADDTREE_F32 = 0, CADDTREE_BF16 = 1, CADDTREE_F16 = 2 } caddtree_dtype_t;
 
 /* Tree-attention mask format.  U8: [B, cap, cap] bytes, mask[b][i][j] = 1 iff
  * node j is node i or an ancestor of i.  BITS32: [B, cap, ceil(cap/32)] u32
@@ -268,6 +269,148 @@ caddtree_status_t caddtree_accept(caddtree_plan_t plan, const int32_t* topk_ids,
  * bad input and E_UNSUPPORTED if the iteration does not settle. */
 caddtree_status_t caddtree_fit_cost(const double* x_host, const double* y_host, int64_t N, double* fit_host,
                                     int32_t cap, double* table_host);
+
+/* ------------------------------------------------------------------------------------------------
+ * Verification: the target's attention over a built tree, and the 4-bit cache it reads.
+ *
+ * After a build the target verifies the tree (Sec. 3.1, 3.3): the bonus token (the root) and the n_star
+ * nodes are its queries, and each sees the cached context, the root, its ancestors and itself.  These
+ * calls are that attention, the cache of keys and values in 4 bits behind it, the attention of a
+ * prompt or of single tokens through a sliding window, and a cache's eviction by accumulated attention
+ * weight.  They take no plan; they run on the current device, with the conventions at the top of this
+ * file (asynchronous on `stream`, no allocation, arguments checked before anything is enqueued, fit for
+ * HIP graph capture).  Lengths and page tables are DEVICE arrays and so are not checked: the kernels
+ * clamp a length to what its buffer holds, and a page number outside the cache holds no key.
+ *
+ * Tensors of 16-bit elements are strided views [B, tokens, heads, head_dim]: element (b, t, h, d) at
+ * data + b stride_b + t stride_t + h stride_h + d (strides in elements).  data must be 16-byte aligned
+ * and the strides multiples of 8; inputs may overlap or repeat (stride 0).
+ *
+ * Visibility.  Query i at position pos_i sees the key at position pos_j if its order allows it and
+ *     window = 0  or  pos_i - pos_j < window  or  pos_j < sinks.
+ * An absent key never sees use: whatever its memory holds (NaN included) does not reach a result, and
+ * what a query does not see does not reach its row.  A query that sees no key gets zeros and
+ * lse = -inf.
+ *     s_ij = scale q_i . k_j       lse_i = log sum_visible exp(s_ij)       out_i = sum_visible exp(s_ij - lse_i) v_j
+ * Products are formed on 16-bit inputs and summed in fp32; the softmax is fp32; a weight is rounded to
+ * the inputs' type for its product with v. */
+typedef struct {
+  void* data;
+  int64_t stride_b, stride_t, stride_h;
+} caddtree_view_t;
+
+/* How the new keys (those given as tensors) are ordered for the queries. */
+typedef enum {
+  CADDTREE_ORDER_CHAIN = 0,  /* causal: pos_j <= pos_i */
+  CADDTREE_ORDER_BLOCK = 1,  /* every query sees every key (a block-diffusion drafter's block) */
+  CADDTREE_ORDER_TREE = 2    /* a draft tree's mask: query 0 is the root, query i node i - 1 */
+} caddtree_order_t;
+
+#define CADDTREE_PAGE 64     /* tokens of a cache page */
+#define CADDTREE_KV_BLOCK 32 /* channels that share a scale */
+
+/* A cache of keys and values in 4 bits: n_pages pages of CADDTREE_PAGE tokens, laid out
+ * [n_pages, n_kv_heads, CADDTREE_PAGE_BYTES(head_dim)].  The bytes of a page and head:
+ *     key codes [64, head_dim / 2], value codes [64, head_dim / 2],
+ *     key scales [64, head_dim / 32], value scales [64, head_dim / 32].
+ * A value is code x 2^(scale - 127): the code is a sign bit and one of 0 0.5 1 1.5 2 3 4 6 (E2M1), an
+ * even channel in the low half of its byte; the scale byte is a power of two for 32 channels, 255 for
+ * a block that holds a NaN or an infinity (all 32 of its values are then NaN).  Slot t of sequence b
+ * lives in page page_table[b, t / 64] at token t % 64.  `dtype` is the type of the keys and values
+ * written and of the queries: scales are kept where every value is a normal number of that type
+ * (exponents -125 .. 125 in BF16, -13 .. 13 in F16; larger values saturate, smaller ones round on that
+ * grid). */
+#define CADDTREE_PAGE_BYTES(head_dim) ((int64_t)68 * (head_dim))
+typedef struct {
+  caddtree_dtype_t dtype;   /* BF16 or F16 */
+  int32_t n_kv_heads;
+  int32_t head_dim;         /* 64 or 128 */
+  int64_t n_pages;
+  void* pages;              /* DEVICE, 256-byte aligned */
+} caddtree_cache_t;
+
+/* One attention call: queries, new keys and values, and for the cached form the sequences' pages. */
+typedef struct {
+  caddtree_dtype_t dtype;       /* BF16 or F16 */
+  int32_t B;                    /* sequences, 0 .. 65535 */
+  int32_t T;                    /* queries of a sequence at most */
+  int32_t S;                    /* keys of a sequence at most (window attention); T with a cache */
+  int32_t n_heads, n_kv_heads;  /* n_heads a multiple of n_kv_heads: query head h reads kv head h / (n_heads / n_kv_heads) */
+  int32_t head_dim;             /* 64 or 128 */
+  caddtree_view_t q, k, v, out; /* [B, T, n_heads, head_dim], [B, S, n_kv_heads, head_dim] twice, as q */
+  float* lse;                   /* [B, T, n_heads], optional */
+  const int32_t* q_len;         /* [B], optional (NULL: T).  With a tree: its nodes, n_star, to which the root is added */
+  const int32_t* k_len;         /* [B], optional (NULL: S); not used with a cache */
+  float scale;
+  int32_t window, sinks;        /* >= 0; window 0: no window */
+  caddtree_order_t order;
+  caddtree_mask_t mask_kind;    /* with ORDER_TREE: U8 or BITS32, as written by caddtree_build */
+  const void* mask;             /* [B, cap, cap] or [B, cap, ceil(cap / 32)] */
+  const int32_t* depth;         /* [B, cap] */
+  int32_t cap;                  /* of the plan that built the trees; T <= cap + 1 */
+  const int32_t* page_table;    /* [B, table_pages]; the cached form only, as the next two */
+  int32_t table_pages;
+  const int64_t* ctx_len;       /* [B] cached tokens */
+} caddtree_attention_t;
+
+/* Attention over the keys given, the queries being the last positions: query i of sequence b is at
+ * position k_len - q_len + i, key j at j.  ORDER_CHAIN or ORDER_BLOCK.  Rows i >= q_len of out and lse
+ * are left untouched.
+ * workspace: caddtree_attention_workspace_bytes(a) bytes, 256-byte aligned, let a call with few rows
+ * split its keys over the card; NULL (or fewer bytes) is accepted and keeps a row's keys in fewer parts. */
+caddtree_status_t caddtree_window_attention(const caddtree_attention_t* a, void* workspace, size_t workspace_bytes,
+                                            hipStream_t stream);
+
+/* Attention over the cached keys, slots 0 .. ctx_len - 1 at positions of the same numbers, followed by
+ * the new ones: key j at position ctx_len + j, in a tree at ctx_len + its depth (the root's is 0), and
+ * query i where key i is.  k and v may be NULL: the queries then see the cached keys alone.  The new
+ * keys are not written to the cache (caddtree_cache_write does that for those accepted). */
+caddtree_status_t caddtree_cache_attention(const caddtree_cache_t* cache, const caddtree_attention_t* a,
+                                           void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* HOST only: the workspace of the two calls above (0 where none is of use). */
+size_t caddtree_attention_workspace_bytes(const caddtree_attention_t* a);
+
+/* Puts the first count[b] (NULL: T) of T new tokens of each sequence into the slots from start[b] on,
+ * rounded to 4 bits.  Token j is k[b, j], or k[b, index[b, j]] where index [B, T] is given (the
+ * accepted path of a tree; an index outside 0 .. rows - 1 writes nothing).  Slots past the table's end,
+ * and pages outside the cache, are not written.  No two sequences may write one page's token.
+ *   Rounding: E = floor(log2 m) - 2 for the largest magnitude m of a block, one more where m is above
+ *   1.75 x 2^floor(log2 m) (8 is then nearer than 6); each value to the nearest code, ties to the even one. */
+caddtree_status_t caddtree_cache_write(const caddtree_cache_t* cache, const caddtree_view_t* k, const caddtree_view_t* v,
+                                       int32_t B, int32_t T, int32_t rows, const int64_t* start, const int32_t* count,
+                                       const int32_t* index, const int32_t* page_table, int32_t table_pages,
+                                       hipStream_t stream);
+
+/* The values that slots start[b] (NULL: 0) .. end[b] - 1 stand for, at most T of them, in the cache's
+ * type: slot start + j into k[b, j] and v[b, j].  Rows past the end, and those of pages outside the
+ * cache, are left untouched. */
+caddtree_status_t caddtree_cache_read(const caddtree_cache_t* cache, const caddtree_view_t* k, const caddtree_view_t* v,
+                                      int32_t B, int32_t T, const int64_t* start, const int64_t* end,
+                                      const int32_t* page_table, int32_t table_pages, hipStream_t stream);
+
+/* Adds the attention weight that the cached keys get from a call's queries to their scores:
+ *     new_scores[b, h, p] = scores[b, h, p] + sum_i weight[b, i] sum_g visible exp(s_igp - lse[b, i, g])
+ * over the kv head's query heads g, for slots p < ctx_len; further slots are copied.  a: the arguments
+ * of the caddtree_cache_attention call (q, lse as it wrote it, lengths, scale, window, sinks, order;
+ * k, v, out and the mask are not used).  weight [B, T] (NULL: 1) picks and weighs queries; one at or
+ * below 0 leaves its query out.  scores, new_scores [B, n_kv_heads, slots], slots >= the longest
+ * ctx_len's, may be one array.  The order of the sums is fixed. */
+caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const caddtree_attention_t* a, const float* weight,
+                                       const float* scores, float* new_scores, int64_t slots, hipStream_t stream);
+
+/* Cuts each sequence to at most `budget` slots, by kv head: the first `sinks`, the last `recent`, and of
+ * the others those with the largest scores (ties: the lower slot; a NaN counts as the lowest), in their
+ * old order.  sinks + recent <= budget.
+ *   scores [B, n_kv_heads, slots]; new_table [B, new_pages]: pages for budget slots that are in none of
+ *   the tables in use (the old pages are free once the call is done); new_scores [B, n_kv_heads,
+ *   new_slots], new_slots >= budget: the kept slots' scores, then zeros; new_len [B] = min(ctx_len,
+ *   budget); kept [B, n_kv_heads, budget]: the old slots, then -1. */
+caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B, const int32_t* page_table,
+                                       int32_t table_pages, const int64_t* ctx_len, const float* scores, int64_t slots,
+                                       int32_t budget, int32_t sinks, int32_t recent, const int32_t* new_table,
+                                       int32_t new_pages, float* new_scores, int64_t new_slots, int64_t* new_len,
+                                       int32_t* kept, hipStream_t stream);
 
 const char* caddtree_status_string(caddtree_status_t status);
 const char* caddtree_last_error(void);

@@ -16,6 +16,9 @@ Context-aware cost (Sec. 4.6): pass ``t_verify`` as [J, cap + 1] tables with
 ``ctx_grid`` (J increasing context lengths) and give ``ctx_len`` (int64 [B],
 on the device) to ``build`` / ``expand``.  ``fixed_budget=True`` selects the
 fixed-budget (DDTree) construction: the top ``cap`` nodes, no stop rule.
+
+``KVCache`` and ``window_attention`` (attention.py) are the target's attention over the built trees: a
+cache of keys and values in 4 bits, read under the tree's mask, and its eviction.
 """
 
 from __future__ import annotations
@@ -28,8 +31,10 @@ import numpy as np
 
 from . import _lib
 from ._lib import CaddtreeError, MAX_CAP, MAX_CTX, MAX_K, MAX_L
+from .attention import KVCache, attention_workspace, window_attention
 
-__all__ = ["Plan", "TreeOutputs", "CaddtreeError", "fit_cost", "MAX_L", "MAX_K", "MAX_CAP", "MAX_CTX"]
+__all__ = ["Plan", "TreeOutputs", "KVCache", "window_attention", "attention_workspace", "CaddtreeError", "fit_cost",
+           "MAX_L", "MAX_K", "MAX_CAP", "MAX_CTX"]
 
 
 def _torch():

@@ -10,6 +10,9 @@ LIB_PATH = os.path.join(_HERE, "libcaddtree.so")
 
 OK, E_INVALID, E_UNSUPPORTED, E_COST, E_WORKSPACE, E_HIP = range(6)
 DTYPES = {"f32": 0, "bf16": 1}
+ATTENTION_DTYPES = {"bf16": 1, "f16": 2}
+ORDERS = {"chain": 0, "block": 1, "tree": 2}
+PAGE, KV_BLOCK = 64, 32
 MASKS = {"none": 0, "u8": 1, "bits": 2}
 ALLOW_NONCONVEX = 1
 FIXED_BUDGET = 2
@@ -45,11 +48,41 @@ class Outputs(ctypes.Structure):
         "mask", "pos_ids", "topk_ids", "topk_logit", "topk_lq", "lse")]
 
 
+class View(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64),
+                ("stride_h", ctypes.c_int64)]
+
+
+class Cache(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("n_kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("n_pages", ctypes.c_int64), ("pages", ctypes.c_void_p)]
+
+
+class Attention(ctypes.Structure):
+    _fields_ = [
+        ("dtype", ctypes.c_int),
+        *((n, ctypes.c_int32) for n in ("B", "T", "S", "n_heads", "n_kv_heads", "head_dim")),
+        *((n, View) for n in ("q", "k", "v", "out")),
+        *((n, ctypes.c_void_p) for n in ("lse", "q_len", "k_len")),
+        ("scale", ctypes.c_float),
+        *((n, ctypes.c_int32) for n in ("window", "sinks")),
+        ("order", ctypes.c_int),
+        ("mask_kind", ctypes.c_int),
+        *((n, ctypes.c_void_p) for n in ("mask", "depth")),
+        ("cap", ctypes.c_int32),
+        ("page_table", ctypes.c_void_p),
+        ("table_pages", ctypes.c_int32),
+        ("ctx_len", ctypes.c_void_p),
+    ]
+
+
 EXPORTS = [
     "caddtree_plan_create", "caddtree_plan_destroy", "caddtree_workspace_bytes", "caddtree_build",
     "caddtree_build_noalloc",
     "caddtree_reduce_topk", "caddtree_expand", "caddtree_emit", "caddtree_accept", "caddtree_fit_cost", "caddtree_status_string",
     "caddtree_last_error",
+    "caddtree_attention_workspace_bytes", "caddtree_window_attention", "caddtree_cache_attention",
+    "caddtree_cache_write", "caddtree_cache_read", "caddtree_cache_score", "caddtree_cache_evict",
 ]
 
 
@@ -85,6 +118,21 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.caddtree_accept.restype = ctypes.c_int
     lib.caddtree_fit_cost.argtypes = [vp, vp, i64, vp, i32, vp]
     lib.caddtree_fit_cost.restype = ctypes.c_int
+    ap, cp, wp = ctypes.POINTER(Attention), ctypes.POINTER(Cache), ctypes.POINTER(View)
+    lib.caddtree_attention_workspace_bytes.argtypes = [ap]
+    lib.caddtree_attention_workspace_bytes.restype = sz
+    lib.caddtree_window_attention.argtypes = [ap, vp, sz, vp]
+    lib.caddtree_window_attention.restype = ctypes.c_int
+    lib.caddtree_cache_attention.argtypes = [cp, ap, vp, sz, vp]
+    lib.caddtree_cache_attention.restype = ctypes.c_int
+    lib.caddtree_cache_write.argtypes = [cp, wp, wp, i32, i32, i32, vp, vp, vp, vp, i32, vp]
+    lib.caddtree_cache_write.restype = ctypes.c_int
+    lib.caddtree_cache_read.argtypes = [cp, wp, wp, i32, i32, vp, vp, vp, i32, vp]
+    lib.caddtree_cache_read.restype = ctypes.c_int
+    lib.caddtree_cache_score.argtypes = [cp, ap, vp, vp, vp, i64, vp]
+    lib.caddtree_cache_score.restype = ctypes.c_int
+    lib.caddtree_cache_evict.argtypes = [cp, i32, vp, i32, vp, vp, i64, i32, i32, i32, vp, i32, vp, i64, vp, vp, vp]
+    lib.caddtree_cache_evict.restype = ctypes.c_int
     lib.caddtree_status_string.argtypes = [ctypes.c_int]
     lib.caddtree_status_string.restype = ctypes.c_char_p
     lib.caddtree_last_error.argtypes = []

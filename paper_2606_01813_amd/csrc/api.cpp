@@ -3,13 +3,18 @@
 
 #include <algorithm>
 #include <cmath>
-#include <cstdarg>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
 #include <new>
 
 #include "internal.h"
+#include "status.h"
+
+using caddtree::enum_value;
+using caddtree::fail;
+using caddtree::hip_fail;
+using caddtree::ok;
 
 struct caddtree_plan {
   int32_t L;
@@ -40,37 +45,7 @@ struct caddtree_plan {
 
 namespace {
 
-thread_local char g_last_error[512];   // (a string could throw out of a C function)
-
-caddtree_status_t fail(caddtree_status_t st, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
-caddtree_status_t fail(caddtree_status_t st, const char* fmt, ...) {
-  va_list ap;
-  va_start(ap, fmt);
-  vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
-  va_end(ap);
-  return st;
-}
-
-caddtree_status_t ok() {
-  g_last_error[0] = '\0';
-  return CADDTREE_OK;
-}
-
-caddtree_status_t hip_fail(hipError_t e, const char* what) {
-  return fail(CADDTREE_E_HIP, "%s: %s (%d)", what, hipGetErrorString(e), (int)e);
-}
-
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// The value a C caller stored in an enum-typed field or argument, read as the int it is: a C
-// caller may pass any int there, which a C++ enum object must not hold.
-template <typename E>
-int enum_value(const E& e) {
-  static_assert(sizeof(E) == sizeof(int), "the C enums of the interface are int-sized");
-  int v;
-  std::memcpy(&v, &e, sizeof v);
-  return v;
-}
 
 caddtree_status_t check_plan(const caddtree_plan* p) {
   if (p == nullptr) return fail(CADDTREE_E_INVALID, "plan is NULL");
@@ -238,7 +213,7 @@ const char* caddtree_status_string(caddtree_status_t s) {
   return "unknown status";
 }
 
-const char* caddtree_last_error(void) { return g_last_error; }
+const char* caddtree_last_error(void) { return caddtree::g_last_error; }
 
 caddtree_status_t caddtree_plan_create(const caddtree_config_t* cfg, caddtree_plan_t* plan_out) {
   if (plan_out == nullptr) return fail(CADDTREE_E_INVALID, "plan_out is NULL");

@@ -1,0 +1,269 @@
+// Host side of the attention and cache calls declared in caddtree.h: argument checks and launches on the
+// caller's stream.
+
+#include <cmath>
+#include <cstdint>
+
+#include "attn_args.h"
+#include "status.h"
+
+using caddtree::enum_value;
+using caddtree::fail;
+using caddtree::hip_fail;
+using caddtree::ok;
+
+namespace {
+
+using caddtree::AttnArgs;
+using caddtree::PagedKV;
+using caddtree::View;
+
+constexpr int64_t kMaxTokens = (int64_t)1 << 30;   // positions, and the tokens of a table, stay within int32
+
+caddtree_status_t check_type(int dtype, int32_t head_dim) {
+  if (dtype == CADDTREE_F32) return fail(CADDTREE_E_UNSUPPORTED, "dtype F32 is not supported here: BF16 or F16");
+  if (dtype != CADDTREE_BF16 && dtype != CADDTREE_F16) return fail(CADDTREE_E_INVALID, "unknown dtype %d", dtype);
+  if (head_dim < 1) return fail(CADDTREE_E_INVALID, "head_dim = %d must be >= 1", head_dim);
+  if (head_dim != 64 && head_dim != 128)
+    return fail(CADDTREE_E_UNSUPPORTED, "head_dim = %d: only 64 and 128 are supported", head_dim);
+  return CADDTREE_OK;
+}
+
+caddtree_status_t check_view(const char* name, const caddtree_view_t& v, bool required) {
+  if (v.data == nullptr) return required ? fail(CADDTREE_E_INVALID, "%s is NULL", name) : CADDTREE_OK;
+  if (reinterpret_cast<uintptr_t>(v.data) % 16 != 0) return fail(CADDTREE_E_INVALID, "%s must be 16-byte aligned", name);
+  if (v.stride_b % 8 != 0 || v.stride_t % 8 != 0 || v.stride_h % 8 != 0)
+    return fail(CADDTREE_E_INVALID, "the strides of %s must be multiples of 8 elements", name);
+  return CADDTREE_OK;
+}
+
+caddtree_status_t check_cache(const caddtree_cache_t* c) {
+  if (c == nullptr) return fail(CADDTREE_E_INVALID, "cache is NULL");
+  const caddtree_status_t st = check_type(enum_value(c->dtype), c->head_dim);
+  if (st != CADDTREE_OK) return st;
+  if (c->n_kv_heads < 1 || c->n_kv_heads > 65535)
+    return fail(CADDTREE_E_INVALID, "n_kv_heads = %d must be in 1 .. 65535", c->n_kv_heads);
+  if (c->n_pages < 0 || c->n_pages > INT32_MAX)
+    return fail(CADDTREE_E_INVALID, "n_pages = %lld must be in 0 .. 2^31 - 1", (long long)c->n_pages);
+  if (c->pages == nullptr) return fail(CADDTREE_E_INVALID, "the cache's pages are NULL");
+  if (reinterpret_cast<uintptr_t>(c->pages) % 256 != 0)
+    return fail(CADDTREE_E_INVALID, "the cache's pages must be 256-byte aligned");
+  return CADDTREE_OK;
+}
+
+caddtree_status_t check_table(const char* name, const int32_t* table, int32_t pages) {
+  if (pages < 0 || (int64_t)pages * CADDTREE_PAGE > kMaxTokens)
+    return fail(CADDTREE_E_INVALID, "%s: %d pages a sequence, 0 .. 2^30 / %d are possible", name, pages, CADDTREE_PAGE);
+  if (table == nullptr && pages > 0) return fail(CADDTREE_E_INVALID, "%s is NULL", name);
+  return CADDTREE_OK;
+}
+
+caddtree_status_t check_batch(int32_t B) {
+  if (B < 0) return fail(CADDTREE_E_INVALID, "B = %d is negative", B);
+  if (B > 65535) return fail(CADDTREE_E_UNSUPPORTED, "B = %d exceeds 65535", B);
+  return CADDTREE_OK;
+}
+
+View view(const caddtree_view_t& v) { return View{static_cast<char*>(v.data), v.stride_b, v.stride_t, v.stride_h}; }
+
+PagedKV paged(const caddtree_cache_t* c, const int32_t* table, int32_t pages) {
+  return PagedKV{static_cast<uint8_t*>(c->pages), c->n_pages, table, pages, c->n_kv_heads,
+                 (int32_t)CADDTREE_PAGE_BYTES(c->head_dim)};
+}
+
+// What every attention call and the scores share; the tensors that a call reads are checked by it.
+caddtree_status_t check_attention(const caddtree_attention_t* a, const caddtree_cache_t* cache) {
+  if (a == nullptr) return fail(CADDTREE_E_INVALID, "the attention arguments are NULL");
+  caddtree_status_t st = check_type(enum_value(a->dtype), a->head_dim);
+  if (st != CADDTREE_OK) return st;
+  if ((st = check_batch(a->B)) != CADDTREE_OK) return st;
+  if (a->T < 0 || a->S < 0) return fail(CADDTREE_E_INVALID, "T = %d and S = %d must not be negative", a->T, a->S);
+  if (a->n_kv_heads < 1 || a->n_heads < 1 || a->n_heads % a->n_kv_heads != 0)
+    return fail(CADDTREE_E_INVALID, "n_heads = %d must be a positive multiple of n_kv_heads = %d", a->n_heads, a->n_kv_heads);
+  if (a->n_heads > 65535) return fail(CADDTREE_E_UNSUPPORTED, "n_heads = %d exceeds 65535", a->n_heads);
+  if (a->T > kMaxTokens || a->S > kMaxTokens || (int64_t)a->T * (a->n_heads / a->n_kv_heads) > kMaxTokens)
+    return fail(CADDTREE_E_UNSUPPORTED, "more than 2^30 tokens, or rows of a kv head, in a sequence");
+  if (!std::isfinite(a->scale)) return fail(CADDTREE_E_INVALID, "scale must be finite");
+  if (a->window < 0 || a->sinks < 0)
+    return fail(CADDTREE_E_INVALID, "window = %d and sinks = %d must not be negative", a->window, a->sinks);
+  const int order = enum_value(a->order), mask = enum_value(a->mask_kind);
+  if (order != CADDTREE_ORDER_CHAIN && order != CADDTREE_ORDER_BLOCK && order != CADDTREE_ORDER_TREE)
+    return fail(CADDTREE_E_INVALID, "unknown order %d", order);
+  if (order == CADDTREE_ORDER_TREE) {
+    if (cache == nullptr) return fail(CADDTREE_E_INVALID, "a tree's attention reads a cache");
+    if (mask != CADDTREE_MASK_NONE && mask != CADDTREE_MASK_U8 && mask != CADDTREE_MASK_BITS32)
+      return fail(CADDTREE_E_INVALID, "unknown mask kind %d", mask);
+    if (a->cap < 0 || a->cap > CADDTREE_MAX_CAP || a->T > a->cap + 1)
+      return fail(CADDTREE_E_INVALID, "T = %d queries do not fit a tree of cap = %d nodes and its root", a->T, a->cap);
+    if (a->T > 1 && a->depth == nullptr) return fail(CADDTREE_E_INVALID, "a tree needs depth");
+  }
+  if (cache != nullptr) {
+    if ((st = check_cache(cache)) != CADDTREE_OK) return st;
+    if (enum_value(cache->dtype) != enum_value(a->dtype) || cache->n_kv_heads != a->n_kv_heads ||
+        cache->head_dim != a->head_dim)
+      return fail(CADDTREE_E_INVALID, "the cache's dtype, n_kv_heads or head_dim is not the call's");
+    if ((st = check_table("page_table", a->page_table, a->table_pages)) != CADDTREE_OK) return st;
+    if (a->B > 0 && a->ctx_len == nullptr) return fail(CADDTREE_E_INVALID, "ctx_len is NULL");
+  }
+  return check_view("q", a->q, a->B > 0 && a->T > 0);
+}
+
+AttnArgs args_of(const caddtree_attention_t* a, const caddtree_cache_t* cache) {
+  AttnArgs k = {};
+  k.q = view(a->q);
+  k.k = view(a->k);
+  k.v = view(a->v);
+  k.out = view(a->out);
+  k.lse = a->lse;
+  k.q_len = a->q_len;
+  k.k_len = cache ? nullptr : a->k_len;
+  k.B = a->B;
+  k.T = a->T;
+  k.S = a->S;
+  k.Hq = a->n_heads;
+  k.Hkv = a->n_kv_heads;
+  k.G = a->n_heads / a->n_kv_heads;
+  k.scale = a->scale;
+  k.window = a->window;
+  k.sinks = a->sinks;
+  k.order = enum_value(a->order);
+  k.mask_kind = enum_value(a->mask_kind);
+  k.mask = a->mask;
+  k.depth = a->depth;
+  k.cap = a->cap;
+  if (cache) {
+    k.kv = paged(cache, a->page_table, a->table_pages);
+    k.ctx_len = a->ctx_len;
+  }
+  return k;
+}
+
+caddtree_status_t check_workspace(const void* workspace) {
+  if (reinterpret_cast<uintptr_t>(workspace) % 256 != 0)
+    return fail(CADDTREE_E_WORKSPACE, "workspace must be 256-byte aligned");
+  return CADDTREE_OK;
+}
+
+caddtree_status_t run_attention(const caddtree_attention_t* a, const caddtree_cache_t* cache, hipStream_t stream) {
+  if (a->B == 0 || a->T == 0) return ok();
+  const hipError_t e = caddtree::launch_attention(args_of(a, cache), (caddtree_dtype_t)enum_value(a->dtype), a->head_dim, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "attention launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t caddtree_attention_workspace_bytes(const caddtree_attention_t*) { return 0; }
+
+caddtree_status_t caddtree_window_attention(const caddtree_attention_t* a, void* workspace, size_t, hipStream_t stream) {
+  caddtree_status_t st = check_attention(a, nullptr);
+  if (st != CADDTREE_OK) return st;
+  const bool some = a->B > 0 && a->T > 0;
+  if ((st = check_view("k", a->k, some && a->S > 0)) != CADDTREE_OK) return st;
+  if ((st = check_view("v", a->v, some && a->S > 0)) != CADDTREE_OK) return st;
+  if ((st = check_view("out", a->out, some)) != CADDTREE_OK) return st;
+  if ((st = check_workspace(workspace)) != CADDTREE_OK) return st;
+  return run_attention(a, nullptr, stream);
+}
+
+caddtree_status_t caddtree_cache_attention(const caddtree_cache_t* cache, const caddtree_attention_t* a, void* workspace,
+                                           size_t, hipStream_t stream) {
+  if (cache == nullptr) return fail(CADDTREE_E_INVALID, "cache is NULL");
+  caddtree_status_t st = check_attention(a, cache);
+  if (st != CADDTREE_OK) return st;
+  if ((st = check_view("k", a->k, false)) != CADDTREE_OK) return st;
+  if ((st = check_view("v", a->v, a->k.data != nullptr)) != CADDTREE_OK) return st;
+  if (a->v.data != nullptr && a->k.data == nullptr) return fail(CADDTREE_E_INVALID, "v is given without k");
+  if ((st = check_view("out", a->out, a->B > 0 && a->T > 0)) != CADDTREE_OK) return st;
+  if (enum_value(a->order) == CADDTREE_ORDER_TREE && a->k.data != nullptr && a->T > 1 &&
+      (a->mask == nullptr || enum_value(a->mask_kind) == CADDTREE_MASK_NONE))
+    return fail(CADDTREE_E_INVALID, "a tree's new keys need its mask");
+  if ((st = check_workspace(workspace)) != CADDTREE_OK) return st;
+  return run_attention(a, cache, stream);
+}
+
+caddtree_status_t caddtree_cache_write(const caddtree_cache_t* cache, const caddtree_view_t* k, const caddtree_view_t* v,
+                                       int32_t B, int32_t T, int32_t rows, const int64_t* start, const int32_t* count,
+                                       const int32_t* index, const int32_t* page_table, int32_t table_pages,
+                                       hipStream_t stream) {
+  caddtree_status_t st = check_cache(cache);
+  if (st != CADDTREE_OK) return st;
+  if ((st = check_batch(B)) != CADDTREE_OK) return st;
+  if (T < 0 || rows < 0) return fail(CADDTREE_E_INVALID, "T = %d and rows = %d must not be negative", T, rows);
+  if (T > kMaxTokens) return fail(CADDTREE_E_UNSUPPORTED, "T = %d exceeds 2^30", T);
+  if (index == nullptr && rows < T) return fail(CADDTREE_E_INVALID, "rows = %d hold fewer than T = %d tokens", rows, T);
+  if (k == nullptr || v == nullptr) return fail(CADDTREE_E_INVALID, "k and v are required");
+  if ((st = check_table("page_table", page_table, table_pages)) != CADDTREE_OK) return st;
+  const bool some = B > 0 && T > 0 && table_pages > 0;
+  if ((st = check_view("k", *k, some)) != CADDTREE_OK) return st;
+  if ((st = check_view("v", *v, some)) != CADDTREE_OK) return st;
+  if (B > 0 && start == nullptr) return fail(CADDTREE_E_INVALID, "start is NULL");
+  if (!some) return ok();
+  caddtree::CacheMoveArgs a = {view(*k), view(*v), paged(cache, page_table, table_pages), start, nullptr, count, index, B, T, rows};
+  const hipError_t e = caddtree::launch_cache_write(a, (caddtree_dtype_t)enum_value(cache->dtype), cache->head_dim, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "cache write launch");
+}
+
+caddtree_status_t caddtree_cache_read(const caddtree_cache_t* cache, const caddtree_view_t* k, const caddtree_view_t* v,
+                                      int32_t B, int32_t T, const int64_t* start, const int64_t* end,
+                                      const int32_t* page_table, int32_t table_pages, hipStream_t stream) {
+  caddtree_status_t st = check_cache(cache);
+  if (st != CADDTREE_OK) return st;
+  if ((st = check_batch(B)) != CADDTREE_OK) return st;
+  if (T < 0) return fail(CADDTREE_E_INVALID, "T = %d must not be negative", T);
+  if (T > kMaxTokens) return fail(CADDTREE_E_UNSUPPORTED, "T = %d exceeds 2^30", T);
+  if (k == nullptr || v == nullptr) return fail(CADDTREE_E_INVALID, "k and v are required");
+  if ((st = check_table("page_table", page_table, table_pages)) != CADDTREE_OK) return st;
+  const bool some = B > 0 && T > 0 && table_pages > 0;
+  if ((st = check_view("k", *k, some)) != CADDTREE_OK) return st;
+  if ((st = check_view("v", *v, some)) != CADDTREE_OK) return st;
+  if (B > 0 && end == nullptr) return fail(CADDTREE_E_INVALID, "end is NULL");
+  if (!some) return ok();
+  caddtree::CacheMoveArgs a = {view(*k), view(*v), paged(cache, page_table, table_pages), start, end, nullptr, nullptr, B, T, T};
+  const hipError_t e = caddtree::launch_cache_read(a, (caddtree_dtype_t)enum_value(cache->dtype), cache->head_dim, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "cache read launch");
+}
+
+caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const caddtree_attention_t* a, const float* weight,
+                                       const float* scores, float* new_scores, int64_t slots, hipStream_t stream) {
+  if (cache == nullptr) return fail(CADDTREE_E_INVALID, "cache is NULL");
+  caddtree_status_t st = check_attention(a, cache);
+  if (st != CADDTREE_OK) return st;
+  if (slots < 0 || slots > kMaxTokens) return fail(CADDTREE_E_INVALID, "slots = %lld must be in 0 .. 2^30", (long long)slots);
+  if (a->B == 0 || slots == 0) return ok();
+  if (a->T > 0 && a->lse == nullptr) return fail(CADDTREE_E_INVALID, "lse is NULL");
+  if (scores == nullptr || new_scores == nullptr) return fail(CADDTREE_E_INVALID, "scores and new_scores are required");
+  caddtree::ScoreArgs s = {args_of(a, cache), weight, scores, new_scores, slots};
+  const hipError_t e = caddtree::launch_cache_score(s, (caddtree_dtype_t)enum_value(a->dtype), a->head_dim, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "cache score launch");
+}
+
+caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B, const int32_t* page_table,
+                                       int32_t table_pages, const int64_t* ctx_len, const float* scores, int64_t slots,
+                                       int32_t budget, int32_t sinks, int32_t recent, const int32_t* new_table,
+                                       int32_t new_pages, float* new_scores, int64_t new_slots, int64_t* new_len,
+                                       int32_t* kept, hipStream_t stream) {
+  caddtree_status_t st = check_cache(cache);
+  if (st != CADDTREE_OK) return st;
+  if ((st = check_batch(B)) != CADDTREE_OK) return st;
+  if ((st = check_table("page_table", page_table, table_pages)) != CADDTREE_OK) return st;
+  if ((st = check_table("new_table", new_table, new_pages)) != CADDTREE_OK) return st;
+  if (budget < 0 || sinks < 0 || recent < 0 || (int64_t)sinks + recent > budget)
+    return fail(CADDTREE_E_INVALID, "sinks = %d and recent = %d must not be negative and must fit budget = %d", sinks, recent, budget);
+  if (slots < 0 || slots > kMaxTokens || new_slots < budget || new_slots > kMaxTokens)
+    return fail(CADDTREE_E_INVALID, "slots = %lld must be in 0 .. 2^30 and new_slots = %lld in budget = %d .. 2^30",
+                (long long)slots, (long long)new_slots, budget);
+  if ((int64_t)new_pages * CADDTREE_PAGE < budget)
+    return fail(CADDTREE_E_INVALID, "new_table's %d pages hold fewer than budget = %d slots", new_pages, budget);
+  if (B == 0) return ok();
+  if (ctx_len == nullptr || new_len == nullptr) return fail(CADDTREE_E_INVALID, "ctx_len and new_len are required");
+  if ((slots > 0 && scores == nullptr) || (new_slots > 0 && new_scores == nullptr) || (budget > 0 && kept == nullptr))
+    return fail(CADDTREE_E_INVALID, "scores, new_scores and kept are required");
+  caddtree::EvictArgs a = {paged(cache, page_table, table_pages), B, cache->head_dim, ctx_len, scores, slots, budget, sinks,
+                           recent, new_table, new_pages, new_scores, new_slots, new_len, kept};
+  const hipError_t e = caddtree::launch_cache_evict(a, stream);
+  return e == hipSuccess ? ok() : hip_fail(e, "cache evict launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,611 @@
+"""The verification operators against their definitions in fp64 (GPU): windowed attention, the 4-bit cache's
+write, read and attention under chains, blocks and tree masks, accumulated weights and eviction.
+
+Unused memory is filled with NaN throughout: rows past a length, slots past ctx_len (scale bytes of 255),
+mask words past a tree's nodes (random bits).  None of it may reach a result.  The error bounds are derived
+in _attention_ref.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_01813_amd import KVCache, Plan, attention_workspace, window_attention
+from tests import _attention_ref as ref
+from tests._parity import say
+
+pytestmark = pytest.mark.gpu
+BF, F16 = torch.bfloat16, torch.float16
+
+
+def make(shape, dtype, seed, order="bthd", scale=1.0):
+    g = torch.Generator().manual_seed(seed)
+    x = (torch.randn(shape, generator=g) * scale).to(dtype).cuda()
+    if order == "bhtd":                                   # heads outermost in memory
+        return x.transpose(1, 2).contiguous().transpose(1, 2)
+    if order == "wide":                                   # rows of a wider buffer
+        big = torch.full((shape[0], shape[1], shape[2] + 3, shape[3] + 8), float("nan"), dtype=dtype, device="cuda")
+        big[:, :, 1:1 + shape[2], :shape[3]] = x
+        return big[:, :, 1:1 + shape[2], :shape[3]]
+    return x
+
+
+def i32(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def i64(v):
+    return torch.tensor(v, dtype=torch.int64, device="cuda")
+
+
+def check(rows, out, lse, untouched=None):
+    """Every (b, i, out, lse, tol, ltol) of `rows` against the tensors; rows that are not listed keep `untouched`."""
+    o, l = out.double().cpu().numpy(), lse.double().cpu().numpy()
+    there = np.zeros(o.shape[:2], dtype=bool)
+    worst = 0.0
+    for b, i, eo, el, tol, ltol in rows:
+        there[b, i] = True
+        bad = np.isnan(eo)
+        assert np.array_equal(bad, np.isnan(o[b, i])), (b, i, "NaN")
+        inf = np.isinf(eo)
+        assert np.array_equal(o[b, i][inf], eo[inf]), (b, i, "infinity")
+        fin = ~bad & ~inf
+        off = np.abs(o[b, i][fin] - eo[fin])
+        assert np.all(off <= tol[fin]), (b, i, float((off / tol[fin]).max()))
+        worst = max(worst, float((off / np.maximum(tol[fin], 1e-300)).max()) if fin.any() else 0.0)
+        none = np.isinf(el)
+        assert np.array_equal(l[b, i][none], el[none]), (b, i, l[b, i], el)
+        ok = np.isfinite(el)
+        assert np.all(np.abs(l[b, i][ok] - el[ok]) <= ltol[ok]), (b, i, l[b, i], el, ltol)
+    if untouched is not None:
+        assert np.all(o[~there] == untouched) and np.all(l[~there] == untouched)
+    return worst
+
+
+def windowed(q, k, v, q_len, k_len, window, sinks, causal=True, scale=None, workspace=True, **kw):
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    lse = torch.full(q.shape[:3], 7.0, device="cuda")
+    ws = attention_workspace(q, k) if workspace else None
+    if ws is not None:
+        ws.fill_(255)                                     # NaN, whatever type reads it
+    window_attention(q, k, v, window=window, sinks=sinks, causal=causal, scale=scale, q_len=q_len, k_len=k_len, out=out, lse=lse,
+                     workspace=ws, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+WINDOW = [
+    # B, T, S, Hq, Hkv, D, window, sinks, causal, q_len, k_len, order
+    (1, 1, 1, 1, 1, 64, 0, 0, True, None, None, "bthd"),
+    (2, 1, 300, 4, 2, 128, 0, 0, True, None, [300, 257], "bthd"),
+    (3, 1, 700, 8, 1, 64, 100, 5, True, [1, 0, 1], [700, 33, 0], "bhtd"),
+    (2, 5, 129, 5, 5, 128, 0, 0, True, [5, 3], [129, 64], "wide"),
+    (2, 16, 200, 8, 2, 64, 0, 0, False, None, None, "bthd"),
+    (1, 70, 70, 2, 1, 128, 0, 0, True, None, None, "bthd"),
+    (1, 200, 200, 3, 3, 64, 17, 0, True, None, None, "bhtd"),
+    (2, 150, 333, 4, 4, 128, 64, 4, True, [150, 149], [333, 150], "wide"),
+    (1, 130, 130, 6, 2, 128, 1, 0, True, None, None, "bthd"),          # each query sees itself alone
+    (1, 90, 90, 2, 2, 64, 30, 200, True, None, None, "bthd"),          # more sinks than keys
+    (2, 40, 30, 4, 2, 128, 0, 0, True, [40, 20], [30, 5], "bthd"),     # more queries than keys: the first see none
+    (2, 33, 257, 4, 1, 64, 50, 3, False, None, [257, 1], "bhtd"),
+    (4, 65, 65, 7, 1, 128, 40, 2, True, [65, 1, 0, 64], [65, 1, 0, 64], "bthd"),
+    (1, 3, 2000, 16, 2, 64, 900, 70, True, None, None, "bthd"),        # sinks past a tile, far from the window
+    (1, 257, 1200, 4, 2, 128, 500, 130, True, None, None, "bthd"),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("case", WINDOW, ids=[str(i) for i in range(len(WINDOW))])
+def test_window_attention(case, dtype):
+    B, T, S, Hq, Hkv, D, window, sinks, causal, q_len, k_len, order = case
+    say(f"[attention] window {case} {dtype}")
+    q, k, v = make((B, T, Hq, D), dtype, 1, order), make((B, S, Hkv, D), dtype, 2, order), make((B, S, Hkv, D), dtype, 3, order)
+    ql, kl = q_len or [T] * B, k_len or [S] * B
+    for b in range(B):
+        q[b, ql[b]:] = float("nan")
+        k[b, kl[b]:] = float("nan")
+        v[b, kl[b]:] = float("nan")
+    rows = list(ref.window_reference(q, k, v, window, sinks, causal, D ** -0.5, ql, kl))
+    for workspace in (True, False):
+        out, lse = windowed(q, k, v, q_len and i32(q_len), k_len and i32(k_len), window, sinks, causal, workspace=workspace)
+        check(rows, out, lse, untouched=7.0)
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("T,causal,window", [(1, True, 20), (50, True, 20), (130, True, 0), (90, False, 33)])
+def test_what_a_query_does_not_see_does_not_reach_it(T, causal, window, dtype):
+    """NaN and infinities in keys and values: exactly the queries that see them are affected."""
+    S, D = 150, 64
+    q, k, v = make((1, T, 2, D), dtype, 1), make((1, S, 1, D), dtype, 2), make((1, S, 1, D), dtype, 3)
+    v[0, 100, 0, 5] = float("nan")
+    v[0, 141, 0, 7] = float("inf")
+    v[0, 60, 0, 9] = -float("inf")
+    k[0, 80, 0, 3] = float("nan")
+    rows = list(ref.window_reference(q, k, v, window, 2, causal, D ** -0.5, [T], [S]))
+    out, lse = windowed(q, k, v, None, None, window, 2, causal)
+    got, want = out.double().cpu().numpy(), {}
+    for b, i, eo, el, tol, ltol in rows:
+        bad = np.isnan(eo)
+        assert np.array_equal(bad, np.isnan(got[b, i])), i
+        inf = np.isinf(eo)
+        assert np.array_equal(got[b, i][inf], eo[inf]), i
+        fin = ~bad & ~inf
+        assert np.all(np.abs(got[b, i][fin] - eo[fin]) <= np.nan_to_num(tol[fin], nan=0.0) + 2 * ref.ROUNDOFF[dtype] * 4), i
+
+
+def test_scores_of_large_spread():
+    """A scale that puts single keys far above the rest: weights of 0 and 1, and running maxima that jump."""
+    q, k, v = make((1, 40, 2, 64), BF, 1), make((1, 300, 2, 64), BF, 2), make((1, 300, 2, 64), BF, 3)
+    for scale in (3.0, -2.0, 0.0):
+        rows = list(ref.window_reference(q, k, v, 0, 0, True, scale, [40], [300]))
+        out, lse = windowed(q, k, v, None, None, 0, 0, True, scale=scale)
+        check(rows, out, lse)
+
+
+def test_repeated_and_broadcast_inputs():
+    """Keys of one head for all (stride 0), a batch that shares its keys, outputs with the heads outermost."""
+    q = make((2, 20, 4, 64), BF, 1)
+    k, v = make((1, 100, 1, 64), BF, 2).expand(2, 100, 4, 64), make((1, 100, 1, 64), BF, 3).expand(2, 100, 4, 64)
+    out = torch.zeros((2, 4, 20, 64), dtype=BF, device="cuda").transpose(1, 2)
+    lse = torch.zeros((2, 20, 4), device="cuda")
+    assert window_attention(q, k, v, out=out, lse=lse) is out
+    check(ref.window_reference(q, k, v, 0, 0, True, 0.125, [20] * 2, [100] * 2), out, lse)
+
+
+# ---------------------------------------------------------------- the cache
+
+class Filled:
+    """A cache of random pages with NaN everywhere that a sequence's slots are not, and what it holds."""
+
+    def __init__(self, B, Hkv, D, ctx, dtype, seed=0, spare=3, room=None, missing=()):
+        g = torch.Generator().manual_seed(seed)
+        self.ctx, self.D, self.dtype = list(ctx), D, dtype
+        pages = max(1, -(-max(list(ctx) + [room or 1]) // 64))
+        n = B * pages + spare
+        self.cache = KVCache(Hkv, D, n, dtype="bf16" if dtype == BF else "f16")
+        self.cache.pages.fill_(255)
+        table = torch.randperm(n, generator=g)[:B * pages].to(torch.int32).view(B, pages)
+        self.table = table.cuda()
+        S = max(1, max(ctx))
+        self.k, self.v = make((B, S, Hkv, D), dtype, seed + 1), make((B, S, Hkv, D), dtype, seed + 2)
+        self.cache.write(self.k, self.v, self.table, i64([0] * B), count=i32(ctx))
+        for b, p in missing:
+            self.table[b, p] = -1 if (b + p) % 2 else n
+        gone = set(missing)
+        self.slots = [np.array([t for t in range(ctx[b]) if (b, t // 64) not in gone], dtype=np.int64) for b in range(B)]
+        qk, qv = ref.quantise(self.k), ref.quantise(self.v)
+        self.ck = [(s, qk[b][s]) for b, s in enumerate(self.slots)]
+        self.cv = [(s, qv[b][s]) for b, s in enumerate(self.slots)]
+
+
+def random_tree(rng, n, cap, kind):
+    """Depths, ancestor sets (in rows: 0 the root) and the mask of a tree of n nodes, breadth-first."""
+    parent = sorted(int(rng.integers(-1, max(0, min(j, j * 2 // 3 + 1)))) if j else -1 for j in range(n))
+    parent = [min(p, j - 1) for j, p in enumerate(parent)]
+    depth, anc = [], [{0}]
+    for j, p in enumerate(parent):
+        depth.append(1 if p < 0 else depth[p] + 1)
+        anc.append(anc[p + 1] | {j + 1})
+    m = rng.integers(0, 2, (cap, cap)).astype(np.uint8)          # random where nothing is written
+    m[:n, :n] = 0
+    for j in range(n):
+        for r in anc[j + 1]:
+            if r:
+                m[j, r - 1] = 1
+    if kind == "u8":
+        return depth, anc, m
+    words = (cap + 31) // 32
+    bits = np.zeros((cap, words * 32), dtype=np.uint8)
+    bits[:, :cap] = m
+    return depth, anc, np.packbits(bits, axis=1, bitorder="little").view(np.int32).reshape(cap, words)
+
+
+def attend_cache(f, q, k, v, order, count, window, sinks, trees=None, kind="u8", workspace=True, stream=None):
+    out = torch.full(q.shape, 7.0, dtype=q.dtype, device="cuda")
+    lse = torch.full(q.shape[:3], 7.0, device="cuda")
+    kw = dict(causal=order == "chain")
+    if order == "tree":
+        cap = trees[0][2].shape[0]
+        depth = torch.full((q.shape[0], cap), 99, dtype=torch.int32)
+        for b, (d, _, _) in enumerate(trees):
+            depth[b, :len(d)] = torch.tensor(d, dtype=torch.int32)
+        kw = dict(mask=torch.from_numpy(np.stack([t[2] for t in trees])).cuda() if k is not None else None, depth=depth.cuda())
+    ws = attention_workspace(q, cache=f.cache, page_table=f.table) if workspace else None
+    if ws is not None:
+        ws.fill_(255)
+    f.cache.attention(q, f.table, i64(f.ctx), k, v, count=None if count is None else i32(count), window=window, sinks=sinks, out=out,
+                      lse=lse, workspace=ws, stream=stream, **kw)
+    torch.cuda.synchronize()
+    return out, lse
+
+
+def cache_rows(f, q, k, v, order, count, window, sinks, trees=None):
+    n = count if count is not None else [q.shape[1] - (order == "tree")] * q.shape[0]
+    return ref.cache_reference(q, f.ck, f.cv, f.ctx, k, v, order, trees and [t[1] for t in trees],
+                               trees and [t[0] for t in trees], n, window, sinks, f.D ** -0.5)
+
+
+CACHE = [
+    # B, T, Hq, Hkv, D, ctx, order, count, window, sinks, new keys
+    (1, 1, 1, 1, 64, [0], "chain", None, 0, 0, True),
+    (1, 1, 4, 1, 128, [1], "chain", None, 0, 0, True),
+    (3, 1, 8, 2, 128, [63, 64, 65], "chain", None, 0, 0, True),
+    (3, 1, 5, 5, 64, [0, 200, 1], "chain", [1, 0, 1], 0, 0, True),
+    (2, 1, 4, 2, 64, [500, 130], "chain", None, 100, 4, True),
+    (2, 1, 4, 2, 128, [0, 130], "chain", None, 0, 0, False),            # no new keys; an empty cache: no key at all
+    (2, 7, 4, 4, 128, [300, 129], "chain", [7, 4], 0, 0, True),
+    (2, 16, 8, 2, 64, [1000, 77], "block", None, 0, 0, True),
+    (2, 16, 8, 2, 128, [1000, 3], "block", [16, 9], 10, 2, True),       # a window shorter than the block
+    (1, 40, 6, 2, 64, [257], "chain", None, 30, 3, True),
+    (2, 20, 4, 2, 128, [100, 40], "tree", [19, 0], 0, 0, True),
+    (3, 70, 3, 1, 64, [200, 0, 64], "tree", [69, 33, 64], 0, 0, True),
+    (2, 41, 4, 1, 128, [300, 5], "tree", [40, 12], 2, 0, True),         # a window shorter than the tree is deep
+    (2, 41, 4, 1, 128, [300, 5], "tree", [40, 12], 3, 8, True),         # ... and sinks among the tree's positions
+    (2, 33, 8, 2, 64, [700, 90], "tree", [32, 7], 128, 70, True),
+    (2, 12, 4, 2, 64, [100, 40], "tree", [11, 3], 0, 0, False),
+    (1, 130, 2, 2, 128, [321], "tree", [129], 0, 0, True),
+    (1, 2, 32, 2, 64, [3000], "chain", None, 0, 0, True),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("case", CACHE, ids=[str(i) for i in range(len(CACHE))])
+def test_cache_attention(case, dtype):
+    B, T, Hq, Hkv, D, ctx, order, count, window, sinks, new = case
+    say(f"[attention] cache {case} {dtype}")
+    f = Filled(B, Hkv, D, ctx, dtype)
+    q = make((B, T, Hq, D), dtype, 5)
+    k, v = (make((B, T, Hkv, D), dtype, s, "bhtd") for s in (6, 7)) if new else (None, None)
+    rng = np.random.default_rng(3)
+    for kind in ("u8", "bits") if order == "tree" else ("u8",):
+        trees = None
+        if order == "tree":
+            trees = [random_tree(rng, n, T + 5, kind) for n in count]
+        for b in range(B):
+            n = (count[b] if count else T - (order == "tree")) + (order == "tree")
+            for x in (q, k, v):
+                if x is not None:
+                    x[b, n:] = float("nan")
+        rows = list(cache_rows(f, q, k, v, order, count, window, sinks, trees))
+        for workspace in (True, False):
+            out, lse = attend_cache(f, q, k, v, order, count, window, sinks, trees, kind, workspace)
+            check(rows, out, lse, untouched=7.0)
+
+
+def test_cached_nan_reaches_only_those_who_see_it():
+    f = Filled(1, 1, 64, [300], BF)
+    bad = make((1, 1, 1, 64), BF, 9)
+    bad[0, 0, 0, 40] = float("inf")                       # the second block of the token becomes NaN
+    f.cache.write(bad, bad, f.table, i64([150]))
+    f.ck[0][1][150] = ref.quantise(bad)[0, 0]
+    f.cv[0][1][150] = ref.quantise(bad)[0, 0]
+    assert np.isnan(f.cv[0][1][150]).sum() == 32
+    q, k, v = make((1, 200, 2, 64), BF, 5), make((1, 200, 1, 64), BF, 6), make((1, 200, 1, 64), BF, 7)
+    for T in (200, 3):
+        a = (q[:, :T], k[:, :T], v[:, :T])
+        rows = list(cache_rows(f, *a, "chain", None, 160, 0))
+        out, _ = attend_cache(f, *a, "chain", None, 160, 0)
+        got = out.double().cpu().numpy()
+        for b, i, eo, el, tol, ltol in rows:
+            assert np.array_equal(np.isnan(eo), np.isnan(got[b, i])), (T, i)
+            if not np.isnan(eo).any():
+                assert np.all(np.abs(got[b, i] - eo) <= tol), (T, i)
+
+
+@pytest.mark.parametrize("T", [1, 24, 100])
+def test_pages_outside_the_cache_hold_no_key(T):
+    f = Filled(2, 2, 64, [400, 190], BF, missing=[(0, 0), (0, 4), (1, 2)])
+    q, k, v = make((2, T, 4, 64), BF, 5), make((2, T, 2, 64), BF, 6), make((2, T, 2, 64), BF, 7)
+    out, lse = attend_cache(f, q, k, v, "chain", None, 0, 0)
+    check(cache_rows(f, q, k, v, "chain", None, 0, 0), out, lse)
+
+
+def test_lengths_past_their_buffers_are_clamped():
+    f = Filled(2, 1, 64, [64, 64], BF)
+    q, k, v = make((2, 3, 2, 64), BF, 5), make((2, 3, 1, 64), BF, 6), make((2, 3, 1, 64), BF, 7)
+    want, wl = attend_cache(f, q, k, v, "chain", None, 0, 0)
+    f.ctx = [1 << 40, 65]
+    got, gl = attend_cache(f, q, k, v, "chain", [100, 2 ** 31 - 1], 0, 0)
+    assert torch.equal(want, got) and torch.equal(wl, gl)
+    f.ctx = [-5, -(1 << 50)]
+    out, lse = attend_cache(f, q, None, None, "chain", [-1, 3], 0, 0)
+    assert torch.all(out[0] == 7.0) and torch.all(out[1] == 0.0) and torch.all(lse[1] == -float("inf"))
+
+
+def test_offsets_past_32_bits():
+    """Pages at the end of a cache of more than 4 GiB, and keys at strides whose products pass 32 bits."""
+    n = (1 << 32) // (2 * 8704) + 70
+    cache = KVCache(2, 128, n)
+    table = torch.tensor([[n - 1, 0, n - 2, 5]], dtype=torch.int32, device="cuda")
+    k, v, q = make((1, 250, 2, 128), BF, 1), make((1, 250, 2, 128), BF, 2), make((1, 5, 4, 128), BF, 3)
+    cache.write(k, v, table, i64([0]))
+    f = Filled.__new__(Filled)
+    f.cache, f.table, f.ctx, f.D = cache, table, [250], 128
+    s = np.arange(250)
+    f.ck, f.cv = [(s, ref.quantise(k)[0])], [(s, ref.quantise(v)[0])]
+    out, lse = attend_cache(f, q, None, None, "chain", None, 0, 0)
+    check(cache_rows(f, q, None, None, "chain", None, 0, 0), out, lse)
+    scores, new = torch.zeros((1, 2, 256), device="cuda"), torch.zeros((1, 2, 256), device="cuda")
+    cache.score(q, table, i64([250]), lse, scores, new)
+    torch.cuda.synchronize()
+    assert abs(float(new.sum()) - 5 * 4) < 1e-3                  # the weights of 5 queries of 4 heads
+    del cache, f, table
+    big = torch.zeros((2, 40000, 1, 64 * 900), dtype=BF, device="cuda")      # 4.6e9 elements
+    x = big[1:, 39000:39300, :, 64 * 899:]
+    x.copy_(k[:, :, :1, :64].repeat(1, 2, 1, 1)[:, :300])
+    out, lse = windowed(q[..., :64].contiguous(), x, x, None, None, 0, 0)
+    check(ref.window_reference(q[..., :64], x, x, 0, 0, True, 0.125, [5], [300]), out, lse)
+
+
+# ---------------------------------------------------------------- in and out of the cache
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("D,Hkv", [(64, 3), (128, 2)])
+def test_write_and_read(D, Hkv, dtype):
+    B, T = 3, 70
+    k, v = make((B, T, Hkv, D), dtype, 1, "bhtd"), make((B, T, Hkv, D), dtype, 2, "wide", scale=100.0)
+    top = torch.finfo(dtype).max
+    small = 2.0 ** -24 if dtype == F16 else 2.0 ** -133
+    k[0, 0, 0, :32] = 0.0
+    k[0, 1, 0, :8] = torch.tensor([-0.0, 0.0, small, -small, 2 * small, top, -top, 1.0]).to(dtype)
+    k[0, 2, 0, :32] = 0.0
+    k[0, 2, 0, 3] = small
+    k[0, 3, 0, 0] = float("nan")
+    k[0, 4, 0, 33] = -float("inf")
+    for j, m in enumerate((1.0, 1.5, 1.75, 1.7578125, 1.9921875, 2.0)):      # around the step of the exponent
+        k[1, j, 0, :32] = torch.linspace(-m, m, 32).to(dtype)
+        k[1, j, 0, 0] = m
+    for j, x in enumerate((0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0)):          # ties
+        k[2, j, 0, :32] = x
+        k[2, j, 0, 0] = 6.0
+    cache = KVCache(Hkv, D, 9, dtype="bf16" if dtype == BF else "f16")
+    cache.pages.fill_(77)
+    table = torch.tensor([[8, 3, 0], [1, 7, 2], [4, 6, 5]], dtype=torch.int32, device="cuda")
+    start, count = [0, 61, 100], [70, 65, 0]
+    cache.write(k, v, table, i64(start), count=i32(count))
+    end = i64([s + c for s, c in zip(start, count)])
+    gk, gv = (torch.full((B, T, Hkv, D), 7.0, dtype=dtype, device="cuda") for _ in range(2))
+    cache.read(table, end, gk, gv, start=i64(start))
+    for got, src in ((gk, k), (gv, v)):
+        want, got = ref.quantise(src), got.double().cpu().numpy()
+        for b in range(B):
+            assert np.array_equal(got[b, :count[b]], want[b, :count[b]], equal_nan=True), b
+            assert np.all(got[b, count[b]:] == 7.0)
+    # nothing else was written: all slots of the pages that no token went to
+    used = set()
+    for b in range(B):
+        for t in range(start[b], start[b] + count[b]):
+            used.add((int(table[b, t // 64]), t % 64))
+    pages = cache.pages.cpu().numpy()
+    for p in range(9):
+        for t in range(64):
+            if (p, t) not in used:
+                row = D // 2
+                assert np.all(pages[p, :, t * row:(t + 1) * row] == 77) and np.all(pages[p, :, 64 * row * 2 + t * D // 32] == 77)
+
+
+def test_write_of_an_accepted_path_and_past_the_end():
+    k, v = make((2, 20, 1, 64), BF, 1), make((2, 20, 1, 64), BF, 2)
+    cache = KVCache(1, 64, 4)
+    table = torch.tensor([[0, 1], [2, 99]], dtype=torch.int32, device="cuda")
+    index = i32([[0, 3, 7, 19, 5], [1, -1, 20, 2, 0]])
+    cache.write(k, v, table, i64([125, 62]), count=i32([5, 4]), index=index)
+    got = [torch.full((2, 128, 1, 64), 7.0, dtype=BF, device="cuda") for _ in range(2)]
+    cache.read(table, i64([1000, 128]), *got)
+    for g, src in zip(got, (k, v)):
+        want, g = ref.quantise(src)[:, :, 0], g.double().cpu().numpy()[:, :, 0]
+        for j, r in enumerate((0, 3, 7)):                 # slots 125 .. 127; 128 and 129 are past the table
+            assert np.array_equal(g[0, 125 + j], want[0, r])
+        assert np.array_equal(g[1, 62], want[1, 1])
+        assert np.all(g[1, 63] == 0.0)                    # index -1: nothing written
+        assert np.all(g[1, 64:] == 7.0)                   # no such page
+
+
+# ---------------------------------------------------------------- scores and eviction
+
+SCORE = [
+    # B, T, Hq, Hkv, D, ctx, order, count, window, sinks
+    (1, 1, 1, 1, 64, [1], "chain", None, 0, 0),
+    (3, 1, 8, 2, 128, [63, 0, 200], "chain", None, 0, 0),
+    (2, 5, 4, 4, 64, [300, 64], "chain", [5, 2], 70, 3),
+    (2, 30, 12, 2, 128, [129, 500], "tree", [29, 11], 0, 0),
+    (2, 30, 3, 1, 64, [129, 500], "tree", [0, 29], 40, 66),
+    (1, 16, 16, 2, 64, [1000], "block", None, 0, 0),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF, F16], ids=["bf16", "f16"])
+@pytest.mark.parametrize("weighted", [False, True])
+@pytest.mark.parametrize("case", SCORE, ids=[str(i) for i in range(len(SCORE))])
+def test_score(case, weighted, dtype):
+    B, T, Hq, Hkv, D, ctx, order, count, window, sinks = case
+    f = Filled(B, Hkv, D, ctx, dtype, room=max(ctx) + 70)
+    q, k, v = make((B, T, Hq, D), dtype, 5), make((B, T, Hkv, D), dtype, 6), make((B, T, Hkv, D), dtype, 7)
+    rng = np.random.default_rng(3)
+    trees = [random_tree(rng, n, T - 1, "u8") for n in count] if order == "tree" else None
+    n = [min(T, (count[b] if count else T) + (order == "tree")) for b in range(B)]
+    for b in range(B):
+        q[b, n[b]:] = float("nan")
+    _, lse = attend_cache(f, q, k, v, order, count, window, sinks, trees)
+    weight = None
+    if weighted:
+        weight = torch.from_numpy(rng.choice([0.0, 1.0, 0.25, -1.0], (B, T)).astype(np.float32)).cuda()
+        weight[:, T // 2] = 1.0
+    slots = f.table.shape[1] * 64
+    old = torch.rand((B, Hkv, slots), generator=torch.Generator().manual_seed(1)).cuda()
+    depth = None
+    if order == "tree":
+        depth = torch.full((B, T - 1), 50, dtype=torch.int32)
+        for b, t in enumerate(trees):
+            depth[b, :len(t[0])] = torch.tensor(t[0], dtype=torch.int32)
+        depth = depth.cuda()
+    new = torch.full_like(old, 7.0)
+    kw = dict(weight=weight, count=None if count is None else i32(count), depth=depth, window=window, sinks=sinks)
+    f.cache.score(q, f.table, i64(f.ctx), lse, old, new, **kw)
+    again = old.clone()
+    f.cache.score(q, f.table, i64(f.ctx), lse, again, **kw)        # in place
+    torch.cuda.synchronize()
+    assert torch.equal(new, again)
+    got, base, l, qq = (x.double().cpu().numpy() for x in (new, old, lse, q))
+    G, scale = Hq // Hkv, D ** -0.5
+    for b in range(B):
+        for h in range(Hkv):
+            want, tol = base[b, h].copy(), np.zeros(slots)
+            kk = f.ck[b][1][:, h]
+            for i in range(n[b]):
+                w = 1.0 if weight is None else float(weight[b, i])
+                if not w > 0:
+                    continue
+                step = 0 if order == "tree" and i == 0 else trees[b][0][i - 1] if order == "tree" else i
+                seen = ref.in_window(ctx[b] + step, f.slots[b], window, sinks)
+                for g in range(G):
+                    s = scale * (kk @ qq[b, i, h * G + g])
+                    p = np.where(seen, w * np.exp(s - l[b, i, h * G + g]), 0.0)
+                    want[:ctx[b]] += p
+                    ds = D * 2.0 ** -24 * scale * (np.abs(kk) @ np.abs(qq[b, i, h * G + g]))
+                    tol[:ctx[b]] += p * (ds + 2.0 ** -18)
+            tol += 2.0 ** -22 * np.abs(want) * 4
+            assert np.all(np.abs(got[b, h] - want) <= tol), (b, h, float(np.max(np.abs(got[b, h] - want) / np.maximum(tol, 1e-30))))
+
+
+def evict(f, scores, budget, sinks, recent, extra=0):
+    B, Hkv = scores.shape[:2]
+    new_pages = max(1, -(-budget // 64)) + extra
+    free = [p for p in range(f.cache.pages.shape[0]) if p not in set(f.table.flatten().tolist())]
+    new_table = torch.tensor(free[:B * new_pages], dtype=torch.int32).view(B, new_pages).cuda()
+    new_len = torch.full((B,), -1, dtype=torch.int64, device="cuda")
+    new_scores = torch.full((B, Hkv, new_pages * 64), 7.0, device="cuda")
+    kept = torch.full((B, Hkv, budget), -7, dtype=torch.int32, device="cuda")
+    f.cache.evict(f.table, i64(f.ctx), scores, new_table, new_len, new_scores, kept, budget=budget, sinks=sinks, recent=recent)
+    torch.cuda.synchronize()
+    return new_table, new_len, new_scores, kept
+
+
+EVICT = [
+    # Hkv, D, ctx, budget, sinks, recent, scores
+    (1, 64, [1], 1, 0, 0, "rand"),
+    (2, 64, [100, 0, 5, 64], 20, 4, 8, "rand"),
+    (1, 128, [500, 130], 130, 0, 0, "rand"),
+    (2, 128, [300, 299], 65, 65, 0, "rand"),             # nothing but sinks
+    (2, 64, [300, 299], 64, 0, 64, "rand"),              # nothing but recent ones
+    (1, 64, [777, 400], 100, 3, 7, "zeros"),             # all equal: the lowest slots
+    (1, 64, [777, 400], 100, 3, 7, "ties"),
+    (1, 64, [300], 90, 1, 1, "odd"),                     # NaN, infinities, negative ones, -0 and 0
+    (3, 64, [5000, 4097, 1024], 1000, 4, 100, "heavy"),
+    (1, 64, [0, 0], 0, 0, 0, "rand"),
+    (1, 64, [70, 3], 0, 0, 0, "rand"),                   # a budget of nothing
+    (1, 64, [70000], 9000, 4, 1000, "heavy"),
+]
+
+
+@pytest.mark.parametrize("case", EVICT, ids=[str(i) for i in range(len(EVICT))])
+def test_evict(case):
+    Hkv, D, ctx, budget, sinks, recent, kind = case
+    say(f"[attention] evict {case}")
+    B = len(ctx)
+    room = -(-max(max(ctx), 1) // 64)
+    f = Filled.__new__(Filled)
+    f.ctx, f.D = ctx, D
+    need = B * (room + max(1, -(-budget // 64)) + 1)
+    f.cache = KVCache(Hkv, D, need)
+    f.table = torch.randperm(need, generator=torch.Generator().manual_seed(3))[:B * room].to(torch.int32).view(B, room).cuda()
+    T = room * 64
+    k, v = make((B, T, Hkv, D), BF, 1), make((B, T, Hkv, D), BF, 2)
+    f.cache.write(k, v, f.table, i64([0] * B), count=i32(ctx))
+    wk, wv = (torch.zeros((B, T, Hkv, D), dtype=BF, device="cuda") for _ in range(2))
+    f.cache.read(f.table, i64(ctx), wk, wv)
+    g = torch.Generator().manual_seed(9)
+    x = torch.rand((B, Hkv, T), generator=g)
+    if kind == "zeros":
+        x = torch.zeros_like(x)
+    elif kind == "ties":
+        x = (x * 4).floor()
+    elif kind == "heavy":
+        x = torch.where(x > 0.3, 4 * x ** 8, 0.0)
+    elif kind == "odd":
+        odd = torch.tensor([float("nan"), float("inf"), -float("inf"), -0.0, 0.0, -1.5, 1e-42, -1e-42, -float("nan")])
+        x = torch.where(x > 0.5, odd[(x * 1000).long() % 9], x - 0.2)
+    new_table, new_len, new_scores, kept = evict(f, x.cuda(), budget, sinks, recent, extra=1 if kind == "ties" else 0)
+    assert new_len.tolist() == [min(n, budget) for n in ctx]
+    rk, rv = (torch.full((B, max(budget, 1), Hkv, D), 7.0, dtype=BF, device="cuda") for _ in range(2))
+    f.cache.read(new_table, new_len, rk, rv)
+    for b in range(B):
+        m = min(ctx[b], budget)
+        for h in range(Hkv):
+            want = ref.evict(x[b, h].tolist(), ctx[b], budget, sinks, recent)
+            assert kept[b, h].tolist() == want + [-1] * (budget - m), (b, h)
+            assert np.array_equal(new_scores[b, h, :m].cpu().numpy(), x[b, h].numpy()[want], equal_nan=True)
+            assert torch.all(new_scores[b, h, m:] == 0.0)
+            at = torch.tensor(want, dtype=torch.int64, device="cuda")
+            assert torch.equal(rk[b, :m, h], wk[b, at, h]) and torch.equal(rv[b, :m, h], wv[b, at, h])
+    assert torch.all(rk[:, max(min(max(ctx), budget), 0):] == 7.0)
+
+
+# ---------------------------------------------------------------- streams, graphs, repeats
+
+def test_the_same_bits_every_time_and_on_another_stream():
+    f = Filled(2, 2, 128, [900, 333], BF)
+    q, k, v = make((2, 20, 8, 128), BF, 5), make((2, 20, 2, 128), BF, 6), make((2, 20, 2, 128), BF, 7)
+    want, wl = attend_cache(f, q, k, v, "block", None, 0, 0)
+    side = torch.cuda.Stream()
+    for _ in range(5):
+        got, gl = attend_cache(f, q, k, v, "block", None, 0, 0)
+        assert torch.equal(want, got) and torch.equal(wl, gl)
+    got, gl = attend_cache(f, q, k, v, "block", None, 0, 0, stream=side)
+    assert torch.equal(want, got) and torch.equal(wl, gl)
+    made = window_attention(q, k, v, window=7, stream=side)
+    side.synchronize()
+    assert torch.equal(made, window_attention(q, k, v, window=7))
+
+
+def test_under_graph_capture():
+    """A verification round captured once: replays, with eager work and synchronisations between them, write what
+    eager calls write."""
+    B, T, Hq, Hkv, D = 2, 9, 4, 2, 64
+    f = Filled(B, Hkv, D, [200, 70], BF, room=300, spare=12)
+    q, k, v = make((B, T, Hq, D), BF, 5), make((B, T, Hkv, D), BF, 6), make((B, T, Hkv, D), BF, 7)
+    ctx, scores = i64(f.ctx), torch.zeros((B, Hkv, 320), device="cuda")
+    free = [p for p in range(f.cache.pages.shape[0]) if p not in set(f.table.flatten().tolist())]
+    new_table = torch.tensor(free[:4], dtype=torch.int32).view(B, 2).cuda()
+    res = dict(out=torch.zeros_like(q), lse=torch.zeros((B, T, Hq), device="cuda"), new_scores=torch.zeros_like(scores),
+               new_len=torch.zeros_like(ctx), cut=torch.zeros((B, Hkv, 128), device="cuda"),
+               kept=torch.zeros((B, Hkv, 100), dtype=torch.int32, device="cuda"), k=torch.zeros((B, 100, Hkv, D), dtype=BF, device="cuda"),
+               v=torch.zeros((B, 100, Hkv, D), dtype=BF, device="cuda"), win=torch.zeros_like(q))
+    ws = attention_workspace(q, cache=f.cache, page_table=f.table)
+    ws2 = attention_workspace(q, k)
+
+    def round_():
+        f.cache.attention(q, f.table, ctx, k, v, out=res["out"], lse=res["lse"], workspace=ws)
+        f.cache.write(k, v, f.table, ctx)
+        f.cache.score(q, f.table, ctx, res["lse"], scores, res["new_scores"])
+        f.cache.evict(f.table, ctx, res["new_scores"], new_table, res["new_len"], res["cut"], res["kept"], budget=100, sinks=2, recent=10)
+        f.cache.read(new_table, res["new_len"], res["k"], res["v"])
+        window_attention(q, k, v, window=5, sinks=1, out=res["win"], workspace=ws2)
+
+    def values():
+        torch.cuda.synchronize()
+        return {n: t.clone() for n, t in res.items()}
+
+    round_()
+    first = values()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        round_()
+    torch.cuda.current_stream().wait_stream(side)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        round_()
+    for i in range(3):
+        for t in res.values():
+            t.fill_(3)
+        q.copy_(make((B, T, Hq, D), BF, 50 + i))
+        g.replay()
+        got = values()
+        for t in res.values():
+            t.fill_(3)
+        round_()
+        want = values()
+        for n in res:
+            assert torch.equal(got[n], want[n]), (i, n)
+        assert i > 0 or not torch.equal(got["out"], first["out"])
