@@ -1,123 +1,685 @@
-// Attention over the keys of a tensor or of a 4-bit cache: one wavefront a query and head.
+// Attention over the keys of a tensor and of a 4-bit cache, in two kernels.
 //
-// Lanes are keys for the scores and channels for the sum over values; a running maximum and sum carry
-// the softmax over tiles of 64 keys.  Keys that a row does not see are never read for it.
-#include "attn_common.h"
+// Few rows (at most 64 of a kv head: single tokens, blocks, small trees) are bound by reading the keys.
+// The narrow kernel's wavefronts each take tiles of their own: codes go from memory to registers, keys
+// are converted there into the operand of the matrix product, values pass through LDS to be transposed.
+// Many rows (prompts, large trees) are bound by the matrix products; the wide kernel's four wavefronts
+// share each tile, converted once into LDS, and hold 32 rows each.
+//
+// Where there are too few workgroups for the card, the tiles of a row are split over several, whose
+// partial sums the combining kernel joins in a fixed order.
+#include "attn_tile.h"
 
 namespace caddtree {
 namespace {
 
 using namespace at;
 
-// one row's state: channels lane, lane + 64
+// partial results of (sequence, kv head, row, split): D sums, relative to the maximum, in `sum`; the
+// maximum (in units of log2) and the sum of the weights in `ml`
+__device__ int64_t part_of(const AttnArgs& a, const Split& sp, int b, int hk, int r) {
+  return (((int64_t)b * a.Hkv + hk) * ((int64_t)a.T * a.G) + r) * sp.n;
+}
+
+// ---------------------------------------------------------------- few rows
+
+// A wavefront's tile of a page: lane (col, g) holds the codes of tokens 16 s + col, channels g D / 4 .. of
+// keys, and whole blocks of values, token by token.
 template <int D>
-struct Row {
-  float m = -INFINITY, l = 0.f, acc[D / 64] = {};
+struct PageStage {
+  uint32_t kc[4][D / 32];
+  uint32_t ks[4];
+  u32x4 vc[D / 32];
+  uint32_t vs[D / 32];
+
+  __device__ void load(const uint8_t* page, int lane) {
+    using L = PageLayout<D>;
+    const int col = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const uint32_t* c = reinterpret_cast<const uint32_t*>(page + L::kK + (16 * s + col) * L::kRow + g * (D / 8));
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) kc[s][w] = c[w];
+      ks[s] = page[L::kKs + (16 * s + col) * L::kScales + g * (D / 4) / kBlock];
+    }
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) {
+      const int q = lane + 64 * u;
+      vc[u] = *reinterpret_cast<const u32x4*>(page + L::kV + q * 16);
+      vs[u] = page[L::kVs + q];
+    }
+  }
+  __device__ void clear() {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      ks[s] = 127;
+#pragma unroll
+      for (int w = 0; w < D / 32; ++w) kc[s][w] = 0;
+    }
+#pragma unroll
+    for (int u = 0; u < D / 32; ++u) {
+      vc[u] = u32x4{0, 0, 0, 0};
+      vs[u] = 127;
+    }
+  }
+  // the operand of keys 16 s .. 16 s + 15: D / 32 instructions' worth
+  template <typename E>
+  __device__ void keys(int s, u32x4 out[D / 32]) const {
+    const float f = scale_of(ks[s]);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+      out[j][0] = E::template from4<0>(kc[s][j], f);
+      out[j][1] = E::template from4<1>(kc[s][j], f);
+      out[j][2] = E::template from4<2>(kc[s][j], f);
+      out[j][3] = E::template from4<3>(kc[s][j], f);
+    }
+    if (ks[s] == 255)
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) out[j] = u32x4{E::kNaN, E::kNaN, E::kNaN, E::kNaN};
+  }
+  // values of tokens 32 half .. + 31 into LDS.  there: tokens of the tile that are there; returns the tokens
+  // (bit by bit of the tile) that hold what is not finite, for a tile that is not seen in full
+  template <typename E>
+  __device__ uint64_t values(int half, char* lds, int lane, bool full, int there) const {
+    constexpr int kPer = D / 32, kU = kPer / 2;    // blocks of a token; loads of a half
+    uint64_t bad = 0;
+#pragma unroll
+    for (int v = 0; v < kU; ++v) {
+      const int u = half * kU + v, q = lane + 64 * u, token = q / kPer, blk = q % kPer, row = token & 31;
+      uint32_t x[16];
+      decode_block<E>(vc[u], vs[u], x);
+      if (!full) {
+        const bool gone = token >= there, nan = !gone && vs[u] == 255;
+        if (gone || nan)
+#pragma unroll
+          for (int w = 0; w < 16; ++w) x[w] = 0;
+        for (uint64_t m = __ballot(nan); m; m &= m - 1) bad |= 1ull << ((__builtin_ctzll(m) + 64 * u) / kPer);
+      }
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        *reinterpret_cast<u32x4*>(lds + v_at<D>(row, blk * 64 + w * 16)) =
+            u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
+    }
+    return bad;
+  }
 };
 
-// keys of a tile of 64: lane's score (or -inf where it is not seen), then the values of the seen ones
-template <typename E, int D, typename ValueOf>
-__device__ void take(Row<D>& r, float s, ValueOf value) {
-  float m = s;
+// A wavefront's tile of 32 keys of a tensor.
+template <int D>
+struct TensorStage {
+  u32x4 kr[2][D / 32];
+  u32x4 vr[D / 16];
+
+  __device__ void load(const char* k, const char* v, int64_t kt, int64_t vt, int j0, int nk, int lane) {
+    const int col = lane & 15, g = lane >> 4;
 #pragma unroll
-  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
-  const uint64_t seen = __ballot(s != -INFINITY);       // (a NaN is seen)
-  if (seen == 0) return;
-  m = fmaxf(m, r.m);
-  const float was = r.m == -INFINITY ? 0.f : __expf(r.m - m);
-  const float p = s == -INFINITY ? 0.f : __expf(s - m);
-  float l = p;
+    for (int s = 0; s < 2; ++s) {
+      const u32x4* p = reinterpret_cast<const u32x4*>(k + 2 * (min(j0 + 16 * s + col, nk - 1) * kt + g * (D / 4)));
 #pragma unroll
-  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
-  r.l = r.l * was + l;
-  r.m = m;
+      for (int j = 0; j < D / 32; ++j) kr[s][j] = p[j];
+    }
 #pragma unroll
-  for (int c = 0; c < D / 64; ++c) r.acc[c] *= was;
-  for (uint64_t left = seen; left; left &= left - 1) {
-    const int j = __builtin_ctzll(left);
-    const float pj = __shfl(p, j);
+    for (int u = 0; u < D / 16; ++u) {
+      const int q = lane + 64 * u;
+      vr[u] = *reinterpret_cast<const u32x4*>(v + 2 * (min(j0 + q / (D / 8), nk - 1) * vt + q % (D / 8) * 8));
+    }
+  }
+  template <typename E>
+  __device__ void keys(int s, u32x4 out[D / 32]) const {
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) r.acc[c] += pj * value(j, c);
+    for (int j = 0; j < D / 32; ++j) out[j] = kr[s][j];
+  }
+  template <typename E>
+  __device__ uint64_t values(int, char* lds, int lane, bool full, int there) const {
+    uint64_t bad = 0;
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) {
+      const int q = lane + 64 * u, token = q / (D / 8);
+      u32x4 x = vr[u];
+      if (!full) {
+        if (token >= there) x = u32x4{0, 0, 0, 0};
+        for (uint64_t m = __ballot(clean_pairs<E>(x)); m; m &= m - 1) bad |= 1ull << ((__builtin_ctzll(m) + 64 * u) / (D / 8));
+      }
+      *reinterpret_cast<u32x4*>(lds + v_at<D>(token, q % (D / 8) * 16)) = x;
+    }
+    return bad;
+  }
+};
+
+// The running softmax of 16 kR rows: lane (col, g) has rows 16 n + col and channels 16 t + 4 g .. + 3.
+template <int D, int kR>
+struct NarrowState {
+  float m[kR], l[kR];
+  f32x4 acc[D / 16][kR];
+};
+
+// Takes a tile of 32 kH keys.  value(token, d): a cached or new value that is not finite, else 0.
+template <typename E, int D, int kR, int kH, typename Stage, typename Value>
+__device__ void narrow_tile(NarrowState<D, kR>& st, const Stage& x, const u32x4 (&q)[kR][D / 32], float c, bool full,
+                            const uint64_t (&seen)[kR], int there, char* lds, int lane, Value value) {
+  const int g = lane >> 4;
+  f32x4 s[2 * kH][kR];
+#pragma unroll
+  for (int t = 0; t < 2 * kH; ++t) {
+    u32x4 k[D / 32];
+    x.template keys<E>(t, k);
+#pragma unroll
+    for (int n = 0; n < kR; ++n) {
+      s[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) s[t][n] = Mfma<E>::m16(k[j], q[n][j], s[t][n]);
+    }
+  }
+  u32x4 p[kH][kR];
+#pragma unroll
+  for (int n = 0; n < kR; ++n) {
+    float top = -INFINITY;
+    const uint64_t bits = seen[n] >> (4 * g);       // key 16 t + 4 g + r is bit 16 t + r
+#pragma unroll
+    for (int t = 0; t < 2 * kH; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float y = s[t][n][r] * c;
+        if (!full && !((bits >> (16 * t + r)) & 1)) y = -INFINITY;
+        s[t][n][r] = y;
+        top = fmaxf(top, y);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float m = fmaxf(st.m[n], top);
+    const float base = m == -INFINITY ? 0.f : m - kBias<E>;
+    const float was = __builtin_amdgcn_exp2f(st.m[n] - kBias<E> - base);
+    float sum = 0.f;
+#pragma unroll
+    for (int t = 0; t < 2 * kH; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        s[t][n][r] = __builtin_amdgcn_exp2f(s[t][n][r] - base);
+        sum += s[t][n][r];
+      }
+    st.l[n] = st.l[n] * was + sum;                  // (of this lane's keys: the four g are added at the end)
+    st.m[n] = m;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) st.acc[t][n] *= was;
+#pragma unroll
+    for (int h = 0; h < kH; ++h)
+      p[h][n] = u32x4{E::pair(s[2 * h][n][0], s[2 * h][n][1]), E::pair(s[2 * h][n][2], s[2 * h][n][3]),
+                      E::pair(s[2 * h + 1][n][0], s[2 * h + 1][n][1]), E::pair(s[2 * h + 1][n][2], s[2 * h + 1][n][3])};
+  }
+#pragma unroll
+  for (int h = 0; h < kH; ++h) {
+    __builtin_amdgcn_wave_barrier();
+    uint64_t bad = x.template values<E>(h, lds, lane, full, there);
+    __builtin_amdgcn_wave_barrier();
+    const int row = 4 * g + (lane & 15) / 4;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) {
+      const int byte = 32 * t + (lane & 3) * 8;
+      const u32x2 lo = read_transposed(lds + v_at<D>(row, byte)), hi = read_transposed(lds + v_at<D>(row + 16, byte));
+      const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
+#pragma unroll
+      for (int n = 0; n < kR; ++n) st.acc[t][n] = Mfma<E>::m16(v, p[h][n], st.acc[t][n]);
+    }
+    for (; bad; bad &= bad - 1) {
+      const int token = __builtin_ctzll(bad);
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float v = value(token, 16 * t + 4 * g + r);
+#pragma unroll
+          for (int n = 0; n < kR; ++n)
+            if ((seen[n] >> token) & 1) st.acc[t][n][r] += v;
+        }
+    }
   }
 }
 
-template <typename E>
-__device__ float dot(const char* q, const char* k, int D) {
-  float s = 0.f;
-  for (int d = 0; d < D; d += 2) {
-    const uint32_t x = *reinterpret_cast<const uint32_t*>(q + 2 * d), y = *reinterpret_cast<const uint32_t*>(k + 2 * d);
-    s += E::lo(x) * E::lo(y);
-    s += E::hi(x) * E::hi(y);
+template <typename E, int D, int kR, bool kPaged>
+__global__ __launch_bounds__(256) void narrow_kernel(AttnArgs a, Split sp) {
+  using L = PageLayout<D>;
+  constexpr int kVBytes = 32 * 2 * D;               // 32 tokens' values; as many fp32 sums of 16 rows
+  __shared__ __align__(16) char lds[4 * kVBytes];
+  __shared__ float ml[4][2][16 * kR];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+  const Seq s = sequence(a, b);
+  const int R = s.nq * a.G;
+  if (R == 0) return;
+  const Span span = span_of<kPage, 32>(a, s, 0, s.nq - 1);
+  const int per = ceil_div(span.n, sp.n), t0 = split * per, t1 = min(span.n, t0 + per);
+
+  u32x4 q[kR][D / 32];
+  RowAt rows[kR];
+#pragma unroll
+  for (int n = 0; n < kR; ++n) {
+    const int r = min(16 * n + col, R - 1), i = r / a.G, h = hk * a.G + r % a.G;
+    rows[n] = row_at(a, s, b, i);
+    const u32x4* p = reinterpret_cast<const u32x4*>(a.q.data + 2 * (b * a.q.b + i * a.q.t + h * a.q.h + g * (D / 4)));
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) q[n][j] = p[j];
   }
-  return s;
+  NarrowState<D, kR> st;
+#pragma unroll
+  for (int n = 0; n < kR; ++n) {
+    st.m[n] = -INFINITY;
+    st.l[n] = 0.f;
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t) st.acc[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c = a.scale * kLog2e;
+  char* vt = lds + wave * kVBytes;
+  uint64_t seen[kR];
+
+  int t = t0 + wave;
+  if constexpr (kPaged) {
+    const int nc = min(t1, span.a + span.c - span.b);    // this split's cached tiles come first
+    PageStage<D> cur, next;
+    const uint8_t* page = nullptr;
+    int p0 = 0;
+    auto fetch = [&](int tile, PageStage<D>& x) {
+      bool cached;
+      p0 = tile_of<kPage, 32>(span, tile, &cached);
+      page = page_of(a.kv, b, p0 / kPage, hk);
+      if (page) x.load(page, lane);
+      else x.clear();
+    };
+    if (t < nc) fetch(t, cur);
+    for (; t < nc; t += 4) {
+      const uint8_t* now = page;
+      const int at = p0;
+      if (t + 4 < nc) fetch(t + 4, next);
+      const bool full = now && full_cached(a, s, s.nq - 1, at, kPage);
+#pragma unroll
+      for (int n = 0; n < kR; ++n) seen[n] = full ? ~0ull : now ? sees_cached(a, s, rows[n], at) : 0;
+      narrow_tile<E, D, kR, 2>(st, cur, q, c, full, seen, now ? s.ctx - at : 0, vt, lane, [&](int token, int d) {
+        return now[L::kVs + token * L::kScales + d / kBlock] == 255 ? __builtin_nanf("") : 0.f;
+      });
+      cur = next;
+    }
+  }
+  {
+    const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
+    const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
+    TensorStage<D> cur, next;
+    bool cached;
+    int at = 0;
+    if (t < t1) {
+      at = tile_of<kPage, 32>(span, t, &cached);
+      cur.load(kb, vb, a.k.t, a.v.t, at, s.nk, lane);
+    }
+    for (; t < t1; t += 4) {
+      int after = 0;
+      if (t + 4 < t1) {
+        after = tile_of<kPage, 32>(span, t + 4, &cached);
+        next.load(kb, vb, a.k.t, a.v.t, after, s.nk, lane);
+      }
+      const bool full = full_new(a, s, 0, s.nq - 1, at, 32);
+#pragma unroll
+      for (int n = 0; n < kR; ++n) seen[n] = full ? ~0ull : sees_new(a, s, b, rows[n], at);
+      narrow_tile<E, D, kR, 1>(st, cur, q, c, full, seen, s.nk - at, vt, lane, [&](int token, int d) {
+        return unclean<E>(vb + 2 * ((at + token) * a.v.t), d);
+      });
+      cur = next;
+      at = after;
+    }
+  }
+
+  // the four wavefronts' sums, 16 rows at a time: a thread adds D / 16 channels of a row
+#pragma unroll
+  for (int n = 0; n < kR; ++n) {
+    st.l[n] += __shfl_xor(st.l[n], 16);
+    st.l[n] += __shfl_xor(st.l[n], 32);
+    if (g == 0) {
+      ml[wave][0][16 * n + col] = st.m[n];
+      ml[wave][1][16 * n + col] = st.l[n];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int n = 0; n < kR; ++n) {
+    float m = -INFINITY;
+    for (int w = 0; w < 4; ++w) m = fmaxf(m, ml[w][0][16 * n + col]);
+    const float f = st.m[n] == -INFINITY ? (st.l[n] == 0.f ? 0.f : 1.f) : __builtin_amdgcn_exp2f(st.m[n] - m);
+#pragma unroll
+    for (int t = 0; t < D / 16; ++t)
+      *reinterpret_cast<f32x4*>(vt + col * (4 * D) + (((4 * t + g) ^ (col & 7)) << 4)) = st.acc[t][n] * f;
+    __syncthreads();
+    const int row = tid >> 4, part = tid & 15, r = 16 * n + row;
+    if (r < R) {
+      float mm = -INFINITY, ll = 0.f;
+      for (int w = 0; w < 4; ++w) mm = fmaxf(mm, ml[w][0][r]);
+      for (int w = 0; w < 4; ++w) {
+        const float mw = ml[w][0][r], lw = ml[w][1][r];
+        ll += lw == 0.f ? 0.f : mw == -INFINITY ? lw : lw * __builtin_amdgcn_exp2f(mw - mm);
+      }
+      f32x4 o[D / 64];
+#pragma unroll
+      for (int j = 0; j < D / 64; ++j) {
+        o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int w = 0; w < 4; ++w)
+          if (ml[w][1][r] != 0.f)
+            o[j] += *reinterpret_cast<const f32x4*>(lds + w * kVBytes + row * (4 * D) + (((part * (D / 64) + j) ^ (row & 7)) << 4));
+      }
+      const int i = r / a.G, h = hk * a.G + r % a.G, d = part * (D / 16);
+      if (sp.n == 1) {
+        const float inv = ll == 0.f ? 0.f : 1.f / ll;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h + d));
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+          const u32x2 y = {E::pair(o[j][0] * inv, o[j][1] * inv), E::pair(o[j][2] * inv, o[j][3] * inv)};
+          *reinterpret_cast<u32x2*>(dst + 2 * j) = y;
+        }
+        if (a.lse && part == 0)
+          a.lse[((int64_t)b * a.T + i) * a.Hq + h] = ll == 0.f ? -INFINITY : (mm - kBias<E> + __builtin_amdgcn_logf(ll)) * kLn2;
+      } else {
+        const int64_t at = part_of(a, sp, b, hk, r) + split;
+        if (part == 0) {
+          sp.ml[2 * at] = mm;
+          sp.ml[2 * at + 1] = ll;
+        }
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) *reinterpret_cast<f32x4*>(sp.sum + at * D + d + 4 * j) = o[j];
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- many rows
+
+constexpr int kWideRows = 128;
+
+// A tile's 64 keys and values on their way to LDS, a workgroup's 256 threads' shares.
+template <int D>
+struct WideTensor {
+  static constexpr int kN = D / 32;                 // 16-byte pieces of keys, and of values, a thread
+  u32x4 k[kN], v[kN];
+  __device__ void load(const char* kp, const char* vp, int64_t kt, int64_t vt, int j0, int nk, int tid) {
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+      const int q = tid + 256 * u, token = min(j0 + q / (D / 8), nk - 1), d = q % (D / 8) * 8;
+      k[u] = *reinterpret_cast<const u32x4*>(kp + 2 * (token * kt + d));
+      v[u] = *reinterpret_cast<const u32x4*>(vp + 2 * (token * vt + d));
+    }
+  }
+  template <typename E>
+  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* bad) {
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
+      const int q = tid + 256 * u, token = q / (D / 8), piece = q % (D / 8);
+      if (!full) {
+        if (token >= there) v[u] = u32x4{0, 0, 0, 0};
+        if (clean_pairs<E>(v[u])) atomicOr(&bad[token >> 5], 1u << (token & 31));
+      }
+      *reinterpret_cast<u32x4*>(kl + k_at<D>(token, piece)) = k[u];
+      *reinterpret_cast<u32x4*>(vl + v_at<D>(token, piece * 16)) = v[u];
+    }
+  }
+};
+// ... of a page: a block of keys and one of values a thread (D = 64: half the threads)
+template <int D>
+struct WidePage {
+  u32x4 k, v;
+  uint32_t ks, vs;
+  static constexpr int kThreads = kPage * (D / kBlock);
+  __device__ void load(const uint8_t* page, int tid) {
+    using L = PageLayout<D>;
+    if (tid >= kThreads) return;
+    if (page == nullptr) {
+      k = v = u32x4{0, 0, 0, 0};
+      ks = vs = 127;
+      return;
+    }
+    k = *reinterpret_cast<const u32x4*>(page + L::kK + tid * 16);
+    v = *reinterpret_cast<const u32x4*>(page + L::kV + tid * 16);
+    ks = page[L::kKs + tid];
+    vs = page[L::kVs + tid];
+  }
+  template <typename E>
+  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* bad) {
+    if (tid >= kThreads) return;
+    const int token = tid / (D / kBlock), blk = tid % (D / kBlock);
+    uint32_t x[16];
+    decode_block<E>(k, ks, x);
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      *reinterpret_cast<u32x4*>(kl + k_at<D>(token, blk * 4 + w)) = u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
+    decode_block<E>(v, vs, x);
+    if (!full) {
+      const bool gone = token >= there, nan = !gone && vs == 255;
+      if (nan) atomicOr(&bad[token >> 5], 1u << (token & 31));
+      if (gone || nan)
+#pragma unroll
+        for (int w = 0; w < 16; ++w) x[w] = 0;
+    }
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+      *reinterpret_cast<u32x4*>(vl + v_at<D>(token, blk * 64 + w * 16)) = u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
+  }
+};
+
+template <typename E, int D, bool kPaged>
+__global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
+  using L = PageLayout<D>;
+  __shared__ __align__(16) char kl[64 * 2 * D];
+  __shared__ __align__(16) char vl[64 * 2 * D];
+  __shared__ uint32_t bad[2][2];
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+  const int split = blockIdx.x % sp.n, tile_row = blockIdx.x / sp.n, hk = blockIdx.y, b = blockIdx.z;
+  const Seq s = sequence(a, b);
+  const int R = s.nq * a.G, r0 = tile_row * kWideRows;
+  if (r0 >= R) return;
+  const int i0 = r0 / a.G, i1 = min(R - 1, r0 + kWideRows - 1) / a.G;
+  const Span span = span_of<kPage, 64>(a, s, i0, i1);
+  const int per = ceil_div(span.n, sp.n), t0 = split * per, t1 = min(span.n, t0 + per);
+
+  const int r = r0 + 32 * wave + col, rr = min(r, R - 1), i = rr / a.G, h = hk * a.G + rr % a.G;
+  const bool mine = r0 + 32 * wave < R;             // this wavefront has rows
+  const RowAt row = row_at(a, s, b, i);
+  u32x4 q[D / 16];
+  {
+    const u32x4* p = reinterpret_cast<const u32x4*>(a.q.data + 2 * (b * a.q.b + i * a.q.t + h * a.q.h + half * 8));
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) q[j] = p[2 * j];
+  }
+  float m = -INFINITY, l = 0.f;
+  f32x16 acc[D / 32];
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
+  const float c = a.scale * kLog2e;
+  const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
+  const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
+
+  WideTensor<D> xt;
+  WidePage<D> xp;
+  const uint8_t* page = nullptr;
+  bool cached = false;
+  int at = 0;
+  auto fetch = [&](int t) {
+    at = tile_of<kPage, 64>(span, t, &cached);
+    if (kPaged && cached) {
+      page = page_of(a.kv, b, at / kPage, hk);
+      xp.load(page, tid);
+    } else {
+      xt.load(kb, vb, a.k.t, a.v.t, at, s.nk, tid);
+    }
+  };
+  if (t0 < t1) fetch(t0);
+  if (tid < 4) (&bad[0][0])[tid] = 0;
+  for (int t = t0; t < t1; ++t) {
+    const bool of_page = kPaged && cached;
+    const uint8_t* now = page;
+    const int here = at;
+    const bool full = of_page ? now && full_cached(a, s, i1, here, 64) : full_new(a, s, i0, i1, here, 64);
+    __syncthreads();                                // the last tile has been read
+    uint32_t* flags = bad[t & 1];
+    if (of_page) xp.template store<E>(kl, vl, tid, full, now ? s.ctx - here : 0, flags);
+    else xt.template store<E>(kl, vl, tid, full, s.nk - here, flags);
+    if (t + 1 < t1) fetch(t + 1);
+    __syncthreads();
+    if (tid < 2) bad[(t + 1) & 1][tid] = 0;         // (read last before the barrier above)
+    if (!mine) continue;
+    // scores: lane (col, half) has row col's keys 32 u + 8 (e / 4) + 4 half + e % 4
+    f32x16 x[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[u][e] = 0.f;
+#pragma unroll
+      for (int j = 0; j < D / 16; ++j)
+        x[u] = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(kl + k_at<D>(32 * u + col, 2 * j + half)), q[j], x[u]);
+    }
+    float top = -INFINITY;
+    uint64_t seen = ~0ull;
+    if (!full) {
+      seen = of_page ? (now ? sees_cached(a, s, row, here) : 0) : sees_new(a, s, b, row, here);
+      const uint64_t bits = seen >> (4 * half);
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          x[u][e] = (bits >> (32 * u + 8 * (e / 4) + e % 4)) & 1 ? x[u][e] * c : -INFINITY;
+    } else {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[u][e] *= c;
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, x[u][e]);
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float mm = fmaxf(m, top);
+    const float base = mm == -INFINITY ? 0.f : mm - kBias<E>;
+    if (__any(mm > m)) {
+      const float was = __builtin_amdgcn_exp2f(m - kBias<E> - base);
+      l *= was;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) acc[d] *= was;
+      m = mm;
+    }
+    float sum = 0.f;
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[u][e] = __builtin_amdgcn_exp2f(x[u][e] - base);
+        sum += x[u][e];
+      }
+    l += sum;                                       // (of this half's keys)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {                   // 16 keys an instruction
+      const f32x16& y = x[u / 2];
+      const int e = 8 * (u & 1);
+      const u32x4 p = {E::pair(y[e], y[e + 1]), E::pair(y[e + 2], y[e + 3]), E::pair(y[e + 4], y[e + 5]), E::pair(y[e + 6], y[e + 7])};
+      const int key = 16 * u + 4 * half + (lane & 15) / 4;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) {
+        const int byte = 64 * d + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+        const u32x2 lo = read_transposed(vl + v_at<D>(key, byte)), hi = read_transposed(vl + v_at<D>(key + 8, byte));
+        acc[d] = Mfma<E>::m32(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, acc[d]);
+      }
+    }
+    if (!full) {
+      for (uint64_t left = (uint64_t)flags[1] << 32 | flags[0]; left; left &= left - 1) {
+        const int token = __builtin_ctzll(left);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int ch = 32 * d + 8 * (e / 4) + 4 * half + e % 4;
+            const float v = of_page ? (now[L::kVs + token * L::kScales + ch / kBlock] == 255 ? __builtin_nanf("") : 0.f)
+                                    : unclean<E>(vb + 2 * ((here + token) * a.v.t), ch);
+            if ((seen >> token) & 1) acc[d][e] += v;
+          }
+      }
+    }
+  }
+  l += __shfl_xor(l, 32);
+  if (r >= R) return;
+  if (sp.n == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    char* dst = a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const u32x2 y = {E::pair(acc[d][4 * e] * inv, acc[d][4 * e + 1] * inv), E::pair(acc[d][4 * e + 2] * inv, acc[d][4 * e + 3] * inv)};
+        *reinterpret_cast<u32x2*>(dst + 2 * (32 * d + 8 * e + 4 * half)) = y;
+      }
+    if (a.lse && half == 0)
+      a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - kBias<E> + __builtin_amdgcn_logf(l)) * kLn2;
+  } else {
+    const int64_t to = part_of(a, sp, b, hk, r) + split;
+    if (half == 0) {
+      sp.ml[2 * to] = m;
+      sp.ml[2 * to + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(sp.sum + to * D + 32 * d + 8 * e + 4 * half) =
+            f32x4{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+  }
+}
+
+// Joins the splits of a row: one wavefront a row, a lane D / 64 channels.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void combine_kernel(AttnArgs a, Split sp) {
+  const int lane = threadIdx.x & 63, hk = blockIdx.y, b = blockIdx.z;
+  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const Seq s = sequence(a, b);
+  if (r >= (int64_t)s.nq * a.G) return;
+  const int64_t at = part_of(a, sp, b, hk, (int)r);
+  float m = -INFINITY, l = 0.f, o[D / 64] = {};
+  for (int k = 0; k < sp.n; ++k) m = fmaxf(m, sp.ml[2 * (at + k)]);
+  for (int k = 0; k < sp.n; ++k) {
+    const float mk = sp.ml[2 * (at + k)], lk = sp.ml[2 * (at + k) + 1];
+    if (lk == 0.f) continue;                        // a split without a key left its sums unset
+    const float f = mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - m);
+    l += lk * f;
+#pragma unroll
+    for (int c = 0; c < D / 64; ++c) o[c] += f * sp.sum[(at + k) * D + lane * (D / 64) + c];
+  }
+  const int i = (int)(r / a.G), h = hk * a.G + (int)(r % a.G);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  char* dst = a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h + lane * (D / 64));
+  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = E::pair(o[0] * inv, o[1] * inv);
+  else *reinterpret_cast<uint16_t*>(dst) = (uint16_t)E::pair(o[0] * inv, 0.f);
+  if (a.lse && lane == 0)
+    a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - kBias<E> + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <typename E, int D, bool kPaged>
+hipError_t launch(const AttnArgs& a, const Split& sp, hipStream_t stream) {
+  const int64_t R = (int64_t)a.T * a.G;
+  const dim3 few(sp.n, a.Hkv, a.B);
+  if (R <= 16) narrow_kernel<E, D, 1, kPaged><<<few, 256, 0, stream>>>(a, sp);
+  else if (R <= 32) narrow_kernel<E, D, 2, kPaged><<<few, 256, 0, stream>>>(a, sp);
+  else if (R <= 64) narrow_kernel<E, D, 4, kPaged><<<few, 256, 0, stream>>>(a, sp);
+  else
+    wide_kernel<E, D, kPaged><<<dim3((unsigned)((R + kWideRows - 1) / kWideRows * sp.n), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || sp.n == 1) return e;
+  combine_kernel<E, D><<<dim3((unsigned)((R + 3) / 4), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  return hipGetLastError();
 }
 
 template <typename E, int D>
-__global__ __launch_bounds__(64) void attention_kernel(AttnArgs a) {
-  using L = PageLayout<D>;
-  const int lane = threadIdx.x, i = blockIdx.x, h = blockIdx.y, b = blockIdx.z, hk = h / a.G;
-  const Seq s = sequence(a, b);
-  if (i >= s.nq) return;
-  const int pos = s.base + step(a, b, i);
-  const char* q = a.q.data + 2 * (b * a.q.b + i * a.q.t + h * a.q.h);
-  Row<D> r;
-  for (int t = 0; t < s.ctx; t += 64) {
-    const int p = t + lane;
-    const uint8_t* page = page_of(a.kv, b, t / kPage, hk);
-    float x = -INFINITY;
-    if (page && p < s.ctx && in_window(a, pos, p)) {
-      x = 0.f;
-      for (int blk = 0; blk < D / kBlock; ++blk) {
-        uint32_t y[16];
-        decode_block<E>(*reinterpret_cast<const u32x4*>(page + L::kK + lane * L::kRow + blk * 16),
-                        page[L::kKs + lane * L::kScales + blk], y);
-        for (int w = 0; w < 16; ++w) {
-          const uint32_t z = *reinterpret_cast<const uint32_t*>(q + 2 * (blk * kBlock + 2 * w));
-          x += E::lo(z) * E::lo(y[w]);
-          x += E::hi(z) * E::hi(y[w]);
-        }
-      }
-      x *= a.scale;
-    }
-    take<E, D>(r, x, [&](int j, int c) {
-      const int d = lane + 64 * c;
-      const uint8_t sc = page[L::kVs + j * L::kScales + d / kBlock];
-      const uint32_t y = sc == 255 ? E::kNaN : E::template from4<0>(page[L::kV + j * L::kRow + d / 2], scale_of(sc));
-      return d & 1 ? E::hi(y) : E::lo(y);
-    });
-  }
-  for (int t = 0; t < s.nk; t += 64) {
-    const int j = t + lane;
-    float x = -INFINITY;
-    if (j < s.nk) {
-      const int pj = (a.kv.pages ? s.base : 0) + step(a, b, j);
-      bool seen = in_window(a, pos, pj);
-      if (a.order == CADDTREE_ORDER_CHAIN) seen = seen && pj <= pos;
-      if (a.order == CADDTREE_ORDER_TREE) seen = seen && tree_sees(a, b, i, j);
-      if (seen) x = a.scale * dot<E>(q, a.k.data + 2 * (b * a.k.b + j * a.k.t + hk * a.k.h), D);
-    }
-    take<E, D>(r, x, [&](int jj, int c) {
-      const uint16_t v = *reinterpret_cast<const uint16_t*>(a.v.data + 2 * (b * a.v.b + (t + jj) * a.v.t + hk * a.v.h + lane + 64 * c));
-      return E::lo(v);
-    });
-  }
-  uint16_t* o = reinterpret_cast<uint16_t*>(a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h));
-  for (int c = 0; c < D / 64; ++c) o[lane + 64 * c] = (uint16_t)E::pair(r.m == -INFINITY ? 0.f : r.acc[c] / r.l, 0.f);
-  if (a.lse && lane == 0) a.lse[((int64_t)b * a.T + i) * a.Hq + h] = r.m == -INFINITY ? -INFINITY : r.m + __logf(r.l);
+hipError_t launch(const AttnArgs& a, const Split& sp, hipStream_t stream) {
+  return a.kv.pages ? launch<E, D, true>(a, sp, stream) : launch<E, D, false>(a, sp, stream);
 }
 
 }  // namespace
 
-hipError_t launch_attention(const AttnArgs& a, caddtree_dtype_t dtype, int32_t D, hipStream_t stream) {
-  const dim3 g(a.T, a.Hq, a.B);
-  if (dtype == CADDTREE_BF16) {
-    if (D == 64) attention_kernel<BF16, 64><<<g, 64, 0, stream>>>(a);
-    else attention_kernel<BF16, 128><<<g, 64, 0, stream>>>(a);
-  } else {
-    if (D == 64) attention_kernel<F16, 64><<<g, 64, 0, stream>>>(a);
-    else attention_kernel<F16, 128><<<g, 64, 0, stream>>>(a);
-  }
-  return hipGetLastError();
+hipError_t launch_attention(const AttnArgs& a, const Split& sp, caddtree_dtype_t dtype, int32_t D, hipStream_t stream) {
+  if (dtype == CADDTREE_BF16) return D == 64 ? launch<BF16, 64>(a, sp, stream) : launch<BF16, 128>(a, sp, stream);
+  return D == 64 ? launch<F16, 64>(a, sp, stream) : launch<F16, 128>(a, sp, stream);
 }
 
 }  // namespace caddtree

@@ -1,6 +1,7 @@
 // Host side of the attention and cache calls declared in caddtree.h: argument checks and launches on the
 // caller's stream.
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 
@@ -18,6 +19,7 @@ using caddtree::AttnArgs;
 using caddtree::PagedKV;
 using caddtree::View;
 
+constexpr int kCUs = 256;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;   // positions, and the tokens of a table, stay within int32
 
 caddtree_status_t check_type(int dtype, int32_t head_dim) {
@@ -144,9 +146,36 @@ caddtree_status_t check_workspace(const void* workspace) {
   return CADDTREE_OK;
 }
 
-caddtree_status_t run_attention(const caddtree_attention_t* a, const caddtree_cache_t* cache, hipStream_t stream) {
+// How many parts a row's keys are cut into, from the sizes alone (lengths are on the device).
+int32_t splits_of(const caddtree_attention_t* a) {
+  const int64_t rows = (int64_t)a->T * (a->n_heads / a->n_kv_heads);
+  const int64_t groups = (int64_t)a->B * a->n_kv_heads * (rows <= 64 ? 1 : (rows + 127) / 128);
+  const int64_t keys = (int64_t)a->table_pages * CADDTREE_PAGE + a->S;
+  int64_t reach = keys;
+  if (a->window > 0) reach = std::min(keys, (int64_t)a->window + a->sinks + a->T);
+  const int64_t most = std::max<int64_t>(1, reach / 256);             // at least a few tiles each
+  if (groups == 0) return 1;
+  return (int32_t)std::min<int64_t>(std::min<int64_t>(most, 128), std::max<int64_t>(1, (4 * kCUs + groups - 1) / groups));
+}
+size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
+size_t split_bytes(const caddtree_attention_t* a, int32_t n) {
+  if (n <= 1) return 0;
+  const size_t rows = (size_t)a->B * a->T * a->n_heads * n;
+  return align256(rows * 8) + rows * a->head_dim * 4;
+}
+
+caddtree_status_t run_attention(const caddtree_attention_t* a, const caddtree_cache_t* cache, void* workspace, size_t bytes,
+                                hipStream_t stream) {
   if (a->B == 0 || a->T == 0) return ok();
-  const hipError_t e = caddtree::launch_attention(args_of(a, cache), (caddtree_dtype_t)enum_value(a->dtype), a->head_dim, stream);
+  caddtree::Split sp = {1, nullptr, nullptr};
+  if (workspace != nullptr) {
+    int32_t n = splits_of(a);
+    while (n > 1 && split_bytes(a, n) > bytes) n /= 2;
+    sp.n = n;
+    sp.ml = static_cast<float*>(workspace);
+    sp.sum = reinterpret_cast<float*>(static_cast<char*>(workspace) + align256((size_t)a->B * a->T * a->n_heads * n * 8));
+  }
+  const hipError_t e = caddtree::launch_attention(args_of(a, cache), sp, (caddtree_dtype_t)enum_value(a->dtype), a->head_dim, stream);
   return e == hipSuccess ? ok() : hip_fail(e, "attention launch");
 }
 
@@ -154,9 +183,12 @@ caddtree_status_t run_attention(const caddtree_attention_t* a, const caddtree_ca
 
 extern "C" {
 
-size_t caddtree_attention_workspace_bytes(const caddtree_attention_t*) { return 0; }
+size_t caddtree_attention_workspace_bytes(const caddtree_attention_t* a) {
+  if (a == nullptr || a->B <= 0 || a->T <= 0 || a->n_kv_heads < 1 || a->n_heads < 1 || a->head_dim < 1 || a->S < 0 || a->table_pages < 0) return 0;
+  return split_bytes(a, splits_of(a));
+}
 
-caddtree_status_t caddtree_window_attention(const caddtree_attention_t* a, void* workspace, size_t, hipStream_t stream) {
+caddtree_status_t caddtree_window_attention(const caddtree_attention_t* a, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   caddtree_status_t st = check_attention(a, nullptr);
   if (st != CADDTREE_OK) return st;
   const bool some = a->B > 0 && a->T > 0;
@@ -164,11 +196,11 @@ caddtree_status_t caddtree_window_attention(const caddtree_attention_t* a, void*
   if ((st = check_view("v", a->v, some && a->S > 0)) != CADDTREE_OK) return st;
   if ((st = check_view("out", a->out, some)) != CADDTREE_OK) return st;
   if ((st = check_workspace(workspace)) != CADDTREE_OK) return st;
-  return run_attention(a, nullptr, stream);
+  return run_attention(a, nullptr, workspace, workspace_bytes, stream);
 }
 
 caddtree_status_t caddtree_cache_attention(const caddtree_cache_t* cache, const caddtree_attention_t* a, void* workspace,
-                                           size_t, hipStream_t stream) {
+                                           size_t workspace_bytes, hipStream_t stream) {
   if (cache == nullptr) return fail(CADDTREE_E_INVALID, "cache is NULL");
   caddtree_status_t st = check_attention(a, cache);
   if (st != CADDTREE_OK) return st;
@@ -180,7 +212,7 @@ caddtree_status_t caddtree_cache_attention(const caddtree_cache_t* cache, const 
       (a->mask == nullptr || enum_value(a->mask_kind) == CADDTREE_MASK_NONE))
     return fail(CADDTREE_E_INVALID, "a tree's new keys need its mask");
   if ((st = check_workspace(workspace)) != CADDTREE_OK) return st;
-  return run_attention(a, cache, stream);
+  return run_attention(a, cache, workspace, workspace_bytes, stream);
 }
 
 caddtree_status_t caddtree_cache_write(const caddtree_cache_t* cache, const caddtree_view_t* k, const caddtree_view_t* v,

@@ -41,7 +41,13 @@ struct AttnArgs {
   const int64_t* ctx_len;    // [B]
 };
 
-hipError_t launch_attention(const AttnArgs& a, caddtree_dtype_t dtype, int32_t head_dim, hipStream_t stream);
+// The tiles of a row in n parts, each a workgroup's; above 1 their results go to the workspace.
+struct Split {
+  int32_t n;
+  float* ml;                 // [B, Hkv, T G, n, 2]
+  float* sum;                // [B, Hkv, T G, n, head_dim]
+};
+hipError_t launch_attention(const AttnArgs& a, const Split& sp, caddtree_dtype_t dtype, int32_t head_dim, hipStream_t stream);
 
 struct CacheMoveArgs {       // write: views -> slots; read: slots -> views
   View k, v;

@@ -1,0 +1,198 @@
+// Device code of the attention kernels: which keys a tile of rows reads, which of them each row sees, and
+// the layouts of keys and values in LDS.
+//
+// Both kernels form S^T = K Q^T and O^T = V^T P^T, so a lane holds one query row in both products: the
+// scores' layout is the one the second product wants of its weights (the key index of a matrix
+// instruction is a sum's, any order serves), and a row's maximum and sum are a lane's own but for the
+// lanes that hold the same row.  V^T comes out of a row-major tile through the transposing LDS read.
+#pragma once
+
+#include "attn_common.h"
+
+namespace caddtree {
+namespace at {
+
+template <typename E>
+struct Mfma;
+template <>
+struct Mfma<BF16> {
+  static __device__ f32x4 m16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+  static __device__ f32x16 m32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+  }
+};
+template <>
+struct Mfma<F16> {
+  static __device__ f32x4 m16(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+  static __device__ f32x16 m32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+  }
+};
+
+// Weights are exp2(x - m + kBias): 1 at most in bf16; in f16, whose normal numbers end at 2^-14, 2^14 at
+// most, so that a weight keeps its 11 bits down to 2^-28 of the largest.
+template <typename E>
+constexpr float kBias = 0.f;
+template <>
+constexpr float kBias<F16> = 14.f;
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// The tiles that queries i0 .. i1 read: cached ones [0, a) and [b, c) of kC slots, new ones [0, d) and
+// [e, f) of kN keys (first the sinks, then the window or everything); n of them in this order.
+struct Span {
+  int a, b, c, d, e, f, n;
+};
+__device__ inline int ceil_div(int x, int y) { return (x + y - 1) / y; }
+
+template <int kC, int kN>
+__device__ Span span_of(const AttnArgs& a, const Seq& s, int i0, int i1) {
+  const bool tree = a.order == CADDTREE_ORDER_TREE, paged = a.kv.pages != nullptr;
+  Span t;
+  t.a = t.b = t.d = t.e = 0;
+  t.c = ceil_div(s.ctx, kC);
+  const int lo_idx = paged ? i0 : s.base + i0, hi_idx = paged ? i1 : s.base + i1;
+  const int hi = a.order == CADDTREE_ORDER_CHAIN ? max(0, min(hi_idx + 1, s.nk)) : s.nk;
+  t.f = ceil_div(hi, kN);
+  if (a.window != 0) {
+    const int lo = max(0, s.base + (tree ? 0 : i0) - a.window + 1);
+    t.a = ceil_div(min(a.sinks, s.ctx), kC);
+    t.b = lo >= s.ctx ? t.a : max(lo / kC, t.a);
+    t.c = lo >= s.ctx ? t.a : max(t.c, t.b);
+    if (!tree) {
+      const int lj = max(0, lo_idx - a.window + 1);
+      t.d = ceil_div(max(0, min(a.sinks - s.ctx, hi)), kN);
+      t.e = lj >= hi ? t.d : max(lj / kN, t.d);
+      t.f = lj >= hi ? t.d : max(t.f, t.e);
+    }
+  }
+  t.n = t.a + (t.c - t.b) + t.d + (t.f - t.e);
+  return t;
+}
+// tile t of a span: its first slot or key; *cached
+template <int kC, int kN>
+__device__ int tile_of(const Span& s, int t, bool* cached) {
+  *cached = true;
+  if (t < s.a) return t * kC;
+  t -= s.a;
+  if (t < s.c - s.b) return (s.b + t) * kC;
+  t -= s.c - s.b;
+  *cached = false;
+  return (t < s.d ? t : s.e + t - s.d) * kN;
+}
+
+// A query row: its query, its position, and the new key's index that its own place has.
+struct RowAt {
+  int i, pos, idx;
+};
+__device__ inline RowAt row_at(const AttnArgs& a, const Seq& s, int b, int i) {
+  return RowAt{i, s.base + step(a, b, i), a.kv.pages ? i : s.base + i};
+}
+
+__device__ inline uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
+
+// Which of the 64 slots from p0 on, or new keys from j0 on, a row sees: bit k for the k-th.
+__device__ inline uint64_t sees_cached(const AttnArgs& a, const Seq& s, const RowAt& r, int p0) {
+  uint64_t v = below(s.ctx - p0);
+  if (a.window != 0) v &= ~below(r.pos - a.window + 1 - p0) | below(a.sinks - p0);
+  return v;
+}
+__device__ inline uint64_t sees_tree(const AttnArgs& a, const Seq& s, int b, const RowAt& r, int j0) {
+  uint64_t v = 0;
+  if (r.i > 0) {                                   // bit k: node j0 + k - 1 of the mask's row i - 1
+    const int64_t row = (int64_t)b * a.cap + r.i - 1;
+    const int end = min(s.nk - j0, 64);            // (nodes at or past the tree's end are not looked at)
+    if (a.mask_kind == CADDTREE_MASK_U8) {
+      const uint8_t* m = static_cast<const uint8_t*>(a.mask) + row * a.cap + j0 - 1;
+      for (int k = j0 == 0 ? 1 : 0; k < end; ++k) v |= (uint64_t)(m[k] != 0) << k;
+    } else {
+      const int words = (a.cap + 31) / 32, w = j0 / 32;
+      const uint32_t* m = static_cast<const uint32_t*>(a.mask) + row * words;
+      v = w < words ? m[w] : 0;
+      if (w + 1 < words) v |= (uint64_t)m[w + 1] << 32;
+      v = v << 1 | (w > 0 ? m[w - 1] >> 31 : 0);
+    }
+  }
+  if (j0 == 0) v |= 1;                             // the root
+  v &= below(s.nk - j0);
+  const int depth = r.pos - s.base;
+  if (a.window != 0 && depth >= a.window) {        // ancestors further up than the window
+    for (uint64_t left = v; left; left &= left - 1) {
+      const int k = __builtin_ctzll(left), pk = s.base + step(a, b, j0 + k);
+      if (!in_window(a, r.pos, pk)) v &= ~(1ull << k);
+    }
+  }
+  return v;
+}
+__device__ inline uint64_t sees_new(const AttnArgs& a, const Seq& s, int b, const RowAt& r, int j0) {
+  if (a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, r, j0);
+  uint64_t v = below((a.order == CADDTREE_ORDER_CHAIN ? min(s.nk, r.idx + 1) : s.nk) - j0);
+  if (a.window != 0) v &= ~below(r.idx - a.window + 1 - j0) | below(a.sinks - s.ctx - j0);
+  return v;
+}
+// every query of i0 .. i1 sees all n keys of the tile
+__device__ inline bool full_cached(const AttnArgs& a, const Seq& s, int i1, int p0, int n) {
+  const int last = s.base + (a.order == CADDTREE_ORDER_TREE ? s.nq : i1);
+  return p0 + n <= s.ctx && (a.window == 0 || p0 > last - a.window || p0 + n <= a.sinks);
+}
+__device__ inline bool full_new(const AttnArgs& a, const Seq& s, int i0, int i1, int j0, int n) {
+  if (a.order == CADDTREE_ORDER_TREE) return false;
+  const int off = a.kv.pages ? 0 : s.base;
+  return j0 + n <= (a.order == CADDTREE_ORDER_CHAIN ? min(s.nk, off + i0 + 1) : s.nk) &&
+         (a.window == 0 || j0 > off + i1 - a.window || j0 + n <= a.sinks - s.ctx);
+}
+
+// LDS layouts.  A row is a token's D channels; 16-byte pieces trade places by the row so that no two lanes
+// of one access meet in a bank: keys are read 16 bytes a lane with the rows side by side, values 8 bytes a
+// lane, four rows by 32 or 64 bytes, through the transposing read.
+template <int D>
+__device__ int k_at(int row, int piece) {          // piece: 16 bytes
+  return row * (2 * D) + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
+}
+template <int D>
+__device__ int v_at(int row, int byte) {
+  const int block = byte >> 6, sub = (byte >> 4) & 3;
+  if (D == 128) return row * 256 + ((block ^ (row & 3)) << 6) + ((sub ^ (row & 3) ^ ((row >> 1) & 2)) << 4) + (byte & 15);
+  const int y = (row >> 1) & 3;
+  return row * 128 + ((block ^ (y & 1)) << 6) + ((sub ^ y) << 4) + (byte & 15);
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+// four rows of one channel: lane l of 16 gives the address of row l / 4 and channels 4 (l % 4) .. + 3 and
+// gets channel l's four rows
+__device__ inline u32x2 read_transposed(const char* lds) {
+  typedef __attribute__((address_space(3))) s16x4* P;
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds)));
+}
+
+// Values that a row does not see must not meet its weights of zero (0 x NaN), so a tile that some row sees
+// in part is staged with zeros for keys that are not there and for values that are not finite; the latter
+// are then added to the rows that see them.
+template <typename E>
+__device__ bool clean_pairs(u32x4& x) {
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if ((x[i] & E::kInf) == E::kInf) {
+      bad = true;
+      x[i] &= 0xffff0000u;
+    }
+    if ((x[i] & (E::kInf << 16)) == (E::kInf << 16)) {
+      bad = true;
+      x[i] &= 0x0000ffffu;
+    }
+  }
+  return bad;
+}
+// a value that is not finite, else 0
+template <typename E>
+__device__ float unclean(const char* row, int d) {
+  const uint16_t x = *reinterpret_cast<const uint16_t*>(row + 2 * d);
+  return (x & E::kInf) == E::kInf ? E::lo(x) : 0.f;
+}
+
+}  // namespace at
+}  // namespace caddtree
