@@ -32,9 +32,18 @@ struct PageStage {
   u32x4 vc[D / 32];
   uint32_t vs[D / 32];
 
-  __device__ void load(const uint8_t* page, int lane) {
+  __device__ void load_keys(const uint8_t* page, int lane) {
     using L = PageLayout<D>;
     const int col = lane & 15, g = lane >> 4;
+    if (page == nullptr) {
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        ks[s] = 127;
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w) kc[s][w] = 0;
+      }
+      return;
+    }
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
       const uint32_t* c = reinterpret_cast<const uint32_t*>(page + L::kK + (16 * s + col) * L::kRow + g * (D / 8));
@@ -42,24 +51,22 @@ struct PageStage {
       for (int w = 0; w < D / 32; ++w) kc[s][w] = c[w];
       ks[s] = page[L::kKs + (16 * s + col) * L::kScales + g * (D / 4) / kBlock];
     }
+  }
+  __device__ void load_values(const uint8_t* page, int lane) {
+    using L = PageLayout<D>;
+    if (page == nullptr) {
+#pragma unroll
+      for (int u = 0; u < D / 32; ++u) {
+        vc[u] = u32x4{0, 0, 0, 0};
+        vs[u] = 127;
+      }
+      return;
+    }
 #pragma unroll
     for (int u = 0; u < D / 32; ++u) {
       const int q = lane + 64 * u;
       vc[u] = *reinterpret_cast<const u32x4*>(page + L::kV + q * 16);
       vs[u] = page[L::kVs + q];
-    }
-  }
-  __device__ void clear() {
-#pragma unroll
-    for (int s = 0; s < 4; ++s) {
-      ks[s] = 127;
-#pragma unroll
-      for (int w = 0; w < D / 32; ++w) kc[s][w] = 0;
-    }
-#pragma unroll
-    for (int u = 0; u < D / 32; ++u) {
-      vc[u] = u32x4{0, 0, 0, 0};
-      vs[u] = 127;
     }
   }
   // the operand of keys 16 s .. 16 s + 15: D / 32 instructions' worth
@@ -77,12 +84,12 @@ struct PageStage {
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) out[j] = u32x4{E::kNaN, E::kNaN, E::kNaN, E::kNaN};
   }
-  // values of tokens 32 half .. + 31 into LDS.  there: tokens of the tile that are there; returns the tokens
-  // (bit by bit of the tile) that hold what is not finite, for a tile that is not seen in full
+  // values of tokens 32 half .. + 31 into LDS.  there: tokens of the tile that are there; returns whether a
+  // tile that is not seen in full had any that are not finite
   template <typename E>
-  __device__ uint64_t values(int half, char* lds, int lane, bool full, int there) const {
+  __device__ bool values(int half, char* lds, int lane, bool full, int there) const {
     constexpr int kPer = D / 32, kU = kPer / 2;    // blocks of a token; loads of a half
-    uint64_t bad = 0;
+    bool odd = false;
 #pragma unroll
     for (int v = 0; v < kU; ++v) {
       const int u = half * kU + v, q = lane + 64 * u, token = q / kPer, blk = q % kPer, row = token & 31;
@@ -93,14 +100,14 @@ struct PageStage {
         if (gone || nan)
 #pragma unroll
           for (int w = 0; w < 16; ++w) x[w] = 0;
-        for (uint64_t m = __ballot(nan); m; m &= m - 1) bad |= 1ull << ((__builtin_ctzll(m) + 64 * u) / kPer);
+        odd = odd || nan;
       }
 #pragma unroll
       for (int w = 0; w < 4; ++w)
         *reinterpret_cast<u32x4*>(lds + v_at<D>(row, blk * 64 + w * 16)) =
             u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
     }
-    return bad;
+    return odd;
   }
 };
 
@@ -110,18 +117,23 @@ struct TensorStage {
   u32x4 kr[2][D / 32];
   u32x4 vr[D / 16];
 
-  __device__ void load(const char* k, const char* v, int64_t kt, int64_t vt, int j0, int nk, int lane) {
+  __device__ void load_keys(const char* k, int64_t kt, int j0, int nk, int lane) {
     const int col = lane & 15, g = lane >> 4;
+    const char* base = k + 2 * (j0 * kt);
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      const u32x4* p = reinterpret_cast<const u32x4*>(k + 2 * (min(j0 + 16 * s + col, nk - 1) * kt + g * (D / 4)));
+    for (int s = 0; s < 2; ++s) {                   // (a key that is not there: the tile's first one in its place)
+      const u32x4* p = reinterpret_cast<const u32x4*>(base + 2 * ((j0 + 16 * s + col < nk ? (16 * s + col) * kt : 0) + g * (D / 4)));
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) kr[s][j] = p[j];
     }
+  }
+  __device__ void load_values(const char* v, int64_t vt, int j0, int nk, int lane) {
+    const char* base = v + 2 * (j0 * vt);
+    const int row = lane / (D / 8), d = lane % (D / 8) * 8;
 #pragma unroll
     for (int u = 0; u < D / 16; ++u) {
-      const int q = lane + 64 * u;
-      vr[u] = *reinterpret_cast<const u32x4*>(v + 2 * (min(j0 + q / (D / 8), nk - 1) * vt + q % (D / 8) * 8));
+      const int token = row + u * (512 / D);
+      vr[u] = *reinterpret_cast<const u32x4*>(base + 2 * ((j0 + token < nk ? token * vt : 0) + d));
     }
   }
   template <typename E>
@@ -130,19 +142,19 @@ struct TensorStage {
     for (int j = 0; j < D / 32; ++j) out[j] = kr[s][j];
   }
   template <typename E>
-  __device__ uint64_t values(int, char* lds, int lane, bool full, int there) const {
-    uint64_t bad = 0;
+  __device__ bool values(int, char* lds, int lane, bool full, int there) const {
+    bool odd = false;
 #pragma unroll
     for (int u = 0; u < D / 16; ++u) {
-      const int q = lane + 64 * u, token = q / (D / 8);
+      const int token = lane / (D / 8) + u * (512 / D);
       u32x4 x = vr[u];
       if (!full) {
         if (token >= there) x = u32x4{0, 0, 0, 0};
-        for (uint64_t m = __ballot(clean_pairs<E>(x)); m; m &= m - 1) bad |= 1ull << ((__builtin_ctzll(m) + 64 * u) / (D / 8));
+        if (clean_pairs<E>(x)) odd = true;
       }
-      *reinterpret_cast<u32x4*>(lds + v_at<D>(token, q % (D / 8) * 16)) = x;
+      *reinterpret_cast<u32x4*>(lds + v_at<D>(token, lane % (D / 8) * 16)) = x;
     }
-    return bad;
+    return odd;
   }
 };
 
@@ -153,11 +165,14 @@ struct NarrowState {
   f32x4 acc[D / 16][kR];
 };
 
-// Takes a tile of 32 kH keys.  value(token, d): a cached or new value that is not finite, else 0.
-template <typename E, int D, int kR, int kH, typename Stage, typename Value>
-__device__ void narrow_tile(NarrowState<D, kR>& st, const Stage& x, const u32x4 (&q)[kR][D / 32], float c, bool full,
-                            const uint64_t (&seen)[kR], int there, char* lds, int lane, Value value) {
+// Takes a tile of 32 kH keys.  next_keys, next_values: load the following tile's into the registers that this
+// one's have left.  Returns whether a lane met values that are not finite in a tile not seen in full.
+template <typename E, int D, int kR, int kH, typename Stage, typename NextKeys, typename NextValues>
+__device__ __forceinline__ bool narrow_tile(NarrowState<D, kR>& st, Stage& x, const u32x4 (&q)[kR][D / 32], float c, bool full,
+                            const uint64_t (&seen)[kR], int there, char* lds, int lane, NextKeys next_keys,
+                            NextValues next_values) {
   const int g = lane >> 4;
+  bool odd = false;
   f32x4 s[2 * kH][kR];
 #pragma unroll
   for (int t = 0; t < 2 * kH; ++t) {
@@ -170,6 +185,7 @@ __device__ void narrow_tile(NarrowState<D, kR>& st, const Stage& x, const u32x4 
       for (int j = 0; j < D / 32; ++j) s[t][n] = Mfma<E>::m16(k[j], q[n][j], s[t][n]);
     }
   }
+  next_keys();
   u32x4 p[kH][kR];
 #pragma unroll
   for (int n = 0; n < kR; ++n) {
@@ -179,14 +195,12 @@ __device__ void narrow_tile(NarrowState<D, kR>& st, const Stage& x, const u32x4 
     for (int t = 0; t < 2 * kH; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        float y = s[t][n][r] * c;
-        if (!full && !((bits >> (16 * t + r)) & 1)) y = -INFINITY;
-        s[t][n][r] = y;
-        top = fmaxf(top, y);
+        if (!full && !((bits >> (16 * t + r)) & 1)) s[t][n][r] = -INFINITY;
+        top = fmaxf(top, s[t][n][r]);
       }
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    const float m = fmaxf(st.m[n], top);
+    const float m = fmaxf(st.m[n], top * c);
     const float base = m == -INFINITY ? 0.f : m - kBias<E>;
     const float was = __builtin_amdgcn_exp2f(st.m[n] - kBias<E> - base);
     float sum = 0.f;
@@ -194,7 +208,7 @@ __device__ void narrow_tile(NarrowState<D, kR>& st, const Stage& x, const u32x4 
     for (int t = 0; t < 2 * kH; ++t)
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        s[t][n][r] = __builtin_amdgcn_exp2f(s[t][n][r] - base);
+        s[t][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], c, -base));
         sum += s[t][n][r];
       }
     st.l[n] = st.l[n] * was + sum;                  // (of this lane's keys: the four g are added at the end)
@@ -209,39 +223,28 @@ __device__ void narrow_tile(NarrowState<D, kR>& st, const Stage& x, const u32x4 
 #pragma unroll
   for (int h = 0; h < kH; ++h) {
     __builtin_amdgcn_wave_barrier();
-    uint64_t bad = x.template values<E>(h, lds, lane, full, there);
+    if (x.template values<E>(h, lds, lane, full, there)) odd = true;
+    if (h == kH - 1) next_values();
     __builtin_amdgcn_wave_barrier();
-    const int row = 4 * g + (lane & 15) / 4;
+    const int v0 = v_at<D>(4 * g + (lane & 15) / 4, (lane & 3) * 8);
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) {
-      const int byte = 32 * t + (lane & 3) * 8;
-      const u32x2 lo = read_transposed(lds + v_at<D>(row, byte)), hi = read_transposed(lds + v_at<D>(row + 16, byte));
+    for (int t = 0; t < D / 16; ++t) {              // (v_at of 32 t bytes further is v0 ^ 32 t; 16 rows keep its swizzle)
+      const u32x2 lo = read_transposed(lds + (v0 ^ (t << 5))), hi = read_transposed(lds + (v0 ^ (t << 5)) + 16 * 2 * D);
       const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
       for (int n = 0; n < kR; ++n) st.acc[t][n] = Mfma<E>::m16(v, p[h][n], st.acc[t][n]);
     }
-    for (; bad; bad &= bad - 1) {
-      const int token = __builtin_ctzll(bad);
-#pragma unroll
-      for (int t = 0; t < D / 16; ++t)
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const float v = value(token, 16 * t + 4 * g + r);
-#pragma unroll
-          for (int n = 0; n < kR; ++n)
-            if ((seen[n] >> token) & 1) st.acc[t][n][r] += v;
-        }
-    }
   }
+  return odd;
 }
 
 template <typename E, int D, int kR, bool kPaged>
-__global__ __launch_bounds__(256) void narrow_kernel(AttnArgs a, Split sp) {
+__global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a, Split sp) {
   using L = PageLayout<D>;
   constexpr int kVBytes = 32 * 2 * D;               // 32 tokens' values; as many fp32 sums of 16 rows
   __shared__ __align__(16) char lds[4 * kVBytes];
   __shared__ float ml[4][2][16 * kR];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 15, g = lane >> 4;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 15, g = lane >> 4;
   const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
   const Seq s = sequence(a, b);
   const int R = s.nq * a.G;
@@ -257,7 +260,7 @@ __global__ __launch_bounds__(256) void narrow_kernel(AttnArgs a, Split sp) {
     rows[n] = row_at(a, s, b, i);
     const u32x4* p = reinterpret_cast<const u32x4*>(a.q.data + 2 * (b * a.q.b + i * a.q.t + h * a.q.h + g * (D / 4)));
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j) q[n][j] = p[j];
+    for (int j = 0; j < D / 32; ++j) q[n][j] = signed_queries(p[j], a.scale);
   }
   NarrowState<D, kR> st;
 #pragma unroll
@@ -267,61 +270,93 @@ __global__ __launch_bounds__(256) void narrow_kernel(AttnArgs a, Split sp) {
 #pragma unroll
     for (int t = 0; t < D / 16; ++t) st.acc[t][n] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const float c = a.scale * kLog2e;
+  const float c = score_factor(a.scale);
   char* vt = lds + wave * kVBytes;
   uint64_t seen[kR];
+  bool odd = false;
+  const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
+  const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
+  auto sees = [&](bool cached, const RowAt& row, int at) -> uint64_t {
+    if (kPaged && cached) return sees_cached(a, s, row).at(at);
+    if (kPaged && a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, row, at);
+    return sees_new(a, s, row).at(at);
+  };
 
   int t = t0 + wave;
   if constexpr (kPaged) {
     const int nc = min(t1, span.a + span.c - span.b);    // this split's cached tiles come first
-    PageStage<D> cur, next;
-    const uint8_t* page = nullptr;
-    int p0 = 0;
-    auto fetch = [&](int tile, PageStage<D>& x) {
+    PageStage<D> x;
+    auto page_at = [&](int tile) -> const uint8_t* {
       bool cached;
-      p0 = tile_of<kPage, 32>(span, tile, &cached);
-      page = page_of(a.kv, b, p0 / kPage, hk);
-      if (page) x.load(page, lane);
-      else x.clear();
+      return tile < nc ? page_of(a.kv, b, tile_of<kPage, 32>(span, tile, &cached) / kPage, hk) : nullptr;
     };
-    if (t < nc) fetch(t, cur);
+    const uint8_t *page = page_at(t), *next = page_at(t + 4);
+    if (t < nc) {
+      x.load_keys(page, lane);
+      x.load_values(page, lane);
+    }
     for (; t < nc; t += 4) {
-      const uint8_t* now = page;
-      const int at = p0;
-      if (t + 4 < nc) fetch(t + 4, next);
-      const bool full = now && full_cached(a, s, s.nq - 1, at, kPage);
+      bool cached;
+      const int at = tile_of<kPage, 32>(span, t, &cached);
+      const uint8_t* after = page_at(t + 8);
+      const bool more = t + 4 < nc;
+      const bool full = page && full_cached(a, s, s.nq - 1, at, kPage);
 #pragma unroll
-      for (int n = 0; n < kR; ++n) seen[n] = full ? ~0ull : now ? sees_cached(a, s, rows[n], at) : 0;
-      narrow_tile<E, D, kR, 2>(st, cur, q, c, full, seen, now ? s.ctx - at : 0, vt, lane, [&](int token, int d) {
-        return now[L::kVs + token * L::kScales + d / kBlock] == 255 ? __builtin_nanf("") : 0.f;
-      });
-      cur = next;
+      for (int n = 0; n < kR; ++n) seen[n] = full ? ~0ull : page ? sees(true, rows[n], at) : 0;
+      if (narrow_tile<E, D, kR, 2>(
+              st, x, q, c, full, seen, page ? s.ctx - at : 0, vt, lane, [&] { if (more) x.load_keys(next, lane); },
+              [&] { if (more) x.load_values(next, lane); }))
+        odd = true;
+      page = next;
+      next = after;
     }
   }
   {
-    const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
-    const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
-    TensorStage<D> cur, next;
+    TensorStage<D> x;
     bool cached;
     int at = 0;
     if (t < t1) {
       at = tile_of<kPage, 32>(span, t, &cached);
-      cur.load(kb, vb, a.k.t, a.v.t, at, s.nk, lane);
+      x.load_keys(kb, a.k.t, at, s.nk, lane);
+      x.load_values(vb, a.v.t, at, s.nk, lane);
     }
     for (; t < t1; t += 4) {
-      int after = 0;
-      if (t + 4 < t1) {
-        after = tile_of<kPage, 32>(span, t + 4, &cached);
-        next.load(kb, vb, a.k.t, a.v.t, after, s.nk, lane);
-      }
+      const bool more = t + 4 < t1;
+      const int after = more ? tile_of<kPage, 32>(span, t + 4, &cached) : 0;
       const bool full = full_new(a, s, 0, s.nq - 1, at, 32);
 #pragma unroll
-      for (int n = 0; n < kR; ++n) seen[n] = full ? ~0ull : sees_new(a, s, b, rows[n], at);
-      narrow_tile<E, D, kR, 1>(st, cur, q, c, full, seen, s.nk - at, vt, lane, [&](int token, int d) {
-        return unclean<E>(vb + 2 * ((at + token) * a.v.t), d);
-      });
-      cur = next;
+      for (int n = 0; n < kR; ++n)
+        seen[n] = full ? ~0ull : sees(false, rows[n], at);
+      if (narrow_tile<E, D, kR, 1>(
+              st, x, q, c, full, seen, s.nk - at, vt, lane, [&] { if (more) x.load_keys(kb, a.k.t, after, s.nk, lane); },
+              [&] { if (more) x.load_values(vb, a.v.t, after, s.nk, lane); }))
+        odd = true;
       at = after;
+    }
+  }
+  if (__any(odd)) {
+    for (t = t0 + wave; t < t1; t += 4) {
+      bool cached;
+      const int at = tile_of<kPage, 32>(span, t, &cached), n = min(cached ? 64 : 32, (cached ? s.ctx : s.nk) - at);
+      const uint8_t* page = kPaged && cached ? page_of(a.kv, b, at / kPage, hk) : nullptr;
+      if (cached ? page == nullptr || full_cached(a, s, s.nq - 1, at, kPage) : full_new(a, s, 0, s.nq - 1, at, 32)) continue;
+#pragma unroll
+      for (int r = 0; r < kR; ++r) seen[r] = sees(cached, rows[r], at);
+      for (int token = 0; token < n; ++token) {
+#pragma unroll
+        for (int u = 0; u < D / 16; ++u) {
+          f32x4 v;
+          if (kPaged && cached) {
+            const float x = page[L::kVs + token * L::kScales + 16 * u / kBlock] == 255 ? __builtin_nanf("") : 0.f;
+            v = f32x4{x, x, x, x};
+          } else {
+            v = unclean<E>(vb + 2 * ((at + token) * a.v.t + 16 * u + 4 * g));
+          }
+#pragma unroll
+          for (int r = 0; r < kR; ++r)
+            if ((seen[r] >> token) & 1) st.acc[u][r] += v;
+        }
+      }
     }
   }
 
@@ -388,7 +423,6 @@ __global__ __launch_bounds__(256) void narrow_kernel(AttnArgs a, Split sp) {
 
 // ---------------------------------------------------------------- many rows
 
-constexpr int kWideRows = 128;
 
 // A tile's 64 keys and values on their way to LDS, a workgroup's 256 threads' shares.
 template <int D>
@@ -396,24 +430,29 @@ struct WideTensor {
   static constexpr int kN = D / 32;                 // 16-byte pieces of keys, and of values, a thread
   u32x4 k[kN], v[kN];
   __device__ void load(const char* kp, const char* vp, int64_t kt, int64_t vt, int j0, int nk, int tid) {
+    const char *kb = kp + 2 * (j0 * kt), *vb = vp + 2 * (j0 * vt);
+    const int row = tid / (D / 8), d = tid % (D / 8) * 8;
+    const int64_t ko = row * kt + d, vo = row * vt + d;
 #pragma unroll
-    for (int u = 0; u < kN; ++u) {
-      const int q = tid + 256 * u, token = min(j0 + q / (D / 8), nk - 1), d = q % (D / 8) * 8;
-      k[u] = *reinterpret_cast<const u32x4*>(kp + 2 * (token * kt + d));
-      v[u] = *reinterpret_cast<const u32x4*>(vp + 2 * (token * vt + d));
+    for (int u = 0; u < kN; ++u) {                  // (a key that is not there: the tile's first one in its place)
+      const int token = u * (2048 / D);             // ... rows further
+      const bool there = j0 + token + row < nk;
+      k[u] = *reinterpret_cast<const u32x4*>(kb + 2 * (there ? token * kt + ko : d));
+      v[u] = *reinterpret_cast<const u32x4*>(vb + 2 * (there ? token * vt + vo : d));
     }
   }
   template <typename E>
-  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* bad) {
+  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* odd) {
+    const int row = tid / (D / 8), piece = tid % (D / 8), k0 = k_at<D>(row, piece), v0 = v_at<D>(row, piece * 16);
 #pragma unroll
-    for (int u = 0; u < kN; ++u) {
-      const int q = tid + 256 * u, token = q / (D / 8), piece = q % (D / 8);
+    for (int u = 0; u < kN; ++u) {                  // (16 or 32 rows further: the same swizzle)
+      const int token = row + u * (2048 / D);
       if (!full) {
         if (token >= there) v[u] = u32x4{0, 0, 0, 0};
-        if (clean_pairs<E>(v[u])) atomicOr(&bad[token >> 5], 1u << (token & 31));
+        if (clean_pairs<E>(v[u])) *odd = 1;
       }
-      *reinterpret_cast<u32x4*>(kl + k_at<D>(token, piece)) = k[u];
-      *reinterpret_cast<u32x4*>(vl + v_at<D>(token, piece * 16)) = v[u];
+      *reinterpret_cast<u32x4*>(kl + k0 + u * 4096) = k[u];
+      *reinterpret_cast<u32x4*>(vl + v0 + u * 4096) = v[u];
     }
   }
 };
@@ -437,7 +476,7 @@ struct WidePage {
     vs = page[L::kVs + tid];
   }
   template <typename E>
-  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* bad) {
+  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* odd) {
     if (tid >= kThreads) return;
     const int token = tid / (D / kBlock), blk = tid % (D / kBlock);
     uint32_t x[16];
@@ -448,7 +487,7 @@ struct WidePage {
     decode_block<E>(v, vs, x);
     if (!full) {
       const bool gone = token >= there, nan = !gone && vs == 255;
-      if (nan) atomicOr(&bad[token >> 5], 1u << (token & 31));
+      if (nan) *odd = 1;
       if (gone || nan)
 #pragma unroll
         for (int w = 0; w < 16; ++w) x[w] = 0;
@@ -459,147 +498,220 @@ struct WidePage {
   }
 };
 
-template <typename E, int D, bool kPaged>
+// A row's running softmax: lane (col, half) has row col and channels 32 d + 8 (e / 4) + 4 half + e % 4.
+template <int D>
+struct WideState {
+  float m = -INFINITY, l = 0.f;
+  f32x16 acc[D / 32];
+};
+
+// Takes 32 kU keys of a tile in LDS, k0 and v0 being the lane's first places: 16 j channels further is
+// k0 ^ 32 j, 32 d channels v0 ^ 64 d, and 8, 16 or 32 rows keep the swizzle.
+template <typename E, int D, int kU>
+__device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D / 16], const char* kl, const char* vl, int k0,
+                                          int v0, float c, bool full, uint64_t seen) {
+  f32x16 x[kU];                                     // row col's keys 32 u + 8 (e / 4) + 4 half + e % 4
+#pragma unroll
+  for (int u = 0; u < kU; ++u) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[u][e] = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j)
+      x[u] = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(kl + (k0 ^ (j << 5)) + u * 32 * 2 * D), q[j], x[u]);
+  }
+  if (!full) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[u][e] = (seen >> (32 * u + 8 * (e / 4) + e % 4)) & 1 ? x[u][e] : -INFINITY;
+  }
+  float top = -INFINITY;
+#pragma unroll
+  for (int u = 0; u < kU; ++u)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) top = fmaxf(top, x[u][e]);
+  top = fmaxf(top, __shfl_xor(top, 32));
+  const float m = fmaxf(st.m, top * c);
+  const float base = m == -INFINITY ? 0.f : m - kBias<E>;
+  if (__any(m > st.m)) {
+    const float was = __builtin_amdgcn_exp2f(st.m - kBias<E> - base);
+    st.l *= was;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) st.acc[d] *= was;
+    st.m = m;
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int u = 0; u < kU; ++u)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      x[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][e], c, -base));
+      sum += x[u][e];
+    }
+  st.l += sum;                                      // (of this half's keys)
+#pragma unroll
+  for (int u = 0; u < 2 * kU; ++u) {                // 16 keys an instruction
+    const f32x16& y = x[u / 2];
+    const int e = 8 * (u & 1);
+    const u32x4 p = {E::pair(y[e], y[e + 1]), E::pair(y[e + 2], y[e + 3]), E::pair(y[e + 4], y[e + 5]), E::pair(y[e + 6], y[e + 7])};
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      const char* at = vl + (v0 ^ (d << 6)) + u * 16 * 2 * D;
+      const u32x2 lo = read_transposed(at), hi = read_transposed(at + 8 * 2 * D);
+      st.acc[d] = Mfma<E>::m32(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, st.acc[d]);
+    }
+  }
+}
+
+// kW wavefronts of the four share out the rows, 32 each; with kW = 2 the two pairs take half of a tile's keys
+// each and join their sums at the end.
+template <typename E, int D, int kW, bool kPaged>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   using L = PageLayout<D>;
-  __shared__ __align__(16) char kl[64 * 2 * D];
-  __shared__ __align__(16) char vl[64 * 2 * D];
-  __shared__ uint32_t bad[2][2];
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, col = lane & 31, half = lane >> 5;
+  constexpr int kRows = 32 * kW, kU = kW / 2;       // rows of a workgroup; 32-key parts of a tile a wavefront
+  __shared__ __align__(16) char lds[2][64 * 2 * D];
+  __shared__ uint32_t odd;                          // a tile not seen in full had values that are not finite
+  char *const kl = lds[0], *const vl = lds[1];
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int split = blockIdx.x % sp.n, tile_row = blockIdx.x / sp.n, hk = blockIdx.y, b = blockIdx.z;
   const Seq s = sequence(a, b);
-  const int R = s.nq * a.G, r0 = tile_row * kWideRows;
+  const int R = s.nq * a.G, r0 = tile_row * kRows;
   if (r0 >= R) return;
-  const int i0 = r0 / a.G, i1 = min(R - 1, r0 + kWideRows - 1) / a.G;
+  const int i0 = r0 / a.G, i1 = min(R - 1, r0 + kRows - 1) / a.G;
   const Span span = span_of<kPage, 64>(a, s, i0, i1);
   const int per = ceil_div(span.n, sp.n), t0 = split * per, t1 = min(span.n, t0 + per);
+  const int nc = kPaged ? max(t0, min(t1, span.a + span.c - span.b)) : t0;   // this split's cached tiles come first
 
-  const int r = r0 + 32 * wave + col, rr = min(r, R - 1), i = rr / a.G, h = hk * a.G + rr % a.G;
-  const bool mine = r0 + 32 * wave < R;             // this wavefront has rows
+  const int r = r0 + 32 * (wave % kW) + col, rr = min(r, R - 1), i = rr / a.G, h = hk * a.G + rr % a.G;
+  const int u0 = kW == 4 ? 0 : wave / kW;           // its first 32-key part
+  const bool mine = r0 + 32 * (wave % kW) < R;      // this wavefront has rows
   const RowAt row = row_at(a, s, b, i);
   u32x4 q[D / 16];
   {
     const u32x4* p = reinterpret_cast<const u32x4*>(a.q.data + 2 * (b * a.q.b + i * a.q.t + h * a.q.h + half * 8));
 #pragma unroll
-    for (int j = 0; j < D / 16; ++j) q[j] = p[2 * j];
+    for (int j = 0; j < D / 16; ++j) q[j] = signed_queries(p[2 * j], a.scale);
   }
-  float m = -INFINITY, l = 0.f;
-  f32x16 acc[D / 32];
+  WideState<D> st;
 #pragma unroll
   for (int t = 0; t < D / 32; ++t)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
-  const float c = a.scale * kLog2e;
+    for (int e = 0; e < 16; ++e) st.acc[t][e] = 0.f;
+  const int k0 = k_at<D>(32 * u0 + col, half);
+  const int v0 = v_at<D>(32 * u0 + 4 * half + (lane & 15) / 4, ((lane >> 4) & 1) * 32 + (lane & 3) * 8);
+  const int shift = 4 * half + 32 * u0;             // a lane's first key in a tile
+  const float c = score_factor(a.scale);
+  if (tid == 0) odd = 0;
+
   const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
   const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
-
-  WideTensor<D> xt;
-  WidePage<D> xp;
-  const uint8_t* page = nullptr;
-  bool cached = false;
-  int at = 0;
-  auto fetch = [&](int t) {
-    at = tile_of<kPage, 64>(span, t, &cached);
-    if (kPaged && cached) {
-      page = page_of(a.kv, b, at / kPage, hk);
-      xp.load(page, tid);
-    } else {
-      xt.load(kb, vb, a.k.t, a.v.t, at, s.nk, tid);
-    }
+  auto sees = [&](bool cached, int at) -> uint64_t {
+    if (kPaged && cached) return sees_cached(a, s, row).at(at);
+    if (kPaged && a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, row, at);
+    return sees_new(a, s, row).at(at);
   };
-  if (t0 < t1) fetch(t0);
-  if (tid < 4) (&bad[0][0])[tid] = 0;
-  for (int t = t0; t < t1; ++t) {
-    const bool of_page = kPaged && cached;
-    const uint8_t* now = page;
-    const int here = at;
-    const bool full = of_page ? now && full_cached(a, s, i1, here, 64) : full_new(a, s, i0, i1, here, 64);
-    __syncthreads();                                // the last tile has been read
-    uint32_t* flags = bad[t & 1];
-    if (of_page) xp.template store<E>(kl, vl, tid, full, now ? s.ctx - here : 0, flags);
-    else xt.template store<E>(kl, vl, tid, full, s.nk - here, flags);
-    if (t + 1 < t1) fetch(t + 1);
-    __syncthreads();
-    if (tid < 2) bad[(t + 1) & 1][tid] = 0;         // (read last before the barrier above)
-    if (!mine) continue;
-    // scores: lane (col, half) has row col's keys 32 u + 8 (e / 4) + 4 half + e % 4
-    f32x16 x[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) x[u][e] = 0.f;
-#pragma unroll
-      for (int j = 0; j < D / 16; ++j)
-        x[u] = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(kl + k_at<D>(32 * u + col, 2 * j + half)), q[j], x[u]);
+
+  int t = t0;
+  if constexpr (kPaged) {
+    WidePage<D> x;
+    const uint8_t* page = nullptr;
+    int at = 0;
+    auto fetch = [&](int tile) {
+      bool cached;
+      at = tile_of<kPage, 64>(span, tile, &cached);
+      page = page_of(a.kv, b, at / kPage, hk);
+      x.load(page, tid);
+    };
+    if (t < nc) fetch(t);
+    for (; t < nc; ++t) {
+      const uint8_t* now = page;
+      const int here = at;
+      const bool full = now && full_cached(a, s, i1, here, 64);
+      __syncthreads();                              // the last tile has been read
+      x.template store<E>(kl, vl, tid, full, now ? s.ctx - here : 0, &odd);
+      if (t + 1 < nc) fetch(t + 1);
+      __syncthreads();
+      if (!mine) continue;
+      wide_tile<E, D, kU>(st, q, kl, vl, k0, v0, c, full, full ? 0 : now ? sees(true, here) >> shift : 0);
     }
-    float top = -INFINITY;
-    uint64_t seen = ~0ull;
-    if (!full) {
-      seen = of_page ? (now ? sees_cached(a, s, row, here) : 0) : sees_new(a, s, b, row, here);
-      const uint64_t bits = seen >> (4 * half);
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          x[u][e] = (bits >> (32 * u + 8 * (e / 4) + e % 4)) & 1 ? x[u][e] * c : -INFINITY;
-    } else {
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[u][e] *= c;
+  }
+  {
+    WideTensor<D> x;
+    int at = 0;
+    auto fetch = [&](int tile) {
+      bool cached;
+      at = tile_of<kPage, 64>(span, tile, &cached);
+      x.load(kb, vb, a.k.t, a.v.t, at, s.nk, tid);
+    };
+    if (t < t1) fetch(t);
+    for (; t < t1; ++t) {
+      const int here = at;
+      const bool full = full_new(a, s, i0, i1, here, 64);
+      __syncthreads();
+      x.template store<E>(kl, vl, tid, full, s.nk - here, &odd);
+      if (t + 1 < t1) fetch(t + 1);
+      __syncthreads();
+      if (!mine) continue;
+      wide_tile<E, D, kU>(st, q, kl, vl, k0, v0, c, full, full ? 0 : sees(false, here) >> shift);
     }
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, x[u][e]);
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float mm = fmaxf(m, top);
-    const float base = mm == -INFINITY ? 0.f : mm - kBias<E>;
-    if (__any(mm > m)) {
-      const float was = __builtin_amdgcn_exp2f(m - kBias<E> - base);
-      l *= was;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) acc[d] *= was;
-      m = mm;
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[u][e] = __builtin_amdgcn_exp2f(x[u][e] - base);
-        sum += x[u][e];
-      }
-    l += sum;                                       // (of this half's keys)
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {                   // 16 keys an instruction
-      const f32x16& y = x[u / 2];
-      const int e = 8 * (u & 1);
-      const u32x4 p = {E::pair(y[e], y[e + 1]), E::pair(y[e + 2], y[e + 3]), E::pair(y[e + 4], y[e + 5]), E::pair(y[e + 6], y[e + 7])};
-      const int key = 16 * u + 4 * half + (lane & 15) / 4;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) {
-        const int byte = 64 * d + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
-        const u32x2 lo = read_transposed(vl + v_at<D>(key, byte)), hi = read_transposed(vl + v_at<D>(key + 8, byte));
-        acc[d] = Mfma<E>::m32(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, acc[d]);
-      }
-    }
-    if (!full) {
-      for (uint64_t left = (uint64_t)flags[1] << 32 | flags[0]; left; left &= left - 1) {
-        const int token = __builtin_ctzll(left);
+  }
+  __syncthreads();
+  if (odd && mine) {
+    for (t = t0; t < t1; ++t) {
+      bool cached;
+      const int at = tile_of<kPage, 64>(span, t, &cached), n = min(64, (cached ? s.ctx : s.nk) - at);
+      const uint8_t* page = kPaged && cached ? page_of(a.kv, b, at / kPage, hk) : nullptr;
+      if (cached ? page == nullptr || full_cached(a, s, i1, at, 64) : full_new(a, s, i0, i1, at, 64)) continue;
+      const uint64_t seen = sees(cached, at);
+      for (int token = 32 * u0; token < min(n, 32 * (u0 + kU)); ++token) {
 #pragma unroll
         for (int d = 0; d < D / 32; ++d)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int ch = 32 * d + 8 * (e / 4) + 4 * half + e % 4;
-            const float v = of_page ? (now[L::kVs + token * L::kScales + ch / kBlock] == 255 ? __builtin_nanf("") : 0.f)
-                                    : unclean<E>(vb + 2 * ((here + token) * a.v.t), ch);
-            if ((seen >> token) & 1) acc[d][e] += v;
+          for (int e = 0; e < 4; ++e) {
+            f32x4 v;
+            if (kPaged && cached) {
+              const float x = page[L::kVs + token * L::kScales + d] == 255 ? __builtin_nanf("") : 0.f;
+              v = f32x4{x, x, x, x};
+            } else {
+              v = unclean<E>(vb + 2 * ((at + token) * a.v.t + 32 * d + 8 * e + 4 * half));
+            }
+            if ((seen >> token) & 1)
+#pragma unroll
+              for (int k = 0; k < 4; ++k) st.acc[d][4 * e + k] += v[k];
           }
       }
     }
   }
+  float m = st.m, l = st.l;
+  f32x16(&acc)[D / 32] = st.acc;
   l += __shfl_xor(l, 32);
+  if (kW == 2) {                                    // the second pair's sums to the first, 16 registers at a time
+    __syncthreads();
+    float* box = reinterpret_cast<float*>(lds) + (wave & 1) * 1024 + lane;   // 2 x 64 lanes x 16 values, the lanes side by side
+    float* box_ml = reinterpret_cast<float*>(lds) + 2 * 1024 + (wave & 1) * 128 + lane;
+    if (wave >= 2) {
+      box_ml[0] = m;
+      box_ml[64] = l;
+    }
+    __syncthreads();
+    const float m2 = box_ml[0], l2 = box_ml[64], mm = fmaxf(m, m2);
+    const float f1 = l == 0.f ? 0.f : m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mm);
+    const float f2 = l2 == 0.f ? 0.f : m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mm);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) {
+      if (wave >= 2)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) box[64 * e] = acc[d][e];
+      __syncthreads();
+      if (wave < 2)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[d][e] = acc[d][e] * f1 + box[64 * e] * f2;
+      __syncthreads();
+    }
+    if (wave >= 2) return;
+    l = l * f1 + l2 * f2;
+    m = mm;
+  }
   if (r >= R) return;
   if (sp.n == 1) {
     const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -661,9 +773,8 @@ hipError_t launch(const AttnArgs& a, const Split& sp, hipStream_t stream) {
   const dim3 few(sp.n, a.Hkv, a.B);
   if (R <= 16) narrow_kernel<E, D, 1, kPaged><<<few, 256, 0, stream>>>(a, sp);
   else if (R <= 32) narrow_kernel<E, D, 2, kPaged><<<few, 256, 0, stream>>>(a, sp);
-  else if (R <= 64) narrow_kernel<E, D, 4, kPaged><<<few, 256, 0, stream>>>(a, sp);
-  else
-    wide_kernel<E, D, kPaged><<<dim3((unsigned)((R + kWideRows - 1) / kWideRows * sp.n), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  else if (R <= 64) wide_kernel<E, D, 2, kPaged><<<few, 256, 0, stream>>>(a, sp);
+  else wide_kernel<E, D, 4, kPaged><<<dim3((unsigned)((R + 127) / 128 * sp.n), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.n == 1) return e;
   combine_kernel<E, D><<<dim3((unsigned)((R + 3) / 4), a.Hkv, a.B), 256, 0, stream>>>(a, sp);

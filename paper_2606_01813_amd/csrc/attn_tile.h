@@ -41,6 +41,14 @@ template <>
 constexpr float kBias<F16> = 14.f;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
+// Scores are kept unscaled, so that a weight is one fused multiply-add and one exp2: exp2(s c - base) with
+// c > 0.  A negative scale goes into the signs of q, and a scale of zero is one too small to matter.
+__device__ inline float score_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-30f); }
+__device__ inline u32x4 signed_queries(u32x4 q, float scale) {
+  const uint32_t flip = scale < 0.f ? 0x80008000u : 0u;
+  return u32x4{q[0] ^ flip, q[1] ^ flip, q[2] ^ flip, q[3] ^ flip};
+}
+
 // The tiles that queries i0 .. i1 read: cached ones [0, a) and [b, c) of kC slots, new ones [0, d) and
 // [e, f) of kN keys (first the sinks, then the window or everything); n of them in this order.
 struct Span {
@@ -95,10 +103,16 @@ __device__ inline RowAt row_at(const AttnArgs& a, const Seq& s, int b, int i) {
 __device__ inline uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
 // Which of the 64 slots from p0 on, or new keys from j0 on, a row sees: bit k for the k-th.
-__device__ inline uint64_t sees_cached(const AttnArgs& a, const Seq& s, const RowAt& r, int p0) {
-  uint64_t v = below(s.ctx - p0);
-  if (a.window != 0) v &= ~below(r.pos - a.window + 1 - p0) | below(a.sinks - p0);
-  return v;
+struct Sees {
+  int slots, from, sinks;       // of keys: below `slots`, and from `from` on or below `sinks`
+  __device__ uint64_t at(int k0) const { return below(slots - k0) & (~below(from - k0) | below(sinks - k0)); }
+};
+__device__ inline Sees sees_cached(const AttnArgs& a, const Seq& s, const RowAt& r) {
+  return Sees{s.ctx, a.window == 0 ? 0 : r.pos - a.window + 1, a.sinks};
+}
+__device__ inline Sees sees_new(const AttnArgs& a, const Seq& s, const RowAt& r) {   // (chains and blocks)
+  return Sees{a.order == CADDTREE_ORDER_CHAIN ? min(s.nk, r.idx + 1) : s.nk, a.window == 0 ? 0 : r.idx - a.window + 1,
+              a.sinks - s.ctx};
 }
 __device__ inline uint64_t sees_tree(const AttnArgs& a, const Seq& s, int b, const RowAt& r, int j0) {
   uint64_t v = 0;
@@ -125,12 +139,6 @@ __device__ inline uint64_t sees_tree(const AttnArgs& a, const Seq& s, int b, con
       if (!in_window(a, r.pos, pk)) v &= ~(1ull << k);
     }
   }
-  return v;
-}
-__device__ inline uint64_t sees_new(const AttnArgs& a, const Seq& s, int b, const RowAt& r, int j0) {
-  if (a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, r, j0);
-  uint64_t v = below((a.order == CADDTREE_ORDER_CHAIN ? min(s.nk, r.idx + 1) : s.nk) - j0);
-  if (a.window != 0) v &= ~below(r.idx - a.window + 1 - j0) | below(a.sinks - s.ctx - j0);
   return v;
 }
 // every query of i0 .. i1 sees all n keys of the tile
@@ -169,8 +177,9 @@ __device__ inline u32x2 read_transposed(const char* lds) {
 }
 
 // Values that a row does not see must not meet its weights of zero (0 x NaN), so a tile that some row sees
-// in part is staged with zeros for keys that are not there and for values that are not finite; the latter
-// are then added to the rows that see them.
+// in part is staged with zeros for keys that are not there and for values that are not finite.  Where there
+// were any of the latter, the tiles are gone over again at the end and they are added to the rows that see
+// them: what is not finite outlasts any later rescaling, so it does not matter when it is added.
 template <typename E>
 __device__ bool clean_pairs(u32x4& x) {
   bool bad = false;
@@ -187,11 +196,17 @@ __device__ bool clean_pairs(u32x4& x) {
   }
   return bad;
 }
-// a value that is not finite, else 0
+// four channels of a value row, what is finite among them replaced by 0
 template <typename E>
-__device__ float unclean(const char* row, int d) {
-  const uint16_t x = *reinterpret_cast<const uint16_t*>(row + 2 * d);
-  return (x & E::kInf) == E::kInf ? E::lo(x) : 0.f;
+__device__ f32x4 unclean(const char* at) {
+  const u32x2 x = *reinterpret_cast<const u32x2*>(at);
+  f32x4 v;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    v[2 * i] = (x[i] & E::kInf) == E::kInf ? E::lo(x[i]) : 0.f;
+    v[2 * i + 1] = (x[i] & (E::kInf << 16)) == (E::kInf << 16) ? E::hi(x[i]) : 0.f;
+  }
+  return v;
 }
 
 }  // namespace at
