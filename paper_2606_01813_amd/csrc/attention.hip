@@ -201,8 +201,8 @@ __device__ __forceinline__ bool narrow_tile(NarrowState<D, kR>& st, Stage& x, co
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
     const float m = fmaxf(st.m[n], top * c);
-    const float base = m == -INFINITY ? 0.f : m - kBias<E>;
-    const float was = __builtin_amdgcn_exp2f(st.m[n] - kBias<E> - base);
+    const float base = m == -INFINITY ? 0.f : m - E::kBias;
+    const float was = __builtin_amdgcn_exp2f(st.m[n] - E::kBias - base);
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < 2 * kH; ++t)
@@ -406,7 +406,7 @@ __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a, Split sp) {
           *reinterpret_cast<u32x2*>(dst + 2 * j) = y;
         }
         if (a.lse && part == 0)
-          a.lse[((int64_t)b * a.T + i) * a.Hq + h] = ll == 0.f ? -INFINITY : (mm - kBias<E> + __builtin_amdgcn_logf(ll)) * kLn2;
+          a.lse[((int64_t)b * a.T + i) * a.Hq + h] = ll == 0.f ? -INFINITY : (mm - E::kBias + __builtin_amdgcn_logf(ll)) * kLn2;
       } else {
         const int64_t at = part_of(a, sp, b, hk, r) + split;
         if (part == 0) {
@@ -532,9 +532,9 @@ __device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D /
     for (int e = 0; e < 16; ++e) top = fmaxf(top, x[u][e]);
   top = fmaxf(top, __shfl_xor(top, 32));
   const float m = fmaxf(st.m, top * c);
-  const float base = m == -INFINITY ? 0.f : m - kBias<E>;
+  const float base = m == -INFINITY ? 0.f : m - E::kBias;
   if (__any(m > st.m)) {
-    const float was = __builtin_amdgcn_exp2f(st.m - kBias<E> - base);
+    const float was = __builtin_amdgcn_exp2f(st.m - E::kBias - base);
     st.l *= was;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) st.acc[d] *= was;
@@ -724,7 +724,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
         *reinterpret_cast<u32x2*>(dst + 2 * (32 * d + 8 * e + 4 * half)) = y;
       }
     if (a.lse && half == 0)
-      a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - kBias<E> + __builtin_amdgcn_logf(l)) * kLn2;
+      a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - E::kBias + __builtin_amdgcn_logf(l)) * kLn2;
   } else {
     const int64_t to = part_of(a, sp, b, hk, r) + split;
     if (half == 0) {
@@ -764,7 +764,7 @@ __global__ __launch_bounds__(256) void combine_kernel(AttnArgs a, Split sp) {
   if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = E::pair(o[0] * inv, o[1] * inv);
   else *reinterpret_cast<uint16_t*>(dst) = (uint16_t)E::pair(o[0] * inv, 0.f);
   if (a.lse && lane == 0)
-    a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - kBias<E> + __builtin_amdgcn_logf(l)) * kLn2;
+    a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - E::kBias + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <typename E, int D, bool kPaged>

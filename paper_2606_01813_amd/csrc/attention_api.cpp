@@ -223,7 +223,8 @@ caddtree_status_t caddtree_cache_write(const caddtree_cache_t* cache, const cadd
   if (st != CADDTREE_OK) return st;
   if ((st = check_batch(B)) != CADDTREE_OK) return st;
   if (T < 0 || rows < 0) return fail(CADDTREE_E_INVALID, "T = %d and rows = %d must not be negative", T, rows);
-  if (T > kMaxTokens) return fail(CADDTREE_E_UNSUPPORTED, "T = %d exceeds 2^30", T);
+  if ((int64_t)T * cache->n_kv_heads > kMaxTokens)
+    return fail(CADDTREE_E_UNSUPPORTED, "T = %d tokens of %d heads exceed 2^30", T, cache->n_kv_heads);
   if (index == nullptr && rows < T) return fail(CADDTREE_E_INVALID, "rows = %d hold fewer than T = %d tokens", rows, T);
   if (k == nullptr || v == nullptr) return fail(CADDTREE_E_INVALID, "k and v are required");
   if ((st = check_table("page_table", page_table, table_pages)) != CADDTREE_OK) return st;
@@ -244,7 +245,8 @@ caddtree_status_t caddtree_cache_read(const caddtree_cache_t* cache, const caddt
   if (st != CADDTREE_OK) return st;
   if ((st = check_batch(B)) != CADDTREE_OK) return st;
   if (T < 0) return fail(CADDTREE_E_INVALID, "T = %d must not be negative", T);
-  if (T > kMaxTokens) return fail(CADDTREE_E_UNSUPPORTED, "T = %d exceeds 2^30", T);
+  if ((int64_t)T * cache->n_kv_heads > kMaxTokens)
+    return fail(CADDTREE_E_UNSUPPORTED, "T = %d tokens of %d heads exceed 2^30", T, cache->n_kv_heads);
   if (k == nullptr || v == nullptr) return fail(CADDTREE_E_INVALID, "k and v are required");
   if ((st = check_table("page_table", page_table, table_pages)) != CADDTREE_OK) return st;
   const bool some = B > 0 && T > 0 && table_pages > 0;

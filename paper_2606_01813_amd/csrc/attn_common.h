@@ -22,10 +22,13 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // The 16-bit element types: pairs in a 32-bit register, the 4-bit conversions (exact: a code times a
-// power of two) and the range of the scales' exponents.
+// power of two) and the range of the scales' exponents.  Weights of the softmax are exp2(x - m + kBias):
+// 1 at most in bf16; in f16, whose normal numbers end at 2^-14, 2^14 at most, so that a weight keeps its 11
+// bits down to 2^-28 of the largest.
 struct BF16 {
   using T = __bf16;
   static constexpr int kExpLo = -125, kExpHi = 125;
+  static constexpr float kBias = 0.f;
   static constexpr uint32_t kInf = 0x7f80;            // exponent bits, all ones for NaN and infinities
   static constexpr uint32_t kNaN = 0x7fc07fc0;        // a pair
   static __device__ float lo(uint32_t p) { return __builtin_bit_cast(float, p << 16); }
@@ -48,6 +51,7 @@ struct BF16 {
 struct F16 {
   using T = _Float16;
   static constexpr int kExpLo = -13, kExpHi = 13;
+  static constexpr float kBias = 14.f;
   static constexpr uint32_t kInf = 0x7c00;
   static constexpr uint32_t kNaN = 0x7e007e00;
   static __device__ float lo(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[0]; }

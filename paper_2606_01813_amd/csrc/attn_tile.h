@@ -33,12 +33,6 @@ struct Mfma<F16> {
   }
 };
 
-// Weights are exp2(x - m + kBias): 1 at most in bf16; in f16, whose normal numbers end at 2^-14, 2^14 at
-// most, so that a weight keeps its 11 bits down to 2^-28 of the largest.
-template <typename E>
-constexpr float kBias = 0.f;
-template <>
-constexpr float kBias<F16> = 14.f;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Scores are kept unscaled, so that a weight is one fused multiply-add and one exp2: exp2(s c - base) with
