@@ -179,3 +179,18 @@ def call_spec(lib_, handle: int, device: int, L: int, V: int, K: int, cap: int, 
            lib_.caddtree_emit, lib_.caddtree_accept)
     return binding().spec(handle, device, L, V, K, cap, DTYPES[dtype], MASKS[mask],
                           *(ctypes.cast(f, ctypes.c_void_p).value for f in fns))
+
+
+_OPS = None
+
+
+def attention_ops():
+    """The native attention and cache calls: the binding and the library's functions for it, or None where the
+    native calls were not built."""
+    global _OPS
+    if _OPS is None and binding() is not None:
+        l = lib()
+        fns = (l.caddtree_window_attention, l.caddtree_cache_attention, l.caddtree_cache_write, l.caddtree_cache_read,
+               l.caddtree_cache_score, l.caddtree_cache_evict)
+        _OPS = binding(), binding().ops(0, *(ctypes.cast(f, ctypes.c_void_p).value for f in fns))
+    return _OPS

@@ -14,6 +14,10 @@ and each sees the cached context, the root, its ancestors and itself.
 
 Every call checks its tensors, then enqueues kernels on the stream (default: torch's current one) and
 returns; lengths and page tables stay on the device.  include/caddtree.h states what is computed.
+
+As a plan's calls do, these go to the native binding first, which checks the tensors and calls the library
+(about 2 us of host time where the checks here take 10 to 15); what it cannot vouch for comes back as None
+and takes the Python checks here, which raise what is wrong.
 """
 
 from __future__ import annotations
@@ -54,6 +58,41 @@ def _stream(stream, device: int) -> int:
     if stream is None:
         return _torch()._C._cuda_getCurrentRawStream(device)
     return int(stream.cuda_stream) if hasattr(stream, "cuda_stream") else int(stream)
+
+
+def _native(stream):
+    """(binding, its functions, device, raw stream) of the native calls, or None where the Python path is to
+    decide."""
+    ops = _lib.attention_ops()
+    if ops is None:
+        return None
+    torch = _torch()
+    device = torch._C._cuda_getDevice()
+    if stream is None:
+        return ops[0], ops[1], device, torch._C._cuda_getCurrentRawStream(device)
+    return (ops[0], ops[1], device, stream.cuda_stream) if isinstance(stream, torch.cuda.Stream) else None
+
+
+def _done(status) -> bool:
+    """Whether a native call was made; raises its error."""
+    if status is None:
+        return False
+    if status:
+        _lib.check(status)
+    return True
+
+
+def _made(q, out, stream):
+    """out, or where it is not given a new one (of zeros, on the call's stream: rows without a query keep them)."""
+    torch = _torch()
+    if out is not None or not isinstance(q, torch.Tensor):
+        return out
+    if stream is None:
+        return torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+    if not hasattr(stream, "cuda_stream"):
+        raise ValueError("out is required with a raw stream handle")
+    with torch.cuda.stream(stream):
+        return torch.zeros(q.shape, dtype=q.dtype, device=q.device)
 
 
 def _tensor(name: str, t, dtype, device: int):
@@ -127,21 +166,10 @@ def _queries(q, device: int):
     return a, name
 
 
-def _new_like(q, out, lse, a, device: int, stream):
-    """Checks out and lse, or makes out (of zeros, on the call's stream: rows without a query keep them)."""
-    torch = _torch()
-    if out is None:
-        if stream is None:
-            out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
-        else:
-            if not hasattr(stream, "cuda_stream"):
-                raise ValueError("out is required with a raw stream handle")
-            with torch.cuda.stream(stream):
-                out = torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+def _results(q, out, lse, a, device: int) -> None:
     a.out = _output("out", out, q.dtype, tuple(q.shape), device)
     if lse is not None:
-        a.lse = _array("lse", lse, torch.float32, tuple(q.shape[:3]), device)
-    return out
+        a.lse = _array("lse", lse, _torch().float32, tuple(q.shape[:3]), device)
 
 
 def window_attention(q, k, v, *, window: int = 0, sinks: int = 0, causal: bool = True, scale: Optional[float] = None,
@@ -151,6 +179,12 @@ def window_attention(q, k, v, *, window: int = 0, sinks: int = 0, causal: bool =
     last ``window`` positions (0: all) and the first ``sinks``; ``causal=False`` lets it see later keys too.
     Writes ``out`` (made of zeros if not given) and ``lse`` (float32 [B, T, heads], if given); rows past
     q_len are left as they are.  Returns out."""
+    out = _made(q, out, stream)
+    native = _native(stream)
+    if native is not None:
+        binding, ops, device, raw = native
+        if _done(binding.window_attention(ops, device, raw, q, k, v, window, sinks, causal, scale, q_len, k_len, out, lse, workspace)):
+            return out
     torch = _torch()
     device = _device()
     a, _ = _queries(q, device)
@@ -166,7 +200,7 @@ def window_attention(q, k, v, *, window: int = 0, sinks: int = 0, causal: bool =
         a.q_len = _array("q_len", q_len, torch.int32, (a.B,), device)
     if k_len is not None:
         a.k_len = _array("k_len", k_len, torch.int32, (a.B,), device)
-    out = _new_like(q, out, lse, a, device, stream)
+    _results(q, out, lse, a, device)
     ws, n = _workspace(workspace, device)
     _lib.check(_lib.lib().caddtree_window_attention(ctypes.byref(a), ws, n, _stream(stream, device)))
     return out
@@ -211,7 +245,14 @@ class KVCache:
                 pages.dim() != 3 or tuple(pages.shape[1:]) != (self.n_kv_heads, self.page_bytes):
             raise ValueError(f"pages must be a contiguous uint8 tensor [num_pages, {self.n_kv_heads}, {self.page_bytes}]")
         self.pages = pages
+        self._device = pages.device.index if pages.is_cuda else -1
         self._c = _lib.Cache(_lib.ATTENTION_DTYPES[dtype], self.n_kv_heads, self.head_dim, pages.shape[0], pages.data_ptr())
+        self._at = ctypes.addressof(self._c)
+
+    def _native(self, stream):
+        """As the module's _native, and the address of the cache's description."""
+        native = _native(stream)
+        return None if native is None or native[2] != self._device else native
 
     def _on(self) -> int:
         device = _device()
@@ -227,6 +268,11 @@ class KVCache:
     def write(self, k, v, page_table, start, count=None, index=None, stream=None) -> None:
         """Puts the first ``count[b]`` tokens (default: all) of k, v [B, rows, kv heads, D] into the slots from
         start[b] on.  With ``index`` (int32 [B, T]) token j is row index[b, j]: the accepted path of a tree."""
+        native = self._native(stream)
+        if native is not None:
+            binding, ops, device, raw = native
+            if _done(binding.cache_write(ops, device, raw, self._at, k, v, page_table, start, count, index)):
+                return
         torch = _torch()
         device = self._on()
         B = page_table.shape[0] if isinstance(page_table, torch.Tensor) and page_table.dim() == 2 else None
@@ -245,6 +291,11 @@ class KVCache:
     def read(self, page_table, end, k, v, start=None, stream=None) -> None:
         """Writes the values of the slots start[b] (default 0) .. end[b] - 1 into k, v [B, T, kv heads, D], at most
         T of them; further rows are left as they are."""
+        native = self._native(stream)
+        if native is not None:
+            binding, ops, device, raw = native
+            if _done(binding.cache_read(ops, device, raw, self._at, k, v, page_table, start, end)):
+                return
         torch = _torch()
         device = self._on()
         B = page_table.shape[0] if isinstance(page_table, torch.Tensor) and page_table.dim() == 2 else None
@@ -285,6 +336,13 @@ class KVCache:
         its root, row i node i - 1.  ``count`` int32 [B]: the tokens of each sequence, in a tree its n_star.
         Writes ``out`` (made of zeros if not given) and ``lse`` (float32 [B, T, heads], if given); rows without a
         query are left as they are.  Returns out."""
+        out = _made(q, out, stream)
+        native = self._native(stream)
+        if native is not None:
+            binding, ops, device, raw = native
+            if _done(binding.cache_attention(ops, device, raw, self._at, q, page_table, ctx_len, k, v, count, causal, mask, depth,
+                                             window, sinks, scale, out, lse, workspace)):
+                return out
         torch = _torch()
         device = self._on()
         if (mask is None) != (depth is None) and k is not None:
@@ -308,7 +366,7 @@ class KVCache:
         if k is not None:
             shape = (a.B, a.T, self.n_kv_heads, self.head_dim)
             a.k, a.v = _view("k", k, q.dtype, shape, device), _view("v", v, q.dtype, shape, device)
-        out = _new_like(q, out, lse, a, device, stream)
+        _results(q, out, lse, a, device)
         ws, n = _workspace(workspace, device)
         _lib.check(_lib.lib().caddtree_cache_attention(ctypes.byref(self._c), ctypes.byref(a), ws, n, _stream(stream, device)))
         return out
@@ -320,6 +378,12 @@ class KVCache:
         into ``new_scores``: the arguments of the ``attention`` call that wrote ``lse``, and ``weight``
         (float32 [B, T], default 1) to pick and weigh its queries (in a tree: the accepted ones).  ``depth``
         says that the queries are a tree's."""
+        native = self._native(stream)
+        if native is not None:
+            binding, ops, device, raw = native
+            if _done(binding.cache_score(ops, device, raw, self._at, q, page_table, ctx_len, lse, scores, new_scores, weight, count,
+                                         depth, window, sinks, scale)):
+                return
         torch = _torch()
         device = self._on()
         a = self._attention(q, page_table, ctx_len, count, depth, window, sinks, scale, device)
@@ -337,6 +401,12 @@ class KVCache:
         (int32 [B, pages], none of them in use), their scores to ``new_scores`` (float32 [B, kv heads, slots],
         zeros behind), the lengths to ``new_len`` (int64 [B]) and the old slots to ``kept`` (int32
         [B, kv heads, budget], -1 behind)."""
+        native = self._native(stream)
+        if native is not None:
+            binding, ops, device, raw = native
+            if _done(binding.cache_evict(ops, device, raw, self._at, page_table, ctx_len, scores, new_table, new_len, new_scores, kept,
+                                         budget, sinks, recent)):
+                return
         torch = _torch()
         device = self._on()
         B = page_table.shape[0] if isinstance(page_table, torch.Tensor) and page_table.dim() == 2 else None

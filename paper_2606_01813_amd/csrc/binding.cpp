@@ -11,6 +11,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
 #include <cstdint>
 #include <initializer_list>
 
@@ -394,8 +395,404 @@ PyObject* py_spec(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return cap;
 }
 
+// ---------------------------------------------------------------- attention and the cache
+
+// The library's functions, and the device of the calls' tensors where it is not a GPU (tests of the checks).
+struct Ops {
+  bool host;
+  decltype(&caddtree_window_attention) window;
+  decltype(&caddtree_cache_attention) attention;
+  decltype(&caddtree_cache_write) write;
+  decltype(&caddtree_cache_read) read;
+  decltype(&caddtree_cache_score) score;
+  decltype(&caddtree_cache_evict) evict;
+};
+const char* const kOpsName = "caddtree.ops";
+constexpr int64_t kAny = -1;
+
+// One call's view of its arguments, as Call above: ok falls at the first one that is not as it should be.
+struct Attn {
+  const Ops& s;
+  int device;
+  bool ok = true;
+
+  Attn(const Ops& ops, PyObject* dev) : s(ops) { device = (int)integer(dev, 0, 1 << 20); }
+
+  c10::TensorImpl* tensor(PyObject* o) {
+    if (!ok || !THPVariable_CheckExact(o)) {
+      ok = false;
+      return nullptr;
+    }
+    c10::TensorImpl* t = THPVariable_Unpack(o).unsafeGetTensorImpl();
+    const c10::Device d = t->device();
+    const bool here = s.host ? d.is_cpu() : d.is_cuda() && d.index() == device;
+    if (!here || t->layout() != c10::kStrided || !t->has_storage() || t->has_symbolic_sizes_strides() || t->numel() == 0) {
+      ok = false;
+      return nullptr;
+    }
+    return t;
+  }
+
+  // a contiguous tensor of `type` with exactly these sizes (kAny: any); None gives nullptr unless it is required
+  void* array(PyObject* o, c10::ScalarType type, std::initializer_list<int64_t> dims, bool required = true) {
+    if (o == Py_None) {
+      if (required) ok = false;
+      return nullptr;
+    }
+    c10::TensorImpl* t = tensor(o);
+    if (t == nullptr) return nullptr;
+    const auto sz = t->sizes();
+    bool good = c10::typeMetaToScalarType(t->dtype()) == type && sz.size() == dims.size() && t->is_contiguous();
+    size_t i = 0;
+    if (good)
+      for (const int64_t d : dims) {
+        good = good && (d == kAny || sz[i] == d) && sz[i] <= INT32_MAX;
+        ++i;
+      }
+    if (!good) {
+      ok = false;
+      return nullptr;
+    }
+    return t->mutable_data();
+  }
+  int64_t size(PyObject* o, size_t dim) {
+    c10::TensorImpl* t = tensor(o);
+    if (t == nullptr || t->sizes().size() <= dim) {
+      ok = false;
+      return 0;
+    }
+    return t->sizes()[dim];
+  }
+
+  // [B, tokens, heads, head_dim] with a unit last stride, 16-byte aligned rows, and for an output no two elements
+  // in one place
+  caddtree_view_t view(PyObject* o, c10::ScalarType type, const int64_t (&dims)[4], bool output = false) {
+    caddtree_view_t v = {nullptr, 0, 0, 0};
+    c10::TensorImpl* t = tensor(o);
+    if (t == nullptr) return v;
+    const auto sz = t->sizes();
+    const auto st = t->strides();
+    bool good = c10::typeMetaToScalarType(t->dtype()) == type && sz.size() == 4;
+    for (int i = 0; good && i < 4; ++i) good = (dims[i] == kAny || sz[i] == dims[i]) && sz[i] <= INT32_MAX;
+    if (!good) {
+      ok = false;
+      return v;
+    }
+    v.stride_b = sz[0] > 1 ? st[0] : 0;
+    v.stride_t = sz[1] > 1 ? st[1] : 0;
+    v.stride_h = sz[2] > 1 ? st[2] : 0;
+    v.data = output ? t->mutable_data() : const_cast<void*>(t->data());
+    if (st[3] != 1 || (v.stride_b | v.stride_t | v.stride_h) % 8 != 0 || reinterpret_cast<uintptr_t>(v.data) % 16 != 0) ok = false;
+    if (output) {
+      int64_t n[3] = {sz[0], sz[1], sz[2]}, s3[3] = {v.stride_b, v.stride_t, v.stride_h}, room = sz[3];
+      for (int pass = 0; pass < 3; ++pass) {        // strides in ascending order, each past the ones before
+        int least = -1;
+        for (int i = 0; i < 3; ++i)
+          if (n[i] > 1 && (least < 0 || s3[i] < s3[least])) least = i;
+        if (least < 0) break;
+        if (s3[least] < room) ok = false;
+        room += s3[least] * (n[least] - 1);
+        n[least] = 1;
+      }
+    }
+    return v;
+  }
+
+  int64_t integer(PyObject* o, int64_t lo, int64_t hi) {
+    int over = 0;
+    const long long v = PyLong_CheckExact(o) ? PyLong_AsLongLongAndOverflow(o, &over) : lo - 1;
+    if (over != 0 || v < lo || v > hi) ok = false;
+    return v;
+  }
+  int32_t count(PyObject* o) { return (int32_t)integer(o, 0, INT32_MAX); }
+  float scale(PyObject* o, int64_t head_dim) {
+    if (o == Py_None) return (float)(1.0 / std::sqrt((double)head_dim));
+    if (!PyFloat_CheckExact(o)) ok = false;
+    return ok ? (float)PyFloat_AS_DOUBLE(o) : 0.f;
+  }
+  bool truth(PyObject* o) {
+    if (o != Py_True && o != Py_False) ok = false;
+    return o == Py_True;
+  }
+  hipStream_t stream(PyObject* o) {
+    const unsigned long long v = PyLong_CheckExact(o) ? PyLong_AsUnsignedLongLong(o) : 0;
+    if (!PyLong_CheckExact(o) || PyErr_Occurred()) {
+      PyErr_Clear();
+      ok = false;
+    }
+    return reinterpret_cast<hipStream_t>(static_cast<uintptr_t>(v));
+  }
+  void* workspace(PyObject* o, size_t* bytes) {
+    *bytes = 0;
+    if (o == Py_None) return nullptr;
+    c10::TensorImpl* t = tensor(o);
+    if (t == nullptr || !t->is_contiguous()) {
+      ok = false;
+      return nullptr;
+    }
+    *bytes = (size_t)t->numel() * t->itemsize();
+    return t->mutable_data();
+  }
+  const caddtree_cache_t* cache(PyObject* o) {      // the address of the cache object's own description
+    return reinterpret_cast<const caddtree_cache_t*>(static_cast<uintptr_t>(integer(o, 1, INT64_MAX)));
+  }
+  c10::ScalarType type(const caddtree_cache_t* c) { return c->dtype == CADDTREE_BF16 ? c10::kBFloat16 : c10::kHalf; }
+
+  // what every attention call says of its queries
+  c10::ScalarType queries(PyObject* q, caddtree_attention_t* a) {
+    c10::TensorImpl* t = tensor(q);
+    if (t == nullptr || t->sizes().size() != 4) {
+      ok = false;
+      return c10::kFloat;
+    }
+    const c10::ScalarType type = c10::typeMetaToScalarType(t->dtype());
+    if (type != c10::kBFloat16 && type != c10::kHalf) ok = false;
+    a->q = view(q, type, {kAny, kAny, kAny, kAny});
+    if (!ok) return type;
+    a->dtype = type == c10::kBFloat16 ? CADDTREE_BF16 : CADDTREE_F16;
+    a->B = (int32_t)t->sizes()[0];
+    a->T = (int32_t)t->sizes()[1];
+    a->n_heads = (int32_t)t->sizes()[2];
+    a->head_dim = (int32_t)t->sizes()[3];
+    return type;
+  }
+  // ... and a call over a cache of its pages, lengths and form
+  c10::ScalarType cached(const caddtree_cache_t* c, PyObject* q, PyObject* table, PyObject* ctx, PyObject* cnt, PyObject* depth,
+                         PyObject* window, PyObject* sinks, PyObject* sc, caddtree_attention_t* a) {
+    const c10::ScalarType t = queries(q, a);
+    if (!ok || a->dtype != c->dtype || a->head_dim != c->head_dim) {
+      ok = false;
+      return t;
+    }
+    a->n_kv_heads = c->n_kv_heads;
+    a->S = a->T;
+    a->page_table = as<int32_t>(array(table, c10::kInt, {a->B, kAny}));
+    a->ctx_len = as<int64_t>(array(ctx, c10::kLong, {a->B}));
+    a->q_len = as<int32_t>(array(cnt, c10::kInt, {a->B}, false));
+    if (!ok) return t;
+    a->table_pages = (int32_t)size(table, 1);
+    if (depth != Py_None) {
+      a->depth = as<int32_t>(array(depth, c10::kInt, {a->B, kAny}));
+      if (!ok) return t;
+      a->cap = (int32_t)size(depth, 1);
+      a->order = CADDTREE_ORDER_TREE;
+    }
+    a->window = count(window);
+    a->sinks = count(sinks);
+    a->scale = scale(sc, a->head_dim);
+    return t;
+  }
+};
+
+template <typename F>
+PyObject* guarded_ops(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t want, F&& body) {
+  if (nargs != want) {
+    PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, nargs);
+    return nullptr;
+  }
+  const Ops* s = static_cast<const Ops*>(PyCapsule_GetPointer(args[0], kOpsName));
+  if (s == nullptr) return nullptr;
+  int status = -1;
+  try {
+    status = body(*s);
+  } catch (const LibraryThrew&) {
+    PyErr_SetString(PyExc_RuntimeError, "the caddtree library threw an exception");
+    return nullptr;
+  } catch (...) {          // a tensor that cannot be looked at this way
+    status = -1;
+  }
+  if (status < 0) Py_RETURN_NONE;
+  return PyLong_FromLong(status);
+}
+
+// ops, device, stream, q, k, v, window, sinks, causal, scale, q_len, k_len, out, lse, workspace
+PyObject* py_window_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_ops(p, n, 15, [&](const Ops& s) -> int {
+    Attn c(s, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    caddtree_attention_t a = {};
+    const c10::ScalarType t = c.queries(p[3], &a);
+    if (!c.ok) return -1;
+    a.k = c.view(p[4], t, {a.B, kAny, kAny, a.head_dim});
+    if (!c.ok) return -1;
+    a.S = (int32_t)c.size(p[4], 1);
+    a.n_kv_heads = (int32_t)c.size(p[4], 2);
+    a.v = c.view(p[5], t, {a.B, a.S, a.n_kv_heads, a.head_dim});
+    a.window = c.count(p[6]);
+    a.sinks = c.count(p[7]);
+    a.order = c.truth(p[8]) ? CADDTREE_ORDER_CHAIN : CADDTREE_ORDER_BLOCK;
+    a.scale = c.scale(p[9], a.head_dim);
+    a.q_len = as<int32_t>(c.array(p[10], c10::kInt, {a.B}, false));
+    a.k_len = as<int32_t>(c.array(p[11], c10::kInt, {a.B}, false));
+    a.out = c.view(p[12], t, {a.B, a.T, a.n_heads, a.head_dim}, true);
+    a.lse = as<float>(c.array(p[13], c10::kFloat, {a.B, a.T, a.n_heads}, false));
+    size_t bytes;
+    void* ws = c.workspace(p[14], &bytes);
+    if (!c.ok) return -1;
+    return unlocked([&] { return s.window(&a, ws, bytes, st); });
+  });
+}
+
+// ops, device, stream, cache, q, page_table, ctx_len, k, v, count, causal, mask, depth, window, sinks, scale, out, lse,
+// workspace
+PyObject* py_cache_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_ops(p, n, 19, [&](const Ops& s) -> int {
+    Attn c(s, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    const caddtree_cache_t* cache = c.cache(p[3]);
+    if (!c.ok) return -1;
+    caddtree_attention_t a = {};
+    const c10::ScalarType t = c.cached(cache, p[4], p[5], p[6], p[9], p[12], p[13], p[14], p[15], &a);
+    if (!c.ok) return -1;
+    const bool causal = c.truth(p[10]), tree = p[12] != Py_None, keys = p[7] != Py_None;
+    if (!tree) a.order = causal ? CADDTREE_ORDER_CHAIN : CADDTREE_ORDER_BLOCK;
+    if (keys != (p[8] != Py_None) || (p[11] != Py_None && !tree) || (tree && keys && p[11] == Py_None)) return -1;
+    if (p[11] != Py_None) {
+      c10::TensorImpl* m = c.tensor(p[11]);
+      if (m == nullptr) return -1;
+      const c10::ScalarType mt = c10::typeMetaToScalarType(m->dtype());
+      if (mt == c10::kByte) {
+        a.mask_kind = CADDTREE_MASK_U8;
+        a.mask = c.array(p[11], mt, {a.B, a.cap, a.cap});
+      } else if (mt == c10::kInt || mt == c10::kUInt32) {
+        a.mask_kind = CADDTREE_MASK_BITS32;
+        a.mask = c.array(p[11], mt, {a.B, a.cap, (a.cap + 31) / 32});
+      } else {
+        return -1;
+      }
+    }
+    if (keys) {
+      a.k = c.view(p[7], t, {a.B, a.T, a.n_kv_heads, a.head_dim});
+      a.v = c.view(p[8], t, {a.B, a.T, a.n_kv_heads, a.head_dim});
+    }
+    a.out = c.view(p[16], t, {a.B, a.T, a.n_heads, a.head_dim}, true);
+    a.lse = as<float>(c.array(p[17], c10::kFloat, {a.B, a.T, a.n_heads}, false));
+    size_t bytes;
+    void* ws = c.workspace(p[18], &bytes);
+    if (!c.ok) return -1;
+    return unlocked([&] { return s.attention(cache, &a, ws, bytes, st); });
+  });
+}
+
+// ops, device, stream, cache, k, v, page_table, start, count, index
+PyObject* py_cache_write(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_ops(p, n, 10, [&](const Ops& s) -> int {
+    Attn c(s, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    const caddtree_cache_t* cache = c.cache(p[3]);
+    if (!c.ok) return -1;
+    const int64_t B = c.size(p[6], 0);
+    const auto* table = as<int32_t>(c.array(p[6], c10::kInt, {B, kAny}));
+    if (!c.ok) return -1;
+    const int32_t pages = (int32_t)c.size(p[6], 1);
+    const caddtree_view_t k = c.view(p[4], c.type(cache), {B, kAny, cache->n_kv_heads, cache->head_dim});
+    if (!c.ok) return -1;
+    const int64_t rows = c.size(p[4], 1);
+    const caddtree_view_t v = c.view(p[5], c.type(cache), {B, rows, cache->n_kv_heads, cache->head_dim});
+    const auto* start = as<int64_t>(c.array(p[7], c10::kLong, {B}));
+    const auto* count = as<int32_t>(c.array(p[8], c10::kInt, {B}, false));
+    const auto* index = as<int32_t>(c.array(p[9], c10::kInt, {B, kAny}, false));
+    if (!c.ok) return -1;
+    const int64_t T = index ? c.size(p[9], 1) : rows;
+    return unlocked([&] { return s.write(cache, &k, &v, (int32_t)B, (int32_t)T, (int32_t)rows, start, count, index, table, pages, st); });
+  });
+}
+
+// ops, device, stream, cache, k, v, page_table, start, end
+PyObject* py_cache_read(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_ops(p, n, 9, [&](const Ops& s) -> int {
+    Attn c(s, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    const caddtree_cache_t* cache = c.cache(p[3]);
+    if (!c.ok) return -1;
+    const int64_t B = c.size(p[6], 0);
+    const auto* table = as<int32_t>(c.array(p[6], c10::kInt, {B, kAny}));
+    if (!c.ok) return -1;
+    const int32_t pages = (int32_t)c.size(p[6], 1);
+    const caddtree_view_t k = c.view(p[4], c.type(cache), {B, kAny, cache->n_kv_heads, cache->head_dim}, true);
+    if (!c.ok) return -1;
+    const int64_t T = c.size(p[4], 1);
+    const caddtree_view_t v = c.view(p[5], c.type(cache), {B, T, cache->n_kv_heads, cache->head_dim}, true);
+    const auto* start = as<int64_t>(c.array(p[7], c10::kLong, {B}, false));
+    const auto* end = as<int64_t>(c.array(p[8], c10::kLong, {B}));
+    if (!c.ok) return -1;
+    return unlocked([&] { return s.read(cache, &k, &v, (int32_t)B, (int32_t)T, start, end, table, pages, st); });
+  });
+}
+
+// ops, device, stream, cache, q, page_table, ctx_len, lse, scores, new_scores, weight, count, depth, window, sinks, scale
+PyObject* py_cache_score(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_ops(p, n, 16, [&](const Ops& s) -> int {
+    Attn c(s, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    const caddtree_cache_t* cache = c.cache(p[3]);
+    if (!c.ok) return -1;
+    caddtree_attention_t a = {};
+    c.cached(cache, p[4], p[5], p[6], p[11], p[12], p[13], p[14], p[15], &a);
+    if (!c.ok) return -1;
+    a.lse = as<float>(c.array(p[7], c10::kFloat, {a.B, a.T, a.n_heads}));
+    auto* scores = as<float>(c.array(p[8], c10::kFloat, {a.B, a.n_kv_heads, kAny}));
+    if (!c.ok) return -1;
+    const int64_t slots = c.size(p[8], 2);
+    float* fresh = p[9] == Py_None ? scores : as<float>(c.array(p[9], c10::kFloat, {a.B, a.n_kv_heads, slots}));
+    const auto* weight = as<float>(c.array(p[10], c10::kFloat, {a.B, a.T}, false));
+    if (!c.ok) return -1;
+    return unlocked([&] { return s.score(cache, &a, weight, scores, fresh, slots, st); });
+  });
+}
+
+// ops, device, stream, cache, page_table, ctx_len, scores, new_table, new_len, new_scores, kept, budget, sinks, recent
+PyObject* py_cache_evict(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_ops(p, n, 14, [&](const Ops& s) -> int {
+    Attn c(s, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    const caddtree_cache_t* cache = c.cache(p[3]);
+    if (!c.ok) return -1;
+    const int64_t B = c.size(p[4], 0), H = cache->n_kv_heads;
+    const auto* table = as<int32_t>(c.array(p[4], c10::kInt, {B, kAny}));
+    const auto* ctx = as<int64_t>(c.array(p[5], c10::kLong, {B}));
+    const auto* scores = as<float>(c.array(p[6], c10::kFloat, {B, H, kAny}));
+    const auto* to = as<int32_t>(c.array(p[7], c10::kInt, {B, kAny}));
+    auto* len = as<int64_t>(c.array(p[8], c10::kLong, {B}));
+    auto* fresh = as<float>(c.array(p[9], c10::kFloat, {B, H, kAny}));
+    const int32_t budget = c.count(p[11]), sinks = c.count(p[12]), recent = c.count(p[13]);
+    auto* kept = as<int32_t>(c.array(p[10], c10::kInt, {B, H, budget}));
+    if (!c.ok) return -1;
+    const int64_t pages = c.size(p[4], 1), slots = c.size(p[6], 2), to_pages = c.size(p[7], 1), to_slots = c.size(p[9], 2);
+    return unlocked([&] {
+      return s.evict(cache, (int32_t)B, table, (int32_t)pages, ctx, scores, slots, budget, sinks, recent, to, (int32_t)to_pages,
+                     fresh, to_slots, len, kept, st);
+    });
+  });
+}
+
+// host, the addresses of window_attention, cache_attention, cache_write, cache_read, cache_score, cache_evict
+PyObject* py_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 7) {
+    PyErr_Format(PyExc_TypeError, "7 arguments expected, got %zd", n);
+    return nullptr;
+  }
+  uint64_t v[7];
+  for (int i = 0; i < 7; ++i) {
+    v[i] = PyLong_AsUnsignedLongLongMask(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  Ops* s = new Ops{v[0] != 0,
+                   reinterpret_cast<decltype(Ops::window)>(v[1]),
+                   reinterpret_cast<decltype(Ops::attention)>(v[2]),
+                   reinterpret_cast<decltype(Ops::write)>(v[3]),
+                   reinterpret_cast<decltype(Ops::read)>(v[4]),
+                   reinterpret_cast<decltype(Ops::score)>(v[5]),
+                   reinterpret_cast<decltype(Ops::evict)>(v[6])};
+  PyObject* cap = PyCapsule_New(s, kOpsName, [](PyObject* o) { delete static_cast<Ops*>(PyCapsule_GetPointer(o, kOpsName)); });
+  if (cap == nullptr) delete s;
+  return cap;
+}
+
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {CALL(spec), CALL(build), CALL(reduce_topk), CALL(expand), CALL(emit), CALL(accept),
+                           CALL(ops), CALL(window_attention), CALL(cache_attention), CALL(cache_write), CALL(cache_read),
+                           CALL(cache_score), CALL(cache_evict),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
