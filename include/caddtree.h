@@ -284,7 +284,7 @@ caddtree_status_t caddtree_fit_cost(const double* x_host, const double* y_host, 
  *
  * Tensors of 16-bit elements are strided views [B, tokens, heads, head_dim]: element (b, t, h, d) at
  * data + b stride_b + t stride_t + h stride_h + d (strides in elements).  data must be 16-byte aligned
- * and the strides multiples of 8; inputs may overlap or repeat (stride 0).
+ * and the strides multiples of 8, stride_t below 2^24; inputs may overlap or repeat (stride 0).
  *
  * Visibility.  Query i at position pos_i sees the key at position pos_j if its order allows it and
  *     window = 0  or  pos_i - pos_j < window  or  pos_j < sinks.

@@ -27,46 +27,33 @@ __device__ int64_t part_of(const AttnArgs& a, const Split& sp, int b, int hk, in
 // keys, and whole blocks of values, token by token.
 template <int D>
 struct PageStage {
-  uint32_t kc[4][D / 32];
-  uint32_t ks[4];
-  u32x4 vc[D / 32];
-  uint32_t vs[D / 32];
+  uint32_t kc[4][D / 32] = {};
+  uint32_t ks[4] = {};
+  u32x4 vc[D / 32] = {};
+  uint32_t vs[D / 32] = {};
 
   __device__ void load_keys(const uint8_t* page, int lane) {
     using L = PageLayout<D>;
-    const int col = lane & 15, g = lane >> 4;
-    if (page == nullptr) {
-#pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        ks[s] = 127;
-#pragma unroll
-        for (int w = 0; w < D / 32; ++w) kc[s][w] = 0;
-      }
-      return;
-    }
+    const uint32_t col = lane & 15, g = lane >> 4;
+    if (page == nullptr) return;                    // (no key of it is seen: what the registers hold does not matter)
+    const uint32_t code = col * L::kRow + g * (D / 8), scale = col * L::kScales + g * (D / 4) / kBlock;
+    const uint8_t* scales = page + L::kKs;
 #pragma unroll
     for (int s = 0; s < 4; ++s) {
-      const uint32_t* c = reinterpret_cast<const uint32_t*>(page + L::kK + (16 * s + col) * L::kRow + g * (D / 8));
+      const uint32_t* c = reinterpret_cast<const uint32_t*>(page + (code + 16 * s * L::kRow));
 #pragma unroll
       for (int w = 0; w < D / 32; ++w) kc[s][w] = c[w];
-      ks[s] = page[L::kKs + (16 * s + col) * L::kScales + g * (D / 4) / kBlock];
+      ks[s] = scales[scale + 16 * s * L::kScales];
     }
   }
   __device__ void load_values(const uint8_t* page, int lane) {
     using L = PageLayout<D>;
-    if (page == nullptr) {
-#pragma unroll
-      for (int u = 0; u < D / 32; ++u) {
-        vc[u] = u32x4{0, 0, 0, 0};
-        vs[u] = 127;
-      }
-      return;
-    }
+    if (page == nullptr) return;
+    const uint8_t *codes = page + L::kV, *scales = page + L::kVs;
 #pragma unroll
     for (int u = 0; u < D / 32; ++u) {
-      const int q = lane + 64 * u;
-      vc[u] = *reinterpret_cast<const u32x4*>(page + L::kV + q * 16);
-      vs[u] = page[L::kVs + q];
+      vc[u] = *reinterpret_cast<const u32x4*>(codes + ((uint32_t)lane * 16 + u * 1024));
+      vs[u] = scales[(uint32_t)lane + 64 * u];
     }
   }
   // the operand of keys 16 s .. 16 s + 15: D / 32 instructions' worth
@@ -80,9 +67,7 @@ struct PageStage {
       out[j][2] = E::template from4<2>(kc[s][j], f);
       out[j][3] = E::template from4<3>(kc[s][j], f);
     }
-    if (ks[s] == 255)
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) out[j] = u32x4{E::kNaN, E::kNaN, E::kNaN, E::kNaN};
+    if (ks[s] == 255) out[0][0] = E::kNaN;          // (one is enough for the key's scores)
   }
   // values of tokens 32 half .. + 31 into LDS.  there: tokens of the tile that are there; returns whether a
   // tile that is not seen in full had any that are not finite
@@ -119,21 +104,22 @@ struct TensorStage {
 
   __device__ void load_keys(const char* k, int64_t kt, int j0, int nk, int lane) {
     const int col = lane & 15, g = lane >> 4;
-    const char* base = k + 2 * (j0 * kt);
+    const char* base = k + 2 * (j0 * kt);           // (uniform; a lane's offset in a tile is below 2^32: see kMaxStride)
 #pragma unroll
     for (int s = 0; s < 2; ++s) {                   // (a key that is not there: the tile's first one in its place)
-      const u32x4* p = reinterpret_cast<const u32x4*>(base + 2 * ((j0 + 16 * s + col < nk ? (16 * s + col) * kt : 0) + g * (D / 4)));
+      const uint32_t row = j0 + 16 * s + col < nk ? 16 * s + col : 0;
+      const u32x4* p = reinterpret_cast<const u32x4*>(base + (row * (2 * (uint32_t)kt) + (uint32_t)g * (D / 2)));
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) kr[s][j] = p[j];
     }
   }
   __device__ void load_values(const char* v, int64_t vt, int j0, int nk, int lane) {
     const char* base = v + 2 * (j0 * vt);
-    const int row = lane / (D / 8), d = lane % (D / 8) * 8;
+    const uint32_t piece = lane % (D / 8) * 16;
 #pragma unroll
     for (int u = 0; u < D / 16; ++u) {
-      const int token = row + u * (512 / D);
-      vr[u] = *reinterpret_cast<const u32x4*>(base + 2 * ((j0 + token < nk ? token * vt : 0) + d));
+      const int token = lane / (D / 8) + u * (512 / D);
+      vr[u] = *reinterpret_cast<const u32x4*>(base + ((uint32_t)(j0 + token < nk ? token : 0) * (2 * (uint32_t)vt) + piece));
     }
   }
   template <typename E>
@@ -198,11 +184,15 @@ __device__ __forceinline__ bool narrow_tile(NarrowState<D, kR>& st, Stage& x, co
         if (!full && !((bits >> (16 * t + r)) & 1)) s[t][n][r] = -INFINITY;
         top = fmaxf(top, s[t][n][r]);
       }
-    top = fmaxf(top, __shfl_xor(top, 16));
-    top = fmaxf(top, __shfl_xor(top, 32));
-    const float m = fmaxf(st.m[n], top * c);
-    const float base = m == -INFINITY ? 0.f : m - E::kBias;
-    const float was = __builtin_amdgcn_exp2f(st.m[n] - E::kBias - base);
+    top = max_across_32(max_across_16(top)) * c;
+    if (__any(top > st.m[n] + kLag)) {
+      const float m = fmaxf(st.m[n], top), was = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m[n] - m);
+      st.l[n] *= was;
+#pragma unroll
+      for (int t = 0; t < D / 16; ++t) st.acc[t][n] *= was;
+      st.m[n] = m;
+    }
+    const float base = st.m[n] == -INFINITY ? 0.f : st.m[n] - E::kBias;
     float sum = 0.f;
 #pragma unroll
     for (int t = 0; t < 2 * kH; ++t)
@@ -211,10 +201,7 @@ __device__ __forceinline__ bool narrow_tile(NarrowState<D, kR>& st, Stage& x, co
         s[t][n][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], c, -base));
         sum += s[t][n][r];
       }
-    st.l[n] = st.l[n] * was + sum;                  // (of this lane's keys: the four g are added at the end)
-    st.m[n] = m;
-#pragma unroll
-    for (int t = 0; t < D / 16; ++t) st.acc[t][n] *= was;
+    st.l[n] += sum;                                 // (of this lane's keys: the four g are added at the end)
 #pragma unroll
     for (int h = 0; h < kH; ++h)
       p[h][n] = u32x4{E::pair(s[2 * h][n][0], s[2 * h][n][1]), E::pair(s[2 * h][n][2], s[2 * h][n][3]),
@@ -228,8 +215,9 @@ __device__ __forceinline__ bool narrow_tile(NarrowState<D, kR>& st, Stage& x, co
     __builtin_amdgcn_wave_barrier();
     const int v0 = v_at<D>(4 * g + (lane & 15) / 4, (lane & 3) * 8);
 #pragma unroll
-    for (int t = 0; t < D / 16; ++t) {              // (v_at of 32 t bytes further is v0 ^ 32 t; 16 rows keep its swizzle)
-      const u32x2 lo = read_transposed(lds + (v0 ^ (t << 5))), hi = read_transposed(lds + (v0 ^ (t << 5)) + 16 * 2 * D);
+    for (int t = 0; t < D / 16; ++t) {              // (16 rows further: the same swizzle)
+      const char* at = lds + (v0 ^ v_step(32 * t));
+      const u32x2 lo = read_transposed(at), hi = read_transposed(at + 16 * 2 * D);
       const u32x4 v = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
       for (int n = 0; n < kR; ++n) st.acc[t][n] = Mfma<E>::m16(v, p[h][n], st.acc[t][n]);
@@ -286,37 +274,41 @@ __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a, Split sp) {
   if constexpr (kPaged) {
     const int nc = min(t1, span.a + span.c - span.b);    // this split's cached tiles come first
     PageStage<D> x;
-    auto page_at = [&](int tile) -> const uint8_t* {
+    auto entry = [&](int tile) -> int32_t {
       bool cached;
-      return tile < nc ? page_of(a.kv, b, tile_of<kPage, 32>(span, tile, &cached) / kPage, hk) : nullptr;
+      return tile < nc ? table_entry(a.kv, b, tile_of<kPage, 32>(span, tile, &cached) / kPage) : -1;
     };
-    const uint8_t *page = page_at(t), *next = page_at(t + 4);
-    if (t < nc) {
-      x.load_keys(page, lane);
-      x.load_values(page, lane);
-    }
+    const uint8_t* page = page_at(a.kv, entry(t), hk);
+    int32_t ahead = entry(t + 4);
+    x.load_keys(page, lane);
+    x.load_values(page, lane);
     for (; t < nc; t += 4) {
       bool cached;
       const int at = tile_of<kPage, 32>(span, t, &cached);
-      const uint8_t* after = page_at(t + 8);
-      const bool more = t + 4 < nc;
+      const int32_t after = entry(t + 8);
+      const uint8_t* next = nullptr;
       const bool full = page && full_cached(a, s, s.nq - 1, at, kPage);
 #pragma unroll
       for (int n = 0; n < kR; ++n) seen[n] = full ? ~0ull : page ? sees(true, rows[n], at) : 0;
       if (narrow_tile<E, D, kR, 2>(
-              st, x, q, c, full, seen, page ? s.ctx - at : 0, vt, lane, [&] { if (more) x.load_keys(next, lane); },
-              [&] { if (more) x.load_values(next, lane); }))
+              st, x, q, c, full, seen, page ? s.ctx - at : 0, vt, lane,
+              [&] {
+                next = page_at(a.kv, ahead, hk);
+                x.load_keys(next, lane);
+              },
+              [&] { x.load_values(next, lane); }))
         odd = true;
       page = next;
-      next = after;
+      ahead = after;
     }
   }
   {
+    // A cache's few new tiles (kPaged) are loaded as they are needed: keys, then values while the weights are
+    // formed, which keeps the registers of this loop below those of the cached one's.
     TensorStage<D> x;
     bool cached;
-    int at = 0;
-    if (t < t1) {
-      at = tile_of<kPage, 32>(span, t, &cached);
+    int at = t < t1 ? tile_of<kPage, 32>(span, t, &cached) : 0;
+    if (!kPaged && t < t1) {
       x.load_keys(kb, a.k.t, at, s.nk, lane);
       x.load_values(vb, a.v.t, at, s.nk, lane);
     }
@@ -325,11 +317,15 @@ __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a, Split sp) {
       const int after = more ? tile_of<kPage, 32>(span, t + 4, &cached) : 0;
       const bool full = full_new(a, s, 0, s.nq - 1, at, 32);
 #pragma unroll
-      for (int n = 0; n < kR; ++n)
-        seen[n] = full ? ~0ull : sees(false, rows[n], at);
+      for (int n = 0; n < kR; ++n) seen[n] = full ? ~0ull : sees(false, rows[n], at);
+      if (kPaged) x.load_keys(kb, a.k.t, at, s.nk, lane);
       if (narrow_tile<E, D, kR, 1>(
-              st, x, q, c, full, seen, s.nk - at, vt, lane, [&] { if (more) x.load_keys(kb, a.k.t, after, s.nk, lane); },
-              [&] { if (more) x.load_values(vb, a.v.t, after, s.nk, lane); }))
+              st, x, q, c, full, seen, s.nk - at, vt, lane,
+              [&] {
+                if (kPaged) x.load_values(vb, a.v.t, at, s.nk, lane);
+                else if (more) x.load_keys(kb, a.k.t, after, s.nk, lane);
+              },
+              [&] { if (!kPaged && more) x.load_values(vb, a.v.t, after, s.nk, lane); }))
         odd = true;
       at = after;
     }
@@ -431,19 +427,18 @@ struct WideTensor {
   u32x4 k[kN], v[kN];
   __device__ void load(const char* kp, const char* vp, int64_t kt, int64_t vt, int j0, int nk, int tid) {
     const char *kb = kp + 2 * (j0 * kt), *vb = vp + 2 * (j0 * vt);
-    const int row = tid / (D / 8), d = tid % (D / 8) * 8;
-    const int64_t ko = row * kt + d, vo = row * vt + d;
+    const uint32_t piece = k_piece<D>(tid % (D / 8)) * 16;
 #pragma unroll
     for (int u = 0; u < kN; ++u) {                  // (a key that is not there: the tile's first one in its place)
-      const int token = u * (2048 / D);             // ... rows further
-      const bool there = j0 + token + row < nk;
-      k[u] = *reinterpret_cast<const u32x4*>(kb + 2 * (there ? token * kt + ko : d));
-      v[u] = *reinterpret_cast<const u32x4*>(vb + 2 * (there ? token * vt + vo : d));
+      const int token = tid / (D / 8) + u * (2048 / D);
+      const uint32_t row = j0 + token < nk ? token : 0;
+      k[u] = *reinterpret_cast<const u32x4*>(kb + (row * (2 * (uint32_t)kt) + piece));
+      v[u] = *reinterpret_cast<const u32x4*>(vb + (row * (2 * (uint32_t)vt) + piece));
     }
   }
   template <typename E>
   __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* odd) {
-    const int row = tid / (D / 8), piece = tid % (D / 8), k0 = k_at<D>(row, piece), v0 = v_at<D>(row, piece * 16);
+    const int row = tid / (D / 8), piece = k_piece<D>(tid % (D / 8)), k0 = k_at<D>(row, piece), v0 = v_at<D>(row, piece * 16);
 #pragma unroll
     for (int u = 0; u < kN; ++u) {                  // (16 or 32 rows further: the same swizzle)
       const int token = row + u * (2048 / D);
@@ -459,21 +454,17 @@ struct WideTensor {
 // ... of a page: a block of keys and one of values a thread (D = 64: half the threads)
 template <int D>
 struct WidePage {
-  u32x4 k, v;
-  uint32_t ks, vs;
+  u32x4 k = {}, v = {};
+  uint32_t ks = 0, vs = 0;
   static constexpr int kThreads = kPage * (D / kBlock);
   __device__ void load(const uint8_t* page, int tid) {
     using L = PageLayout<D>;
-    if (tid >= kThreads) return;
-    if (page == nullptr) {
-      k = v = u32x4{0, 0, 0, 0};
-      ks = vs = 127;
-      return;
-    }
-    k = *reinterpret_cast<const u32x4*>(page + L::kK + tid * 16);
-    v = *reinterpret_cast<const u32x4*>(page + L::kV + tid * 16);
-    ks = page[L::kKs + tid];
-    vs = page[L::kVs + tid];
+    if (tid >= kThreads || page == nullptr) return; // (no key of such a page is seen)
+    const uint8_t *values = page + L::kV, *k_scales = page + L::kKs, *v_scales = page + L::kVs;
+    k = *reinterpret_cast<const u32x4*>(page + (uint32_t)tid * 16);
+    v = *reinterpret_cast<const u32x4*>(values + (uint32_t)tid * 16);
+    ks = k_scales[(uint32_t)tid];
+    vs = v_scales[(uint32_t)tid];
   }
   template <typename E>
   __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* odd) {
@@ -505,8 +496,8 @@ struct WideState {
   f32x16 acc[D / 32];
 };
 
-// Takes 32 kU keys of a tile in LDS, k0 and v0 being the lane's first places: 16 j channels further is
-// k0 ^ 32 j, 32 d channels v0 ^ 64 d, and 8, 16 or 32 rows keep the swizzle.
+// Takes 32 kU keys of a tile in LDS, k0 and v0 being the lane's first places (8 rows further for values, 16 for
+// keys, have the same swizzle).
 template <typename E, int D, int kU>
 __device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D / 16], const char* kl, const char* vl, int k0,
                                           int v0, float c, bool full, uint64_t seen) {
@@ -517,7 +508,7 @@ __device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D /
     for (int e = 0; e < 16; ++e) x[u][e] = 0.f;
 #pragma unroll
     for (int j = 0; j < D / 16; ++j)
-      x[u] = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(kl + (k0 ^ (j << 5)) + u * 32 * 2 * D), q[j], x[u]);
+      x[u] = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(kl + (k0 ^ k_step<D>(j)) + u * 32 * 2 * D), q[j], x[u]);
   }
   if (!full) {
 #pragma unroll
@@ -530,16 +521,15 @@ __device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D /
   for (int u = 0; u < kU; ++u)
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, x[u][e]);
-  top = fmaxf(top, __shfl_xor(top, 32));
-  const float m = fmaxf(st.m, top * c);
-  const float base = m == -INFINITY ? 0.f : m - E::kBias;
-  if (__any(m > st.m)) {
-    const float was = __builtin_amdgcn_exp2f(st.m - E::kBias - base);
+  top = max_across_32(top) * c;
+  if (__any(top > st.m + kLag)) {
+    const float m = fmaxf(st.m, top), was = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
     st.l *= was;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) st.acc[d] *= was;
     st.m = m;
   }
+  const float base = st.m == -INFINITY ? 0.f : st.m - E::kBias;
   float sum = 0.f;
 #pragma unroll
   for (int u = 0; u < kU; ++u)
@@ -556,7 +546,7 @@ __device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D /
     const u32x4 p = {E::pair(y[e], y[e + 1]), E::pair(y[e + 2], y[e + 3]), E::pair(y[e + 4], y[e + 5]), E::pair(y[e + 6], y[e + 7])};
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
-      const char* at = vl + (v0 ^ (d << 6)) + u * 16 * 2 * D;
+      const char* at = vl + (v0 ^ v_step(64 * d)) + u * 16 * 2 * D;
       const u32x2 lo = read_transposed(at), hi = read_transposed(at + 8 * 2 * D);
       st.acc[d] = Mfma<E>::m32(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, st.acc[d]);
     }
@@ -569,9 +559,9 @@ template <typename E, int D, int kW, bool kPaged>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   using L = PageLayout<D>;
   constexpr int kRows = 32 * kW, kU = kW / 2;       // rows of a workgroup; 32-key parts of a tile a wavefront
-  __shared__ __align__(16) char lds[2][64 * 2 * D];
+  constexpr int kTile = 64 * 2 * D;
+  __shared__ __align__(16) char lds[2][2 * kTile];  // two tiles, keys then values: one is read while the next is written
   __shared__ uint32_t odd;                          // a tile not seen in full had values that are not finite
-  char *const kl = lds[0], *const vl = lds[1];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
   const int split = blockIdx.x % sp.n, tile_row = blockIdx.x / sp.n, hk = blockIdx.y, b = blockIdx.z;
   const Seq s = sequence(a, b);
@@ -602,6 +592,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   const int shift = 4 * half + 32 * u0;             // a lane's first key in a tile
   const float c = score_factor(a.scale);
   if (tid == 0) odd = 0;
+  __syncthreads();
 
   const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
   const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
@@ -611,54 +602,92 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
     return sees_new(a, s, row).at(at);
   };
 
-  int t = t0;
+  int t = t0, buf = 0;
+  bool cached;
   if constexpr (kPaged) {
-    WidePage<D> x;
-    const uint8_t* page = nullptr;
-    int at = 0;
-    auto fetch = [&](int tile) {
-      bool cached;
-      at = tile_of<kPage, 64>(span, tile, &cached);
-      page = page_of(a.kv, b, at / kPage, hk);
-      x.load(page, tid);
+    // Two tiles are on their way in registers while one is in LDS: a tile's codes are a few registers, and
+    // memory takes longer than the products of one.
+    struct Stage {
+      WidePage<D> x;
+      const uint8_t* page;
+    } a0, a1;
+    auto entry = [&](int tile) -> int32_t {
+      return tile < nc ? table_entry(a.kv, b, tile_of<kPage, 64>(span, tile, &cached) / kPage) : -1;
     };
-    if (t < nc) fetch(t);
-    for (; t < nc; ++t) {
-      const uint8_t* now = page;
-      const int here = at;
-      const bool full = now && full_cached(a, s, i1, here, 64);
-      __syncthreads();                              // the last tile has been read
-      x.template store<E>(kl, vl, tid, full, now ? s.ctx - here : 0, &odd);
-      if (t + 1 < nc) fetch(t + 1);
+    auto load = [&](Stage& g, int32_t e) {
+      g.page = page_at(a.kv, e, hk);
+      g.x.load(g.page, tid);
+    };
+    auto full_at = [&](int here, bool there) { return there && full_cached(a, s, i1, here, 64); };
+    auto store = [&](Stage& g, int tile, int to) {
+      const int here = tile_of<kPage, 64>(span, tile, &cached);
+      g.x.template store<E>(lds[to], lds[to] + kTile, tid, full_at(here, g.page), g.page ? s.ctx - here : 0, &odd);
+    };
+    int32_t ahead = -1;
+    bool there = false;                             // the tile in LDS has a page
+    if (t < nc) {
+      const int32_t e0 = entry(t), e1 = entry(t + 1), e2 = entry(t + 2);
+      ahead = entry(t + 3);
+      load(a0, e0);
+      load(a1, e1);
+      store(a0, t, 0);
+      there = a0.page;
+      load(a0, e2);
       __syncthreads();
-      if (!mine) continue;
-      wide_tile<E, D, kU>(st, q, kl, vl, k0, v0, c, full, full ? 0 : now ? sees(true, here) >> shift : 0);
+    }
+    auto step = [&](Stage& g) {                     // tile t is in LDS, t + 1 in g
+      if (mine) {
+        const int here = tile_of<kPage, 64>(span, t, &cached);
+        const bool full = full_at(here, there);
+        wide_tile<E, D, kU>(st, q, lds[buf], lds[buf] + kTile, k0, v0, c, full, full ? 0 : there ? sees(true, here) >> shift : 0);
+      }
+      if (t + 1 < nc) {
+        store(g, t + 1, buf ^ 1);
+        there = g.page;
+        load(g, ahead);
+        ahead = entry(t + 4);
+      }
+      __syncthreads();
+      buf ^= 1;
+      ++t;
+    };
+    while (t < nc) {
+      step(a1);
+      if (t < nc) step(a0);
     }
   }
   {
     WideTensor<D> x;
-    int at = 0;
-    auto fetch = [&](int tile) {
-      bool cached;
-      at = tile_of<kPage, 64>(span, tile, &cached);
-      x.load(kb, vb, a.k.t, a.v.t, at, s.nk, tid);
+    auto load = [&](int tile) {
+      if (tile < t1) x.load(kb, vb, a.k.t, a.v.t, tile_of<kPage, 64>(span, tile, &cached), s.nk, tid);
     };
-    if (t < t1) fetch(t);
+    auto store = [&](int tile, int to) {
+      const int here = tile_of<kPage, 64>(span, tile, &cached);
+      x.template store<E>(lds[to], lds[to] + kTile, tid, full_new(a, s, i0, i1, here, 64), s.nk - here, &odd);
+    };
+    if (t < t1) {
+      load(t);
+      store(t, buf);
+      load(t + 1);
+      __syncthreads();
+    }
     for (; t < t1; ++t) {
-      const int here = at;
-      const bool full = full_new(a, s, i0, i1, here, 64);
+      if (mine) {
+        const int here = tile_of<kPage, 64>(span, t, &cached);
+        const bool full = full_new(a, s, i0, i1, here, 64);
+        wide_tile<E, D, kU>(st, q, lds[buf], lds[buf] + kTile, k0, v0, c, full, full ? 0 : sees(false, here) >> shift);
+      }
+      if (t + 1 < t1) {
+        store(t + 1, buf ^ 1);
+        load(t + 2);
+      }
       __syncthreads();
-      x.template store<E>(kl, vl, tid, full, s.nk - here, &odd);
-      if (t + 1 < t1) fetch(t + 1);
-      __syncthreads();
-      if (!mine) continue;
-      wide_tile<E, D, kU>(st, q, kl, vl, k0, v0, c, full, full ? 0 : sees(false, here) >> shift);
+      buf ^= 1;
     }
   }
   __syncthreads();
   if (odd && mine) {
     for (t = t0; t < t1; ++t) {
-      bool cached;
       const int at = tile_of<kPage, 64>(span, t, &cached), n = min(64, (cached ? s.ctx : s.nk) - at);
       const uint8_t* page = kPaged && cached ? page_of(a.kv, b, at / kPage, hk) : nullptr;
       if (cached ? page == nullptr || full_cached(a, s, i1, at, 64) : full_new(a, s, i0, i1, at, 64)) continue;
@@ -740,30 +769,47 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   }
 }
 
-// Joins the splits of a row: one wavefront a row, a lane D / 64 channels.
-template <typename E, int D>
+// Joins the splits of a row.  D / 4 lanes have a row's channels; kGroups such groups take every kGroups-th split
+// of one row and add up through LDS, so that a row of many splits keeps many loads in flight.
+template <typename E, int D, int kGroups>
 __global__ __launch_bounds__(256) void combine_kernel(AttnArgs a, Split sp) {
-  const int lane = threadIdx.x & 63, hk = blockIdx.y, b = blockIdx.z;
-  const int64_t r = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kGroups);
+  __shared__ __align__(16) f32x4 part[kGroups > 1 ? 256 : 1];
+  const int tid = threadIdx.x, ch = tid % kLanes, group = tid / kLanes % kGroups, hk = blockIdx.y, b = blockIdx.z;
+  const int64_t r = (int64_t)blockIdx.x * kRows + tid / (kLanes * kGroups);
   const Seq s = sequence(a, b);
-  if (r >= (int64_t)s.nq * a.G) return;
-  const int64_t at = part_of(a, sp, b, hk, (int)r);
-  float m = -INFINITY, l = 0.f, o[D / 64] = {};
-  for (int k = 0; k < sp.n; ++k) m = fmaxf(m, sp.ml[2 * (at + k)]);
-  for (int k = 0; k < sp.n; ++k) {
-    const float mk = sp.ml[2 * (at + k)], lk = sp.ml[2 * (at + k) + 1];
-    if (lk == 0.f) continue;                        // a split without a key left its sums unset
-    const float f = mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - m);
-    l += lk * f;
+  const bool there = r < (int64_t)s.nq * a.G;
+  if (kGroups == 1 && !there) return;
+  const int64_t at = part_of(a, sp, b, hk, there ? (int)r : 0);
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const float* ml = sp.ml + 2 * at;
+  if (there) {
+    for (int k = 0; k < sp.n; ++k) m = fmaxf(m, ml[2 * k]);
+    for (int k = 0; k < sp.n; ++k) {
+      const float mk = ml[2 * k], lk = ml[2 * k + 1];
+      l += lk == 0.f ? 0.f : mk == -INFINITY ? lk : lk * __builtin_amdgcn_exp2f(mk - m);
+    }
+#pragma unroll 4
+    for (int k = group; k < sp.n; k += kGroups) {
+      const float mk = ml[2 * k], lk = ml[2 * k + 1];
+      const f32x4 x = *reinterpret_cast<const f32x4*>(sp.sum + (at + k) * D + 4 * ch);
+      const float f = mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - m);
+      if (lk != 0.f) o += f * x;                    // (a split without a key left its sums unset)
+    }
+  }
+  if constexpr (kGroups > 1) {
+    part[tid] = o;
+    __syncthreads();
+    if (group != 0 || !there) return;
 #pragma unroll
-    for (int c = 0; c < D / 64; ++c) o[c] += f * sp.sum[(at + k) * D + lane * (D / 64) + c];
+    for (int g = 1; g < kGroups; ++g) o += part[tid + g * kLanes];
   }
   const int i = (int)(r / a.G), h = hk * a.G + (int)(r % a.G);
   const float inv = l == 0.f ? 0.f : 1.f / l;
-  char* dst = a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h + lane * (D / 64));
-  if constexpr (D == 128) *reinterpret_cast<uint32_t*>(dst) = E::pair(o[0] * inv, o[1] * inv);
-  else *reinterpret_cast<uint16_t*>(dst) = (uint16_t)E::pair(o[0] * inv, 0.f);
-  if (a.lse && lane == 0)
+  *reinterpret_cast<u32x2*>(a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h + 4 * ch)) =
+      u32x2{E::pair(o[0] * inv, o[1] * inv), E::pair(o[2] * inv, o[3] * inv)};
+  if (a.lse && ch == 0)
     a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - E::kBias + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
@@ -777,7 +823,9 @@ hipError_t launch(const AttnArgs& a, const Split& sp, hipStream_t stream) {
   else wide_kernel<E, D, 4, kPaged><<<dim3((unsigned)((R + 127) / 128 * sp.n), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.n == 1) return e;
-  combine_kernel<E, D><<<dim3((unsigned)((R + 3) / 4), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  const int lanes = D / 4;
+  if (sp.n < 8) combine_kernel<E, D, 1><<<dim3((unsigned)((R * lanes + 255) / 256), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  else combine_kernel<E, D, 256 / lanes><<<dim3((unsigned)R, a.Hkv, a.B), 256, 0, stream>>>(a, sp);
   return hipGetLastError();
 }
 

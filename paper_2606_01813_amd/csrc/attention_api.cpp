@@ -19,7 +19,8 @@ using caddtree::AttnArgs;
 using caddtree::PagedKV;
 using caddtree::View;
 
-constexpr int kCUs = 256;
+constexpr int kResident = 512;                     // workgroups of the attention kernels on the card at a time
+constexpr int64_t kMaxStride = (int64_t)1 << 24;   // of a token: 64 of them stay within 2^31 bytes
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;   // positions, and the tokens of a table, stay within int32
 
 caddtree_status_t check_type(int dtype, int32_t head_dim) {
@@ -34,8 +35,10 @@ caddtree_status_t check_type(int dtype, int32_t head_dim) {
 caddtree_status_t check_view(const char* name, const caddtree_view_t& v, bool required) {
   if (v.data == nullptr) return required ? fail(CADDTREE_E_INVALID, "%s is NULL", name) : CADDTREE_OK;
   if (reinterpret_cast<uintptr_t>(v.data) % 16 != 0) return fail(CADDTREE_E_INVALID, "%s must be 16-byte aligned", name);
-  if (v.stride_b % 8 != 0 || v.stride_t % 8 != 0 || v.stride_h % 8 != 0)
-    return fail(CADDTREE_E_INVALID, "the strides of %s must be multiples of 8 elements", name);
+  if (v.stride_b < 0 || v.stride_t < 0 || v.stride_h < 0 || v.stride_b % 8 != 0 || v.stride_t % 8 != 0 || v.stride_h % 8 != 0)
+    return fail(CADDTREE_E_INVALID, "the strides of %s must be multiples of 8 elements, and not negative", name);
+  if (v.stride_t >= kMaxStride)
+    return fail(CADDTREE_E_UNSUPPORTED, "stride_t = %lld of %s exceeds 2^24 elements", (long long)v.stride_t, name);
   return CADDTREE_OK;
 }
 
@@ -146,16 +149,16 @@ caddtree_status_t check_workspace(const void* workspace) {
   return CADDTREE_OK;
 }
 
-// How many parts a row's keys are cut into, from the sizes alone (lengths are on the device).
+// How many parts a row's keys are cut into, from the sizes alone (lengths are on the device): as many as fill the
+// card, two workgroups a compute unit, where each keeps a few tiles a wavefront.  A call that fills it by itself is
+// not cut: the parts' sums cost more than an uneven last round does (32 trees of 257 rows, 2304 workgroups: 712 us
+// whole, 736 in two parts).
 int32_t splits_of(const caddtree_attention_t* a) {
-  const int64_t rows = (int64_t)a->T * (a->n_heads / a->n_kv_heads);
+  const int64_t G = a->n_heads / a->n_kv_heads, rows = a->T * G;
   const int64_t groups = (int64_t)a->B * a->n_kv_heads * (rows <= 64 ? 1 : (rows + 127) / 128);
-  const int64_t keys = (int64_t)a->table_pages * CADDTREE_PAGE + a->S;
-  int64_t reach = keys;
-  if (a->window > 0) reach = std::min(keys, (int64_t)a->window + a->sinks + a->T);
-  const int64_t most = std::max<int64_t>(1, reach / 256);             // at least a few tiles each
-  if (groups == 0) return 1;
-  return (int32_t)std::min<int64_t>(std::min<int64_t>(most, 128), std::max<int64_t>(1, (4 * kCUs + groups - 1) / groups));
+  int64_t reach = (int64_t)a->table_pages * CADDTREE_PAGE + a->S;      // keys of a workgroup's rows at most
+  if (a->window > 0) reach = std::min(reach, (int64_t)a->window + a->sinks + std::min<int64_t>(a->T, 128 / G + 1) + 64);
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(kResident / std::max<int64_t>(groups, 1), reach / 384));
 }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t split_bytes(const caddtree_attention_t* a, int32_t n) {

@@ -22,9 +22,9 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 // The 16-bit element types: pairs in a 32-bit register, the 4-bit conversions (exact: a code times a
-// power of two) and the range of the scales' exponents.  Weights of the softmax are exp2(x - m + kBias):
-// 1 at most in bf16; in f16, whose normal numbers end at 2^-14, 2^14 at most, so that a weight keeps its 11
-// bits down to 2^-28 of the largest.
+// power of two) and the range of the scales' exponents.  Weights of the softmax are exp2(x - m + kBias) with a
+// maximum m that may lag up to 8 behind (kLag): 2^8 at most in bf16; in f16, whose normal numbers end at
+// 2^-14, 2^14 at most, and a weight keeps its 11 bits down to 2^-20 of 2^m.
 struct BF16 {
   using T = __bf16;
   static constexpr int kExpLo = -125, kExpHi = 125;
@@ -51,7 +51,7 @@ struct BF16 {
 struct F16 {
   using T = _Float16;
   static constexpr int kExpLo = -13, kExpHi = 13;
-  static constexpr float kBias = 14.f;
+  static constexpr float kBias = 6.f;
   static constexpr uint32_t kInf = 0x7c00;
   static constexpr uint32_t kNaN = 0x7e007e00;
   static __device__ float lo(uint32_t p) { return (float)__builtin_bit_cast(f16x2, p)[0]; }
@@ -119,6 +119,13 @@ __device__ inline uint8_t* page_of(const PagedKV& kv, int b, int page, int h) {
   if (p < 0 || p >= kv.n_pages) return nullptr;
   return kv.pages + ((int64_t)p * kv.heads + h) * kv.page_bytes;
 }
+// ... in two steps for a page that all lanes look up together: its table entry, loaded ahead, and the pointer in
+// scalar registers, so that a lane's loads need no more than its 32-bit offset.
+__device__ inline int32_t table_entry(const PagedKV& kv, int b, int page) { return kv.table[(int64_t)b * kv.table_pages + page]; }
+__device__ inline uint8_t* page_at(const PagedKV& kv, int32_t entry, int h) {
+  const int32_t p = __builtin_amdgcn_readfirstlane(entry);
+  return p < 0 || p >= kv.n_pages ? nullptr : kv.pages + ((int64_t)p * kv.heads + h) * kv.page_bytes;
+}
 // Offsets in a page and head of head dimension D.
 template <int D>
 struct PageLayout {
@@ -137,9 +144,9 @@ __device__ inline void decode_block(const u32x4 codes, uint32_t scale_byte, uint
     out[4 * w + 2] = E::template from4<2>(codes[w], s);
     out[4 * w + 3] = E::template from4<3>(codes[w], s);
   }
-  if (scale_byte == 255)
+  if (__any(scale_byte == 255))                      // (rare: one branch in place of 16 selects)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) out[i] = E::kNaN;
+    for (int i = 0; i < 16; ++i) out[i] = scale_byte == 255 ? E::kNaN : out[i];
 }
 
 }  // namespace at

@@ -33,6 +33,9 @@ struct Mfma<F16> {
   }
 };
 
+// A row's sums are rescaled when its maximum has risen by more than this (in powers of two): they grow by 2^8 at
+// most in between, and most tiles spare the products with every sum.
+constexpr float kLag = 8.f;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Scores are kept unscaled, so that a weight is one fused multiply-add and one exp2: exp2(s c - base) with
@@ -147,19 +150,46 @@ __device__ inline bool full_new(const AttnArgs& a, const Seq& s, int i0, int i1,
          (a.window == 0 || j0 > off + i1 - a.window || j0 + n <= a.sinks - s.ctx);
 }
 
-// LDS layouts.  A row is a token's D channels; 16-byte pieces trade places by the row so that no two lanes
-// of one access meet in a bank: keys are read 16 bytes a lane with the rows side by side, values 8 bytes a
-// lane, four rows by 32 or 64 bytes, through the transposing read.
+// LDS layouts.  A row is a token's D channels; 16-byte pieces trade places by the row so that the lanes that
+// access LDS together (eight of 16 bytes, sixteen of 8) meet no bank twice: keys are read 16 bytes a lane,
+// eight rows side by side; values 8 bytes a lane, four rows by 32 bytes, through the transposing read; both
+// are written 16 bytes a lane, either a row's pieces in turn or, from a page, a piece of every block of
+// 2 (D = 128) or 4 rows.
 template <int D>
 __device__ int k_at(int row, int piece) {          // piece: 16 bytes
-  return row * (2 * D) + ((piece ^ (D == 128 ? row & 15 : (row >> 1) & 7)) << 4);
+  if (D == 128) return row * 256 + ((((piece & 3) << 2 | piece >> 2) ^ ((row & 1) << 2 | ((row >> 1) & 3) | (row & 8))) << 4);
+  return row * 128 + ((((piece & 3) << 1 | piece >> 2) ^ ((row & 3) << 1 | ((row >> 2) & 1))) << 4);
+}
+// keys 16 j channels further (two pieces a step) are at k_at ^ k_step(j)
+template <int D>
+__device__ constexpr int k_step(int j) {
+  const int piece = 2 * j;
+  return (D == 128 ? (piece & 3) << 2 | piece >> 2 : (piece & 3) << 1 | piece >> 2) << 4;
+}
+// the n-th piece of a row that is written piece after piece
+template <int D>
+__device__ int k_piece(int n) {
+  return D == 128 ? (n & 3) << 2 | n >> 2 : n;
 }
 template <int D>
 __device__ int v_at(int row, int byte) {
-  const int block = byte >> 6, sub = (byte >> 4) & 3;
-  if (D == 128) return row * 256 + ((block ^ (row & 3)) << 6) + ((sub ^ (row & 3) ^ ((row >> 1) & 2)) << 4) + (byte & 15);
-  const int y = (row >> 1) & 3;
+  const int block = byte >> 6, sub = (byte >> 4) & 3, y = row & 3;
+  if (D == 128) return row * 256 + ((block ^ y) << 6) + ((sub ^ y ^ ((row >> 1) & 2) ^ (block & 2)) << 4) + (byte & 15);
   return row * 128 + ((block ^ (y & 1)) << 6) + ((sub ^ y) << 4) + (byte & 15);
+}
+// values `byte` (a multiple of 32) bytes further are at v_at ^ v_step(byte)
+__device__ constexpr int v_step(int byte) { return byte ^ ((byte >> 6) & 2) << 4; }
+
+// the larger of the values of lanes l and l ^ 32, l ^ 16
+__device__ inline float max_across_32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t lo = r[0], hi = r[1];
+  return fmaxf(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
+}
+__device__ inline float max_across_16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, x), __builtin_bit_cast(uint32_t, x), false, false);
+  const uint32_t lo = r[0], hi = r[1];
+  return fmaxf(__builtin_bit_cast(float, lo), __builtin_bit_cast(float, hi));
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));

@@ -269,6 +269,7 @@ BAD_ATTENTION = [
     (dict(scale=float("nan")), INVALID), (dict(scale=float("inf")), INVALID), (dict(window=-1), INVALID), (dict(sinks=-1), INVALID),
     (dict(order=3), INVALID), (dict(q=(0, 0, 0, 0)), INVALID), (dict(q=(0x1008, 640, 128, 64)), INVALID),
     (dict(q=(0x1000, 641, 128, 64)), INVALID), (dict(out=(0, 0, 0, 0)), INVALID), (dict(out=(0x1000, 640, 128, 4)), INVALID),
+    (dict(q=(0x1000, 640, -128, 64)), INVALID), (dict(q=(0x1000, 640, 2 ** 24, 64)), UNSUPPORTED),
 ]
 
 
