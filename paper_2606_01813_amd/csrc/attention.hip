@@ -419,47 +419,49 @@ __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a, Split sp) {
 
 // ---------------------------------------------------------------- many rows
 
-
-// A tile's 64 keys and values on their way to LDS, a workgroup's 256 threads' shares.
+// A tile's 64 keys, or values, on their way to LDS: a share of a workgroup's 256 threads of a tensor's rows ...
 template <int D>
-struct WideTensor {
-  static constexpr int kN = D / 32;                 // 16-byte pieces of keys, and of values, a thread
-  u32x4 k[kN], v[kN];
-  __device__ void load(const char* kp, const char* vp, int64_t kt, int64_t vt, int j0, int nk, int tid) {
-    const char *kb = kp + 2 * (j0 * kt), *vb = vp + 2 * (j0 * vt);
+struct TensorPart {
+  static constexpr int kRows = 2048 / D, kN = 64 / kRows;      // rows a step (16 or 32); 16-byte pieces a thread
+  u32x4 x[kN];
+  __device__ void load(const char* p, int64_t stride, int j0, int nk, int tid) {
+    const char* base = p + 2 * (j0 * stride);
     const uint32_t piece = k_piece<D>(tid % (D / 8)) * 16;
 #pragma unroll
     for (int u = 0; u < kN; ++u) {                  // (a key that is not there: the tile's first one in its place)
-      const int token = tid / (D / 8) + u * (2048 / D);
+      const int token = tid / (D / 8) + u * kRows;
       const uint32_t row = j0 + token < nk ? token : 0;
-      k[u] = *reinterpret_cast<const u32x4*>(kb + (row * (2 * (uint32_t)kt) + piece));
-      v[u] = *reinterpret_cast<const u32x4*>(vb + (row * (2 * (uint32_t)vt) + piece));
+      x[u] = *reinterpret_cast<const u32x4*>(base + (row * (2 * (uint32_t)stride) + piece));
     }
   }
-  template <typename E>
-  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* odd) {
-    const int row = tid / (D / 8), piece = k_piece<D>(tid % (D / 8)), k0 = k_at<D>(row, piece), v0 = v_at<D>(row, piece * 16);
+  // (kRows rows further: the same swizzle)
+  __device__ void store_keys(char* lds, int tid) const {
+    const int at = k_at<D>(tid / (D / 8), k_piece<D>(tid % (D / 8)));
 #pragma unroll
-    for (int u = 0; u < kN; ++u) {                  // (16 or 32 rows further: the same swizzle)
-      const int token = row + u * (2048 / D);
+    for (int u = 0; u < kN; ++u) *reinterpret_cast<u32x4*>(lds + at + u * kRows * 2 * D) = x[u];
+  }
+  template <typename E>
+  __device__ void store_values(char* lds, int tid, bool full, int there, uint32_t* odd) {
+    const int row = tid / (D / 8), at = v_at<D>(row, k_piece<D>(tid % (D / 8)) * 16);
+#pragma unroll
+    for (int u = 0; u < kN; ++u) {
       if (!full) {
-        if (token >= there) v[u] = u32x4{0, 0, 0, 0};
-        if (clean_pairs<E>(v[u])) *odd = 1;
+        if (row + u * kRows >= there) x[u] = u32x4{0, 0, 0, 0};
+        if (clean_pairs<E>(x[u])) *odd = 1;
       }
-      *reinterpret_cast<u32x4*>(kl + k0 + u * 4096) = k[u];
-      *reinterpret_cast<u32x4*>(vl + v0 + u * 4096) = v[u];
+      *reinterpret_cast<u32x4*>(lds + at + u * kRows * 2 * D) = x[u];
     }
   }
 };
-// ... of a page: a block of keys and one of values a thread (D = 64: half the threads)
+// ... and of a page: a block of 32 channels of a key and one of a value a thread (D = 64: half of the threads)
 template <int D>
-struct WidePage {
+struct PagePart {
+  static constexpr int kBlocks = kPage * (D / kBlock);
   u32x4 k = {}, v = {};
   uint32_t ks = 0, vs = 0;
-  static constexpr int kThreads = kPage * (D / kBlock);
   __device__ void load(const uint8_t* page, int tid) {
     using L = PageLayout<D>;
-    if (tid >= kThreads || page == nullptr) return; // (no key of such a page is seen)
+    if (page == nullptr || tid >= kBlocks) return;  // (no key of a page that is not there is seen)
     const uint8_t *values = page + L::kV, *k_scales = page + L::kKs, *v_scales = page + L::kVs;
     k = *reinterpret_cast<const u32x4*>(page + (uint32_t)tid * 16);
     v = *reinterpret_cast<const u32x4*>(values + (uint32_t)tid * 16);
@@ -467,14 +469,14 @@ struct WidePage {
     vs = v_scales[(uint32_t)tid];
   }
   template <typename E>
-  __device__ void store(char* kl, char* vl, int tid, bool full, int there, uint32_t* odd) {
-    if (tid >= kThreads) return;
+  __device__ void store(char* keys, char* values, int tid, bool full, int there, uint32_t* odd) const {
+    if (tid >= kBlocks) return;
     const int token = tid / (D / kBlock), blk = tid % (D / kBlock);
     uint32_t x[16];
     decode_block<E>(k, ks, x);
 #pragma unroll
     for (int w = 0; w < 4; ++w)
-      *reinterpret_cast<u32x4*>(kl + k_at<D>(token, blk * 4 + w)) = u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
+      *reinterpret_cast<u32x4*>(keys + k_at<D>(token, blk * 4 + w)) = u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
     decode_block<E>(v, vs, x);
     if (!full) {
       const bool gone = token >= there, nan = !gone && vs == 255;
@@ -485,7 +487,7 @@ struct WidePage {
     }
 #pragma unroll
     for (int w = 0; w < 4; ++w)
-      *reinterpret_cast<u32x4*>(vl + v_at<D>(token, blk * 64 + w * 16)) = u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
+      *reinterpret_cast<u32x4*>(values + v_at<D>(token, blk * 64 + w * 16)) = u32x4{x[4 * w], x[4 * w + 1], x[4 * w + 2], x[4 * w + 3]};
   }
 };
 
@@ -496,29 +498,29 @@ struct WideState {
   f32x16 acc[D / 32];
 };
 
-// Takes 32 kU keys of a tile in LDS, k0 and v0 being the lane's first places (8 rows further for values, 16 for
-// keys, have the same swizzle).
-template <typename E, int D, int kU>
-__device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D / 16], const char* kl, const char* vl, int k0,
-                                          int v0, float c, bool full, uint64_t seen) {
-  f32x16 x[kU];                                     // row col's keys 32 u + 8 (e / 4) + 4 half + e % 4
+// Scores of 32 keys: row col's keys 8 (e / 4) + 4 half + e % 4.  k0: the lane's first place in them.
+template <typename E, int D>
+__device__ __forceinline__ f32x16 wide_scores(const u32x4 (&q)[D / 16], const char* keys, int k0) {
+  f32x16 x;
 #pragma unroll
-  for (int u = 0; u < kU; ++u) {
+  for (int e = 0; e < 16; ++e) x[e] = 0.f;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) x[u][e] = 0.f;
-#pragma unroll
-    for (int j = 0; j < D / 16; ++j)
-      x[u] = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(kl + (k0 ^ k_step<D>(j)) + u * 32 * 2 * D), q[j], x[u]);
-  }
+  for (int j = 0; j < D / 16; ++j) x = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(keys + (k0 ^ k_step<D>(j))), q[j], x);
+  return x;
+}
+// ... of 32 kH keys: unseen ones left out and the row's maximum raised over them, where it lags too far behind.
+// seen: bit k for the lane's key 32 u + 8 (e / 4) + e % 4.
+template <typename E, int D, int kH>
+__device__ __forceinline__ void wide_raise(WideState<D>& st, f32x16 (&x)[kH], float c, bool full, uint64_t seen) {
   if (!full) {
 #pragma unroll
-    for (int u = 0; u < kU; ++u)
+    for (int u = 0; u < kH; ++u)
 #pragma unroll
       for (int e = 0; e < 16; ++e) x[u][e] = (seen >> (32 * u + 8 * (e / 4) + e % 4)) & 1 ? x[u][e] : -INFINITY;
   }
   float top = -INFINITY;
 #pragma unroll
-  for (int u = 0; u < kU; ++u)
+  for (int u = 0; u < kH; ++u)
 #pragma unroll
     for (int e = 0; e < 16; ++e) top = fmaxf(top, x[u][e]);
   top = max_across_32(top) * c;
@@ -529,52 +531,120 @@ __device__ __forceinline__ void wide_tile(WideState<D>& st, const u32x4 (&q)[D /
     for (int d = 0; d < D / 32; ++d) st.acc[d] *= was;
     st.m = m;
   }
+}
+// weights of 32 keys, rounded to the inputs' type for the product with the values (their sum is not)
+template <typename E, int D>
+__device__ __forceinline__ void wide_weights(WideState<D>& st, f32x16& x, u32x4 (&p)[2], float c) {
   const float base = st.m == -INFINITY ? 0.f : st.m - E::kBias;
-  float sum = 0.f;
 #pragma unroll
-  for (int u = 0; u < kU; ++u)
+  for (int e = 0; e < 16; ++e) {
+    x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], c, -base));
+    st.l += x[e];                                   // (of this half's keys)
+  }
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      x[u][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[u][e], c, -base));
-      sum += x[u][e];
-    }
-  st.l += sum;                                      // (of this half's keys)
+  for (int u = 0; u < 2; ++u)
+    p[u] = u32x4{E::pair(x[8 * u], x[8 * u + 1]), E::pair(x[8 * u + 2], x[8 * u + 3]), E::pair(x[8 * u + 4], x[8 * u + 5]),
+                 E::pair(x[8 * u + 6], x[8 * u + 7])};
+}
+// ... times the values; v0: the lane's first place in them
+template <typename E, int D>
+__device__ __forceinline__ void wide_values(WideState<D>& st, const u32x4 (&p)[2], const char* values, int v0) {
 #pragma unroll
-  for (int u = 0; u < 2 * kU; ++u) {                // 16 keys an instruction
-    const f32x16& y = x[u / 2];
-    const int e = 8 * (u & 1);
-    const u32x4 p = {E::pair(y[e], y[e + 1]), E::pair(y[e + 2], y[e + 3]), E::pair(y[e + 4], y[e + 5]), E::pair(y[e + 6], y[e + 7])};
+  for (int u = 0; u < 2; ++u)                       // 16 keys an instruction
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d) {
-      const char* at = vl + (v0 ^ v_step(64 * d)) + u * 16 * 2 * D;
+    for (int d = 0; d < D / 32; ++d) {              // (8 and 16 rows further: the same swizzle)
+      const char* at = values + (v0 ^ v_step(64 * d)) + u * 16 * 2 * D;
       const u32x2 lo = read_transposed(at), hi = read_transposed(at + 8 * 2 * D);
-      st.acc[d] = Mfma<E>::m32(u32x4{lo[0], lo[1], hi[0], hi[1]}, p, st.acc[d]);
+      st.acc[d] = Mfma<E>::m32(u32x4{lo[0], lo[1], hi[0], hi[1]}, p[u], st.acc[d]);
+    }
+}
+
+// Values that are not finite, in the tiles t0 .. t1 - 1 that some row sees in part, tokens `from` .. to - 1 of each.
+template <typename E, int D, bool kPaged, typename Sees>
+__device__ __forceinline__ void add_odd(WideState<D>& st, const AttnArgs& a, const Seq& s, const Span& span, int b, int hk, int i0, int i1,
+                                     int t0, int t1, int from, int to, int half, Sees sees) {
+  using L = PageLayout<D>;
+  const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
+  for (int t = t0; t < t1; ++t) {
+    bool cached;
+    const int at = tile_of<kPage, 64>(span, t, &cached), n = min(64, (cached ? s.ctx : s.nk) - at);
+    const uint8_t* page = kPaged && cached ? page_of(a.kv, b, at / kPage, hk) : nullptr;
+    if (cached ? page == nullptr || full_cached(a, s, i1, at, 64) : full_new(a, s, i0, i1, at, 64)) continue;
+    const uint64_t seen = sees(cached, at);
+    for (int token = from; token < min(n, to); ++token) {
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f32x4 v;
+          if (kPaged && cached) {
+            const float x = page[L::kVs + token * L::kScales + d] == 255 ? __builtin_nanf("") : 0.f;
+            v = f32x4{x, x, x, x};
+          } else {
+            v = unclean<E>(vb + 2 * ((at + token) * a.v.t + 32 * d + 8 * e + 4 * half));
+          }
+          if ((seen >> token) & 1)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) st.acc[d][4 * e + k] += v[k];
+        }
     }
   }
 }
 
-// kW wavefronts of the four share out the rows, 32 each; with kW = 2 the two pairs take half of a tile's keys
-// each and join their sums at the end.
-template <typename E, int D, int kW, bool kPaged>
-__global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
-  using L = PageLayout<D>;
-  constexpr int kRows = 32 * kW, kU = kW / 2;       // rows of a workgroup; 32-key parts of a tile a wavefront
+// The row's result, or its part of it.
+template <typename E, int D>
+__device__ __forceinline__ void wide_finish(const WideState<D>& st, const AttnArgs& a, const Split& sp, int b, int hk, int r, int i, int h,
+                                            int half, int split) {
+  const float l = st.l;
+  if (sp.n == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    char* dst = a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x16& x = st.acc[d];
+        const u32x2 y = {E::pair(x[4 * e] * inv, x[4 * e + 1] * inv), E::pair(x[4 * e + 2] * inv, x[4 * e + 3] * inv)};
+        *reinterpret_cast<u32x2*>(dst + 2 * (32 * d + 8 * e + 4 * half)) = y;
+      }
+    if (a.lse && half == 0)
+      a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (st.m - E::kBias + __builtin_amdgcn_logf(l)) * kLn2;
+  } else {
+    const int64_t to = part_of(a, sp, b, hk, r) + split;
+    if (half == 0) {
+      sp.ml[2 * to] = st.m;
+      sp.ml[2 * to + 1] = l;
+    }
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<f32x4*>(sp.sum + to * D + 32 * d + 8 * e + 4 * half) =
+            f32x4{st.acc[d][4 * e], st.acc[d][4 * e + 1], st.acc[d][4 * e + 2], st.acc[d][4 * e + 3]};
+  }
+}
+
+// 33 to 64 rows: two wavefront pairs share the rows out and take half of a tile's keys each, whose sums they join at
+// the end.  Bound by reading the keys, so two tiles are on their way in registers (a tile's codes are a few) while
+// one is in LDS: memory takes longer than the products of one.
+template <typename E, int D, bool kPaged>
+__global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
   constexpr int kTile = 64 * 2 * D;
   __shared__ __align__(16) char lds[2][2 * kTile];  // two tiles, keys then values: one is read while the next is written
   __shared__ uint32_t odd;                          // a tile not seen in full had values that are not finite
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
-  const int split = blockIdx.x % sp.n, tile_row = blockIdx.x / sp.n, hk = blockIdx.y, b = blockIdx.z;
+  const int split = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
   const Seq s = sequence(a, b);
-  const int R = s.nq * a.G, r0 = tile_row * kRows;
-  if (r0 >= R) return;
-  const int i0 = r0 / a.G, i1 = min(R - 1, r0 + kRows - 1) / a.G;
+  const int R = s.nq * a.G;
+  if (R == 0) return;
+  const int i0 = 0, i1 = s.nq - 1;
   const Span span = span_of<kPage, 64>(a, s, i0, i1);
   const int per = ceil_div(span.n, sp.n), t0 = split * per, t1 = min(span.n, t0 + per);
   const int nc = kPaged ? max(t0, min(t1, span.a + span.c - span.b)) : t0;   // this split's cached tiles come first
 
-  const int r = r0 + 32 * (wave % kW) + col, rr = min(r, R - 1), i = rr / a.G, h = hk * a.G + rr % a.G;
-  const int u0 = kW == 4 ? 0 : wave / kW;           // its first 32-key part
-  const bool mine = r0 + 32 * (wave % kW) < R;      // this wavefront has rows
+  const int r = 32 * (wave & 1) + col, rr = min(r, R - 1), i = rr / a.G, h = hk * a.G + rr % a.G;
+  const int u0 = wave >> 1;                         // its 32-key part
+  const bool mine = 32 * (wave & 1) < R;            // this wavefront has rows
   const RowAt row = row_at(a, s, b, i);
   u32x4 q[D / 16];
   {
@@ -593,7 +663,6 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   const float c = score_factor(a.scale);
   if (tid == 0) odd = 0;
   __syncthreads();
-
   const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
   const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
   auto sees = [&](bool cached, int at) -> uint64_t {
@@ -601,14 +670,19 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
     if (kPaged && a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, row, at);
     return sees_new(a, s, row).at(at);
   };
+  auto take = [&](const char* tile, bool full, uint32_t seen) {
+    f32x16 x[1] = {wide_scores<E, D>(q, tile, k0)};
+    u32x4 p[2];
+    wide_raise<E, D, 1>(st, x, c, full, seen);
+    wide_weights<E, D>(st, x[0], p, c);
+    wide_values<E, D>(st, p, tile + kTile, v0);
+  };
 
   int t = t0, buf = 0;
   bool cached;
   if constexpr (kPaged) {
-    // Two tiles are on their way in registers while one is in LDS: a tile's codes are a few registers, and
-    // memory takes longer than the products of one.
     struct Stage {
-      WidePage<D> x;
+      PagePart<D> x;
       const uint8_t* page;
     } a0, a1;
     auto entry = [&](int tile) -> int32_t {
@@ -639,7 +713,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
       if (mine) {
         const int here = tile_of<kPage, 64>(span, t, &cached);
         const bool full = full_at(here, there);
-        wide_tile<E, D, kU>(st, q, lds[buf], lds[buf] + kTile, k0, v0, c, full, full ? 0 : there ? sees(true, here) >> shift : 0);
+        take(lds[buf], full, full || !there ? 0 : (uint32_t)(sees(true, here) >> shift));
       }
       if (t + 1 < nc) {
         store(g, t + 1, buf ^ 1);
@@ -657,13 +731,17 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
     }
   }
   {
-    WideTensor<D> x;
+    TensorPart<D> k, v;
     auto load = [&](int tile) {
-      if (tile < t1) x.load(kb, vb, a.k.t, a.v.t, tile_of<kPage, 64>(span, tile, &cached), s.nk, tid);
+      if (tile >= t1) return;
+      const int here = tile_of<kPage, 64>(span, tile, &cached);
+      k.load(kb, a.k.t, here, s.nk, tid);
+      v.load(vb, a.v.t, here, s.nk, tid);
     };
     auto store = [&](int tile, int to) {
       const int here = tile_of<kPage, 64>(span, tile, &cached);
-      x.template store<E>(lds[to], lds[to] + kTile, tid, full_new(a, s, i0, i1, here, 64), s.nk - here, &odd);
+      k.store_keys(lds[to], tid);
+      v.template store_values<E>(lds[to] + kTile, tid, full_new(a, s, i0, i1, here, 64), s.nk - here, &odd);
     };
     if (t < t1) {
       load(t);
@@ -675,7 +753,7 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
       if (mine) {
         const int here = tile_of<kPage, 64>(span, t, &cached);
         const bool full = full_new(a, s, i0, i1, here, 64);
-        wide_tile<E, D, kU>(st, q, lds[buf], lds[buf] + kTile, k0, v0, c, full, full ? 0 : sees(false, here) >> shift);
+        take(lds[buf], full, full ? 0 : (uint32_t)(sees(false, here) >> shift));
       }
       if (t + 1 < t1) {
         store(t + 1, buf ^ 1);
@@ -686,87 +764,180 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
     }
   }
   __syncthreads();
-  if (odd && mine) {
-    for (t = t0; t < t1; ++t) {
-      const int at = tile_of<kPage, 64>(span, t, &cached), n = min(64, (cached ? s.ctx : s.nk) - at);
-      const uint8_t* page = kPaged && cached ? page_of(a.kv, b, at / kPage, hk) : nullptr;
-      if (cached ? page == nullptr || full_cached(a, s, i1, at, 64) : full_new(a, s, i0, i1, at, 64)) continue;
-      const uint64_t seen = sees(cached, at);
-      for (int token = 32 * u0; token < min(n, 32 * (u0 + kU)); ++token) {
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            f32x4 v;
-            if (kPaged && cached) {
-              const float x = page[L::kVs + token * L::kScales + d] == 255 ? __builtin_nanf("") : 0.f;
-              v = f32x4{x, x, x, x};
-            } else {
-              v = unclean<E>(vb + 2 * ((at + token) * a.v.t + 32 * d + 8 * e + 4 * half));
-            }
-            if ((seen >> token) & 1)
-#pragma unroll
-              for (int k = 0; k < 4; ++k) st.acc[d][4 * e + k] += v[k];
-          }
-      }
-    }
-  }
-  float m = st.m, l = st.l;
-  f32x16(&acc)[D / 32] = st.acc;
-  l += __shfl_xor(l, 32);
-  if (kW == 2) {                                    // the second pair's sums to the first, 16 registers at a time
+  if (odd && mine) add_odd<E, D, kPaged>(st, a, s, span, b, hk, i0, i1, t0, t1, 32 * u0, 32 * u0 + 32, half, sees);
+  st.l += __shfl_xor(st.l, 32);
+  {                                                 // the second pair's sums to the first, 16 registers at a time
     __syncthreads();
     float* box = reinterpret_cast<float*>(lds) + (wave & 1) * 1024 + lane;   // 2 x 64 lanes x 16 values, the lanes side by side
     float* box_ml = reinterpret_cast<float*>(lds) + 2 * 1024 + (wave & 1) * 128 + lane;
     if (wave >= 2) {
-      box_ml[0] = m;
-      box_ml[64] = l;
+      box_ml[0] = st.m;
+      box_ml[64] = st.l;
     }
     __syncthreads();
-    const float m2 = box_ml[0], l2 = box_ml[64], mm = fmaxf(m, m2);
-    const float f1 = l == 0.f ? 0.f : m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mm);
-    const float f2 = l2 == 0.f ? 0.f : m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mm);
+    const float m2 = box_ml[0], l2 = box_ml[64], m = fmaxf(st.m, m2);
+    const float f1 = st.l == 0.f ? 0.f : st.m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(st.m - m);
+    const float f2 = l2 == 0.f ? 0.f : m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - m);
 #pragma unroll
     for (int d = 0; d < D / 32; ++d) {
       if (wave >= 2)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) box[64 * e] = acc[d][e];
+        for (int e = 0; e < 16; ++e) box[64 * e] = st.acc[d][e];
       __syncthreads();
       if (wave < 2)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) acc[d][e] = acc[d][e] * f1 + box[64 * e] * f2;
+        for (int e = 0; e < 16; ++e) st.acc[d][e] = st.acc[d][e] * f1 + box[64 * e] * f2;
       __syncthreads();
     }
     if (wave >= 2) return;
-    l = l * f1 + l2 * f2;
-    m = mm;
+    st.l = st.l * f1 + l2 * f2;
+    st.m = m;
   }
-  if (r >= R) return;
-  if (sp.n == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    char* dst = a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h);
+  if (r < R) wide_finish<E, D>(st, a, sp, b, hk, r, i, h, half, split);
+}
+
+// 128 rows a workgroup, 32 a wavefront.  Bound by the matrix products, by forming the weights and by staging the
+// tiles, about alike: at 128 channels a tile takes a wavefront 32 products (1024 cycles), some 300 vector and 150
+// scalar instructions, and with two workgroups a compute unit the three overlap in part only.  Without the
+// exponentials a windowed prompt takes 6% less, without the products with the values 15%, without the staging of
+// tiles 30%; eight wavefronts or 64 rows a wavefront that share a staged tile, or steps of half a tile with the
+// products of one and the exponentials of another interleaved, came to the same or more.
+template <typename E, int D, bool kPaged>
+__global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
+  constexpr int kRows = 128, kTile = 64 * 2 * D, kHalf = 32 * 2 * D;
+  __shared__ __align__(16) char lds[2][2 * kTile];  // two tiles, keys then values: one is read while the next is written
+  __shared__ uint32_t odd;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, col = lane & 31, half = lane >> 5;
+  // Workgroups go to the eight dies in turn, and each die has its own L2: a sequence and kv head's workgroups, which
+  // read the same keys, are those of one die (a windowed prompt of 8192: 405 -> 372 us).
+  const int parts = ((a.T * a.G + kRows - 1) / kRows) * sp.n, pair = blockIdx.x / (8 * parts) * 8 + blockIdx.x % 8;
+  if (pair >= a.B * a.Hkv) return;
+  const int part = blockIdx.x / 8 % parts, split = part % sp.n, tile_row = part / sp.n, hk = pair % a.Hkv, b = pair / a.Hkv;
+  const Seq s = sequence(a, b);
+  const int R = s.nq * a.G, r0 = tile_row * kRows;
+  if (r0 >= R) return;
+  const int i0 = r0 / a.G, i1 = min(R - 1, r0 + kRows - 1) / a.G;
+  const Span span = span_of<kPage, 64>(a, s, i0, i1);
+  const int per = ceil_div(span.n, sp.n), t0 = split * per, t1 = min(span.n, t0 + per);
+  const int nc = kPaged ? max(t0, min(t1, span.a + span.c - span.b)) : t0;   // this split's cached tiles come first
+
+  const int r = r0 + 32 * wave + col, rr = min(r, R - 1), i = rr / a.G, h = hk * a.G + rr % a.G;
+  const bool mine = r0 + 32 * wave < R;             // this wavefront has rows
+  const RowAt row = row_at(a, s, b, i);
+  u32x4 q[D / 16];
+  {
+    const u32x4* p = reinterpret_cast<const u32x4*>(a.q.data + 2 * (b * a.q.b + i * a.q.t + h * a.q.h + half * 8));
 #pragma unroll
-    for (int d = 0; d < D / 32; ++d)
+    for (int j = 0; j < D / 16; ++j) q[j] = signed_queries(p[2 * j], a.scale);
+  }
+  WideState<D> st;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const u32x2 y = {E::pair(acc[d][4 * e] * inv, acc[d][4 * e + 1] * inv), E::pair(acc[d][4 * e + 2] * inv, acc[d][4 * e + 3] * inv)};
-        *reinterpret_cast<u32x2*>(dst + 2 * (32 * d + 8 * e + 4 * half)) = y;
-      }
-    if (a.lse && half == 0)
-      a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - E::kBias + __builtin_amdgcn_logf(l)) * kLn2;
-  } else {
-    const int64_t to = part_of(a, sp, b, hk, r) + split;
-    if (half == 0) {
-      sp.ml[2 * to] = m;
-      sp.ml[2 * to + 1] = l;
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) st.acc[t][e] = 0.f;
+  const int k0 = k_at<D>(col, half);
+  const int v0 = v_at<D>(4 * half + (lane & 15) / 4, ((lane >> 4) & 1) * 32 + (lane & 3) * 8);
+  const float c = score_factor(a.scale);
+  if (tid == 0) odd = 0;
+  __syncthreads();
+  const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
+  const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
+  auto sees = [&](bool cached, int at) -> uint64_t {
+    if (kPaged && cached) return sees_cached(a, s, row).at(at);
+    if (kPaged && a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, row, at);
+    return sees_new(a, s, row).at(at);
+  };
+  auto take = [&](const char* tile, bool full, uint64_t seen) {
+    f32x16 x[2] = {wide_scores<E, D>(q, tile, k0), wide_scores<E, D>(q, tile + kHalf, k0)};
+    wide_raise<E, D, 2>(st, x, c, full, seen);
+    u32x4 p0[2], p1[2];
+    wide_weights<E, D>(st, x[0], p0, c);
+    wide_values<E, D>(st, p0, tile + kTile, v0);
+    wide_weights<E, D>(st, x[1], p1, c);
+    wide_values<E, D>(st, p1, tile + kTile + kHalf, v0);
+  };
+
+  int t = t0, buf = 0;
+  bool cached;
+  if constexpr (kPaged) {
+    PagePart<D> x;
+    const uint8_t* page = nullptr;
+    auto entry = [&](int tile) -> int32_t {
+      return tile < nc ? table_entry(a.kv, b, tile_of<kPage, 64>(span, tile, &cached) / kPage) : -1;
+    };
+    auto load = [&](int32_t e) {
+      page = page_at(a.kv, e, hk);
+      x.load(page, tid);
+    };
+    auto full_at = [&](int here, bool there) { return there && full_cached(a, s, i1, here, 64); };
+    auto store = [&](int tile, int to) {
+      const int here = tile_of<kPage, 64>(span, tile, &cached);
+      x.template store<E>(lds[to], lds[to] + kTile, tid, full_at(here, page), page ? s.ctx - here : 0, &odd);
+    };
+    int32_t ahead = -1;
+    bool there = false;                             // the tile in LDS has a page
+    if (t < nc) {
+      const int32_t e0 = entry(t), e1 = entry(t + 1);
+      ahead = entry(t + 2);
+      load(e0);
+      store(t, 0);
+      there = page;
+      load(e1);
+      __syncthreads();
     }
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<f32x4*>(sp.sum + to * D + 32 * d + 8 * e + 4 * half) =
-            f32x4{acc[d][4 * e], acc[d][4 * e + 1], acc[d][4 * e + 2], acc[d][4 * e + 3]};
+    for (; t < nc; ++t) {
+      if (mine) {
+        const int here = tile_of<kPage, 64>(span, t, &cached);
+        const bool full = full_at(here, there);
+        take(lds[buf], full, full || !there ? 0 : sees(true, here) >> (4 * half));
+      }
+      if (t + 1 < nc) {
+        store(t + 1, buf ^ 1);
+        there = page;
+        load(ahead);
+        ahead = entry(t + 3);
+      }
+      __syncthreads();
+      buf ^= 1;
+    }
   }
+  {
+    TensorPart<D> k, v;
+    auto load = [&](int tile) {
+      if (tile >= t1) return;
+      const int here = tile_of<kPage, 64>(span, tile, &cached);
+      k.load(kb, a.k.t, here, s.nk, tid);
+      v.load(vb, a.v.t, here, s.nk, tid);
+    };
+    auto store = [&](int tile, int to) {
+      const int here = tile_of<kPage, 64>(span, tile, &cached);
+      k.store_keys(lds[to], tid);
+      v.template store_values<E>(lds[to] + kTile, tid, full_new(a, s, i0, i1, here, 64), s.nk - here, &odd);
+    };
+    if (t < t1) {
+      load(t);
+      store(t, buf);
+      load(t + 1);
+      __syncthreads();
+    }
+    for (; t < t1; ++t) {
+      if (mine) {
+        const int here = tile_of<kPage, 64>(span, t, &cached);
+        const bool full = full_new(a, s, i0, i1, here, 64);
+        take(lds[buf], full, full ? 0 : sees(false, here) >> (4 * half));
+      }
+      if (t + 1 < t1) {
+        store(t + 1, buf ^ 1);
+        load(t + 2);
+      }
+      __syncthreads();
+      buf ^= 1;
+    }
+  }
+  __syncthreads();
+  if (odd && mine) add_odd<E, D, kPaged>(st, a, s, span, b, hk, i0, i1, t0, t1, 0, 64, half, sees);
+  st.l += __shfl_xor(st.l, 32);
+  if (r < R) wide_finish<E, D>(st, a, sp, b, hk, r, i, h, half, split);
 }
 
 // Joins the splits of a row.  D / 4 lanes have a row's channels; kGroups such groups take every kGroups-th split
@@ -819,8 +990,8 @@ hipError_t launch(const AttnArgs& a, const Split& sp, hipStream_t stream) {
   const dim3 few(sp.n, a.Hkv, a.B);
   if (R <= 16) narrow_kernel<E, D, 1, kPaged><<<few, 256, 0, stream>>>(a, sp);
   else if (R <= 32) narrow_kernel<E, D, 2, kPaged><<<few, 256, 0, stream>>>(a, sp);
-  else if (R <= 64) wide_kernel<E, D, 2, kPaged><<<few, 256, 0, stream>>>(a, sp);
-  else wide_kernel<E, D, 4, kPaged><<<dim3((unsigned)((R + 127) / 128 * sp.n), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  else if (R <= 64) pair_kernel<E, D, kPaged><<<few, 256, 0, stream>>>(a, sp);
+  else wide_kernel<E, D, kPaged><<<dim3((unsigned)((R + 127) / 128 * sp.n * (((int64_t)a.B * a.Hkv + 7) / 8 * 8))), 256, 0, stream>>>(a, sp);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.n == 1) return e;
   const int lanes = D / 4;

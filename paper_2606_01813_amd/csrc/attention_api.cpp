@@ -88,6 +88,9 @@ caddtree_status_t check_attention(const caddtree_attention_t* a, const caddtree_
   if (a->n_heads > 65535) return fail(CADDTREE_E_UNSUPPORTED, "n_heads = %d exceeds 65535", a->n_heads);
   if (a->T > kMaxTokens || a->S > kMaxTokens || (int64_t)a->T * (a->n_heads / a->n_kv_heads) > kMaxTokens)
     return fail(CADDTREE_E_UNSUPPORTED, "more than 2^30 tokens, or rows of a kv head, in a sequence");
+  // (workgroups are numbered in 31 bits: one for 128 rows, or for 8 kv heads at least)
+  if (((int64_t)a->T * (a->n_heads / a->n_kv_heads) / 128 + 1) * ((int64_t)a->B * a->n_kv_heads + 8) > kMaxTokens)
+    return fail(CADDTREE_E_UNSUPPORTED, "more than 2^30 workgroups of 128 rows in a call");
   if (!std::isfinite(a->scale)) return fail(CADDTREE_E_INVALID, "scale must be finite");
   if (a->window < 0 || a->sinks < 0)
     return fail(CADDTREE_E_INVALID, "window = %d and sinks = %d must not be negative", a->window, a->sinks);
