@@ -15,6 +15,8 @@ namespace {
 
 using namespace at;
 
+constexpr int kMaxSplits = 512, kFewSplits = 8;      // (attention_api.cpp: at most as many as workgroups fill the card)
+
 // partial results of (sequence, kv head, row, split): D sums, relative to the maximum, in `sum`; the
 // maximum (in units of log2) and the sum of the weights in `ml`
 __device__ int64_t part_of(const AttnArgs& a, const Split& sp, int b, int hk, int r) {
@@ -940,48 +942,93 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   if (r < R) wide_finish<E, D>(st, a, sp, b, hk, r, i, h, half, split);
 }
 
-// Joins the splits of a row.  D / 4 lanes have a row's channels; kGroups such groups take every kGroups-th split
-// of one row and add up through LDS, so that a row of many splits keeps many loads in flight.
-template <typename E, int D, int kGroups>
-__global__ __launch_bounds__(256) void combine_kernel(AttnArgs a, Split sp) {
-  constexpr int kLanes = D / 4, kRows = 256 / (kLanes * kGroups);
-  __shared__ __align__(16) f32x4 part[kGroups > 1 ? 256 : 1];
-  const int tid = threadIdx.x, ch = tid % kLanes, group = tid / kLanes % kGroups, hk = blockIdx.y, b = blockIdx.z;
-  const int64_t r = (int64_t)blockIdx.x * kRows + tid / (kLanes * kGroups);
-  const Seq s = sequence(a, b);
-  const bool there = r < (int64_t)s.nq * a.G;
-  if (kGroups == 1 && !there) return;
-  const int64_t at = part_of(a, sp, b, hk, there ? (int)r : 0);
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  const float* ml = sp.ml + 2 * at;
-  if (there) {
-    for (int k = 0; k < sp.n; ++k) m = fmaxf(m, ml[2 * k]);
-    for (int k = 0; k < sp.n; ++k) {
-      const float mk = ml[2 * k], lk = ml[2 * k + 1];
-      l += lk == 0.f ? 0.f : mk == -INFINITY ? lk : lk * __builtin_amdgcn_exp2f(mk - m);
-    }
-#pragma unroll 4
-    for (int k = group; k < sp.n; k += kGroups) {
-      const float mk = ml[2 * k], lk = ml[2 * k + 1];
-      const f32x4 x = *reinterpret_cast<const f32x4*>(sp.sum + (at + k) * D + 4 * ch);
-      const float f = mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - m);
-      if (lk != 0.f) o += f * x;                    // (a split without a key left its sums unset)
-    }
-  }
-  if constexpr (kGroups > 1) {
-    part[tid] = o;
-    __syncthreads();
-    if (group != 0 || !there) return;
-#pragma unroll
-    for (int g = 1; g < kGroups; ++g) o += part[tid + g * kLanes];
-  }
-  const int i = (int)(r / a.G), h = hk * a.G + (int)(r % a.G);
+// Joins the splits of a row, few of them: D / 4 lanes a row, 4 channels each.
+template <typename E>
+__device__ void write_row(const AttnArgs& a, int b, int hk, int r, int ch, f32x4 o, float m, float l) {
+  const int i = r / a.G, h = hk * a.G + r % a.G;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   *reinterpret_cast<u32x2*>(a.out.data + 2 * (b * a.out.b + i * a.out.t + h * a.out.h + 4 * ch)) =
       u32x2{E::pair(o[0] * inv, o[1] * inv), E::pair(o[2] * inv, o[3] * inv)};
   if (a.lse && ch == 0)
     a.lse[((int64_t)b * a.T + i) * a.Hq + h] = l == 0.f ? -INFINITY : (m - E::kBias + __builtin_amdgcn_logf(l)) * kLn2;
+}
+// a split's factor for the row's maximum m (a split without a key left its sums unset)
+__device__ inline float split_factor(float mk, float lk, float m) {
+  return lk == 0.f ? 0.f : mk == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mk - m);
+}
+template <typename E, int D>
+__global__ __launch_bounds__(256) void combine_few_kernel(AttnArgs a, Split sp) {
+  constexpr int kLanes = D / 4;
+  const int ch = threadIdx.x % kLanes, hk = blockIdx.y, b = blockIdx.z;
+  const int64_t r = (int64_t)blockIdx.x * (256 / kLanes) + threadIdx.x / kLanes;
+  const Seq s = sequence(a, b);
+  if (r >= (int64_t)s.nq * a.G) return;
+  const int64_t at = part_of(a, sp, b, hk, (int)r);
+  float mk[kFewSplits], lk[kFewSplits], m = -INFINITY, l = 0.f;
+  f32x4 x[kFewSplits], o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int k = 0; k < kFewSplits; ++k) {            // (all loads in flight; a split that is not there reads the first)
+    const int64_t p = at + (k < sp.n ? k : 0);
+    mk[k] = sp.ml[2 * p];
+    lk[k] = k < sp.n ? sp.ml[2 * p + 1] : 0.f;
+    x[k] = *reinterpret_cast<const f32x4*>(sp.sum + p * D + 4 * ch);
+    m = fmaxf(m, mk[k]);
+  }
+#pragma unroll
+  for (int k = 0; k < kFewSplits; ++k) {
+    const float f = split_factor(mk[k], lk[k], m);
+    l += lk[k] * f;
+    if (lk[k] != 0.f) o += f * x[k];
+  }
+  write_row<E>(a, b, hk, (int)r, ch, o, m, l);
+}
+// ... many of them: a workgroup a row.  Its threads look at a split each for the maximum, the sum and the factors;
+// then groups of D / 4 lanes take every n-th split's sums and add up through LDS, in a fixed order.
+template <typename E, int D>
+__global__ __launch_bounds__(256) void combine_many_kernel(AttnArgs a, Split sp) {
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+  __shared__ float factor[kMaxSplits], top[4], total[4];
+  __shared__ __align__(16) f32x4 part[256];
+  const int tid = threadIdx.x, r = blockIdx.x, hk = blockIdx.y, b = blockIdx.z;
+  const Seq s = sequence(a, b);
+  if (r >= (int64_t)s.nq * a.G) return;
+  const int64_t at = part_of(a, sp, b, hk, r);
+  float mk[2], lk[2], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int k = tid + 256 * j;
+    mk[j] = k < sp.n ? sp.ml[2 * (at + k)] : -INFINITY;
+    lk[j] = k < sp.n ? sp.ml[2 * (at + k) + 1] : 0.f;
+    m = fmaxf(m, mk[j]);
+  }
+  for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+  if (tid % 64 == 0) top[tid / 64] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const float f = split_factor(mk[j], lk[j], m);
+    if (tid + 256 * j < sp.n) factor[tid + 256 * j] = lk[j] == 0.f ? -1.f : f;      // (-1: its sums are unset)
+    l += lk[j] * f;
+  }
+  for (int o = 32; o; o >>= 1) l += __shfl_xor(l, o);
+  if (tid % 64 == 0) total[tid / 64] = l;
+  __syncthreads();
+  l = (total[0] + total[1]) + (total[2] + total[3]);
+  const int ch = tid % kLanes, group = tid / kLanes;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int k = group; k < sp.n; k += kGroups) {
+    const f32x4 x = *reinterpret_cast<const f32x4*>(sp.sum + (at + k) * D + 4 * ch);
+    const float f = factor[k];
+    if (f != -1.f) o += f * x;
+  }
+  part[tid] = o;
+  __syncthreads();
+  if (group != 0) return;
+#pragma unroll
+  for (int g = 1; g < kGroups; ++g) o += part[tid + g * kLanes];
+  write_row<E>(a, b, hk, r, ch, o, m, l);
 }
 
 template <typename E, int D, bool kPaged>
@@ -995,8 +1042,8 @@ hipError_t launch(const AttnArgs& a, const Split& sp, hipStream_t stream) {
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.n == 1) return e;
   const int lanes = D / 4;
-  if (sp.n < 8) combine_kernel<E, D, 1><<<dim3((unsigned)((R * lanes + 255) / 256), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
-  else combine_kernel<E, D, 256 / lanes><<<dim3((unsigned)R, a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  if (sp.n <= kFewSplits) combine_few_kernel<E, D><<<dim3((unsigned)((R * lanes + 255) / 256), a.Hkv, a.B), 256, 0, stream>>>(a, sp);
+  else combine_many_kernel<E, D><<<dim3((unsigned)R, a.Hkv, a.B), 256, 0, stream>>>(a, sp);
   return hipGetLastError();
 }
 
