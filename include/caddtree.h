@@ -405,12 +405,16 @@ caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const cadd
  *   scores [B, n_kv_heads, slots]; new_table [B, new_pages]: pages for budget slots that are in none of
  *   the tables in use (the old pages are free once the call is done); new_scores [B, n_kv_heads,
  *   new_slots], new_slots >= budget: the kept slots' scores, then zeros; new_len [B] = min(ctx_len,
- *   budget); kept [B, n_kv_heads, budget]: the old slots, then -1. */
+ *   budget); kept [B, n_kv_heads, budget]: the old slots, then -1.
+ *   workspace: caddtree_evict_workspace_bytes(...) bytes, 256-byte aligned (CADDTREE_E_WORKSPACE if smaller). */
 caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B, const int32_t* page_table,
                                        int32_t table_pages, const int64_t* ctx_len, const float* scores, int64_t slots,
                                        int32_t budget, int32_t sinks, int32_t recent, const int32_t* new_table,
                                        int32_t new_pages, float* new_scores, int64_t new_slots, int64_t* new_len,
-                                       int32_t* kept, hipStream_t stream);
+                                       int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* HOST only: the workspace of caddtree_cache_evict (0 for rows of up to 16384 slots). */
+size_t caddtree_evict_workspace_bytes(const caddtree_cache_t* cache, int32_t B, int32_t table_pages, int64_t slots);
 
 const char* caddtree_status_string(caddtree_status_t status);
 const char* caddtree_last_error(void);

@@ -83,6 +83,7 @@ EXPORTS = [
     "caddtree_last_error",
     "caddtree_attention_workspace_bytes", "caddtree_window_attention", "caddtree_cache_attention",
     "caddtree_cache_write", "caddtree_cache_read", "caddtree_cache_score", "caddtree_cache_evict",
+    "caddtree_evict_workspace_bytes",
 ]
 
 
@@ -131,8 +132,10 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.caddtree_cache_read.restype = ctypes.c_int
     lib.caddtree_cache_score.argtypes = [cp, ap, vp, vp, vp, i64, vp]
     lib.caddtree_cache_score.restype = ctypes.c_int
-    lib.caddtree_cache_evict.argtypes = [cp, i32, vp, i32, vp, vp, i64, i32, i32, i32, vp, i32, vp, i64, vp, vp, vp]
+    lib.caddtree_cache_evict.argtypes = [cp, i32, vp, i32, vp, vp, i64, i32, i32, i32, vp, i32, vp, i64, vp, vp, vp, sz, vp]
     lib.caddtree_cache_evict.restype = ctypes.c_int
+    lib.caddtree_evict_workspace_bytes.argtypes = [cp, i32, i32, i64]
+    lib.caddtree_evict_workspace_bytes.restype = sz
     lib.caddtree_status_string.argtypes = [ctypes.c_int]
     lib.caddtree_status_string.restype = ctypes.c_char_p
     lib.caddtree_last_error.argtypes = []

@@ -395,17 +395,20 @@ class KVCache:
                                                    _stream(stream, device)))
 
     def evict(self, page_table, ctx_len, scores, new_table, new_len, new_scores, kept, *, budget: int, sinks: int = 0,
-              recent: int = 0, stream=None) -> None:
+              recent: int = 0, workspace=None, stream=None) -> None:
         """Cuts every sequence to at most ``budget`` slots a kv head: the first ``sinks``, the last ``recent`` and
         the largest scores of the rest, in their old order.  The kept slots go to the pages of ``new_table``
         (int32 [B, pages], none of them in use), their scores to ``new_scores`` (float32 [B, kv heads, slots],
         zeros behind), the lengths to ``new_len`` (int64 [B]) and the old slots to ``kept`` (int32
-        [B, kv heads, budget], -1 behind)."""
+        [B, kv heads, budget], -1 behind).  Rows of more than 16384 slots need a workspace, made here if not given
+        (with a raw stream handle it has to be)."""
+        if workspace is None and (stream is None or hasattr(stream, "cuda_stream")):
+            workspace = self.evict_workspace(page_table, scores, stream)
         native = self._native(stream)
         if native is not None:
             binding, ops, device, raw = native
             if _done(binding.cache_evict(ops, device, raw, self._at, page_table, ctx_len, scores, new_table, new_len, new_scores, kept,
-                                         budget, sinks, recent)):
+                                         budget, sinks, recent, workspace)):
                 return
         torch = _torch()
         device = self._on()
@@ -419,4 +422,20 @@ class KVCache:
                 _array("new_scores", new_scores, f32, (B, self.n_kv_heads, None), device), int(new_scores.shape[2]),
                 _array("new_len", new_len, torch.int64, (B,), device),
                 _array("kept", kept, torch.int32, (B, self.n_kv_heads, int(budget)), device))
-        _lib.check(_lib.lib().caddtree_cache_evict(ctypes.byref(self._c), B, table, pages, *args, _stream(stream, device)))
+        _lib.check(_lib.lib().caddtree_cache_evict(ctypes.byref(self._c), B, table, pages, *args,
+                                                   *_workspace(workspace, device), _stream(stream, device)))
+
+    def evict_workspace(self, page_table, scores, stream=None):
+        """A workspace for ``evict`` of these page_table and scores (uint8; the contents do not matter), allocated on
+        the stream; None where it needs none."""
+        torch = _torch()
+        if not isinstance(page_table, torch.Tensor) or not isinstance(scores, torch.Tensor) \
+                or page_table.dim() != 2 or scores.dim() != 3 or scores.shape[2] <= 16384:
+            return None
+        n = _lib.lib().caddtree_evict_workspace_bytes(ctypes.byref(self._c), page_table.shape[0], page_table.shape[1], scores.shape[2])
+        if n == 0:
+            return None
+        if stream is None:
+            return torch.empty(n, dtype=torch.uint8, device=self.pages.device)
+        with torch.cuda.stream(stream):
+            return torch.empty(n, dtype=torch.uint8, device=self.pages.device)

@@ -279,11 +279,16 @@ caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const cadd
   return e == hipSuccess ? ok() : hip_fail(e, "cache score launch");
 }
 
+size_t caddtree_evict_workspace_bytes(const caddtree_cache_t* cache, int32_t B, int32_t table_pages, int64_t slots) {
+  if (check_cache(cache) != CADDTREE_OK || check_batch(B) != CADDTREE_OK || table_pages < 0 || slots < 0 || slots > kMaxTokens) return 0;
+  return caddtree::evict_workspace_bytes(paged(cache, nullptr, table_pages), B, slots);
+}
+
 caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B, const int32_t* page_table,
                                        int32_t table_pages, const int64_t* ctx_len, const float* scores, int64_t slots,
                                        int32_t budget, int32_t sinks, int32_t recent, const int32_t* new_table,
                                        int32_t new_pages, float* new_scores, int64_t new_slots, int64_t* new_len,
-                                       int32_t* kept, hipStream_t stream) {
+                                       int32_t* kept, void* workspace, size_t workspace_bytes, hipStream_t stream) {
   caddtree_status_t st = check_cache(cache);
   if (st != CADDTREE_OK) return st;
   if ((st = check_batch(B)) != CADDTREE_OK) return st;
@@ -300,9 +305,14 @@ caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B,
   if (ctx_len == nullptr || new_len == nullptr) return fail(CADDTREE_E_INVALID, "ctx_len and new_len are required");
   if ((slots > 0 && scores == nullptr) || (new_slots > 0 && new_scores == nullptr) || (budget > 0 && kept == nullptr))
     return fail(CADDTREE_E_INVALID, "scores, new_scores and kept are required");
+  if ((st = check_workspace(workspace)) != CADDTREE_OK) return st;
+  const size_t bytes = caddtree::evict_workspace_bytes(paged(cache, page_table, table_pages), B, slots);
+  if (bytes > 0 && (workspace == nullptr || workspace_bytes < bytes))
+    return fail(CADDTREE_E_WORKSPACE, "rows of %lld slots need a workspace of %zu bytes, got %zu", (long long)slots, bytes,
+                workspace ? workspace_bytes : (size_t)0);
   caddtree::EvictArgs a = {paged(cache, page_table, table_pages), B, cache->head_dim, ctx_len, scores, slots, budget, sinks,
                            recent, new_table, new_pages, new_scores, new_slots, new_len, kept};
-  const hipError_t e = caddtree::launch_cache_evict(a, stream);
+  const hipError_t e = caddtree::launch_cache_evict(a, workspace, stream);
   return e == hipSuccess ? ok() : hip_fail(e, "cache evict launch");
 }
 

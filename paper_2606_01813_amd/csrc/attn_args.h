@@ -84,6 +84,7 @@ struct EvictArgs {
   int64_t* new_len;          // [B]
   int32_t* kept;             // [B, heads, budget]
 };
-hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t stream);
+size_t evict_workspace_bytes(const PagedKV& kv, int32_t B, int64_t slots);
+hipError_t launch_cache_evict(const EvictArgs& a, void* workspace, hipStream_t stream);
 
 }  // namespace caddtree

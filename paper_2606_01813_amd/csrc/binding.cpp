@@ -741,9 +741,10 @@ PyObject* py_cache_score(PyObject*, PyObject* const* p, Py_ssize_t n) {
   });
 }
 
-// ops, device, stream, cache, page_table, ctx_len, scores, new_table, new_len, new_scores, kept, budget, sinks, recent
+// ops, device, stream, cache, page_table, ctx_len, scores, new_table, new_len, new_scores, kept, budget, sinks, recent,
+// workspace
 PyObject* py_cache_evict(PyObject*, PyObject* const* p, Py_ssize_t n) {
-  return guarded_ops(p, n, 14, [&](const Ops& s) -> int {
+  return guarded_ops(p, n, 15, [&](const Ops& s) -> int {
     Attn c(s, p[1]);
     const hipStream_t st = c.stream(p[2]);
     const caddtree_cache_t* cache = c.cache(p[3]);
@@ -757,11 +758,13 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* p, Py_ssize_t n) {
     auto* fresh = as<float>(c.array(p[9], c10::kFloat, {B, H, kAny}));
     const int32_t budget = c.count(p[11]), sinks = c.count(p[12]), recent = c.count(p[13]);
     auto* kept = as<int32_t>(c.array(p[10], c10::kInt, {B, H, budget}));
+    size_t bytes = 0;
+    void* ws = c.workspace(p[14], &bytes);
     if (!c.ok) return -1;
     const int64_t pages = c.size(p[4], 1), slots = c.size(p[6], 2), to_pages = c.size(p[7], 1), to_slots = c.size(p[9], 2);
     return unlocked([&] {
       return s.evict(cache, (int32_t)B, table, (int32_t)pages, ctx, scores, slots, budget, sinks, recent, to, (int32_t)to_pages,
-                     fresh, to_slots, len, kept, st);
+                     fresh, to_slots, len, kept, ws, bytes, st);
     });
   });
 }

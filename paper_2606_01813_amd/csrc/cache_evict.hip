@@ -2,10 +2,12 @@
 // rest), and the move of their codes, scales and scores to the new pages.
 //
 // Selection finds the smallest kept score, as an order-preserving 32-bit key, digit by digit (11, 11 and 10
-// bits): a histogram of the first digit over all scores; the keys of the digit that holds the threshold
-// then fit LDS as a rule and the other digits are found there.  A last ordered pass lists the kept slots.
-// Counts are integers, so nothing depends on the order of the additions.  One workgroup a sequence and
-// kv head; up to 16 scores a thread stay in registers throughout, longer rows are read from the L2 again.
+// bits), by a histogram of the digit over the keys that share the digits found so far.  A last ordered pass
+// lists the kept slots.  Counts are integers, so nothing depends on the order of the additions.
+// Rows of up to 16384 slots have a workgroup each and keep their keys in registers throughout.  Longer rows
+// are cut into parts, a workgroup each: a launch a digit counts every part's keys, the next one adds the parts'
+// histograms up, finds the digit and goes on, and the last lists (kept slots before a part follow from the
+// histograms of the parts before it).
 #include <algorithm>
 
 #include "attn_common.h"
@@ -15,7 +17,9 @@ namespace {
 
 using namespace at;
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048, kRoom = 8192;
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 2048;
+constexpr int kHeld = 16;                                    // keys a thread holds at most in select_kernel
+constexpr int kStep = 8, kBlock = kStep * kThreads;          // slots a workgroup of the parts takes at a time
 
 // order-preserving: larger scores, larger keys; -0 as 0, a NaN below everything
 __device__ uint32_t key_of(float x) {
@@ -28,9 +32,19 @@ __device__ int live_slots(const EvictArgs& a, int b) {
   return clamp_len(a.ctx_len[b], min((int64_t)a.kv.table_pages * kPage, a.slots));
 }
 
+// The digits of a key from the top: 11, 11 and 10 bits.
+struct Digit {
+  uint32_t shift, mask, above;      // above: the bits of the digits before it
+  __device__ uint32_t of(uint32_t k) const { return (k >> shift) & mask; }
+  __device__ bool shares(uint32_t k, uint32_t prefix) const { return ((k ^ prefix) & above) == 0; }
+};
+__device__ __forceinline__ Digit digit_of(int step) {
+  return step == 0 ? Digit{21, 2047, 0} : step == 1 ? Digit{10, 2047, 0xffe00000u} : Digit{0, 1023, 0xfffffc00u};
+}
+
 // Adds to hist[d] of every lane with `is`.  Scores repeat (zeros above all), so the digit of the first lane is
 // added once for all lanes that have it.
-__device__ void count_digit(uint32_t* hist, bool is, uint32_t d) {
+__device__ __forceinline__ void count_digit(uint32_t* hist, bool is, uint32_t d) {
   const uint64_t any = __ballot(is);
   if (any == 0) return;
   const uint32_t first = __builtin_amdgcn_readlane(d, __builtin_ctzll(any));
@@ -39,20 +53,18 @@ __device__ void count_digit(uint32_t* hist, bool is, uint32_t d) {
   if ((threadIdx.x & 63) == __builtin_ctzll(same)) atomicAdd(&hist[first], (uint32_t)__popcll(same));
 }
 
-// The digit that holds the want-th largest key, and how many keys lie in larger digits; hist is cleared.
-// With want = 0 it is the top digit, with none above.
-__device__ void find_digit(uint32_t* hist, uint32_t* sums, uint32_t* found, uint32_t want) {
+// The digit that holds the want-th largest key, and how many keys lie in larger digits.  Thread t has the
+// counts of the two digits that rank 2 t and 2 t + 1 from the top.  With want = 0 it is the top digit, with
+// none above.
+__device__ __forceinline__ void find_digit(uint32_t c0, uint32_t c1, uint32_t* sums, uint32_t* found, uint32_t want) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // thread t has the two digits that rank 2 t and 2 t + 1 from the top
   const int top = kBins - 1 - 2 * tid;
-  const uint32_t c0 = hist[top], c1 = hist[top - 1];
   uint32_t s = c0 + c1;
   for (int o = 1; o < 64; o <<= 1) {
     const uint32_t y = (uint32_t)__shfl_up((int)s, o);
     if (lane >= o) s += y;
   }
   if (lane == 63) sums[wave] = s;
-  hist[top] = hist[top - 1] = 0;
   if (tid == 0) {
     found[0] = kBins - 1;
     found[1] = 0;
@@ -70,12 +82,18 @@ __device__ void find_digit(uint32_t* hist, uint32_t* sums, uint32_t* found, uint
   __syncthreads();
 }
 
-// kKept: keys a thread holds (kKept kThreads >= n), or 0: scores are read again each time
+// 2 kept, 1 equal to the threshold, 0 not kept (or no slot: i < 0)
+__device__ __forceinline__ int kind_of(int i, uint32_t k, int lo, int hi, uint32_t threshold) {
+  if (i < 0) return 0;
+  if (i < lo || i >= hi) return 2;
+  return k > threshold ? 2 : k == threshold ? 1 : 0;
+}
+
+// One workgroup a sequence and kv head; a thread holds kKept keys, kKept kThreads >= n.
 template <int kKept>
 __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
   __shared__ uint32_t hist[kBins];
-  __shared__ uint32_t room[kKept ? 1 : kRoom];      // keys of the threshold's first digit
-  __shared__ uint32_t sums[kWaves], equals[kWaves], found[2], filled;
+  __shared__ uint32_t sums[kWaves], equals[kWaves], found[2];
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int n = live_slots(a, b), m = min(n, a.budget);
   int32_t* kept = a.kept + ((int64_t)b * a.kv.heads + h) * a.budget;
@@ -92,90 +110,40 @@ __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
   // a wavefront has a strip of its own, 64 slots a step
   const int strip = ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
   const int from = min(wave * strip, n), to = min(from + strip, n);
-  uint32_t mine[kKept ? kKept : 1];
-  if (kKept)
+  uint32_t mine[kKept];
 #pragma unroll
-    for (int j = 0; j < kKept; ++j) {
-      const int i = from + 64 * j + lane;
-      mine[j] = i < to ? key_of(x[i]) : 0;
-    }
+  for (int j = 0; j < kKept; ++j) {
+    const int i = from + 64 * j + lane;
+    mine[j] = i < to ? key_of(x[i]) : 0;
+  }
   // f(slot, key) for the lanes' slots of a strip, all lanes together; a slot past the strip is -1
   auto every = [&](auto f) {
-    if constexpr (kKept != 0) {
 #pragma unroll
-      for (int j = 0; j < kKept; ++j)
-        if (from + 64 * j < to) {
-          const int i = from + 64 * j + lane;
-          f(i < to ? i : -1, mine[j]);
-        }
-    } else {
-      for (int t = from; t < to; t += 512) {
-        float y[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int i = t + 64 * j + lane;
-          y[j] = i < to ? x[i] : 0.f;
-        }
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (t + 64 * j < to) {
-            const int i = t + 64 * j + lane;
-            f(i < to ? i : -1, key_of(y[j]));
-          }
+    for (int j = 0; j < kKept; ++j)
+      if (from + 64 * j < to) {
+        const int i = from + 64 * j + lane;
+        f(i < to ? i : -1, mine[j]);
       }
-    }
   };
   for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
-  if (tid == 0) filled = 0;
   __syncthreads();
-  every([&](int i, uint32_t k) { count_digit(hist, i >= lo && i < hi, k >> 21); });
-  __syncthreads();
-  find_digit(hist, sums, found, want);
-  uint32_t prefix = found[0] << 21;
-  want -= found[1];
-  bool fits = kKept == 0;
-  if (kKept == 0) {                                 // the keys of this digit, where they fit
-    every([&](int i, uint32_t k) {
-      const bool is = i >= lo && i < hi && k >> 21 == prefix >> 21;
-      const uint64_t some = __ballot(is);
-      if (some == 0) return;
-      uint32_t at = 0;
-      if (lane == 0) at = atomicAdd(&filled, (uint32_t)__popcll(some));
-      at = __builtin_amdgcn_readfirstlane(at) + __popcll(some & ((1ull << lane) - 1));
-      if (is && at < kRoom) room[at] = k;
-    });
+  uint32_t prefix = 0;
+#pragma unroll 1
+  for (int step = 0; step < 3; ++step) {
+    const Digit d = digit_of(step);
+    every([&](int i, uint32_t k) { count_digit(hist, i >= lo && i < hi && d.shares(k, prefix), d.of(k)); });
     __syncthreads();
-    fits = filled <= kRoom;
-  }
-  for (int pass = 0; pass < 2; ++pass) {
-    const int shift = pass == 0 ? 10 : 0, done = pass == 0 ? 21 : 10;
-    const uint32_t mask = pass == 0 ? 2047 : 1023;
-    if (fits) {
-      const int c = (int)filled;
-      for (int i = tid; i < (c + 63) / 64 * 64; i += kThreads) {
-        const uint32_t k = i < c ? room[i] : 0;
-        count_digit(hist, i < c && k >> done == prefix >> done, (k >> shift) & mask);
-      }
-    } else {
-      every([&](int i, uint32_t k) { count_digit(hist, i >= lo && i < hi && k >> done == prefix >> done, (k >> shift) & mask); });
-    }
-    __syncthreads();
-    if (want == 0) prefix |= mask << shift;          // (only where the sinks and the recent ones fill the budget)
-    find_digit(hist, sums, found, want);
-    if (want != 0) {
-      prefix |= found[0] << shift;
-      want -= found[1];
-    }
+    const int top = kBins - 1 - 2 * tid;
+    const uint32_t c0 = hist[top], c1 = hist[top - 1];
+    hist[top] = hist[top - 1] = 0;
+    find_digit(c0, c1, sums, found, want);
+    prefix |= found[0] << d.shift;
+    want -= found[1];
   }
   // kept: keys above prefix, and the first `want` equal to it
-  auto kind = [&](int i, uint32_t k) -> int {       // 2 kept, 1 equal, 0 not kept
-    if (i < 0) return 0;
-    if (i < lo || i >= hi) return 2;
-    return k > prefix ? 2 : k == prefix ? 1 : 0;
-  };
   uint32_t na = 0, ne = 0;
   every([&](int i, uint32_t k) {
-    const int t = kind(i, k);
+    const int t = kind_of(i, k, lo, hi, prefix);
     na += __popcll(__ballot(t == 2));
     ne += __popcll(__ballot(t == 1));
   });
@@ -191,7 +159,7 @@ __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
   }
   const uint64_t below = (1ull << lane) - 1;
   every([&](int i, uint32_t k) {
-    const int t = kind(i, k);
+    const int t = kind_of(i, k, lo, hi, prefix);
     const uint64_t eqs = __ballot(t == 1);
     const bool take = t == 2 || (t == 1 && eq + __popcll(eqs & below) < want);
     const uint64_t takes = __ballot(take);
@@ -199,6 +167,169 @@ __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
     at += __popcll(takes);
     eq += __popcll(eqs);
   });
+}
+
+// What the launches of the parts hand on, a row (sequence and kv head) after the other.
+struct Parts {
+  uint32_t* hist;            // [row][3][parts][kBins]
+  uint32_t* state;           // [row][4 + 2 parts]: prefix and want after the first and second digit, then two
+                             // counts a part: kept slots before it by the first digit, by the first two
+  int parts, span;           // slots of a part (whole blocks)
+  __device__ uint32_t* hist_of(int64_t row, int step, int part) const { return hist + ((row * 3 + step) * parts + part) * (int64_t)kBins; }
+  __device__ uint32_t* state_of(int64_t row) const { return state + row * (4 + 2 * parts); }
+};
+
+// The digit number `step` from the parts' histograms; returns how many keys of the parts before this one lie in
+// larger digits, and (for thread 0 .. all) in *same how many in this digit.
+__device__ __forceinline__ uint32_t add_parts(const Parts& p, int64_t row, int step, int part, int live, uint32_t want,
+                                              uint32_t* sums, uint32_t* found, uint32_t* shared2, uint32_t* same) {
+  const int tid = threadIdx.x, top = kBins - 1 - 2 * tid;
+  uint32_t c0 = 0, c1 = 0, b0 = 0, b1 = 0;
+  const uint32_t* at = p.hist_of(row, step, 0) + (top - 1);
+#pragma unroll 8
+  for (int q = 0; q < live; ++q) {
+    const uint2 c = *reinterpret_cast<const uint2*>(at + (int64_t)q * kBins);      // (digits top - 1 and top)
+    c0 += c.y;
+    c1 += c.x;
+    if (q < part) {
+      b0 += c.y;
+      b1 += c.x;
+    }
+  }
+  if (tid < 2) shared2[tid] = 0;
+  find_digit(c0, c1, sums, found, want);
+  const int digit = (int)found[0];
+  uint32_t above = (top > digit ? b0 : 0) + (top - 1 > digit ? b1 : 0);
+  for (int o = 32; o; o >>= 1) above += (uint32_t)__shfl_down((int)above, o);
+  if ((tid & 63) == 0) atomicAdd(&shared2[0], above);
+  if (top == digit) shared2[1] = b0;
+  if (top - 1 == digit) shared2[1] = b1;
+  __syncthreads();
+  *same = shared2[1];
+  return shared2[0];
+}
+
+// Counts the digit number kDigit of a part's keys; before it, finds the digit before.
+template <int kDigit>
+__global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a, Parts p) {
+  __shared__ uint32_t hist[kBins];
+  __shared__ uint32_t sums[kWaves], found[2], before[2];
+  const int part = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = live_slots(a, b), live = (n + p.span - 1) / p.span;
+  if (n <= a.budget || part >= live) return;
+  const int64_t row = (int64_t)b * a.kv.heads + h;
+  const float* x = a.scores + row * a.slots;
+  const int lo = a.sinks, hi = n - a.recent;
+  const int from = part * p.span, to = min(from + p.span, n);
+  float y[kStep];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const int i = t + (wave * kStep + j) * 64 + lane;
+      y[j] = i < to ? x[i] : 0.f;
+    }
+  };
+  load(from);                                       // (on their way while the digit is found)
+  for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+  uint32_t prefix = 0, want = (uint32_t)(a.budget - a.sinks - a.recent);
+  if constexpr (kDigit > 0) {
+    uint32_t* state = p.state_of(row);
+    if constexpr (kDigit > 1) {
+      prefix = state[0];
+      want = state[1];
+    }
+    uint32_t same;
+    const uint32_t above = add_parts(p, row, kDigit - 1, part, live, want, sums, found, before, &same);
+    prefix |= found[0] << digit_of(kDigit - 1).shift;
+    want -= found[1];
+    if (tid == 0) {
+      uint32_t* mine = state + 4 + 2 * part;
+      mine[kDigit - 1] = above + (kDigit > 1 ? mine[0] : 0u);
+      if (part == 0) {
+        state[2 * (kDigit - 1)] = prefix;
+        state[2 * (kDigit - 1) + 1] = want;
+      }
+    }
+  }
+  __syncthreads();
+  const Digit d = digit_of(kDigit);
+  for (int t = from; t < to; t += kBlock) {
+    if (t != from) load(t);
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const int i = t + (wave * kStep + j) * 64 + lane;
+      const uint32_t k = key_of(y[j]);
+      count_digit(hist, i < to && i >= lo && i < hi && d.shares(k, prefix), d.of(k));
+    }
+  }
+  __syncthreads();
+  uint32_t* out = p.hist_of(row, kDigit, part);
+  for (int i = tid; i < kBins; i += kThreads) out[i] = hist[i];
+}
+
+// Finds the last digit and lists a part's kept slots.
+__global__ __launch_bounds__(kThreads) void list_kernel(EvictArgs a, Parts p) {
+  __shared__ uint32_t sums[kWaves], equals[kWaves], found[2], before[2];
+  const int part = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n = live_slots(a, b), live = (n + p.span - 1) / p.span, m = min(n, a.budget);
+  const int64_t row = (int64_t)b * a.kv.heads + h;
+  int32_t* kept = a.kept + row * a.budget;
+  if (part == 0 && h == 0 && tid == 0) a.new_len[b] = m;
+  if (n <= a.budget) {
+    for (int i = part * kThreads + tid; i < a.budget; i += p.parts * kThreads) kept[i] = i < n ? i : -1;
+    return;
+  }
+  if (part >= live) return;
+  const float* x = a.scores + row * a.slots;
+  const int lo = a.sinks, hi = n - a.recent;
+  const int from = part * p.span, to = min(from + p.span, n);
+  const uint32_t* state = p.state_of(row);
+  uint32_t prefix = state[2], want = state[3], eq;
+  uint32_t at = add_parts(p, row, 2, part, live, want, sums, found, before, &eq) + state[4 + 2 * part + 1];
+  prefix |= found[0];
+  want -= found[1];
+  // places taken before this part: larger keys, the first `want` equal ones, the sinks and the recent ones
+  at += min(eq, want) + (uint32_t)(min(from, lo) + max(from - hi, 0));
+  const uint64_t below = (1ull << lane) - 1;
+  for (int t = from; t < to; t += kBlock) {
+    const int strip = t + wave * kStep * 64;
+    int kind[kStep];
+    uint32_t na = 0, ne = 0;
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const int i = strip + j * 64 + lane;
+      kind[j] = kind_of(i < to ? i : -1, key_of(i < to ? x[i] : 0.f), lo, hi, prefix);
+      na += __popcll(__ballot(kind[j] == 2));
+      ne += __popcll(__ballot(kind[j] == 1));
+    }
+    __syncthreads();                                // the counts of the last block, and those of add_parts, are read
+    if (lane == 0) {
+      sums[wave] = na;
+      equals[wave] = ne;
+    }
+    __syncthreads();
+    uint32_t my_at = at, my_eq = eq;
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t taken = sums[w] + (min(eq + equals[w], want) - min(eq, want));
+      at += taken;
+      eq += equals[w];
+      if (w < wave) {
+        my_at += taken;
+        my_eq += equals[w];
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const uint64_t eqs = __ballot(kind[j] == 1);
+      const bool take = kind[j] == 2 || (kind[j] == 1 && my_eq + __popcll(eqs & below) < want);
+      const uint64_t takes = __ballot(take);
+      if (take) kept[my_at + __popcll(takes & below)] = strip + j * 64 + lane;
+      my_at += __popcll(takes);
+      my_eq += __popcll(eqs);
+    }
+  }
 }
 
 // A wavefront moves the 64 tokens of a new page and head: a lane looks up one token's old place, then
@@ -261,13 +392,37 @@ __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
 
 }  // namespace
 
-hipError_t launch_cache_evict(const EvictArgs& a, hipStream_t stream) {
-  const int64_t most = std::min<int64_t>((int64_t)a.kv.table_pages * kPage, a.slots);
+namespace {
+constexpr int kMaxParts = 64;
+int64_t most_slots(const PagedKV& kv, int64_t slots) { return std::min<int64_t>((int64_t)kv.table_pages * kPage, slots); }
+int64_t span_of(int64_t most) { return ((most + kMaxParts - 1) / kMaxParts + kBlock - 1) / kBlock * kBlock; }
+}  // namespace
+
+size_t evict_workspace_bytes(const PagedKV& kv, int32_t B, int64_t slots) {
+  const int64_t most = most_slots(kv, slots);
+  if (most <= kHeld * kThreads) return 0;
+  const int64_t parts = (most + span_of(most) - 1) / span_of(most);
+  return (size_t)B * kv.heads * (3 * parts * kBins + 4 + 2 * parts) * 4;
+}
+
+hipError_t launch_cache_evict(const EvictArgs& a, void* workspace, hipStream_t stream) {
+  const int64_t most = most_slots(a.kv, a.slots);
   const dim3 g(a.kv.heads, a.B);
   // a strip is whole steps of 64, so a thread holds n / 1024 keys, rounded up
   if (most <= 4 * kThreads) select_kernel<4><<<g, kThreads, 0, stream>>>(a);
-  else if (most <= 16 * kThreads) select_kernel<16><<<g, kThreads, 0, stream>>>(a);
-  else select_kernel<0><<<g, kThreads, 0, stream>>>(a);
+  else if (most <= kHeld * kThreads) select_kernel<kHeld><<<g, kThreads, 0, stream>>>(a);
+  else {
+    Parts p;
+    p.span = (int)span_of(most);
+    p.parts = (int)((most + p.span - 1) / p.span);
+    p.hist = static_cast<uint32_t*>(workspace);
+    p.state = p.hist + (int64_t)a.B * a.kv.heads * 3 * p.parts * kBins;
+    const dim3 pg(p.parts, a.kv.heads, a.B);
+    count_kernel<0><<<pg, kThreads, 0, stream>>>(a, p);
+    count_kernel<1><<<pg, kThreads, 0, stream>>>(a, p);
+    count_kernel<2><<<pg, kThreads, 0, stream>>>(a, p);
+    list_kernel<<<pg, kThreads, 0, stream>>>(a, p);
+  }
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.new_slots == 0) return e;
   const dim3 mg((unsigned)((a.new_slots + 4 * kPage - 1) / (4 * kPage)), a.kv.heads, a.B);

@@ -495,6 +495,12 @@ EVICT = [
     (1, 64, [0, 0], 0, 0, 0, "rand"),
     (1, 64, [70, 3], 0, 0, 0, "rand"),                   # a budget of nothing
     (1, 64, [70000], 9000, 4, 1000, "heavy"),
+    # rows in parts: ragged ones, ties over several parts, an exact fit, nothing but the sinks and the recent ones
+    (2, 64, [16385, 0, 24576, 8193, 30000], 8200, 5, 1000, "ties"),
+    (1, 64, [50000, 16384], 20000, 9000, 9000, "odd"),
+    (1, 64, [40000, 39999], 39999, 0, 0, "zeros"),
+    (2, 64, [33000], 900, 400, 500, "rand"),
+    (1, 64, [20000], 0, 0, 0, "rand"),
 ]
 
 

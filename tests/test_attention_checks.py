@@ -301,7 +301,7 @@ def test_cache_validation(kw, status):
     r = ctypes.byref
     assert lib.caddtree_cache_write(r(c), r(v), r(v), 2, 5, 5, 0x1000, None, None, 0x1000, 3, None) == status
     assert lib.caddtree_cache_read(r(c), r(v), r(v), 2, 5, None, 0x1000, 0x1000, 3, None) == status
-    assert lib.caddtree_cache_evict(r(c), 2, 0x1000, 3, 0x1000, 0x1000, 100, 64, 1, 1, 0x1000, 1, 0x1000, 64, 0x1000, 0x1000, None) == status
+    assert lib.caddtree_cache_evict(r(c), 2, 0x1000, 3, 0x1000, 0x1000, 100, 64, 1, 1, 0x1000, 1, 0x1000, 64, 0x1000, 0x1000, None, 0, None) == status
     assert lib.caddtree_cache_score(r(c), r(a), None, 0x1000, 0x1000, 100, None) == status
     assert lib.caddtree_cache_attention(r(c), r(a), None, 0, None) == status
 
@@ -332,11 +332,17 @@ def test_other_refusals_and_calls_of_nothing():
     assert score(r(c), r(_attention(lse=None)), None, 0x1000, 0x1000, 100) == INVALID
     evict = lambda **kw: lib.caddtree_cache_evict(r(c), *{**dict(
         B=2, table=0x1000, pages=3, ctx=0x1000, scores=0x1000, slots=100, budget=64, sinks=4, recent=9, new_table=0x1000, new_pages=1,
-        new_scores=0x1000, new_slots=64, new_len=0x1000, kept=0x1000), **kw}.values(), None)
+        new_scores=0x1000, new_slots=64, new_len=0x1000, kept=0x1000, workspace=None, bytes=0), **kw}.values(), None)
     for kw in (dict(B=-1), dict(table=None), dict(budget=-1), dict(sinks=-1), dict(recent=-1), dict(sinks=60), dict(slots=-1),
                dict(new_slots=63), dict(new_pages=0), dict(new_table=None), dict(ctx=None), dict(new_len=None), dict(scores=None),
                dict(new_scores=None), dict(kept=None)):
         assert evict(**kw) == INVALID, kw
+    long = dict(pages=257, slots=20000)
+    need = lib.caddtree_evict_workspace_bytes(r(c), 2, 257, 20000)
+    assert need > 0 and lib.caddtree_evict_workspace_bytes(r(c), 2, 256, 20000) == 0
+    assert lib.caddtree_evict_workspace_bytes(None, 2, 257, 20000) == 0
+    for kw in (long, dict(**long, workspace=0x1000, bytes=need - 1), dict(workspace=0x1010, bytes=need)):
+        assert evict(**kw) == WORKSPACE, kw
     # nothing to do: no HIP call is made, pointers may be NULL
     e = _attention(B=0, q=(0, 0, 0, 0), k=(0, 0, 0, 0), v=(0, 0, 0, 0), out=(0, 0, 0, 0), ctx_len=None)
     assert lib.caddtree_window_attention(r(e), None, 0, None) == _lib.OK
