@@ -455,6 +455,26 @@ struct TensorPart {
     }
   }
 };
+// A tile of keys or values straight to LDS: each lane fetches the 16 bytes that belong in its place of the tile, so
+// nothing passes through registers.  The caller waits (tiles_there) before the barrier that hands the tile over.
+template <int D>
+struct TileMove {
+  static constexpr int kRows = 2048 / D, kN = 64 / kRows;      // rows a step of the workgroup
+  uint32_t from, to;         // a lane's bytes in a step's rows, the wavefront's place in a tile's step
+  __device__ TileMove(int64_t stride, int tid, int wave, bool keys) {
+    const int row = tid / (D / 8), n = tid % (D / 8);
+    from = (uint32_t)row * (2 * (uint32_t)stride) + 16 * (keys ? k_there<D>(row, n) : v_there<D>(row, n));
+    to = (uint32_t)wave * 1024;
+  }
+  __device__ __forceinline__ void send(const char* p, int64_t stride, int j0, uint32_t lds) const {
+#pragma unroll
+    for (int u = 0; u < kN; ++u)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
+                   :: "s"(lds + to + u * 4096), "v"(from), "s"(p + 2 * ((j0 + u * kRows) * stride)) : "memory", "m0");
+  }
+};
+__device__ __forceinline__ void tiles_there() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // ... and of a page: a block of 32 channels of a key and one of a value a thread (D = 64: half of the threads)
 template <int D>
 struct PagePart {
@@ -500,15 +520,26 @@ struct WideState {
   f32x16 acc[D / 32];
 };
 
-// Scores of 32 keys: row col's keys 8 (e / 4) + 4 half + e % 4.  k0: the lane's first place in them.
-template <typename E, int D>
-__device__ __forceinline__ f32x16 wide_scores(const u32x4 (&q)[D / 16], const char* keys, int k0) {
-  f32x16 x;
+// Scores of 32 kH keys: x[u] has row col's keys 32 u + 8 (e / 4) + 4 half + e % 4.  k0: the lane's first place in
+// them.  The chains of products alternate, and their keys leave LDS three steps ahead.
+template <typename E, int D, int kH>
+__device__ __forceinline__ void wide_scores(f32x16 (&x)[kH], const u32x4 (&q)[D / 16], const char* keys, int k0) {
 #pragma unroll
-  for (int e = 0; e < 16; ++e) x[e] = 0.f;
+  for (int u = 0; u < kH; ++u)
 #pragma unroll
-  for (int j = 0; j < D / 16; ++j) x = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(keys + (k0 ^ k_step<D>(j))), q[j], x);
-  return x;
+    for (int e = 0; e < 16; ++e) x[u][e] = 0.f;
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j)
+#pragma unroll
+    for (int u = 0; u < kH; ++u)
+      x[u] = Mfma<E>::m32(*reinterpret_cast<const u32x4*>(keys + 64 * D * u + (k0 ^ k_step<D>(j))), q[j], x[u]);
+  __builtin_amdgcn_sched_group_barrier(0x100, 3 * kH, 0);
+#pragma unroll
+  for (int j = 0; j < D / 16 - 3; ++j) {
+    __builtin_amdgcn_sched_group_barrier(0x008, kH, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, kH, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, 3 * kH, 0);
 }
 // ... of 32 kH keys: unseen ones left out and the row's maximum raised over them, where it lags too far behind.
 // seen: bit k for the lane's key 32 u + 8 (e / 4) + e % 4.
@@ -673,7 +704,8 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
     return sees_new(a, s, row).at(at);
   };
   auto take = [&](const char* tile, bool full, uint32_t seen) {
-    f32x16 x[1] = {wide_scores<E, D>(q, tile, k0)};
+    f32x16 x[1];
+    wide_scores<E, D, 1>(x, q, tile, k0);
     u32x4 p[2];
     wide_raise<E, D, 1>(st, x, c, full, seen);
     wide_weights<E, D>(st, x[0], p, c);
@@ -850,7 +882,8 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
     return sees_new(a, s, row).at(at);
   };
   auto take = [&](const char* tile, bool full, uint64_t seen) {
-    f32x16 x[2] = {wide_scores<E, D>(q, tile, k0), wide_scores<E, D>(q, tile + kHalf, k0)};
+    f32x16 x[2];
+    wide_scores<E, D, 2>(x, q, tile, k0);
     wide_raise<E, D, 2>(st, x, c, full, seen);
     u32x4 p0[2], p1[2];
     wide_weights<E, D>(st, x[0], p0, c);
@@ -904,34 +937,41 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
     }
   }
   {
+    // A tile seen in full goes straight to LDS while the one before it is taken; the others pass through registers,
+    // where values that are not to count are taken out.
     TensorPart<D> k, v;
-    auto load = [&](int tile) {
-      if (tile >= t1) return;
+    const TileMove<D> km(a.k.t, tid, wave, true), vm(a.v.t, tid, wave, false);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)&lds[0][0];
+    bool whole = false;
+    auto begin = [&](int tile, int to) {
       const int here = tile_of<kPage, 64>(span, tile, &cached);
-      k.load(kb, a.k.t, here, s.nk, tid);
-      v.load(vb, a.v.t, here, s.nk, tid);
+      whole = full_new(a, s, i0, i1, here, 64);
+      if (whole) {
+        km.send(kb, a.k.t, here, lds0 + to * 2 * kTile);
+        vm.send(vb, a.v.t, here, lds0 + to * 2 * kTile + kTile);
+      } else {
+        k.load(kb, a.k.t, here, s.nk, tid);
+        v.load(vb, a.v.t, here, s.nk, tid);
+      }
     };
-    auto store = [&](int tile, int to) {
-      const int here = tile_of<kPage, 64>(span, tile, &cached);
-      k.store_keys(lds[to], tid);
-      v.template store_values<E>(lds[to] + kTile, tid, full_new(a, s, i0, i1, here, 64), s.nk - here, &odd);
+    auto end = [&](int tile, int to) {
+      if (!whole) {
+        const int here = tile_of<kPage, 64>(span, tile, &cached);
+        k.store_keys(lds[to], tid);
+        v.template store_values<E>(lds[to] + kTile, tid, false, s.nk - here, &odd);
+      }
+      tiles_there();
     };
     if (t < t1) {
-      load(t);
-      store(t, buf);
-      load(t + 1);
+      begin(t, buf);
+      end(t, buf);
       __syncthreads();
     }
     for (; t < t1; ++t) {
-      if (mine) {
-        const int here = tile_of<kPage, 64>(span, t, &cached);
-        const bool full = full_new(a, s, i0, i1, here, 64);
-        take(lds[buf], full, full ? 0 : sees(false, here) >> (4 * half));
-      }
-      if (t + 1 < t1) {
-        store(t + 1, buf ^ 1);
-        load(t + 2);
-      }
+      const bool full = whole;
+      if (t + 1 < t1) begin(t + 1, buf ^ 1);
+      if (mine) take(lds[buf], full, full ? 0 : sees(false, tile_of<kPage, 64>(span, t, &cached)) >> (4 * half));
+      if (t + 1 < t1) end(t + 1, buf ^ 1);
       __syncthreads();
       buf ^= 1;
     }

@@ -177,6 +177,19 @@ __device__ int v_at(int row, int byte) {
   if (D == 128) return row * 256 + ((block ^ y) << 6) + ((sub ^ y ^ ((row >> 1) & 2) ^ (block & 2)) << 4) + (byte & 15);
   return row * 128 + ((block ^ (y & 1)) << 6) + ((sub ^ y) << 4) + (byte & 15);
 }
+// the piece that lies in 16-byte place n of a row: k_at(row, k_there(row, n)) = row's start + 16 n, and of v_at
+template <int D>
+__device__ int k_there(int row, int n) {
+  if (D == 128) return k_piece<D>(n ^ ((row & 1) << 2 | ((row >> 1) & 3) | (row & 8)));
+  const int m = n ^ ((row & 3) << 1 | ((row >> 2) & 1));
+  return m >> 1 | (m & 1) << 2;
+}
+template <int D>
+__device__ int v_there(int row, int n) {
+  const int y = row & 3;
+  if (D == 128) return ((n >> 2) ^ y) << 2 | ((n & 3) ^ y ^ ((row >> 1) & 2) ^ (((n >> 2) ^ y) & 2));
+  return ((n >> 2) ^ (y & 1)) << 2 | ((n & 3) ^ y);
+}
 // values `byte` (a multiple of 32) bytes further are at v_at ^ v_step(byte)
 __device__ constexpr int v_step(int byte) { return byte ^ ((byte >> 6) & 2) << 4; }
 
