@@ -467,10 +467,12 @@ struct TileMove {
     to = (uint32_t)wave * 1024;
   }
   __device__ __forceinline__ void send(const char* p, int64_t stride, int j0, uint32_t lds) const {
+    const char* at = p + 2 * (j0 * stride);
+    const int64_t step = 2 * kRows * stride;
+    lds += to;
 #pragma unroll
-    for (int u = 0; u < kN; ++u)
-      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2"
-                   :: "s"(lds + to + u * 4096), "v"(from), "s"(p + 2 * ((j0 + u * kRows) * stride)) : "memory", "m0");
+    for (int u = 0; u < kN; ++u, at += step, lds += 4096)
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" :: "s"(lds), "v"(from), "s"(at) : "memory", "m0");
   }
 };
 __device__ __forceinline__ void tiles_there() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
