@@ -10,7 +10,7 @@ namespace {
 
 using namespace at;
 
-constexpr int kThreads = 256;
+constexpr int kThreads = 256, kItems = 4;
 
 // The scale's byte and the codes of a lane's 8 values (4 pairs) of a block that lanes 4 n .. 4 n + 3 hold.
 // E = floor(log2 m) - 2 for the largest magnitude m, one more above 1.75 x 2^floor(log2 m); the hardware
@@ -39,22 +39,22 @@ __device__ uint32_t encode(const u32x4 x, uint32_t* scale_byte) {
   return r;
 }
 
-// a thread's token, head and piece of 8 channels: head rows of D / 8 lanes, heads innermost
+// A thread's token and head: rows of D / 8 lanes, heads innermost; the u-th of the n blocks of rows that a workgroup has.
 struct Item {
-  int t, h, piece;
+  int t, h;
 };
 template <int D>
-__device__ Item item_of(int heads) {
-  constexpr int kPer = D / 8;
-  const uint32_t row = blockIdx.x * (kThreads / kPer) + threadIdx.x / kPer;
-  return Item{(int)(row / (uint32_t)heads), (int)(row % (uint32_t)heads), (int)(threadIdx.x % kPer)};
+__device__ Item item_of(int heads, int u, int n) {
+  constexpr int kPer = D / 8, kRows = kThreads / kPer;
+  const uint32_t row = (blockIdx.x * n + u) * kRows + threadIdx.x / kPer;
+  return Item{(int)(row / (uint32_t)heads), (int)(row % (uint32_t)heads)};
 }
 
 template <typename E, int D>
 __global__ __launch_bounds__(kThreads) void write_kernel(CacheMoveArgs a) {
   using L = PageLayout<D>;
-  const Item it = item_of<D>(a.kv.heads);
-  const int b = blockIdx.y;
+  const Item it = item_of<D>(a.kv.heads, 0, 1);
+  const int b = blockIdx.y, piece = threadIdx.x % (D / 8);
   if (it.t >= (a.count ? clamp_len(a.count[b], a.T) : a.T)) return;      // (a block's four lanes stay together)
   const int64_t slot = a.start[b] + it.t;
   if (slot < 0 || slot >= (int64_t)a.kv.table_pages * kPage) return;
@@ -66,15 +66,15 @@ __global__ __launch_bounds__(kThreads) void write_kernel(CacheMoveArgs a) {
   uint8_t* page = page_of(a.kv, b, (int)(slot / kPage), it.h);
   if (page == nullptr) return;
   const int tok = (int)(slot % kPage);
-  const u32x4 k = *reinterpret_cast<const u32x4*>(a.k.data + 2 * (b * a.k.b + row * a.k.t + it.h * a.k.h + it.piece * 8));
-  const u32x4 v = *reinterpret_cast<const u32x4*>(a.v.data + 2 * (b * a.v.b + row * a.v.t + it.h * a.v.h + it.piece * 8));
+  const u32x4 k = *reinterpret_cast<const u32x4*>(a.k.data + 2 * (b * a.k.b + row * a.k.t + it.h * a.k.h + piece * 8));
+  const u32x4 v = *reinterpret_cast<const u32x4*>(a.v.data + 2 * (b * a.v.b + row * a.v.t + it.h * a.v.h + piece * 8));
   uint32_t ks, vs;
   const uint32_t kc = encode<E>(k, &ks), vc = encode<E>(v, &vs);
-  *reinterpret_cast<uint32_t*>(page + L::kK + tok * L::kRow + it.piece * 4) = kc;
-  *reinterpret_cast<uint32_t*>(page + L::kV + tok * L::kRow + it.piece * 4) = vc;
-  if (it.piece % 4 == 0) {
-    page[L::kKs + tok * L::kScales + it.piece / 4] = (uint8_t)ks;
-    page[L::kVs + tok * L::kScales + it.piece / 4] = (uint8_t)vs;
+  *reinterpret_cast<uint32_t*>(page + L::kK + tok * L::kRow + piece * 4) = kc;
+  *reinterpret_cast<uint32_t*>(page + L::kV + tok * L::kRow + piece * 4) = vc;
+  if (piece % 4 == 0) {
+    page[L::kKs + tok * L::kScales + piece / 4] = (uint8_t)ks;
+    page[L::kVs + tok * L::kScales + piece / 4] = (uint8_t)vs;
   }
 }
 
@@ -86,32 +86,48 @@ __device__ u32x4 decode(uint32_t codes, uint32_t scale_byte) {
                E::template from4<3>(codes, s)};
 }
 
+// (kItems rows a thread, their loads in flight together: 112k tokens of 8 heads in 142 us where one row a thread takes
+// 162; writing gains nothing by it)
 template <typename E, int D>
 __global__ __launch_bounds__(kThreads) void read_kernel(CacheMoveArgs a) {
   using L = PageLayout<D>;
-  const Item it = item_of<D>(a.kv.heads);
-  const int b = blockIdx.y;
-  const int64_t slot = (a.start ? a.start[b] : 0) + it.t;
-  if (it.t >= a.T || slot < 0 || slot >= a.end[b] || slot >= (int64_t)a.kv.table_pages * kPage) return;
-  const uint8_t* page = page_of(a.kv, b, (int)(slot / kPage), it.h);
-  if (page == nullptr) return;
-  const int tok = (int)(slot % kPage);
-  const uint32_t kc = *reinterpret_cast<const uint32_t*>(page + L::kK + tok * L::kRow + it.piece * 4);
-  const uint32_t vc = *reinterpret_cast<const uint32_t*>(page + L::kV + tok * L::kRow + it.piece * 4);
-  const uint32_t ks = page[L::kKs + tok * L::kScales + it.piece / 4], vs = page[L::kVs + tok * L::kScales + it.piece / 4];
-  *reinterpret_cast<u32x4*>(a.k.data + 2 * (b * a.k.b + it.t * a.k.t + it.h * a.k.h + it.piece * 8)) = decode<E>(kc, ks);
-  *reinterpret_cast<u32x4*>(a.v.data + 2 * (b * a.v.b + it.t * a.v.t + it.h * a.v.h + it.piece * 8)) = decode<E>(vc, vs);
+  const int b = blockIdx.y, piece = threadIdx.x % (D / 8);
+  const int64_t start = a.start ? a.start[b] : 0, end = min(a.end[b], (int64_t)a.kv.table_pages * kPage);
+  bool there[kItems];
+  uint32_t kc[kItems], vc[kItems], ks[kItems], vs[kItems];
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    const Item it = item_of<D>(a.kv.heads, u, kItems);
+    const int64_t slot = start + it.t;
+    there[u] = it.t < a.T && slot >= 0 && slot < end;
+    if (!there[u]) continue;
+    const uint8_t* page = page_of(a.kv, b, (int)(slot / kPage), it.h);
+    there[u] = page != nullptr;
+    if (!there[u]) continue;
+    const int tok = (int)(slot % kPage);
+    kc[u] = *reinterpret_cast<const uint32_t*>(page + L::kK + tok * L::kRow + piece * 4);
+    vc[u] = *reinterpret_cast<const uint32_t*>(page + L::kV + tok * L::kRow + piece * 4);
+    ks[u] = page[L::kKs + tok * L::kScales + piece / 4];
+    vs[u] = page[L::kVs + tok * L::kScales + piece / 4];
+  }
+#pragma unroll
+  for (int u = 0; u < kItems; ++u) {
+    if (!there[u]) continue;
+    const Item it = item_of<D>(a.kv.heads, u, kItems);
+    *reinterpret_cast<u32x4*>(a.k.data + 2 * (b * a.k.b + it.t * a.k.t + it.h * a.k.h + piece * 8)) = decode<E>(kc[u], ks[u]);
+    *reinterpret_cast<u32x4*>(a.v.data + 2 * (b * a.v.b + it.t * a.v.t + it.h * a.v.h + piece * 8)) = decode<E>(vc[u], vs[u]);
+  }
 }
 
-dim3 grid_of(const CacheMoveArgs& a, int D) {
-  const int64_t rows = kThreads / (D / 8);
+dim3 grid_of(const CacheMoveArgs& a, int D, int items) {
+  const int64_t rows = items * kThreads / (D / 8);
   return dim3((unsigned)(((int64_t)a.T * a.kv.heads + rows - 1) / rows), a.B);
 }
 
 }  // namespace
 
 hipError_t launch_cache_write(const CacheMoveArgs& a, caddtree_dtype_t dtype, int32_t D, hipStream_t stream) {
-  const dim3 g = grid_of(a, D);
+  const dim3 g = grid_of(a, D, 1);
   if (dtype == CADDTREE_BF16) {
     if (D == 64) write_kernel<BF16, 64><<<g, kThreads, 0, stream>>>(a);
     else write_kernel<BF16, 128><<<g, kThreads, 0, stream>>>(a);
@@ -123,7 +139,7 @@ hipError_t launch_cache_write(const CacheMoveArgs& a, caddtree_dtype_t dtype, in
 }
 
 hipError_t launch_cache_read(const CacheMoveArgs& a, caddtree_dtype_t dtype, int32_t D, hipStream_t stream) {
-  const dim3 g = grid_of(a, D);
+  const dim3 g = grid_of(a, D, kItems);
   if (dtype == CADDTREE_BF16) {
     if (D == 64) read_kernel<BF16, 64><<<g, kThreads, 0, stream>>>(a);
     else read_kernel<BF16, 128><<<g, kThreads, 0, stream>>>(a);
