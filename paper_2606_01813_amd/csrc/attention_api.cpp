@@ -153,15 +153,16 @@ caddtree_status_t check_workspace(const void* workspace) {
 }
 
 // How many parts a row's keys are cut into, from the sizes alone (lengths are on the device): as many as fill the
-// card, two workgroups a compute unit, where each keeps a few tiles a wavefront.  A call that fills it by itself is
-// not cut: the parts' sums cost more than an uneven last round does (32 trees of 257 rows, 2304 workgroups: 712 us
-// whole, 736 in two parts).
+// card, two workgroups a compute unit, where each keeps a few tiles: 192 keys for up to 64 rows (one token over 1024:
+// 14.2 us, 15.8 with 384 keys), 384 for more, whose parts' sums are larger (65 rows of 4 heads over 4096: 25 us, 29.5
+// with 192).  A call that fills the card by itself is not cut: the sums cost more than an uneven last round does (32
+// trees of 257 rows, 2304 workgroups: 2% more in two parts).
 int32_t splits_of(const caddtree_attention_t* a) {
   const int64_t G = a->n_heads / a->n_kv_heads, rows = a->T * G;
   const int64_t groups = (int64_t)a->B * a->n_kv_heads * (rows <= 64 ? 1 : (rows + 127) / 128);
   int64_t reach = (int64_t)a->table_pages * CADDTREE_PAGE + a->S;      // keys of a workgroup's rows at most
   if (a->window > 0) reach = std::min(reach, (int64_t)a->window + a->sinks + std::min<int64_t>(a->T, 128 / G + 1) + 64);
-  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(kResident / std::max<int64_t>(groups, 1), reach / 384));
+  return (int32_t)std::max<int64_t>(1, std::min<int64_t>(kResident / std::max<int64_t>(groups, 1), reach / (rows <= 64 ? 192 : 384)));
 }
 size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
 size_t split_bytes(const caddtree_attention_t* a, int32_t n) {

@@ -285,6 +285,15 @@ __global__ __launch_bounds__(kThreads) void list_kernel(EvictArgs a, Parts p) {
   const float* x = a.scores + row * a.slots;
   const int lo = a.sinks, hi = n - a.recent;
   const int from = part * p.span, to = min(from + p.span, n);
+  float y[kStep];
+  auto load = [&](int t) {
+#pragma unroll
+    for (int j = 0; j < kStep; ++j) {
+      const int i = t + (wave * kStep + j) * 64 + lane;
+      y[j] = i < to ? x[i] : 0.f;
+    }
+  };
+  load(from);                                       // (on their way while the digit is found)
   const uint32_t* state = p.state_of(row);
   uint32_t prefix = state[2], want = state[3], eq;
   uint32_t at = add_parts(p, row, 2, part, live, want, sums, found, before, &eq) + state[4 + 2 * part + 1];
@@ -295,12 +304,13 @@ __global__ __launch_bounds__(kThreads) void list_kernel(EvictArgs a, Parts p) {
   const uint64_t below = (1ull << lane) - 1;
   for (int t = from; t < to; t += kBlock) {
     const int strip = t + wave * kStep * 64;
+    if (t != from) load(t);
     int kind[kStep];
     uint32_t na = 0, ne = 0;
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       const int i = strip + j * 64 + lane;
-      kind[j] = kind_of(i < to ? i : -1, key_of(i < to ? x[i] : 0.f), lo, hi, prefix);
+      kind[j] = kind_of(i < to ? i : -1, key_of(y[j]), lo, hi, prefix);
       na += __popcll(__ballot(kind[j] == 2));
       ne += __popcll(__ballot(kind[j] == 1));
     }
@@ -311,6 +321,7 @@ __global__ __launch_bounds__(kThreads) void list_kernel(EvictArgs a, Parts p) {
     }
     __syncthreads();
     uint32_t my_at = at, my_eq = eq;
+#pragma unroll
     for (int w = 0; w < kWaves; ++w) {
       const uint32_t taken = sums[w] + (min(eq + equals[w], want) - min(eq, want));
       at += taken;
