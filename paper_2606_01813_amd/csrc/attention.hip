@@ -1,13 +1,23 @@
-// Attention over the keys of a tensor and of a 4-bit cache, in two kernels.
+// Attention over the keys of a tensor and of a 4-bit cache, in three kernels by the rows (queries x heads) that
+// share a kv head.  All go over the keys once with the running maximum and sum of a softmax, and form S^T = K Q^T and
+// O^T = V^T P^T, so that a row's statistics and sums lie in lanes of the row.
 //
-// Few rows (at most 64 of a kv head: single tokens, blocks, small trees) are bound by reading the keys.
-// The narrow kernel's wavefronts each take tiles of their own: codes go from memory to registers, keys
-// are converted there into the operand of the matrix product, values pass through LDS to be transposed.
-// Many rows (prompts, large trees) are bound by the matrix products; the wide kernel's four wavefronts
-// share each tile, converted once into LDS, and hold 32 rows each.
+// Over a cache few rows (at most 32: single tokens, small blocks) are bound by reading the keys.  The narrow kernel's
+// wavefronts each take tiles of their own: codes go from memory to registers, keys are converted there into the
+// operand of the matrix product, values pass through LDS to be transposed.  33 to 64 rows would convert a tile more
+// often than it is used; the pair kernel's four wavefronts share it.  Many rows (prompts, trees) are bound by the
+// matrix products and the softmax; the wide kernel's four wavefronts share each tile and hold 32 rows each.
+// Over 131072 cached keys of 8 kv heads: 32 rows narrow 48 us, pair 66; 64 rows pair 69, wide 82.
+//
+// A tensor's tiles go to LDS by themselves, so the wide kernel takes few rows as well: over 131072 keys 4 rows 49 us,
+// narrow 58; 32 rows 56 us, narrow 69; 64 rows 73 us, pair 82.  Where there are few keys in all (kFewKeys) and up to 16
+// rows the narrow kernel starts and ends sooner: 1000 keys of 8 kv heads 9.9 us, wide 11.9; 1028 of 64 14.3 us, wide
+// 14.9; 1024 of 512 28.5 us, wide 22.9.
 //
 // Where there are too few workgroups for the card, the tiles of a row are split over several, whose
 // partial sums the combining kernel joins in a fixed order.
+#include <algorithm>
+
 #include "attn_tile.h"
 
 namespace caddtree {
@@ -15,6 +25,7 @@ namespace {
 
 using namespace at;
 
+constexpr int64_t kFewKeys = 1 << 17;               // of all sequences and kv heads
 constexpr int kMaxSplits = 512, kFewSplits = 8;      // (attention_api.cpp: at most as many as workgroups fill the card)
 
 // partial results of (sequence, kv head, row, split): D sums, relative to the maximum, in `sum`; the
@@ -228,6 +239,10 @@ __device__ __forceinline__ bool narrow_tile(NarrowState<D, kR>& st, Stage& x, co
   return odd;
 }
 
+// Up to 16 kR rows.  Bound by reading the keys: 64 single tokens over 4096 to 8192 cached ones, 8 kv heads of 128
+// channels, take 91 us, 5.0 TB/s of codes and scales, what a large copy reaches on this card.  A wavefront has a page's
+// codes on their way while it takes the page before (a page is 8.5 KB, eight wavefronts a compute unit), and the next
+// pages' numbers before that: a number waited for in the loop would hold up the loads behind it.
 template <typename E, int D, int kR, bool kPaged>
 __global__ __launch_bounds__(256, 2) void narrow_kernel(AttnArgs a, Split sp) {
   using L = PageLayout<D>;
@@ -659,10 +674,12 @@ __device__ __forceinline__ void wide_finish(const WideState<D>& st, const AttnAr
   }
 }
 
-// 33 to 64 rows: two wavefront pairs share the rows out and take half of a tile's keys each, whose sums they join at
-// the end.  Bound by reading the keys, so two tiles are on their way in registers (a tile's codes are a few) while
-// one is in LDS: memory takes longer than the products of one.
-template <typename E, int D, bool kPaged>
+// 33 to 64 rows over a cache: two wavefront pairs share the rows out and take half of a tile's keys each, whose sums they join at
+// the end.  Two tiles are on their way in registers (a tile's codes are a few) while one is in LDS.  A block of 16 with 4
+// heads a kv head over 131072 cached tokens of 128 channels takes 70 us, 2.0 TB/s: a tile's chain of conversion, LDS,
+// products and softmax between two barriers takes longer than its bytes, matrix units and vector units being busy 24% and
+// 38% of the time and wavefronts waiting 42% of theirs.
+template <typename E, int D>
 __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
   constexpr int kTile = 64 * 2 * D;
   __shared__ __align__(16) char lds[2][2 * kTile];  // two tiles, keys then values: one is read while the next is written
@@ -675,7 +692,7 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
   const int i0 = 0, i1 = s.nq - 1;
   const Span span = span_of<kPage, 64>(a, s, i0, i1);
   const int per = ceil_div(span.n, sp.n), t0 = split * per, t1 = min(span.n, t0 + per);
-  const int nc = kPaged ? max(t0, min(t1, span.a + span.c - span.b)) : t0;   // this split's cached tiles come first
+  const int nc = max(t0, min(t1, span.a + span.c - span.b));   // this split's cached tiles come first
 
   const int r = 32 * (wave & 1) + col, rr = min(r, R - 1), i = rr / a.G, h = hk * a.G + rr % a.G;
   const int u0 = wave >> 1;                         // its 32-key part
@@ -701,8 +718,8 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
   const char* kb = a.k.data + 2 * (b * a.k.b + hk * a.k.h);
   const char* vb = a.v.data + 2 * (b * a.v.b + hk * a.v.h);
   auto sees = [&](bool cached, int at) -> uint64_t {
-    if (kPaged && cached) return sees_cached(a, s, row).at(at);
-    if (kPaged && a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, row, at);
+    if (cached) return sees_cached(a, s, row).at(at);
+    if (a.order == CADDTREE_ORDER_TREE) return sees_tree(a, s, b, row, at);
     return sees_new(a, s, row).at(at);
   };
   auto take = [&](const char* tile, bool full, uint32_t seen) {
@@ -716,7 +733,7 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
 
   int t = t0, buf = 0;
   bool cached;
-  if constexpr (kPaged) {
+  {
     struct Stage {
       PagePart<D> x;
       const uint8_t* page;
@@ -800,7 +817,7 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
     }
   }
   __syncthreads();
-  if (odd && mine) add_odd<E, D, kPaged>(st, a, s, span, b, hk, i0, i1, t0, t1, 32 * u0, 32 * u0 + 32, half, sees);
+  if (odd && mine) add_odd<E, D, true>(st, a, s, span, b, hk, i0, i1, t0, t1, 32 * u0, 32 * u0 + 32, half, sees);
   st.l += __shfl_xor(st.l, 32);
   {                                                 // the second pair's sums to the first, 16 registers at a time
     __syncthreads();
@@ -832,12 +849,14 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
   if (r < R) wide_finish<E, D>(st, a, sp, b, hk, r, i, h, half, split);
 }
 
-// 128 rows a workgroup, 32 a wavefront.  Bound by the matrix products, by forming the weights and by staging the
-// tiles, about alike: at 128 channels a tile takes a wavefront 32 products (1024 cycles), some 300 vector and 150
-// scalar instructions, and with two workgroups a compute unit the three overlap in part only.  Without the
-// exponentials a windowed prompt takes 6% less, without the products with the values 15%, without the staging of
-// tiles 30%; eight wavefronts or 64 rows a wavefront that share a staged tile, or steps of half a tile with the
-// products of one and the exponentials of another interleaved, came to the same or more.
+// 128 rows a workgroup, 32 a wavefront.  Bound by the matrix products and by forming the weights, which hardly overlap:
+// at 128 channels a tile takes a wavefront 32 products (1024 cycles) and some 230 vector instructions, 32 of them
+// exponentials (1300 cycles), of the 2500 it takes in all.  A prompt of 8192 tokens of 32 heads through a window of 2048
+// takes 288 us (835 TFLOP/s; matrix units busy 46%, vector units 48% of the time); 32 trees of 257 rows over 4096 cached
+// tokens take 625 us (706 TFLOP/s): there a tile is converted on its way into LDS and the wavefronts wait 45% of their
+// time, 23% where tiles go straight to LDS.  The next tile stored earlier (before this one or between its scores and its
+// softmax), or loaded a tile earlier, took 1 to 3% longer; eight wavefronts or 64 rows a wavefront that share a tile,
+// tiles of 32 keys with three wavefronts a SIMD, priorities for the products, or half tiles interleaved, the same or more.
 template <typename E, int D, bool kPaged>
 __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   constexpr int kRows = 128, kTile = 64 * 2 * D, kHalf = 32 * 2 * D;
@@ -984,7 +1003,8 @@ __global__ __launch_bounds__(256, 2) void wide_kernel(AttnArgs a, Split sp) {
   if (r < R) wide_finish<E, D>(st, a, sp, b, hk, r, i, h, half, split);
 }
 
-// Joins the splits of a row, few of them: D / 4 lanes a row, 4 channels each.
+// Joins the splits of a row, few of them: D / 4 lanes a row, 4 channels each.  Two loads deep and bound by their latency:
+// 3 us for 256 rows of 5 splits.
 template <typename E>
 __device__ void write_row(const AttnArgs& a, int b, int hk, int r, int ch, f32x4 o, float m, float l) {
   const int i = r / a.G, h = hk * a.G + r % a.G;
@@ -1025,7 +1045,8 @@ __global__ __launch_bounds__(256) void combine_few_kernel(AttnArgs a, Split sp) 
   write_row<E>(a, b, hk, (int)r, ch, o, m, l);
 }
 // ... many of them: a workgroup a row.  Its threads look at a split each for the maximum, the sum and the factors;
-// then groups of D / 4 lanes take every n-th split's sums and add up through LDS, in a fixed order.
+// then groups of D / 4 lanes take every n-th split's sums and add up through LDS, in a fixed order.  512 rows of 64
+// splits: 6 us (17 MB, 2.8 TB/s); with a group of lanes a row as above, 19.
 template <typename E, int D>
 __global__ __launch_bounds__(256) void combine_many_kernel(AttnArgs a, Split sp) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
@@ -1077,10 +1098,19 @@ template <typename E, int D, bool kPaged>
 hipError_t launch(const AttnArgs& a, const Split& sp, hipStream_t stream) {
   const int64_t R = (int64_t)a.T * a.G;
   const dim3 few(sp.n, a.Hkv, a.B);
-  if (R <= 16) narrow_kernel<E, D, 1, kPaged><<<few, 256, 0, stream>>>(a, sp);
-  else if (R <= 32) narrow_kernel<E, D, 2, kPaged><<<few, 256, 0, stream>>>(a, sp);
-  else if (R <= 64) pair_kernel<E, D, kPaged><<<few, 256, 0, stream>>>(a, sp);
-  else wide_kernel<E, D, kPaged><<<dim3((unsigned)((R + 127) / 128 * sp.n * (((int64_t)a.B * a.Hkv + 7) / 8 * 8))), 256, 0, stream>>>(a, sp);
+  bool done = false;
+  if constexpr (kPaged) {
+    done = R <= 64;
+    if (R <= 16) narrow_kernel<E, D, 1, true><<<few, 256, 0, stream>>>(a, sp);
+    else if (R <= 32) narrow_kernel<E, D, 2, true><<<few, 256, 0, stream>>>(a, sp);
+    else if (R <= 64) pair_kernel<E, D><<<few, 256, 0, stream>>>(a, sp);
+  } else if (R <= 16) {
+    const int64_t reach = a.window == 0 ? a.S : std::min<int64_t>(a.S, (int64_t)a.window + a.sinks + a.T);
+    done = reach * a.Hkv * a.B <= kFewKeys;
+    if (done) narrow_kernel<E, D, 1, false><<<few, 256, 0, stream>>>(a, sp);
+  }
+  if (!done)
+    wide_kernel<E, D, kPaged><<<dim3((unsigned)((R + 127) / 128 * sp.n * (((int64_t)a.B * a.Hkv + 7) / 8 * 8))), 256, 0, stream>>>(a, sp);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || sp.n == 1) return e;
   const int lanes = D / 4;

@@ -7,7 +7,10 @@
 // Rows of up to 16384 slots have a workgroup each and keep their keys in registers throughout.  Longer rows
 // are cut into parts, a workgroup each: a launch a digit counts every part's keys, the next one adds the parts'
 // histograms up, finds the digit and goes on, and the last lists (kept slots before a part follow from the
-// histograms of the parts before it).
+// histograms of the parts before it).  4 rows with the move: of 16384 slots 28 us in a workgroup, of 16448 32 us in
+// parts; of 131072 31 us of selection in parts, 137 in a workgroup that reads its scores again for every digit.
+// Bound by latency: a part's counting takes 5 us, adding the histograms 3 more (parts of 4096 or of 16384 slots: the
+// whole call 46 -> 60 and 51 us).
 #include <algorithm>
 
 #include "attn_common.h"
@@ -89,7 +92,8 @@ __device__ __forceinline__ int kind_of(int i, uint32_t k, int lo, int hi, uint32
   return k > threshold ? 2 : k == threshold ? 1 : 0;
 }
 
-// One workgroup a sequence and kv head; a thread holds kKept keys, kKept kThreads >= n.
+// One workgroup a sequence and kv head; a thread holds kKept keys, kKept kThreads >= n.  512 rows of 4096 to 8192 slots
+// take 39 us (0.35 TB/s): bound by the vector instructions of the counting and the listing, 1024 threads a row.
 template <int kKept>
 __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
   __shared__ uint32_t hist[kBins];
@@ -344,7 +348,9 @@ __global__ __launch_bounds__(kThreads) void list_kernel(EvictArgs a, Parts p) {
 }
 
 // A wavefront moves the 64 tokens of a new page and head: a lane looks up one token's old place, then
-// D / 16 lanes move a token's codes, 16 bytes each, all loads in flight at once.
+// D / 16 lanes move a token's codes, 16 bytes each, all loads in flight at once.  2048 of 4096 to 8192 slots of 64
+// sequences and 8 heads of 128 channels: 100 us, 2.9 TB/s of the bytes moved; kept tokens lie apart, and what memory
+// fetches around their 64 bytes brings it to some 4.
 template <int D>
 __global__ __launch_bounds__(256) void move_kernel(EvictArgs a) {
   using L = PageLayout<D>;

@@ -5,7 +5,10 @@
 // four lanes of that key; it goes over the rows, sums a lane's weights in registers and adds the four lanes
 // at the end.  No two wavefronts add to one score and the order of a sum is fixed.  Queries of no weight
 // (in a tree most: only the accepted path counts) are left out first.  Where there are pages enough a wavefront
-// has several, the next one's codes on their way, and what is set up once serves all of them.
+// has several, the next one's codes on their way, and what is set up once serves all of them.  64 single tokens over
+// 4096 to 8192 cached ones, 8 kv heads of 128 channels: 55 us (4.6 TB/s, vector units busy 74% of the time; a page a
+// wavefront and operands kept for further rows, 88); 8 trees of 65 rows over windows of 4096 of 16384: 36 us, of which
+// the gathering of rows and the chain of first loads are the most.
 #include <algorithm>
 
 #include "attn_tile.h"
@@ -173,7 +176,8 @@ namespace {
 
 template <typename E, int D>
 hipError_t launch(const ScoreArgs& a, hipStream_t stream) {
-  // pages of a wavefront: several where a call reads so many that its workgroups would come in many rounds
+  // pages of a wavefront: several where a call reads so many that its workgroups would come in many rounds (2048 are on
+  // the card at a time)
   const int64_t all = (a.slots + kPage - 1) / kPage;
   int64_t reach = all;
   if (a.at.window > 0) reach = std::min(all, ((int64_t)a.at.window + a.at.sinks) / kPage + 2);
