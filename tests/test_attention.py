@@ -91,6 +91,10 @@ WINDOW = [
     (4, 65, 65, 7, 1, 128, 40, 2, True, [65, 1, 0, 64], [65, 1, 0, 64], "bthd"),
     (1, 3, 2000, 16, 2, 64, 900, 70, True, None, None, "bthd"),        # sinks past a tile, far from the window
     (1, 257, 1200, 4, 2, 128, 500, 130, True, None, None, "bthd"),
+    # few rows over so many keys that the kernel of many rows takes them
+    (1, 1, 17001, 16, 8, 64, 0, 0, True, None, None, "bthd"),
+    (3, 3, 9000, 10, 5, 128, 0, 0, True, [3, 0, 2], [9000, 8999, 70], "wide"),
+    (2, 4, 8300, 8, 8, 128, 8200, 3, False, [4, 1], [8299, 1], "bhtd"),
 ]
 
 
