@@ -1046,7 +1046,7 @@ __global__ __launch_bounds__(256) void combine_few_kernel(AttnArgs a, Split sp) 
 }
 // ... many of them: a workgroup a row.  Its threads look at a split each for the maximum, the sum and the factors;
 // then groups of D / 4 lanes take every n-th split's sums and add up through LDS, in a fixed order.  512 rows of 64
-// splits: 6 us (17 MB, 2.8 TB/s); with a group of lanes a row as above, 19.
+// splits: 6 us (17 MB, 2.8 TB/s); with a group of lanes a row as above the whole call took 87 us in place of 74.
 template <typename E, int D>
 __global__ __launch_bounds__(256) void combine_many_kernel(AttnArgs a, Split sp) {
   constexpr int kLanes = D / 4, kGroups = 256 / kLanes;

@@ -6,8 +6,8 @@
 // at the end.  No two wavefronts add to one score and the order of a sum is fixed.  Queries of no weight
 // (in a tree most: only the accepted path counts) are left out first.  Where there are pages enough a wavefront
 // has several, the next one's codes on their way, and what is set up once serves all of them.  64 single tokens over
-// 4096 to 8192 cached ones, 8 kv heads of 128 channels: 55 us (4.6 TB/s, vector units busy 74% of the time; a page a
-// wavefront and operands kept for further rows, 88); 8 trees of 65 rows over windows of 4096 of 16384: 36 us, of which
+// 4096 to 8192 cached ones, 8 kv heads of 128 channels: 55 us (4.6 TB/s, vector units busy 74% of the time; with a page a
+// wavefront and operands kept for further rows the call took 97 us in place of 64); 8 trees of 65 rows over windows of 4096 of 16384: 36 us, of which
 // the gathering of rows and the chain of first loads are the most.
 #include <algorithm>
 
