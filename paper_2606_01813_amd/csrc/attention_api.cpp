@@ -132,7 +132,10 @@ AttnArgs args_of(const caddtree_attention_t* a, const caddtree_cache_t* cache) {
   k.Hkv = a->n_kv_heads;
   k.G = a->n_heads / a->n_kv_heads;
   k.scale = a->scale;
-  k.window = a->window;
+  // All positions are below `reach` (a query may be before position 0).  A window that long hides no key and is none:
+  // what the kernels subtract from a position then stays below 2^31 (check_attention bounds the lengths).
+  const int64_t reach = cache ? (int64_t)a->table_pages * CADDTREE_PAGE + a->T : a->S;
+  k.window = a->window >= reach ? 0 : a->window;
   k.sinks = a->sinks;
   k.order = enum_value(a->order);
   k.mask_kind = enum_value(a->mask_kind);
