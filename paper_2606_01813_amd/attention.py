@@ -400,8 +400,8 @@ class KVCache:
         the largest scores of the rest, in their old order.  The kept slots go to the pages of ``new_table``
         (int32 [B, pages], none of them in use), their scores to ``new_scores`` (float32 [B, kv heads, slots],
         zeros behind), the lengths to ``new_len`` (int64 [B]) and the old slots to ``kept`` (int32
-        [B, kv heads, budget], -1 behind).  Rows of more than 16384 slots need a workspace, made here if not given
-        (with a raw stream handle it has to be)."""
+        [B, kv heads, budget], -1 behind).  These four are tensors apart from the ones that are read.  Rows of more
+        than 16384 slots need a workspace, made here if not given (with a raw stream handle it has to be)."""
         if workspace is None and (stream is None or hasattr(stream, "cuda_stream")):
             workspace = self.evict_workspace(page_table, scores, stream)
         native = self._native(stream)

@@ -155,6 +155,26 @@ caddtree_status_t check_workspace(const void* workspace) {
   return CADDTREE_OK;
 }
 
+// An array of a call and whether the call writes it.  What is written must lie in no other array: the kernels of a call
+// read and write in no fixed order.
+struct Array {
+  const char* name;
+  const void* data;
+  size_t bytes;              // (of sizes within the limits: below 2^64)
+  bool written;
+};
+template <size_t n>
+caddtree_status_t check_apart(const Array (&all)[n]) {
+  for (size_t i = 0; i < n; ++i)
+    for (size_t j = i + 1; j < n; ++j) {
+      const Array &x = all[i], &y = all[j];
+      const uintptr_t px = reinterpret_cast<uintptr_t>(x.data), py = reinterpret_cast<uintptr_t>(y.data);
+      if ((x.written || y.written) && x.bytes > 0 && y.bytes > 0 && (px <= py ? py - px < x.bytes : px - py < y.bytes))
+        return fail(CADDTREE_E_INVALID, "%s and %s overlap", x.name, y.name);
+    }
+  return CADDTREE_OK;
+}
+
 // How many parts a row's keys are cut into, from the sizes alone (lengths are on the device): as many as fill the
 // card, two workgroups a compute unit, where each keeps a few tiles: 192 keys for up to 64 rows (one token over 1024:
 // 14.2 us, 15.8 with 384 keys), 384 for more, whose parts' sums are larger (65 rows of 4 heads over 4096: 25 us, 29.5
@@ -314,6 +334,20 @@ caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B,
   if (bytes > 0 && (workspace == nullptr || workspace_bytes < bytes))
     return fail(CADDTREE_E_WORKSPACE, "rows of %lld slots need a workspace of %zu bytes, got %zu", (long long)slots, bytes,
                 workspace ? workspace_bytes : (size_t)0);
+  const size_t rows = (size_t)B * cache->n_kv_heads;
+  const Array arrays[] = {{"page_table", page_table, (size_t)B * table_pages * 4, false},
+                          {"ctx_len", ctx_len, (size_t)B * 8, false},
+                          {"scores", scores, rows * slots * 4, false},
+                          {"new_table", new_table, (size_t)B * new_pages * 4, false},
+                          {"new_scores", new_scores, rows * new_slots * 4, true},
+                          {"new_len", new_len, (size_t)B * 8, true},
+                          {"kept", kept, rows * budget * 4, true},
+                          {"workspace", workspace, bytes, true},
+                          {"the cache's pages", cache->pages,
+                           (size_t)(cache->n_pages * cache->n_kv_heads * CADDTREE_PAGE_BYTES(cache->head_dim)), true}};
+  if ((st = check_apart(arrays)) != CADDTREE_OK) return st;
+  if (new_table == page_table && budget > 0)
+    return fail(CADDTREE_E_INVALID, "new_table is page_table: kept slots go to pages that are not in use");
   caddtree::EvictArgs a = {paged(cache, page_table, table_pages), B, cache->head_dim, ctx_len, scores, slots, budget, sinks,
                            recent, new_table, new_pages, new_scores, new_slots, new_len, kept};
   const hipError_t e = caddtree::launch_cache_evict(a, workspace, stream);
