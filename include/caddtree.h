@@ -401,13 +401,14 @@ caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const cadd
 
 /* Cuts each sequence to at most `budget` slots, by kv head: the first `sinks`, the last `recent`, and of
  * the others those with the largest scores (ties: the lower slot; a NaN counts as the lowest), in their
- * old order.  sinks + recent <= budget.
+ * old order.  sinks + recent <= budget.  Slots of pages outside the cache hold no key and are left out,
+ * sinks and recent ones among them.
  *   scores [B, n_kv_heads, slots]; new_table [B, new_pages]: pages for budget slots that are in none of
  *   the tables in use (the old pages are free once the call is done); new_scores [B, n_kv_heads,
- *   new_slots], new_slots >= budget: the kept slots' scores, then zeros; new_len [B] = min(ctx_len,
- *   budget); kept [B, n_kv_heads, budget]: the old slots, then -1.  new_scores, new_len, kept and the
- *   workspace lie in no other array of the call (scores and ctx_len among them), and new_table is not
- *   page_table: CADDTREE_E_INVALID.
+ *   new_slots], new_slots >= budget: the kept slots' scores, then zeros; new_len [B]: how many are kept,
+ *   min(ctx_len, budget) where all pages are there; kept [B, n_kv_heads, budget]: the old slots, then -1.
+ *   new_scores, new_len, kept and the workspace lie in no other array of the call (scores and ctx_len
+ *   among them), and new_table is not page_table: CADDTREE_E_INVALID.
  *   workspace: caddtree_evict_workspace_bytes(...) bytes, 256-byte aligned (CADDTREE_E_WORKSPACE if smaller). */
 caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B, const int32_t* page_table,
                                        int32_t table_pages, const int64_t* ctx_len, const float* scores, int64_t slots,

@@ -397,11 +397,12 @@ class KVCache:
     def evict(self, page_table, ctx_len, scores, new_table, new_len, new_scores, kept, *, budget: int, sinks: int = 0,
               recent: int = 0, workspace=None, stream=None) -> None:
         """Cuts every sequence to at most ``budget`` slots a kv head: the first ``sinks``, the last ``recent`` and
-        the largest scores of the rest, in their old order.  The kept slots go to the pages of ``new_table``
-        (int32 [B, pages], none of them in use), their scores to ``new_scores`` (float32 [B, kv heads, slots],
-        zeros behind), the lengths to ``new_len`` (int64 [B]) and the old slots to ``kept`` (int32
-        [B, kv heads, budget], -1 behind).  These four are tensors apart from the ones that are read.  Rows of more
-        than 16384 slots need a workspace, made here if not given (with a raw stream handle it has to be)."""
+        the largest scores of the rest, in their old order; slots of pages outside the cache hold no key and are
+        left out.  The kept slots go to the pages of ``new_table`` (int32 [B, pages], none of them in use), their
+        scores to ``new_scores`` (float32 [B, kv heads, slots], zeros behind), how many they are to ``new_len``
+        (int64 [B]) and the old slots to ``kept`` (int32 [B, kv heads, budget], -1 behind).  These four are tensors
+        apart from the ones that are read.  Rows of more than 16384 slots need a workspace, made here if not given
+        (with a raw stream handle it has to be)."""
         if workspace is None and (stream is None or hasattr(stream, "cuda_stream")):
             workspace = self.evict_workspace(page_table, scores, stream)
         native = self._native(stream)

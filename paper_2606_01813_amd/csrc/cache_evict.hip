@@ -4,6 +4,8 @@
 // Selection finds the smallest kept score, as an order-preserving 32-bit key, digit by digit (11, 11 and 10
 // bits), by a histogram of the digit over the keys that share the digits found so far.  A last ordered pass
 // lists the kept slots.  Counts are integers, so nothing depends on the order of the additions.
+// Slots of a page that is not in the cache hold no key: they are left out, neither counted nor kept.  A wavefront's step
+// is 64 slots, a page, so whether they are there is a bit for all of them.
 // Rows of up to 16384 slots have a workgroup each and keep their keys in registers throughout.  Longer rows
 // are cut into parts, a workgroup each: a launch a digit counts every part's keys, the next one adds the parts'
 // histograms up, finds the digit and goes on, and the last lists (kept slots before a part follow from the
@@ -33,6 +35,29 @@ __device__ uint32_t key_of(float x) {
 
 __device__ int live_slots(const EvictArgs& a, int b) {
   return clamp_len(a.ctx_len[b], min((int64_t)a.kv.table_pages * kPage, a.slots));
+}
+
+// Lane j's page: of the 64 slots from i0 + 64 j on, where j < steps and they are below `to`; and which of them are there.
+__device__ __forceinline__ int32_t entries(const EvictArgs& a, int b, int i0, int steps, int to) {
+  const int lane = threadIdx.x & 63, i = i0 + 64 * lane;
+  return lane < steps && i < to ? table_entry(a.kv, b, i / kPage) : -1;
+}
+__device__ __forceinline__ uint64_t pages_there(const EvictArgs& a, int32_t entry) { return __ballot(entry >= 0 && entry < a.kv.n_pages); }
+// Of the slots i0 .. i1 - 1 those outside lo .. hi - 1, which do not compete.
+__device__ __forceinline__ int outside(int i0, int i1, int lo, int hi) { return i1 - i0 - max(0, min(i1, hi) - max(i0, lo)); }
+// Adds the slots from i0 on that are there to *slots, and those of them that do not compete to *fixed.
+__device__ __forceinline__ void add_there(uint64_t there, int i0, int steps, int to, int lo, int hi, int* slots, int* fixed) {
+  const int end = min(i0 + 64 * steps, to), n = max(0, (end - i0 + 63) / 64);
+  if (__popcll(there) == n) {
+    *slots += max(0, end - i0);
+    *fixed += n ? outside(i0, end, lo, hi) : 0;
+    return;
+  }
+  for (; there; there &= there - 1) {
+    const int i = i0 + 64 * __builtin_ctzll(there), i1 = min(i + 64, to);
+    *slots += i1 - i;
+    *fixed += outside(i, i1, lo, hi);
+  }
 }
 
 // The digits of a key from the top: 11, 11 and 10 bits.
@@ -99,38 +124,62 @@ __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
   __shared__ uint32_t hist[kBins];
   __shared__ uint32_t sums[kWaves], equals[kWaves], found[2];
   const int h = blockIdx.x, b = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int n = live_slots(a, b), m = min(n, a.budget);
+  const int n = live_slots(a, b);
   int32_t* kept = a.kept + ((int64_t)b * a.kv.heads + h) * a.budget;
   const float* x = a.scores + ((int64_t)b * a.kv.heads + h) * a.slots;
-  if (h == 0 && tid == 0) a.new_len[b] = m;
-  for (int i = m + tid; i < a.budget; i += kThreads) kept[i] = -1;
+  // slots lo .. hi - 1 compete for the places that the sinks and the recent ones leave; where all fit, none does
+  int lo = a.sinks;
+  const int hi = n - a.recent;
   if (n <= a.budget) {
-    for (int i = tid; i < n; i += kThreads) kept[i] = i;
-    return;
+    int gone = 0;
+    for (int i = tid * kPage; i < n; i += kThreads * kPage) {
+      const int32_t p = table_entry(a.kv, b, i / kPage);
+      gone |= p < 0 || p >= a.kv.n_pages;
+    }
+    if (!__syncthreads_or(gone)) {
+      if (h == 0 && tid == 0) a.new_len[b] = n;
+      for (int i = tid; i < a.budget; i += kThreads) kept[i] = i < n ? i : -1;
+      return;
+    }
+    lo = n;
   }
-  // slots lo .. hi - 1 compete for `want` places (the sinks and the recent ones leave room for them)
-  const int lo = a.sinks, hi = n - a.recent;
-  uint32_t want = (uint32_t)(m - a.sinks - a.recent);
   // a wavefront has a strip of its own, 64 slots a step
   const int strip = ((n + kWaves - 1) / kWaves + 63) / 64 * 64;
   const int from = min(wave * strip, n), to = min(from + strip, n);
+  const int32_t entry = entries(a, b, from, kKept, to);
   uint32_t mine[kKept];
 #pragma unroll
   for (int j = 0; j < kKept; ++j) {
     const int i = from + 64 * j + lane;
     mine[j] = i < to ? key_of(x[i]) : 0;
   }
-  // f(slot, key) for the lanes' slots of a strip, all lanes together; a slot past the strip is -1
+  const uint64_t there = pages_there(a, entry);
+  // f(slot, key) for the lanes' slots of a strip that are there, all lanes together; a slot past the strip is -1
   auto every = [&](auto f) {
 #pragma unroll
     for (int j = 0; j < kKept; ++j)
-      if (from + 64 * j < to) {
+      if ((there >> j) & 1) {
         const int i = from + 64 * j + lane;
         f(i < to ? i : -1, mine[j]);
       }
   };
+  int slots = 0, fixed = 0;
+  add_there(there, from, kKept, to, lo, hi, &slots, &fixed);
   for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
+  if (lane == 0) {
+    sums[wave] = (uint32_t)slots;
+    equals[wave] = (uint32_t)fixed;
+  }
   __syncthreads();
+  slots = fixed = 0;
+  for (int w = 0; w < kWaves; ++w) {
+    slots += (int)sums[w];
+    fixed += (int)equals[w];
+  }
+  const int m = min(slots, a.budget);
+  if (h == 0 && tid == 0) a.new_len[b] = m;
+  for (int i = m + tid; i < a.budget; i += kThreads) kept[i] = -1;
+  uint32_t want = (uint32_t)(m - fixed);
   uint32_t prefix = 0;
 #pragma unroll 1
   for (int step = 0; step < 3; ++step) {
@@ -176,16 +225,40 @@ __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
 // What the launches of the parts hand on, a row (sequence and kv head) after the other.
 struct Parts {
   uint32_t* hist;            // [row][3][parts][kBins]
-  uint32_t* state;           // [row][4 + 2 parts]: prefix and want after the first and second digit, then two
-                             // counts a part: kept slots before it by the first digit, by the first two
+  uint32_t* state;           // [row][4 + 4 parts]: prefix and want after the first and second digit, then four counts a
+                             // part: kept slots before it by the first digit, by the first two; its slots that are there,
+                             // those of them that do not compete
   int parts, span;           // slots of a part (whole blocks)
   __device__ uint32_t* hist_of(int64_t row, int step, int part) const { return hist + ((row * 3 + step) * parts + part) * (int64_t)kBins; }
-  __device__ uint32_t* state_of(int64_t row) const { return state + row * (4 + 2 * parts); }
+  __device__ uint32_t* state_of(int64_t row) const { return state + row * (4 + 4 * parts); }
 };
 
+// The slots that are there, those of them that do not compete, and the latter in parts before this one.
+struct There {
+  int slots, fixed, fixed_before;
+};
+__device__ __forceinline__ int wave_sum(int x) {
+  for (int o = 32; o; o >>= 1) x += __shfl_xor(x, o);
+  return x;
+}
+__device__ __forceinline__ int slots_of(const uint32_t* state, int live) {     // of part `lane` (there are at most 64)
+  const int q = threadIdx.x & 63;
+  return q < live ? (int)state[4 + 4 * q + 2] : 0;
+}
+// ... s: slots_of, loaded ahead
+__device__ __forceinline__ There there_of(const Parts& p, const uint32_t* state, int s, int part, int live, int n, int lo, int hi) {
+  const int q = threadIdx.x & 63;
+  if (__all(q >= live || s == min(p.span, n - q * p.span)))
+    return There{n, outside(0, n, lo, hi), outside(0, min(part * p.span, n), lo, hi)};
+  const int f = q < live ? (int)state[4 + 4 * q + 3] : 0;
+  return There{wave_sum(s), wave_sum(f), wave_sum(q < part ? f : 0)};
+}
+
 // The digit number `step` from the parts' histograms; returns how many keys of the parts before this one lie in
-// larger digits, and (for thread 0 .. all) in *same how many in this digit.
-__device__ __forceinline__ uint32_t add_parts(const Parts& p, int64_t row, int step, int part, int live, uint32_t want,
+// larger digits, and (for thread 0 .. all) in *same how many in this digit.  want() is asked for once the histograms are
+// on their way.
+template <typename Want>
+__device__ __forceinline__ uint32_t add_parts(const Parts& p, int64_t row, int step, int part, int live, Want want,
                                               uint32_t* sums, uint32_t* found, uint32_t* shared2, uint32_t* same) {
   const int tid = threadIdx.x, top = kBins - 1 - 2 * tid;
   uint32_t c0 = 0, c1 = 0, b0 = 0, b1 = 0;
@@ -201,7 +274,7 @@ __device__ __forceinline__ uint32_t add_parts(const Parts& p, int64_t row, int s
     }
   }
   if (tid < 2) shared2[tid] = 0;
-  find_digit(c0, c1, sums, found, want);
+  find_digit(c0, c1, sums, found, want());
   const int digit = (int)found[0];
   uint32_t above = (top > digit ? b0 : 0) + (top - 1 > digit ? b1 : 0);
   for (int o = 32; o; o >>= 1) above += (uint32_t)__shfl_down((int)above, o);
@@ -221,13 +294,17 @@ __global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a, Parts p) {
   const int part = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n = live_slots(a, b), live = (n + p.span - 1) / p.span;
-  if (n <= a.budget || part >= live) return;
+  const bool all = n <= a.budget;                   // every slot that is there is kept: only they are counted
+  if ((all && kDigit > 0) || part >= live) return;
   const int64_t row = (int64_t)b * a.kv.heads + h;
   const float* x = a.scores + row * a.slots;
-  const int lo = a.sinks, hi = n - a.recent;
+  uint32_t* state = p.state_of(row);
+  const int lo = all ? n : a.sinks, hi = n - a.recent;
   const int from = part * p.span, to = min(from + p.span, n);
   float y[kStep];
+  int32_t entry;
   auto load = [&](int t) {
+    entry = entries(a, b, t + wave * kStep * 64, kStep, to);
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       const int i = t + (wave * kStep + j) * 64 + lane;
@@ -236,19 +313,26 @@ __global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a, Parts p) {
   };
   load(from);                                       // (on their way while the digit is found)
   for (int i = tid; i < kBins; i += kThreads) hist[i] = 0;
-  uint32_t prefix = 0, want = (uint32_t)(a.budget - a.sinks - a.recent);
+  if (kDigit == 0 && tid < 2) before[tid] = 0;
+  uint32_t prefix = 0, want = 0;
   if constexpr (kDigit > 0) {
-    uint32_t* state = p.state_of(row);
     if constexpr (kDigit > 1) {
       prefix = state[0];
       want = state[1];
     }
+    const int mine = kDigit == 1 ? slots_of(state, live) : 0;
     uint32_t same;
-    const uint32_t above = add_parts(p, row, kDigit - 1, part, live, want, sums, found, before, &same);
+    const uint32_t above = add_parts(p, row, kDigit - 1, part, live, [&] {
+      if constexpr (kDigit == 1) {
+        const There are = there_of(p, state, mine, part, live, n, lo, hi);
+        want = (uint32_t)(min(are.slots, a.budget) - are.fixed);
+      }
+      return want;
+    }, sums, found, before, &same);
     prefix |= found[0] << digit_of(kDigit - 1).shift;
     want -= found[1];
     if (tid == 0) {
-      uint32_t* mine = state + 4 + 2 * part;
+      uint32_t* mine = state + 4 + 4 * part;
       mine[kDigit - 1] = above + (kDigit > 1 ? mine[0] : 0u);
       if (part == 0) {
         state[2 * (kDigit - 1)] = prefix;
@@ -258,16 +342,28 @@ __global__ __launch_bounds__(kThreads) void count_kernel(EvictArgs a, Parts p) {
   }
   __syncthreads();
   const Digit d = digit_of(kDigit);
+  int slots = 0, fixed = 0;
   for (int t = from; t < to; t += kBlock) {
+    const int strip = t + wave * kStep * 64;
     if (t != from) load(t);
+    const uint64_t there = pages_there(a, entry);
+    if (kDigit == 0) add_there(there, strip, kStep, to, lo, hi, &slots, &fixed);
+    if (all) continue;
 #pragma unroll
-    for (int j = 0; j < kStep; ++j) {
-      const int i = t + (wave * kStep + j) * 64 + lane;
-      const uint32_t k = key_of(y[j]);
-      count_digit(hist, i < to && i >= lo && i < hi && d.shares(k, prefix), d.of(k));
-    }
+    for (int j = 0; j < kStep; ++j)
+      if ((there >> j) & 1) {
+        const int i = strip + j * 64 + lane;
+        const uint32_t k = key_of(y[j]);
+        count_digit(hist, i < to && i >= lo && i < hi && d.shares(k, prefix), d.of(k));
+      }
+  }
+  if (kDigit == 0 && lane == 0) {
+    atomicAdd(&before[0], (uint32_t)slots);
+    atomicAdd(&before[1], (uint32_t)fixed);
   }
   __syncthreads();
+  if (kDigit == 0 && tid < 2) state[4 + 4 * part + 2 + tid] = before[tid];
+  if (all) return;
   uint32_t* out = p.hist_of(row, kDigit, part);
   for (int i = tid; i < kBins; i += kThreads) out[i] = hist[i];
 }
@@ -277,20 +373,19 @@ __global__ __launch_bounds__(kThreads) void list_kernel(EvictArgs a, Parts p) {
   __shared__ uint32_t sums[kWaves], equals[kWaves], found[2], before[2];
   const int part = blockIdx.x, h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n = live_slots(a, b), live = (n + p.span - 1) / p.span, m = min(n, a.budget);
+  const int n = live_slots(a, b), live = (n + p.span - 1) / p.span;
+  const bool all = n <= a.budget;
   const int64_t row = (int64_t)b * a.kv.heads + h;
   int32_t* kept = a.kept + row * a.budget;
-  if (part == 0 && h == 0 && tid == 0) a.new_len[b] = m;
-  if (n <= a.budget) {
-    for (int i = part * kThreads + tid; i < a.budget; i += p.parts * kThreads) kept[i] = i < n ? i : -1;
-    return;
-  }
-  if (part >= live) return;
+  const uint32_t* state = p.state_of(row);
+  const int lo = all ? n : a.sinks, hi = n - a.recent;
+  const int mine = slots_of(state, live);
   const float* x = a.scores + row * a.slots;
-  const int lo = a.sinks, hi = n - a.recent;
   const int from = part * p.span, to = min(from + p.span, n);
   float y[kStep];
+  int32_t entry;
   auto load = [&](int t) {
+    entry = entries(a, b, t + wave * kStep * 64, kStep, to);
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       const int i = t + (wave * kStep + j) * 64 + lane;
@@ -298,23 +393,34 @@ __global__ __launch_bounds__(kThreads) void list_kernel(EvictArgs a, Parts p) {
     }
   };
   load(from);                                       // (on their way while the digit is found)
-  const uint32_t* state = p.state_of(row);
-  uint32_t prefix = state[2], want = state[3], eq;
-  uint32_t at = add_parts(p, row, 2, part, live, want, sums, found, before, &eq) + state[4 + 2 * part + 1];
-  prefix |= found[0];
-  want -= found[1];
   // places taken before this part: larger keys, the first `want` equal ones, the sinks and the recent ones
-  at += min(eq, want) + (uint32_t)(min(from, lo) + max(from - hi, 0));
+  uint32_t at = 0, prefix = 0, want = 0, eq = 0;
+  if (!all && part < live) {
+    prefix = state[2];
+    want = state[3];
+    at = add_parts(p, row, 2, part, live, [&] { return want; }, sums, found, before, &eq) + state[4 + 4 * part + 1];
+    prefix |= found[0];
+    want -= found[1];
+    at += min(eq, want);
+  }
+  const There are = there_of(p, state, mine, part, live, n, lo, hi);
+  at += (uint32_t)are.fixed_before;
+  const int m = min(are.slots, a.budget);
+  const bool as_is = all && m == n;                 // every old slot, in its place
+  if (part == 0 && h == 0 && tid == 0) a.new_len[b] = m;
+  for (int i = (as_is ? 0 : m) + part * kThreads + tid; i < a.budget; i += p.parts * kThreads) kept[i] = i < m ? i : -1;
+  if (as_is || part >= live) return;
   const uint64_t below = (1ull << lane) - 1;
   for (int t = from; t < to; t += kBlock) {
     const int strip = t + wave * kStep * 64;
     if (t != from) load(t);
+    const uint64_t there = pages_there(a, entry);
     int kind[kStep];
     uint32_t na = 0, ne = 0;
 #pragma unroll
     for (int j = 0; j < kStep; ++j) {
       const int i = strip + j * 64 + lane;
-      kind[j] = kind_of(i < to ? i : -1, key_of(y[j]), lo, hi, prefix);
+      kind[j] = (there >> j) & 1 ? kind_of(i < to ? i : -1, key_of(y[j]), lo, hi, prefix) : 0;
       na += __popcll(__ballot(kind[j] == 2));
       ne += __popcll(__ballot(kind[j] == 1));
     }
@@ -419,7 +525,7 @@ size_t evict_workspace_bytes(const PagedKV& kv, int32_t B, int64_t slots) {
   const int64_t most = most_slots(kv, slots);
   if (most <= kHeld * kThreads) return 0;
   const int64_t parts = (most + span_of(most) - 1) / span_of(most);
-  return (size_t)B * kv.heads * (3 * parts * kBins + 4 + 2 * parts) * 4;
+  return (size_t)B * kv.heads * (3 * parts * kBins + 4 + 4 * parts) * 4;
 }
 
 hipError_t launch_cache_evict(const EvictArgs& a, void* workspace, hipStream_t stream) {
