@@ -368,7 +368,7 @@ caddtree_status_t caddtree_window_attention(const caddtree_attention_t* a, void*
 caddtree_status_t caddtree_cache_attention(const caddtree_cache_t* cache, const caddtree_attention_t* a,
                                            void* workspace, size_t workspace_bytes, hipStream_t stream);
 
-/* HOST only: the workspace of the two calls above (0 where none is of use). */
+/* HOST only: the workspace of the two calls above (0 where none is of use, or for sizes that they refuse). */
 size_t caddtree_attention_workspace_bytes(const caddtree_attention_t* a);
 
 /* Puts the first count[b] (NULL: T) of T new tokens of each sequence into the slots from start[b] on,

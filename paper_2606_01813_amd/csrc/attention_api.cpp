@@ -76,8 +76,8 @@ PagedKV paged(const caddtree_cache_t* c, const int32_t* table, int32_t pages) {
                  (int32_t)CADDTREE_PAGE_BYTES(c->head_dim)};
 }
 
-// What every attention call and the scores share; the tensors that a call reads are checked by it.
-caddtree_status_t check_attention(const caddtree_attention_t* a, const caddtree_cache_t* cache) {
+// The sizes of a call, which its workspace depends on.
+caddtree_status_t check_sizes(const caddtree_attention_t* a) {
   if (a == nullptr) return fail(CADDTREE_E_INVALID, "the attention arguments are NULL");
   caddtree_status_t st = check_type(enum_value(a->dtype), a->head_dim);
   if (st != CADDTREE_OK) return st;
@@ -91,9 +91,16 @@ caddtree_status_t check_attention(const caddtree_attention_t* a, const caddtree_
   // (workgroups are numbered in 31 bits: one for 128 rows, or for 8 kv heads at least)
   if (((int64_t)a->T * (a->n_heads / a->n_kv_heads) / 128 + 1) * ((int64_t)a->B * a->n_kv_heads + 8) > kMaxTokens)
     return fail(CADDTREE_E_UNSUPPORTED, "more than 2^30 workgroups of 128 rows in a call");
-  if (!std::isfinite(a->scale)) return fail(CADDTREE_E_INVALID, "scale must be finite");
   if (a->window < 0 || a->sinks < 0)
     return fail(CADDTREE_E_INVALID, "window = %d and sinks = %d must not be negative", a->window, a->sinks);
+  return CADDTREE_OK;
+}
+
+// What every attention call and the scores share; the tensors that a call reads are checked by it.
+caddtree_status_t check_attention(const caddtree_attention_t* a, const caddtree_cache_t* cache) {
+  caddtree_status_t st = check_sizes(a);
+  if (st != CADDTREE_OK) return st;
+  if (!std::isfinite(a->scale)) return fail(CADDTREE_E_INVALID, "scale must be finite");
   const int order = enum_value(a->order), mask = enum_value(a->mask_kind);
   if (order != CADDTREE_ORDER_CHAIN && order != CADDTREE_ORDER_BLOCK && order != CADDTREE_ORDER_TREE)
     return fail(CADDTREE_E_INVALID, "unknown order %d", order);
@@ -214,7 +221,8 @@ caddtree_status_t run_attention(const caddtree_attention_t* a, const caddtree_ca
 extern "C" {
 
 size_t caddtree_attention_workspace_bytes(const caddtree_attention_t* a) {
-  if (a == nullptr || a->B <= 0 || a->T <= 0 || a->n_kv_heads < 1 || a->n_heads < 1 || a->head_dim < 1 || a->S < 0 || a->table_pages < 0) return 0;
+  if (check_sizes(a) != CADDTREE_OK || a->B == 0 || a->T == 0) return 0;
+  if (a->table_pages < 0 || (int64_t)a->table_pages * CADDTREE_PAGE > kMaxTokens) return 0;
   return split_bytes(a, splits_of(a));
 }
 

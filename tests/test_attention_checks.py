@@ -360,3 +360,19 @@ def test_workspace_sizes():
     assert size(B=64, T=2048, S=4096, n_heads=32, n_kv_heads=8, table_pages=0) == 0
     one = size(B=1, T=1, S=1, n_heads=8, n_kv_heads=8, table_pages=2048)
     assert 0 < one <= 8 * 128 * (64 * 4 + 8) + 256
+
+
+def test_workspace_of_sizes_that_are_refused():
+    """A query of sizes that no call takes returns 0, as the call returns its error."""
+    lib = _lib.lib()
+    good = dict(B=1, T=1, S=4096, n_heads=8, n_kv_heads=4, table_pages=0)
+    size = lambda **kw: lib.caddtree_attention_workspace_bytes(ctypes.byref(_attention(**dict(good, **kw))))
+    assert size() > 0 and size(window=2 ** 31 - 1, sinks=2 ** 31 - 1) > 0 and size(window=1000) > 0
+    for kw in (dict(n_heads=2), dict(n_heads=2, window=10), dict(n_heads=0), dict(n_heads=10), dict(n_kv_heads=0), dict(n_kv_heads=-4),
+               dict(n_heads=-8), dict(head_dim=96), dict(head_dim=-64), dict(dtype=0), dict(dtype=7), dict(B=-1), dict(B=65536),
+               dict(T=-1), dict(T=2 ** 31 - 1), dict(S=-1), dict(S=2 ** 31 - 1), dict(window=-1), dict(sinks=-1), dict(n_heads=2 ** 17),
+               dict(table_pages=-1), dict(table_pages=2 ** 25), dict(B=65535, T=2 ** 29)):
+        assert size(**kw) == 0, kw
+        if "table_pages" not in kw:
+            a = _attention(**dict(good, **kw))
+            assert lib.caddtree_window_attention(ctypes.byref(a), None, 0, None) in (INVALID, UNSUPPORTED), kw
