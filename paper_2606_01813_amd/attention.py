@@ -105,6 +105,19 @@ def _tensor(name: str, t, dtype, device: int):
         raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
 
 
+def _int32(name: str, n) -> int:
+    """n as the 32-bit integer that the library takes: a larger one would lose its upper bits on the way."""
+    i = int(n)
+    if i != n or not -2 ** 31 <= i < 2 ** 31:
+        raise ValueError(f"{name} must be an integer below 2^31, got {n}")
+    return i
+
+
+def _sizes(name: str, t) -> None:
+    if any(n >= 2 ** 31 for n in t.shape):
+        raise ValueError(f"{name} must have sizes below 2^31, got {tuple(t.shape)}")
+
+
 def _array(name: str, t, dtype, shape, device: int) -> int:
     """The pointer of a contiguous tensor of exactly this shape (None in a place: any size)."""
     _tensor(name, t, dtype, device)
@@ -112,6 +125,7 @@ def _array(name: str, t, dtype, shape, device: int) -> int:
         raise ValueError(f"{name} must have shape {tuple('any' if w is None else w for w in shape)}, got {tuple(t.shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+    _sizes(name, t)
     return t.data_ptr()
 
 
@@ -120,6 +134,7 @@ def _view(name: str, t, dtype, shape, device: int) -> _lib.View:
     _tensor(name, t, dtype, device)
     if t.dim() != 4 or any(w is not None and w != g for w, g in zip(shape, t.shape)):
         raise ValueError(f"{name} must have shape {tuple('any' if w is None else w for w in shape)}, got {tuple(t.shape)}")
+    _sizes(name, t)
     sb, st, sh, sd = t.stride()
     n = t.shape
     sb, st, sh = (s if m > 1 else 0 for s, m in zip((sb, st, sh), n))     # the stride of one element is free
@@ -194,7 +209,7 @@ def window_attention(q, k, v, *, window: int = 0, sinks: int = 0, causal: bool =
     a.k = _view("k", k, q.dtype, shape, device)
     a.v = _view("v", v, q.dtype, shape, device)
     a.S, a.n_kv_heads = shape[1], shape[2]
-    a.scale, a.window, a.sinks = _scale(scale, a.head_dim), int(window), int(sinks)
+    a.scale, a.window, a.sinks = _scale(scale, a.head_dim), _int32("window", window), _int32("sinks", sinks)
     a.order = _lib.ORDERS["chain" if causal else "block"]
     if q_len is not None:
         a.q_len = _array("q_len", q_len, torch.int32, (a.B,), device)
@@ -211,6 +226,9 @@ def attention_workspace(q, k=None, cache: Optional["KVCache"] = None, page_table
     page_table (uint8, as large as any call of these shapes uses; the contents do not matter)."""
     torch = _torch()
     a = _lib.Attention()
+    for name, t in (("q", q), ("k", k), ("page_table", page_table)):
+        if t is not None:
+            _sizes(name, t)
     a.B, a.T, a.n_heads, a.head_dim = q.shape
     a.dtype = _lib.ATTENTION_DTYPES[_dtype_name(q.dtype)]
     if cache is not None:
@@ -234,7 +252,7 @@ class KVCache:
         torch = _torch()
         if dtype not in _lib.ATTENTION_DTYPES:
             raise ValueError(f"dtype must be one of {sorted(_lib.ATTENTION_DTYPES)}")
-        self.n_kv_heads, self.head_dim, self.dtype = int(n_kv_heads), int(head_dim), dtype
+        self.n_kv_heads, self.head_dim, self.dtype = _int32("n_kv_heads", n_kv_heads), _int32("head_dim", head_dim), dtype
         self.torch_dtype = torch.bfloat16 if dtype == "bf16" else torch.float16
         self.page_bytes = 68 * self.head_dim
         if pages is None:
@@ -324,7 +342,7 @@ class KVCache:
             a.depth = _array("depth", depth, torch.int32, (a.B, None), device)
             a.cap = depth.shape[1]
             a.order = _lib.ORDERS["tree"]
-        a.scale, a.window, a.sinks = _scale(scale, a.head_dim), int(window), int(sinks)
+        a.scale, a.window, a.sinks = _scale(scale, a.head_dim), _int32("window", window), _int32("sinks", sinks)
         return a
 
     def attention(self, q, page_table, ctx_len, k=None, v=None, *, count=None, causal: bool = True, mask=None, depth=None,
@@ -419,7 +437,7 @@ class KVCache:
         f32 = torch.float32
         args = (_array("ctx_len", ctx_len, torch.int64, (B,), device),
                 _array("scores", scores, f32, (B, self.n_kv_heads, None), device), int(scores.shape[2]),
-                int(budget), int(sinks), int(recent), new, new_pages,
+                _int32("budget", budget), _int32("sinks", sinks), _int32("recent", recent), new, new_pages,
                 _array("new_scores", new_scores, f32, (B, self.n_kv_heads, None), device), int(new_scores.shape[2]),
                 _array("new_len", new_len, torch.int64, (B,), device),
                 _array("kept", kept, torch.int32, (B, self.n_kv_heads, int(budget)), device))

@@ -376,3 +376,42 @@ def test_workspace_of_sizes_that_are_refused():
         if "table_pages" not in kw:
             a = _attention(**dict(good, **kw))
             assert lib.caddtree_window_attention(ctypes.byref(a), None, 0, None) in (INVALID, UNSUPPORTED), kw
+
+
+INTEGERS = [("window", "window"), ("window", "sinks"), ("tree", "window"), ("tree", "sinks"), ("score", "window"), ("score", "sinks"),
+            ("evict", "budget"), ("evict", "sinks"), ("evict", "recent")]
+
+
+@pytest.mark.parametrize("native", [False, True], ids=["python", "native"])
+@pytest.mark.parametrize("name,arg", INTEGERS, ids=["-".join(x) for x in INTEGERS])
+def test_integers_keep_all_their_bits(name, arg, native, rec, monkeypatch):
+    """What does not fit 32 bits is refused; ctypes would pass on its lower half."""
+    ops = rec.ops()
+    if native:
+        monkeypatch.setattr(attention, "_native", lambda stream: (_lib.binding(), ops, 0, STREAM))
+    for n in (2 ** 31, 2 ** 32, 2 ** 32 + 5, 2 ** 64 + 80, -2 ** 32 + 3, 2.5, np.int64(2 ** 33 + 1)):
+        s = _state()
+        s[arg] = n
+        with pytest.raises(ValueError, match=arg):
+            CALLS[name][0](_cache(), s)
+        assert not rec.calls, n
+    s = _state()
+    s[arg] = np.int64(s[arg])
+    CALLS[name][0](_cache(), s)
+    assert rec.calls
+
+
+def test_sizes_keep_all_their_bits(rec):
+    """Inputs may repeat (stride 0), so a tensor's sizes can pass 32 bits in little memory."""
+    s = _state()
+    far = lambda *dims: _aligned((1,) * (len(dims) - 1) + (dims[-1],), BF).expand(dims)
+    s["k"] = s["v"] = far(B, 2 ** 32 + T, Hkv, D)
+    with pytest.raises(ValueError, match="sizes below"):
+        CALLS["window"][0](None, s)
+    with pytest.raises(ValueError, match="sizes below"):
+        attention_workspace(s["q"], s["k"])
+    with pytest.raises(ValueError, match="sizes below"):
+        CALLS["write"][0](_cache(), s)
+    with pytest.raises(ValueError, match="n_kv_heads"):
+        KVCache(2 ** 32 + 1, D, pages=torch.zeros((0, 2 ** 32 + 1, 68 * D), dtype=torch.uint8))
+    assert not rec.calls
