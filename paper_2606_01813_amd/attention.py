@@ -262,10 +262,15 @@ class KVCache:
         elif not isinstance(pages, torch.Tensor) or pages.dtype != torch.uint8 or not pages.is_contiguous() or \
                 pages.dim() != 3 or tuple(pages.shape[1:]) != (self.n_kv_heads, self.page_bytes):
             raise ValueError(f"pages must be a contiguous uint8 tensor [num_pages, {self.n_kv_heads}, {self.page_bytes}]")
-        self.pages = pages
+        self._pages = pages
         self._device = pages.device.index if pages.is_cuda else -1
         self._c = _lib.Cache(_lib.ATTENTION_DTYPES[dtype], self.n_kv_heads, self.head_dim, pages.shape[0], pages.data_ptr())
         self._at = ctypes.addressof(self._c)
+
+    @property
+    def pages(self):
+        """The cache's memory.  (Not to be replaced: calls go to the address of the tensor that it was made with.)"""
+        return self._pages
 
     def _native(self, stream):
         """As the module's _native, and the address of the cache's description."""

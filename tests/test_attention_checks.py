@@ -415,3 +415,11 @@ def test_sizes_keep_all_their_bits(rec):
     with pytest.raises(ValueError, match="n_kv_heads"):
         KVCache(2 ** 32 + 1, D, pages=torch.zeros((0, 2 ** 32 + 1, 68 * D), dtype=torch.uint8))
     assert not rec.calls
+
+
+def test_the_pages_of_a_cache_are_not_replaced():
+    c = _cache()
+    first, at = c.pages, c._c.pages
+    with pytest.raises(AttributeError):
+        c.pages = _aligned((20, Hkv, 68 * D), torch.uint8)
+    assert c.pages is first and c._c.pages == at == first.data_ptr()
