@@ -13,7 +13,8 @@ and each sees the cached context, the root, its ancestors and itself.
     cache.evict(table, ctx_len, scores, new_table, new_len, new_scores, kept, budget=2048, sinks=4, recent=256)
 
 Every call checks its tensors, then enqueues kernels on the stream (default: torch's current one) and
-returns; lengths and page tables stay on the device.  include/caddtree.h states what is computed.
+returns; lengths and page tables stay on the device.  include/caddtree.h states what is computed.  Nothing here has
+a backward pass: queries, keys and values that require a gradient are refused while gradients are recorded.
 
 As a plan's calls do, these go to the native binding first, which checks the tensors and calls the library
 (about 2 us of host time where the checks here take 10 to 15); what it cannot vouch for comes back as None
@@ -93,6 +94,15 @@ def _made(q, out, stream):
         raise ValueError("out is required with a raw stream handle")
     with torch.cuda.stream(stream):
         return torch.zeros(q.shape, dtype=q.dtype, device=q.device)
+
+
+def _no_gradient(**inputs) -> None:
+    torch = _torch()
+    if torch.is_grad_enabled():
+        for name, t in inputs.items():
+            if isinstance(t, torch.Tensor) and t.requires_grad:
+                raise ValueError(f"{name} requires a gradient, and attention has no backward pass: call it under "
+                                 f"torch.no_grad(), or detach {name}")
 
 
 def _tensor(name: str, t, dtype, device: int):
@@ -200,6 +210,7 @@ def window_attention(q, k, v, *, window: int = 0, sinks: int = 0, causal: bool =
         binding, ops, device, raw = native
         if _done(binding.window_attention(ops, device, raw, q, k, v, window, sinks, causal, scale, q_len, k_len, out, lse, workspace)):
             return out
+    _no_gradient(q=q, k=k, v=v)
     torch = _torch()
     device = _device()
     a, _ = _queries(q, device)
@@ -366,6 +377,7 @@ class KVCache:
             if _done(binding.cache_attention(ops, device, raw, self._at, q, page_table, ctx_len, k, v, count, causal, mask, depth,
                                              window, sinks, scale, out, lse, workspace)):
                 return out
+        _no_gradient(q=q, k=k, v=v)
         torch = _torch()
         device = self._on()
         if (mask is None) != (depth is None) and k is not None:

@@ -9,6 +9,7 @@
 // caller takes the Python path, which decides (and raises) as it always did.  Nothing is kept from one
 // call to the next.
 #define PY_SSIZE_T_CLEAN
+#include <c10/core/GradMode.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -498,6 +499,13 @@ struct Attn {
     return v;
   }
 
+  // attention has no backward pass: an input that wants one is the Python path's to refuse
+  void no_gradient(PyObject* o) {
+    if (!c10::GradMode::is_enabled()) return;
+    const c10::TensorImpl* t = tensor(o);
+    if (t != nullptr && t->requires_grad()) ok = false;
+  }
+
   int64_t integer(PyObject* o, int64_t lo, int64_t hi) {
     int over = 0;
     const long long v = PyLong_CheckExact(o) ? PyLong_AsLongLongAndOverflow(o, &over) : lo - 1;
@@ -628,6 +636,7 @@ PyObject* py_window_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
     a.lse = as<float>(c.array(p[13], c10::kFloat, {a.B, a.T, a.n_heads}, false));
     size_t bytes;
     void* ws = c.workspace(p[14], &bytes);
+    for (int i = 3; i < 6; ++i) c.no_gradient(p[i]);
     if (!c.ok) return -1;
     return unlocked([&] { return s.window(&a, ws, bytes, st); });
   });
@@ -669,6 +678,11 @@ PyObject* py_cache_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
     a.lse = as<float>(c.array(p[17], c10::kFloat, {a.B, a.T, a.n_heads}, false));
     size_t bytes;
     void* ws = c.workspace(p[18], &bytes);
+    c.no_gradient(p[4]);
+    if (keys) {
+      c.no_gradient(p[7]);
+      c.no_gradient(p[8]);
+    }
     if (!c.ok) return -1;
     return unlocked([&] { return s.attention(cache, &a, ws, bytes, st); });
   });

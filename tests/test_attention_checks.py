@@ -423,3 +423,31 @@ def test_the_pages_of_a_cache_are_not_replaced():
     with pytest.raises(AttributeError):
         c.pages = _aligned((20, Hkv, 68 * D), torch.uint8)
     assert c.pages is first and c._c.pages == at == first.data_ptr()
+
+
+@pytest.mark.parametrize("native", [False, True], ids=["python", "native"])
+@pytest.mark.parametrize("name", ["window", "tree", "chain"])
+def test_inputs_that_require_a_gradient(name, native, rec, monkeypatch):
+    """There is no backward pass: such inputs are refused, and taken where no gradient is recorded."""
+    ops = rec.ops()
+    if native:
+        monkeypatch.setattr(attention, "_native", lambda stream: (_lib.binding(), ops, 0, STREAM))
+    for arg in "qkv":
+        s = _state()
+        s[arg].requires_grad_()
+        with pytest.raises(ValueError, match=f"{arg} requires a gradient"):
+            CALLS[name][0](_cache(), s)
+        assert not rec.calls
+        for mode in (torch.no_grad, torch.inference_mode):
+            with mode():
+                CALLS[name][0](_cache(), s)
+            assert rec.calls
+            rec.calls.clear()
+    # what is written to a cache, or weighed, has no gradient to lose
+    s = _state()
+    for arg in "qkv":
+        s[arg].requires_grad_()
+    for other in ("write", "score"):
+        CALLS[other][0](_cache(), s)
+        assert rec.calls
+        rec.calls.clear()
