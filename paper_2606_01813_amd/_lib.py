@@ -12,7 +12,6 @@ OK, E_INVALID, E_UNSUPPORTED, E_COST, E_WORKSPACE, E_HIP = range(6)
 DTYPES = {"f32": 0, "bf16": 1}
 ATTENTION_DTYPES = {"bf16": 1, "f16": 2}
 ORDERS = {"chain": 0, "block": 1, "tree": 2}
-PAGE, KV_BLOCK = 64, 32
 MASKS = {"none": 0, "u8": 1, "bits": 2}
 ALLOW_NONCONVEX = 1
 FIXED_BUDGET = 2

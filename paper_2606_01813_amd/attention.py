@@ -28,7 +28,6 @@ import math
 from typing import Optional
 
 from . import _lib
-from ._lib import PAGE
 
 __all__ = ["KVCache", "window_attention", "attention_workspace"]
 

@@ -103,15 +103,6 @@ __device__ inline int step(const AttnArgs& a, int b, int i) {
 __device__ inline bool in_window(const AttnArgs& a, int pos_q, int pos_k) {
   return a.window == 0 || pos_q - pos_k < a.window || pos_k < a.sinks;
 }
-// a tree's mask: query i >= 1 and new key j >= 1 are nodes i - 1 and j - 1
-__device__ inline bool tree_sees(const AttnArgs& a, int b, int i, int j) {
-  if (j == 0) return true;
-  if (i == 0) return false;
-  if (a.mask_kind == CADDTREE_MASK_U8)
-    return static_cast<const uint8_t*>(a.mask)[((int64_t)b * a.cap + i - 1) * a.cap + j - 1] != 0;
-  const int words = (a.cap + 31) / 32;
-  return (static_cast<const uint32_t*>(a.mask)[((int64_t)b * a.cap + i - 1) * words + (j - 1) / 32] >> ((j - 1) % 32)) & 1;
-}
 
 // The page of a slot and kv head: null where the table names no page of the cache.
 __device__ inline uint8_t* page_of(const PagedKV& kv, int b, int page, int h) {

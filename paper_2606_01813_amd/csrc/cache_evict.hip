@@ -48,7 +48,7 @@ __device__ __forceinline__ int outside(int i0, int i1, int lo, int hi) { return 
 // Adds the slots from i0 on that are there to *slots, and those of them that do not compete to *fixed.
 __device__ __forceinline__ void add_there(uint64_t there, int i0, int steps, int to, int lo, int hi, int* slots, int* fixed) {
   const int end = min(i0 + 64 * steps, to), n = max(0, (end - i0 + 63) / 64);
-  if (__popcll(there) == n) {
+  if ((int)__popcll(there) == n) {
     *slots += max(0, end - i0);
     *fixed += n ? outside(i0, end, lo, hi) : 0;
     return;
