@@ -395,7 +395,8 @@ caddtree_status_t caddtree_cache_read(const caddtree_cache_t* cache, const caddt
  * of the caddtree_cache_attention call (q, lse as it wrote it, lengths, scale, window, sinks, order;
  * k, v, out and the mask are not used).  weight [B, T] (NULL: 1) picks and weighs queries; one at or
  * below 0 leaves its query out.  scores, new_scores [B, n_kv_heads, slots], slots >= the longest
- * ctx_len's, may be one array.  The order of the sums is fixed. */
+ * ctx_len's, may be one array (else they do not overlap: CADDTREE_E_INVALID).  The order of the sums is
+ * fixed. */
 caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const caddtree_attention_t* a, const float* weight,
                                        const float* scores, float* new_scores, int64_t slots, hipStream_t stream);
 

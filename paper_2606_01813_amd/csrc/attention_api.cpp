@@ -306,6 +306,11 @@ caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const cadd
   if (a->B == 0 || slots == 0) return ok();
   if (a->T > 0 && a->lse == nullptr) return fail(CADDTREE_E_INVALID, "lse is NULL");
   if (scores == nullptr || new_scores == nullptr) return fail(CADDTREE_E_INVALID, "scores and new_scores are required");
+  if (new_scores != scores) {
+    const size_t bytes = (size_t)a->B * a->n_kv_heads * slots * 4;
+    const Array arrays[] = {{"scores", scores, bytes, false}, {"new_scores", new_scores, bytes, true}};
+    if ((st = check_apart(arrays)) != CADDTREE_OK) return st;
+  }
   caddtree::ScoreArgs s = {args_of(a, cache), weight, scores, new_scores, slots};
   const hipError_t e = caddtree::launch_cache_score(s, (caddtree_dtype_t)enum_value(a->dtype), a->head_dim, stream);
   return e == hipSuccess ? ok() : hip_fail(e, "cache score launch");

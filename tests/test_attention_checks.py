@@ -451,3 +451,12 @@ def test_inputs_that_require_a_gradient(name, native, rec, monkeypatch):
         CALLS[other][0](_cache(), s)
         assert rec.calls
         rec.calls.clear()
+
+
+def test_scores_that_overlap_in_part():
+    """One array or two that are apart: a score read after another's new one was written would be wrong."""
+    lib, c, a, r = _lib.lib(), _c_cache(), _attention(), ctypes.byref
+    size = 2 * 2 * 100 * 4                                # of the scores
+    for off in (4, 400, size - 4, -4, 4 - size):
+        assert lib.caddtree_cache_score(r(c), r(a), None, 0x10000, 0x10000 + off, 100, None) == INVALID, off
+        assert b"overlap" in lib.caddtree_last_error()
