@@ -383,8 +383,9 @@ caddtree_status_t caddtree_cache_write(const caddtree_cache_t* cache, const cadd
                                        hipStream_t stream);
 
 /* The values that slots start[b] (NULL: 0) .. end[b] - 1 stand for, at most T of them, in the cache's
- * type: slot start + j into k[b, j] and v[b, j].  Rows past the end, and those of pages outside the
- * cache, are left untouched. */
+ * type: slot start + j into k[b, j] and v[b, j], views that share no element (CADDTREE_E_INVALID where
+ * they begin in one place).  Rows past the end, and those of pages outside the cache, are left
+ * untouched. */
 caddtree_status_t caddtree_cache_read(const caddtree_cache_t* cache, const caddtree_view_t* k, const caddtree_view_t* v,
                                       int32_t B, int32_t T, const int64_t* start, const int64_t* end,
                                       const int32_t* page_table, int32_t table_pages, hipStream_t stream);

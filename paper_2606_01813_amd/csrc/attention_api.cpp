@@ -292,6 +292,7 @@ caddtree_status_t caddtree_cache_read(const caddtree_cache_t* cache, const caddt
   if ((st = check_view("v", *v, some)) != CADDTREE_OK) return st;
   if (B > 0 && end == nullptr) return fail(CADDTREE_E_INVALID, "end is NULL");
   if (!some) return ok();
+  if (k->data == v->data) return fail(CADDTREE_E_INVALID, "k and v are written, and both begin in one place");
   caddtree::CacheMoveArgs a = {view(*k), view(*v), paged(cache, page_table, table_pages), start, end, nullptr, nullptr, B, T, T};
   const hipError_t e = caddtree::launch_cache_read(a, (caddtree_dtype_t)enum_value(cache->dtype), cache->head_dim, stream);
   return e == hipSuccess ? ok() : hip_fail(e, "cache read launch");

@@ -460,3 +460,9 @@ def test_scores_that_overlap_in_part():
     for off in (4, 400, size - 4, -4, 4 - size):
         assert lib.caddtree_cache_score(r(c), r(a), None, 0x10000, 0x10000 + off, 100, None) == INVALID, off
         assert b"overlap" in lib.caddtree_last_error()
+
+
+def test_keys_and_values_are_not_read_into_one_place():
+    lib, c, v, r = _lib.lib(), _c_cache(), _lib.View(0x1000, 640, 128, 64), ctypes.byref
+    assert lib.caddtree_cache_read(r(c), r(v), r(v), 2, 5, None, 0x1000, 0x1000, 3, None) == INVALID
+    assert b"one place" in lib.caddtree_last_error()
