@@ -341,7 +341,7 @@ typedef struct {
   float* lse;                   /* [B, T, n_heads], optional */
   const int32_t* q_len;         /* [B], optional (NULL: T).  With a tree: its nodes, n_star, to which the root is added */
   const int32_t* k_len;         /* [B], optional (NULL: S); not used with a cache */
-  float scale;
+  float scale;                  /* finite, at most 2^127 in magnitude */
   int32_t window, sinks;        /* >= 0; window 0: no window */
   caddtree_order_t order;
   caddtree_mask_t mask_kind;    /* with ORDER_TREE: U8 or BITS32, as written by caddtree_build */

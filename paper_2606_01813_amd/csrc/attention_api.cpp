@@ -101,6 +101,8 @@ caddtree_status_t check_attention(const caddtree_attention_t* a, const caddtree_
   caddtree_status_t st = check_sizes(a);
   if (st != CADDTREE_OK) return st;
   if (!std::isfinite(a->scale)) return fail(CADDTREE_E_INVALID, "scale must be finite");
+  if (std::fabs(a->scale) > 0x1p127f)               // (its product with log2(e) is a float)
+    return fail(CADDTREE_E_UNSUPPORTED, "scale = %g: more than 2^127 in magnitude is not supported", a->scale);
   const int order = enum_value(a->order), mask = enum_value(a->mask_kind);
   if (order != CADDTREE_ORDER_CHAIN && order != CADDTREE_ORDER_BLOCK && order != CADDTREE_ORDER_TREE)
     return fail(CADDTREE_E_INVALID, "unknown order %d", order);

@@ -39,8 +39,9 @@ constexpr float kLag = 8.f;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // Scores are kept unscaled, so that a weight is one fused multiply-add and one exp2: exp2(s c - base) with
-// c > 0.  A negative scale goes into the signs of q, and a scale of zero is one too small to matter.
-__device__ inline float score_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-30f); }
+// c > 0 (-inf c has to be -inf).  A negative scale goes into the signs of q, and a scale of zero is the smallest normal
+// number: products s of bf16 inputs may be as large as the largest one.
+__device__ inline float score_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 0x1p-126f); }
 __device__ inline u32x4 signed_queries(u32x4 q, float scale) {
   const uint32_t flip = scale < 0.f ? 0x80008000u : 0u;
   return u32x4{q[0] ^ flip, q[1] ^ flip, q[2] ^ flip, q[3] ^ flip};

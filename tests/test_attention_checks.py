@@ -466,3 +466,14 @@ def test_keys_and_values_are_not_read_into_one_place():
     lib, c, v, r = _lib.lib(), _c_cache(), _lib.View(0x1000, 640, 128, 64), ctypes.byref
     assert lib.caddtree_cache_read(r(c), r(v), r(v), 2, 5, None, 0x1000, 0x1000, 3, None) == INVALID
     assert b"one place" in lib.caddtree_last_error()
+
+
+def test_scales_at_the_limit():
+    lib, c, r = _lib.lib(), _c_cache(), ctypes.byref
+    for scale in (2.0 ** 127 * 1.001, -3e38):
+        a = _attention(scale=scale)
+        assert lib.caddtree_window_attention(r(a), None, 0, None) == UNSUPPORTED
+        assert lib.caddtree_cache_attention(r(c), r(a), None, 0, None) == UNSUPPORTED
+        assert lib.caddtree_cache_score(r(c), r(a), None, 0x1000, 0x1000, 100, None) == UNSUPPORTED
+    a = _attention(B=0, scale=2.0 ** 127)                 # taken: a call of nothing
+    assert lib.caddtree_window_attention(r(a), None, 0, None) == _lib.OK

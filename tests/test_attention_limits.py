@@ -70,3 +70,22 @@ def test_scores_through_windows_past_every_key(T):
         f.cache.score(q, f.table, i64(f.ctx), lse, old, got, window=window, sinks=1)
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_scales_and_inputs_that_cancel(T):
+    """Powers of two moved between the scale and the inputs change nothing, as far as the products stay finite."""
+    q, k, v = make((1, T, 4, 64), BF, 1), make((1, 200, 2, 64), BF, 2), make((1, 200, 2, 64), BF, 3)
+    want, wl = windowed(q, k, v, None, None, 0, 0, True, scale=0.125)
+    check(ref.window_reference(q, k, v, 0, 0, True, 0.125, [T], [200]), want, wl)
+    for up in (20, 50, 57, -40):
+        out, lse = windowed(q * 2.0 ** up, k * 2.0 ** up, v, None, None, 0, 0, True, scale=0.125 * 2.0 ** (-2 * up))
+        assert torch.equal(out, want) and torch.equal(lse, wl), up
+
+
+def test_a_scale_of_zero_weighs_all_keys_alike():
+    """... whatever their products are."""
+    q, k, v = (make((1, 20, 2, 64), BF, s) for s in (1, 2, 3))
+    for up in (0, 50):
+        rows = list(ref.window_reference(q, k, v, 0, 0, True, 0.0, [20], [20]))
+        check(rows, *windowed(q * 2.0 ** up, k * 2.0 ** up, v, None, None, 0, 0, True, scale=0.0))
