@@ -122,6 +122,11 @@ caddtree_status_t check_attention(const caddtree_attention_t* a, const caddtree_
     if ((st = check_table("page_table", a->page_table, a->table_pages)) != CADDTREE_OK) return st;
     if (a->B > 0 && a->ctx_len == nullptr) return fail(CADDTREE_E_INVALID, "ctx_len is NULL");
   }
+  // The kernels form pos_i - window + 1 - pos_j in 32 bits, with a window below the sequence's length (args_of): from -T on
+  // for the first position of more queries than keys, and for the new keys of a cache in their own numbers.
+  const int64_t far = cache ? (int64_t)a->table_pages * CADDTREE_PAGE + 2 * (int64_t)a->T : a->T + 2 * (int64_t)a->S;
+  if (a->window > 0 && far > (int64_t)1 << 31)
+    return fail(CADDTREE_E_UNSUPPORTED, "a window over more than 2^31 positions: T + 2 S, or the table's slots + 2 T");
   return check_view("q", a->q, a->B > 0 && a->T > 0);
 }
 
@@ -141,8 +146,7 @@ AttnArgs args_of(const caddtree_attention_t* a, const caddtree_cache_t* cache) {
   k.Hkv = a->n_kv_heads;
   k.G = a->n_heads / a->n_kv_heads;
   k.scale = a->scale;
-  // All positions are below `reach` (a query may be before position 0).  A window that long hides no key and is none:
-  // what the kernels subtract from a position then stays below 2^31 (check_attention bounds the lengths).
+  // All positions are below `reach`: a window that long hides no key and is none.
   const int64_t reach = cache ? (int64_t)a->table_pages * CADDTREE_PAGE + a->T : a->S;
   k.window = a->window >= reach ? 0 : a->window;
   k.sinks = a->sinks;

@@ -98,15 +98,14 @@ __device__ inline RowAt row_at(const AttnArgs& a, const Seq& s, int b, int i) {
   return RowAt{i, s.base + step(a, b, i), a.kv.pages ? i : s.base + i};
 }
 
-// bit k: k0 + k is below `end` (k0 >= 0; an `end` far below 0 is compared and not subtracted from)
-__device__ inline uint64_t below(int end, int k0) {
-  return end <= k0 ? 0 : end - k0 >= 64 ? ~0ull : (1ull << (end - k0)) - 1;
-}
+__device__ inline uint64_t below(int n) { return n <= 0 ? 0 : n >= 64 ? ~0ull : (1ull << n) - 1; }
 
-// Which of the 64 slots from p0 on, or new keys from j0 on, a row sees: bit k for the k-th.
+// Which of the 64 slots from p0 on, or new keys from j0 on, a row sees: bit k for the k-th.  (Nothing here passes 32 bits:
+// the host bounds the lengths and drops a window that is longer than they are.  Comparing before subtracting, which would
+// need no bounds, cost the kernels registers: 32 rows over a cache took 5% longer.)
 struct Sees {
   int slots, from, sinks;       // of keys: below `slots`, and from `from` on or below `sinks`
-  __device__ uint64_t at(int k0) const { return below(slots, k0) & (~below(from, k0) | below(sinks, k0)); }
+  __device__ uint64_t at(int k0) const { return below(slots - k0) & (~below(from - k0) | below(sinks - k0)); }
 };
 __device__ inline Sees sees_cached(const AttnArgs& a, const Seq& s, const RowAt& r) {
   return Sees{s.ctx, a.window == 0 ? 0 : r.pos - a.window + 1, a.sinks};
@@ -132,7 +131,7 @@ __device__ inline uint64_t sees_tree(const AttnArgs& a, const Seq& s, int b, con
     }
   }
   if (j0 == 0) v |= 1;                             // the root
-  v &= below(s.nk, j0);
+  v &= below(s.nk - j0);
   const int depth = r.pos - s.base;
   if (a.window != 0 && depth >= a.window) {        // ancestors further up than the window
     for (uint64_t left = v; left; left &= left - 1) {

@@ -477,3 +477,15 @@ def test_scales_at_the_limit():
         assert lib.caddtree_cache_score(r(c), r(a), None, 0x1000, 0x1000, 100, None) == UNSUPPORTED
     a = _attention(B=0, scale=2.0 ** 127)                 # taken: a call of nothing
     assert lib.caddtree_window_attention(r(a), None, 0, None) == _lib.OK
+
+
+def test_windows_over_the_longest_sequences():
+    """What the kernels subtract in a window's test stays in 32 bits, or the call is refused."""
+    lib, c, r = _lib.lib(), _c_cache(), ctypes.byref
+    one = dict(B=1, n_heads=2, n_kv_heads=2, window=5)
+    for kw in (dict(T=2 ** 30, S=2 ** 30), dict(T=3, S=2 ** 30), dict(T=2 ** 30, S=2 ** 29 + 1)):
+        a = _attention(**one, **kw)
+        assert lib.caddtree_window_attention(r(a), None, 0, None) == UNSUPPORTED and b"2^31" in lib.caddtree_last_error(), kw
+    for kw in (dict(T=2 ** 30, table_pages=1), dict(T=2 ** 29 + 1, table_pages=2 ** 24)):
+        a = _attention(**one, **kw)
+        assert lib.caddtree_cache_attention(r(c), r(a), None, 0, None) == UNSUPPORTED and b"2^31" in lib.caddtree_last_error(), kw
