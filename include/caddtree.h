@@ -351,6 +351,8 @@ typedef struct {
   const int32_t* page_table;    /* [B, table_pages]; the cached form only, as the next two */
   int32_t table_pages;
   const int64_t* ctx_len;       /* [B] cached tokens */
+  int32_t lse_strided;          /* 0: lse is contiguous.  1, where it is read (caddtree_cache_score): element */
+  int64_t lse_stride_b, lse_stride_t, lse_stride_h; /* (b, t, h) at lse + b lse_stride_b + t ..., any strides >= 0 */
 } caddtree_attention_t;
 
 /* Attention over the keys given, the queries being the last positions: query i of sequence b is at

@@ -72,6 +72,8 @@ class Attention(ctypes.Structure):
         ("page_table", ctypes.c_void_p),
         ("table_pages", ctypes.c_int32),
         ("ctx_len", ctypes.c_void_p),
+        ("lse_strided", ctypes.c_int32),
+        *((n, ctypes.c_int64) for n in ("lse_stride_b", "lse_stride_t", "lse_stride_h")),
     ]
 
 

@@ -127,12 +127,12 @@ def _sizes(name: str, t) -> None:
         raise ValueError(f"{name} must have sizes below 2^31, got {tuple(t.shape)}")
 
 
-def _array(name: str, t, dtype, shape, device: int) -> int:
-    """The pointer of a contiguous tensor of exactly this shape (None in a place: any size)."""
+def _array(name: str, t, dtype, shape, device: int, contiguous: bool = True) -> int:
+    """The pointer of a tensor of exactly this shape (None in a place: any size), contiguous unless that is not asked."""
     _tensor(name, t, dtype, device)
     if t.dim() != len(shape) or any(w is not None and w != g for w, g in zip(shape, t.shape)):
         raise ValueError(f"{name} must have shape {tuple('any' if w is None else w for w in shape)}, got {tuple(t.shape)}")
-    if not t.is_contiguous():
+    if contiguous and not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
     _sizes(name, t)
     return t.data_ptr()
@@ -409,9 +409,9 @@ class KVCache:
     def score(self, q, page_table, ctx_len, lse, scores, new_scores=None, *, weight=None, count=None, depth=None,
               window: int = 0, sinks: int = 0, scale: Optional[float] = None, stream=None) -> None:
         """Adds the attention weight of the cached slots to ``scores`` (float32 [B, kv heads, slots]), in place or
-        into ``new_scores``: the arguments of the ``attention`` call that wrote ``lse``, and ``weight``
-        (float32 [B, T], default 1) to pick and weigh its queries (in a tree: the accepted ones).  ``depth``
-        says that the queries are a tree's."""
+        into ``new_scores``: the arguments of the ``attention`` call that wrote ``lse`` (read here in any strides),
+        and ``weight`` (float32 [B, T], default 1) to pick and weigh its queries (in a tree: the accepted ones).
+        ``depth`` says that the queries are a tree's."""
         native = self._native(stream)
         if native is not None:
             binding, ops, device, raw = native
@@ -421,7 +421,12 @@ class KVCache:
         torch = _torch()
         device = self._on()
         a = self._attention(q, page_table, ctx_len, count, depth, window, sinks, scale, device)
-        a.lse = _array("lse", lse, torch.float32, (a.B, a.T, a.n_heads), device)
+        shape = (a.B, a.T, a.n_heads)
+        if isinstance(lse, torch.Tensor) and lse.dim() == 3 and not lse.is_contiguous():
+            a.lse, a.lse_strided = _array("lse", lse, torch.float32, shape, device, contiguous=False), 1
+            a.lse_stride_b, a.lse_stride_t, a.lse_stride_h = lse.stride()
+        else:
+            a.lse = _array("lse", lse, torch.float32, shape, device)
         w = None if weight is None else _array("weight", weight, torch.float32, (a.B, a.T), device)
         old = _array("scores", scores, torch.float32, (a.B, self.n_kv_heads, None), device)
         new = old if new_scores is None else _array("new_scores", new_scores, torch.float32, tuple(scores.shape), device)

@@ -209,6 +209,7 @@ size_t split_bytes(const caddtree_attention_t* a, int32_t n) {
 
 caddtree_status_t run_attention(const caddtree_attention_t* a, const caddtree_cache_t* cache, void* workspace, size_t bytes,
                                 hipStream_t stream) {
+  if (a->lse != nullptr && a->lse_strided) return fail(CADDTREE_E_INVALID, "lse is written contiguous: lse_strided must be 0");
   if (a->B == 0 || a->T == 0) return ok();
   caddtree::Split sp = {1, nullptr, nullptr};
   if (workspace != nullptr) {
@@ -312,13 +313,20 @@ caddtree_status_t caddtree_cache_score(const caddtree_cache_t* cache, const cadd
   if (slots < 0 || slots > kMaxTokens) return fail(CADDTREE_E_INVALID, "slots = %lld must be in 0 .. 2^30", (long long)slots);
   if (a->B == 0 || slots == 0) return ok();
   if (a->T > 0 && a->lse == nullptr) return fail(CADDTREE_E_INVALID, "lse is NULL");
+  if (a->lse_strided && (a->lse_stride_b < 0 || a->lse_stride_t < 0 || a->lse_stride_h < 0))
+    return fail(CADDTREE_E_INVALID, "the strides of lse must not be negative");
   if (scores == nullptr || new_scores == nullptr) return fail(CADDTREE_E_INVALID, "scores and new_scores are required");
   if (new_scores != scores) {
     const size_t bytes = (size_t)a->B * a->n_kv_heads * slots * 4;
     const Array arrays[] = {{"scores", scores, bytes, false}, {"new_scores", new_scores, bytes, true}};
     if ((st = check_apart(arrays)) != CADDTREE_OK) return st;
   }
-  caddtree::ScoreArgs s = {args_of(a, cache), weight, scores, new_scores, slots};
+  caddtree::ScoreArgs s = {args_of(a, cache), weight, scores, new_scores, slots, (int64_t)a->T * a->n_heads, a->n_heads, 1};
+  if (a->lse_strided) {
+    s.lse_b = a->lse_stride_b;
+    s.lse_t = a->lse_stride_t;
+    s.lse_h = a->lse_stride_h;
+  }
   const hipError_t e = caddtree::launch_cache_score(s, (caddtree_dtype_t)enum_value(a->dtype), a->head_dim, stream);
   return e == hipSuccess ? ok() : hip_fail(e, "cache score launch");
 }

@@ -67,6 +67,7 @@ struct ScoreArgs {
   const float* scores;       // [B, Hkv, slots]
   float* new_scores;
   int64_t slots;
+  int64_t lse_b, lse_t, lse_h;   // strides of at.lse
 };
 hipError_t launch_cache_score(const ScoreArgs& a, caddtree_dtype_t dtype, int32_t head_dim, hipStream_t stream);
 

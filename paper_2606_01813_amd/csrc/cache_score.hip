@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * kWaves, kOne ? 4 : 3) void score_kernel(ScoreA
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int r = min(r0 + 4 * g + e, R - 1), at = r / G, h = hk * G + r % G;
-      base[e] = a.at.lse[((int64_t)b * a.at.T + query[at]) * a.at.Hq + h] * kLog2e;
+      base[e] = a.at.lse[b * a.lse_b + query[at] * a.lse_t + h * a.lse_h] * kLog2e;
       w[e] = r0 + 4 * g + e < R ? weight[at] : 0.f;
       from[e] = a.at.window == 0 ? 0 : position[at] - a.at.window + 1;
     }

@@ -489,3 +489,30 @@ def test_windows_over_the_longest_sequences():
     for kw in (dict(T=2 ** 30, table_pages=1), dict(T=2 ** 29 + 1, table_pages=2 ** 24)):
         a = _attention(**one, **kw)
         assert lib.caddtree_cache_attention(r(c), r(a), None, 0, None) == UNSUPPORTED and b"2^31" in lib.caddtree_last_error(), kw
+
+
+def test_lse_is_read_in_any_strides(rec, monkeypatch):
+    """The scores' lse is an input: a transposed or repeated one is passed on with its strides."""
+    f32, ops = torch.float32, rec.ops()
+    for native in (False, True):
+        monkeypatch.setattr(attention, "_native", lambda stream: (_lib.binding(), ops, 0, STREAM) if native else None)
+        for lse, strides in ((_aligned((B, Hq, T), f32).transpose(1, 2), (Hq * T, 1, T)),
+                             (_aligned((B, T, 1), f32).expand(B, T, Hq), (T, 1, 0)),
+                             (_aligned((1, 1, 1), f32).expand(B, T, Hq), (0, 0, 0)),
+                             (_aligned((B, 2 * T, Hq), f32)[:, ::2], (2 * T * Hq, 2 * Hq, 1))):
+            rec.calls.clear()
+            CALLS["score"][0](_cache(), dict(_state(), lse=lse))
+            (_, args), = rec.calls
+            a = dict(zip((f for f, _ in _lib.Attention._fields_), args[1]))
+            assert a["lse"] == lse.data_ptr() and a["lse_strided"] == 1
+            assert (a["lse_stride_b"], a["lse_stride_t"], a["lse_stride_h"]) == strides
+
+
+def test_strides_of_lse():
+    lib, c, r = _lib.lib(), _c_cache(), ctypes.byref
+    for kw in (dict(lse_stride_b=-1), dict(lse_stride_t=-1), dict(lse_stride_h=-4)):
+        a = _attention(lse_strided=1, **kw)
+        assert lib.caddtree_cache_score(r(c), r(a), None, 0x1000, 0x1000, 100, None) == INVALID
+    a = _attention(lse_strided=1, lse_stride_b=20, lse_stride_t=4, lse_stride_h=1)
+    assert lib.caddtree_window_attention(r(a), None, 0, None) == INVALID        # (written there: contiguous)
+    assert lib.caddtree_cache_attention(r(c), r(a), None, 0, None) == INVALID

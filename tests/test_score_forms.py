@@ -11,7 +11,7 @@ import torch
 
 from paper_2606_01813_amd import KVCache
 from tests._parity import say
-from tests.test_attention import BF, F16, i32, i64, make
+from tests.test_attention import BF, F16, Filled, i32, i64, make
 
 pytestmark = pytest.mark.gpu
 
@@ -105,3 +105,26 @@ def test_score_forms(case, dtype):
     assert torch.equal(new[~there[:, None].expand_as(new)], old[~there[:, None].expand_as(old)])
     off = (new.double() - want).abs()
     assert torch.all(off <= tol), float((off / tol.clamp(min=1e-30)).max())
+
+
+@pytest.mark.parametrize("T", [3, 40])
+def test_lse_in_any_strides(T):
+    f = Filled(2, 4, 64, [300, 70], BF)
+    q = make((2, T, 4, 64), BF, 5)
+    lse = torch.zeros((2, T, 4), device="cuda")
+    f.cache.attention(q, f.table, i64(f.ctx), lse=lse)
+    zero = torch.zeros((2, 4, f.table.shape[1] * 64), device="cuda")
+
+    def score(x):
+        got = torch.full_like(zero, 7.0)
+        f.cache.score(q, f.table, i64(f.ctx), x, zero, got)
+        torch.cuda.synchronize()
+        return got
+
+    want = score(lse)
+    wide = torch.full((2, 2 * T, 9), float("nan"), device="cuda")
+    wide[:, ::2, 3:7] = lse
+    for x in (lse.transpose(1, 2).contiguous().transpose(1, 2), lse.permute(2, 1, 0).contiguous().permute(2, 1, 0), wide[:, ::2, 3:7]):
+        assert not x.is_contiguous() and torch.equal(score(x), want)
+    same = lse[:, :1, :1]
+    assert torch.equal(score(same.expand(2, T, 4)), score(same.expand(2, T, 4).contiguous()))
