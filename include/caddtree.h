@@ -288,6 +288,8 @@ caddtree_status_t caddtree_fit_cost(const double* x_host, const double* y_host, 
  *
  * Visibility.  Query i at position pos_i sees the key at position pos_j if its order allows it and
  *     window = 0  or  pos_i - pos_j < window  or  pos_j < sinks.
+ * Positions in a cache are slot numbers.  After an eviction (caddtree_cache_evict) the kept slots lie next to
+ * each other, so a window counts kept slots, not the tokens that were between them.
  * An absent key never sees use: whatever its memory holds (NaN included) does not reach a result, and
  * what a query does not see does not reach its row.  A query that sees no key gets zeros and
  * lse = -inf.

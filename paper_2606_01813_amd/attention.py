@@ -7,7 +7,8 @@ and each sees the cached context, the root, its ancestors and itself.
     out = window_attention(q, k, v, window=4096, sinks=4)                # a prompt, [B, T, heads, 128]
     cache.write(k, v, table, start)                                      # ... goes into the cache
     plan.build(logits, tree, workspace=ws, ctx_len=ctx_len)              # a draft tree
-    o = cache.attention(q, table, ctx_len, k, v, mask=tree.mask, depth=tree.depth, count=tree.n_star, lse=lse)
+    aws = attention_workspace(q, cache=cache, page_table=table)          # (without one, a row's keys stay in one part)
+    o = cache.attention(q, table, ctx_len, k, v, mask=tree.mask, depth=tree.depth, count=tree.n_star, lse=lse, workspace=aws)
     cache.write(k, v, table, ctx_len, count=accepted, index=path)        # the accepted path
     cache.score(q, table, ctx_len, lse, scores, weight=on_path, count=tree.n_star, depth=tree.depth)
     cache.evict(table, ctx_len, scores, new_table, new_len, new_scores, kept, budget=2048, sinks=4, recent=256)
@@ -441,7 +442,8 @@ class KVCache:
         scores to ``new_scores`` (float32 [B, kv heads, slots], zeros behind), how many they are to ``new_len``
         (int64 [B]) and the old slots to ``kept`` (int32 [B, kv heads, budget], -1 behind).  These four are tensors
         apart from the ones that are read.  Rows of more than 16384 slots need a workspace, made here if not given
-        (with a raw stream handle it has to be)."""
+        (with a raw stream handle it has to be).  Positions are slot numbers, so a window over an evicted cache
+        counts kept slots."""
         if workspace is None and (stream is None or hasattr(stream, "cuda_stream")):
             workspace = self.evict_workspace(page_table, scores, stream)
         native = self._native(stream)

@@ -240,7 +240,7 @@ __device__ __forceinline__ bool narrow_tile(NarrowState<D, kR>& st, Stage& x, co
 }
 
 // Up to 16 kR rows.  Bound by reading the keys: 64 single tokens over 4096 to 8192 cached ones, 8 kv heads of 128
-// channels, take 91 us, 5.0 TB/s of codes and scales, what a large copy reaches on this card.  A wavefront has a page's
+// channels, take 92 us, 5.0 TB/s of codes and scales: what a large copy reaches on this card, 71% of a pure read.  A wavefront has a page's
 // codes on their way while it takes the page before (a page is 8.5 KB, eight wavefronts a compute unit), and the next
 // pages' numbers before that: a number waited for in the loop would hold up the loads behind it.
 template <typename E, int D, int kR, bool kPaged>
@@ -676,7 +676,7 @@ __device__ __forceinline__ void wide_finish(const WideState<D>& st, const AttnAr
 
 // 33 to 64 rows over a cache: two wavefront pairs share the rows out and take half of a tile's keys each, whose sums they join at
 // the end.  Two tiles are on their way in registers (a tile's codes are a few) while one is in LDS.  A block of 16 with 4
-// heads a kv head over 131072 cached tokens of 128 channels takes 70 us, 2.0 TB/s: a tile's chain of conversion, LDS,
+// heads a kv head over 131072 cached tokens of 128 channels takes 64 us, 2.2 TB/s: a tile's chain of conversion, LDS,
 // products and softmax between two barriers takes longer than its bytes, matrix units and vector units being busy 24% and
 // 38% of the time and wavefronts waiting 42% of theirs.
 template <typename E, int D>
@@ -852,8 +852,8 @@ __global__ __launch_bounds__(256, 2) void pair_kernel(AttnArgs a, Split sp) {
 // 128 rows a workgroup, 32 a wavefront.  Bound by the matrix products and by forming the weights, which hardly overlap:
 // at 128 channels a tile takes a wavefront 32 products (1024 cycles) and some 230 vector instructions, 32 of them
 // exponentials (1300 cycles), of the 2500 it takes in all.  A prompt of 8192 tokens of 32 heads through a window of 2048
-// takes 288 us (835 TFLOP/s; matrix units busy 46%, vector units 48% of the time); 32 trees of 257 rows over 4096 cached
-// tokens take 625 us (706 TFLOP/s): there a tile is converted on its way into LDS and the wavefronts wait 45% of their
+// takes 276 us (873 TFLOP/s; matrix units busy 46%, vector units 48% of the time); 32 trees of 257 rows over 4096 cached
+// tokens take 618 us (713 TFLOP/s): there a tile is converted on its way into LDS and the wavefronts wait 45% of their
 // time, 23% where tiles go straight to LDS.  The next tile stored earlier (before this one or between its scores and its
 // softmax), or loaded a tile earlier, took 1 to 3% longer; eight wavefronts or 64 rows a wavefront that share a tile,
 // tiles of 32 keys with three wavefronts a SIMD, priorities for the products, or half tiles interleaved, the same or more.

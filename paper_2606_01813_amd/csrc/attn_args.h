@@ -35,7 +35,7 @@ struct AttnArgs {
   int32_t order;             // caddtree_order_t
   int32_t mask_kind;         // caddtree_mask_t of a tree
   const void* mask;
-  const int32_t* depth;      // [B, cap]; score: non-null says that the queries are a tree's
+  const int32_t* depth;      // [B, cap] of a tree (order says whether the queries are one's)
   int32_t cap;
   PagedKV kv;
   const int64_t* ctx_len;    // [B]

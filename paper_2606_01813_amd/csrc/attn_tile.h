@@ -1,7 +1,7 @@
 // Device code of the attention kernels: which keys a tile of rows reads, which of them each row sees, and
 // the layouts of keys and values in LDS.
 //
-// Both kernels form S^T = K Q^T and O^T = V^T P^T, so a lane holds one query row in both products: the
+// All of them form S^T = K Q^T and O^T = V^T P^T, so a lane holds one query row in both products: the
 // scores' layout is the one the second product wants of its weights (the key index of a matrix
 // instruction is a sum's, any order serves), and a row's maximum and sum are a lane's own but for the
 // lanes that hold the same row.  V^T comes out of a row-major tile through the transposing LDS read.

@@ -9,8 +9,8 @@
 // Rows of up to 16384 slots have a workgroup each and keep their keys in registers throughout.  Longer rows
 // are cut into parts, a workgroup each: a launch a digit counts every part's keys, the next one adds the parts'
 // histograms up, finds the digit and goes on, and the last lists (kept slots before a part follow from the
-// histograms of the parts before it).  4 rows with the move: of 16384 slots 28 us in a workgroup, of 16448 32 us in
-// parts; of 131072 31 us of selection in parts, 137 in a workgroup that reads its scores again for every digit.
+// histograms of the parts before it).  4 rows with the move: of 16384 slots 29 us in a workgroup, of 16448 32 us in
+// parts; of 131072 34 us of selection in parts, 137 in a workgroup that reads its scores again for every digit.
 // Bound by latency: a part's counting takes 5 us, adding the histograms 3 more (parts of 4096 or of 16384 slots: the
 // whole call 46 -> 60 and 51 us).
 #include <algorithm>
@@ -118,7 +118,7 @@ __device__ __forceinline__ int kind_of(int i, uint32_t k, int lo, int hi, uint32
 }
 
 // One workgroup a sequence and kv head; a thread holds kKept keys, kKept kThreads >= n.  512 rows of 4096 to 8192 slots
-// take 39 us (0.35 TB/s): bound by the vector instructions of the counting and the listing, 1024 threads a row.
+// take 41 us (0.34 TB/s): bound by the vector instructions of the counting and the listing, 1024 threads a row.
 template <int kKept>
 __global__ __launch_bounds__(kThreads) void select_kernel(EvictArgs a) {
   __shared__ uint32_t hist[kBins];

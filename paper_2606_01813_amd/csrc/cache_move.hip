@@ -3,7 +3,7 @@
 // Both directions are bound by memory: 4 D bytes of 16-bit values and 1.0625 D of codes and scales a token
 // and head.  A lane has 8 channels of keys and of values, 16 bytes, and four lanes a block of 32, so that
 // neighbouring lanes read and write neighbouring pieces on either side.  Writing 4 x 4096 tokens of 8 heads of 128
-// channels takes 17 us (85 MB, 5.0 TB/s), reading them back 15 us (5.8 TB/s).
+// channels takes 17 us (85 MB, 5.0 TB/s), reading them back 15 us (5.7 TB/s).
 #include "attn_common.h"
 
 namespace caddtree {
