@@ -67,7 +67,7 @@ typedef enum {
   CADDTREE_E_HIP = 5           /* a HIP runtime call or kernel launch failed */
 } caddtree_status_t;
 
-/* Logits are F32 or BF16; the attention operators below take BF16 or F16. */
+/* Logits are F32 or BF16; the attention operators below take BF16 or F16, the operators on logits all three. */
 typedef enum { CADDTREE_F32 = 0, CADDTREE_BF16 = 1, CADDTREE_F16 = 2 } caddtree_dtype_t;
 
 /* Tree-attention mask format.  U8: [B, cap, cap] bytes, mask[b][i][j] = 1 iff
@@ -424,6 +424,140 @@ caddtree_status_t caddtree_cache_evict(const caddtree_cache_t* cache, int32_t B,
 
 /* HOST only: the workspace of caddtree_cache_evict (0 for rows of up to 16384 slots). */
 size_t caddtree_evict_workspace_bytes(const caddtree_cache_t* cache, int32_t B, int32_t table_pages, int64_t slots);
+
+/* ------------------------------------------------------------------------------------------------
+ * Logits: what stands before and behind a tree, and what trains its drafter.
+ *
+ * Penalties, biases and grammar masks on the drafter's or the target's logits; the target's choice along a
+ * built tree; and the loss, with its gradient, of a drafter that learns from a teacher's top logits (as
+ * caddtree_reduce_topk writes them).  They take no plan; they run on the current device, with the
+ * conventions at the top of this file, but for these: logits may be BF16, F16 or F32, and may be infinite
+ * or NaN where a call says so.  Arithmetic is fp32 or fp64, with one rounding to the logits' type.
+ *
+ * Rows of V elements are strided views [B, T, V]: element (b, t, v) at data + b stride_b + t stride_t + v
+ * (strides in elements, >= 0).  data is aligned to its elements; rows that start at multiples of 16 bytes
+ * are somewhat faster.  An input's rows may overlap or repeat (stride 0), an output's may not.  An output
+ * may be the call's logits themselves (same data and strides); else the stretches of memory from its first
+ * to its last element and from the logits' first to their last do not overlap (CADDTREE_E_INVALID). */
+#define CADDTREE_MAX_VOCAB (1 << 20)    /* V of these calls */
+#define CADDTREE_MAX_HISTORY ((1 << 20) - 64)
+#define CADDTREE_MAX_BIAS 4095
+#define CADDTREE_MAX_TEACHER 256
+
+typedef struct {
+  void* data;
+  int64_t stride_b, stride_t;
+} caddtree_rows_t;
+
+/* One call of caddtree_adjust_logits. */
+typedef struct {
+  caddtree_dtype_t dtype;
+  int32_t B;                    /* sequences, 0 .. 65535 */
+  int32_t T;                    /* rows of a sequence at most; with a tree: cap + 1 */
+  int32_t V;                    /* 1 .. CADDTREE_MAX_VOCAB */
+  caddtree_rows_t logits, out;
+  const int32_t* count;         /* [B], optional (NULL: T).  With a tree: its nodes, n_star, to which the root is added */
+  const int32_t* history;       /* [B, H], optional: token ids; one outside 0 .. V - 1 is padding */
+  const int32_t* history_len;   /* [B], optional (NULL: H) */
+  int32_t H;                    /* 0 .. CADDTREE_MAX_HISTORY */
+  const float* repetition;      /* [B] each, optional (NULL: 1, 0 and 0) */
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_ids;      /* [B, n_bias], optional: token ids; one outside 0 .. V - 1 is padding */
+  const float* bias;            /* [B, n_bias] */
+  int32_t n_bias;               /* 0 .. CADDTREE_MAX_BIAS */
+  const void* allowed;          /* u32 words, optional: bit (v % 32) of word v / 32 of row (b, t), which starts at word */
+  int64_t allowed_stride_b;     /*   b allowed_stride_b + t allowed_stride_t (strides >= 0; 0: one mask for all) */
+  int64_t allowed_stride_t;
+  const int32_t* token_ids;     /* [B, T - 1] each, with a tree (else both NULL): as written by caddtree_build */
+  const int32_t* parent;
+  float fill;                   /* what a token that is not allowed gets, not NaN; 0 stands for -inf.  A plan's calls
+                                   take finite logits: the drafter's get a finite one */
+} caddtree_adjust_t;
+
+/* Penalties for repeated tokens, biases and a grammar's mask.  x = the logit of token v in row (b, t), in fp32:
+ *     c > 0:  x = x > 0 ? x / repetition[b] : x repetition[b];  x = x - frequency[b] c - presence[b]
+ *     x = x + bias of v (of a token listed twice the last);  x = fill where v is not allowed
+ * with c how often v is among the first history_len[b] tokens of history[b] and, in a tree, on the row's path:
+ * the tokens of node t - 1 and of its ancestors (row 0, the root, has none; its own token belongs in the
+ * history).  Of a path of more than CADDTREE_MAX_L nodes the last CADDTREE_MAX_L count; a parent that is not
+ * below its node ends it.  A logit that nothing applies to is copied as it is, NaN and infinities included; one
+ * that is not allowed is fill whatever it was.  A row may be left with nothing allowed: it is all fill.
+ * Rows past count are left untouched.  In place (out is logits) only what changes is read and written. */
+caddtree_status_t caddtree_adjust_logits(const caddtree_adjust_t* a, hipStream_t stream);
+
+/* One call of caddtree_verify_tree. */
+typedef struct {
+  caddtree_dtype_t dtype;
+  int32_t B;                    /* trees, 0 .. 65535 */
+  int32_t T;                    /* rows of a tree: cap + 1, the root and the nodes */
+  int32_t V;                    /* 1 .. CADDTREE_MAX_VOCAB */
+  caddtree_rows_t logits;       /* [B, T, V]; data NULL where `chosen` is given */
+  const int32_t* chosen;        /* [B, T], optional: the target's token at each row, chosen by the caller; -1: none */
+  const int32_t* token_ids;     /* [B, T - 1] each: as written by caddtree_build */
+  const int32_t* parent;
+  const int32_t* count;         /* [B], n_star */
+  int32_t M;                    /* rows of a path at most, >= 1 */
+  int32_t* accepted;            /* [B] */
+  int32_t* index;               /* [B, M] */
+  int32_t* tokens;              /* [B, M] */
+  float* weight;                /* [B, T], optional */
+} caddtree_verify_t;
+
+/* The target's choice along a tree (Sec. 3.3).  From the root's row on: the row's token is the largest logit's (of
+ * equals the lowest id; NaN and -inf are never chosen), or chosen[b, row]; if a child of the row (of several the
+ * first node) carries it, the path goes on there, else it ends, as it does after M rows and where a row has no token
+ * to choose.
+ *   accepted[b]: rows on the path, 1 .. M;  index[b, j]: the path's rows in order, then -1;  tokens[b, j]: each
+ *   one's token (-1: none), then -1.  tokens[b, accepted - 1] is the bonus token, the next tree's root.
+ *   weight[b, row]: 1 on the path, else 0.
+ * accepted and index are caddtree_cache_write's count and index, weight is caddtree_cache_score's.  The outputs
+ * overlap nothing else.  workspace: caddtree_verify_workspace_bytes(a) bytes, 256-byte aligned, lets a call on few
+ * logits read all of their rows at once; NULL (or fewer bytes) is accepted, and the rows are read one after the other. */
+caddtree_status_t caddtree_verify_tree(const caddtree_verify_t* a, void* workspace, size_t workspace_bytes, hipStream_t stream);
+/* HOST only (0 where none is of use, or for sizes that the call refuses). */
+size_t caddtree_verify_workspace_bytes(const caddtree_verify_t* a);
+
+/* One call of caddtree_distill or caddtree_distill_grad. */
+typedef struct {
+  caddtree_dtype_t dtype;
+  int32_t B;                    /* 0 .. 65535 */
+  int32_t T;
+  int32_t V;                    /* 1 .. CADDTREE_MAX_VOCAB */
+  caddtree_rows_t logits;       /* the student's, [B, T, V] */
+  int32_t K;                    /* tokens that the teacher lists, 1 .. CADDTREE_MAX_TEACHER */
+  const int32_t* ids;           /* [B, T, K]; one outside 0 .. V - 1 is padding */
+  const float* target;          /* [B, T, K]: the teacher's logits, or with `tail` its log-probabilities */
+  const float* weight;          /* [B, T], optional (NULL: 1) */
+  float temperature;            /* finite, 2^-20 .. 2^20 */
+  int32_t tail;                 /* 0 or 1 */
+  float* loss;                  /* [B, T] (caddtree_distill) */
+  float* stats;                 /* [B, T, 3]: optional in caddtree_distill, an input of caddtree_distill_grad */
+  caddtree_rows_t grad;         /* [B, T, V] of the logits' type: optional (data NULL) in caddtree_distill */
+} caddtree_distill_t;
+
+/* Distillation from a teacher's top logits: with q = softmax(logits / temperature) of a row,
+ *     p_k = exp(t_k / temperature) / sum_j exp(t_j / temperature),  rho = 0           (tail = 0)
+ *     p_k = exp(t_k),  rho = max(0, 1 - sum_k p_k), the probability of all others     (tail = 1)
+ *     loss = weight [ sum_k p_k (log p_k - log q_k) + rho (log rho - log(1 - Q)) ],  Q = sum of q over the listed
+ *     grad_v = weight / temperature [ q_v M - (v is listed: the sum of its p_k; else: rho q_v / (1 - Q)) ]
+ * with M = sum_k p_k + rho.  A term with p_k = 0 (t_k = -inf) is 0.  Where all t_k are -inf and tail = 0
+ * nothing counts as listed.  The rest's term is left out where the student
+ * gives the rest nothing.  Padding is in no sum: with nothing listed, loss and gradient are 0.  A token listed twice
+ * is two terms.  Where weight is 0 the row is not read: loss, gradient and stats are 0.  A student's logit of -inf
+ * (a mask) has q = 0; in a row of nothing else every q is 0.  NaN and +inf spread over their row.
+ *   stats[b, t]: the row's largest logit, the sum of exp((logit - largest) / temperature) (0 if all are -inf), and
+ *   the same sum without the listed tokens.
+ * caddtree_distill writes the loss and, where asked for, the gradient in one pass over the logits;
+ * caddtree_distill_grad the gradient alone, from the stats that such a call kept of the same logits, ids and
+ * temperature (weight: the loss's gradient).
+ * The gradient may overwrite the logits.  The order of the sums is fixed by the sizes and the workspace.
+ *   workspace: caddtree_distill_workspace_bytes(a) bytes, 256-byte aligned, lets a call of few rows split them over
+ *   the card; NULL (or fewer bytes) is accepted. */
+caddtree_status_t caddtree_distill(const caddtree_distill_t* a, void* workspace, size_t workspace_bytes, hipStream_t stream);
+caddtree_status_t caddtree_distill_grad(const caddtree_distill_t* a, hipStream_t stream);
+/* HOST only (0 where none is of use, or for sizes that the call refuses). */
+size_t caddtree_distill_workspace_bytes(const caddtree_distill_t* a);
 
 const char* caddtree_status_string(caddtree_status_t status);
 const char* caddtree_last_error(void);

@@ -19,6 +19,9 @@ fixed-budget (DDTree) construction: the top ``cap`` nodes, no stop rule.
 
 ``KVCache`` and ``window_attention`` (attention.py) are the target's attention over the built trees: a
 cache of keys and values in 4 bits, read under the tree's mask, and its eviction.
+
+``adjust_logits``, ``verify_tree`` and ``distill`` (logits.py) work on logits: penalties, biases and grammar masks before
+a tree is built or verified, the path that the target agrees with, and the loss that trains the drafter.
 """
 
 from __future__ import annotations
@@ -32,9 +35,11 @@ import numpy as np
 from . import _lib
 from ._lib import CaddtreeError, MAX_CAP, MAX_CTX, MAX_K, MAX_L
 from .attention import KVCache, attention_workspace, window_attention
+from .logits import adjust_logits, distill, distill_grad, distill_workspace, verify_tree, verify_workspace
 
-__all__ = ["Plan", "TreeOutputs", "KVCache", "window_attention", "attention_workspace", "CaddtreeError", "fit_cost",
-           "MAX_L", "MAX_K", "MAX_CAP", "MAX_CTX"]
+__all__ = ["Plan", "TreeOutputs", "KVCache", "window_attention", "attention_workspace", "adjust_logits", "verify_tree",
+           "verify_workspace", "distill", "distill_grad", "distill_workspace", "CaddtreeError", "fit_cost", "MAX_L", "MAX_K",
+           "MAX_CAP", "MAX_CTX"]
 
 
 def _torch():

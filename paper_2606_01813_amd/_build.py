@@ -25,7 +25,7 @@ PROBE_LIB = os.path.join(PKG, "libcaddtree_probe.so")
 PROBE_SOURCES = ["probe.hip"]
 SOURCES = ["api.cpp", "reduce_topk.hip", "expand.hip", "expand_level.hip", "expand_wide.hip", "emit.hip", "accept.hip",
            "scratch.hip", "costfit.cpp", "attention_api.cpp", "attention.hip", "cache_move.hip", "cache_score.hip",
-           "cache_evict.hip"]
+           "cache_evict.hip", "logits_api.cpp", "adjust.hip", "verify.hip", "distill.hip"]
 # the Python binding's native calls (host code, against torch's headers): an extension module
 BINDING = os.path.join(PKG, "_binding.so")
 BINDING_SOURCE = "binding.cpp"

@@ -11,6 +11,7 @@ LIB_PATH = os.path.join(_HERE, "libcaddtree.so")
 OK, E_INVALID, E_UNSUPPORTED, E_COST, E_WORKSPACE, E_HIP = range(6)
 DTYPES = {"f32": 0, "bf16": 1}
 ATTENTION_DTYPES = {"bf16": 1, "f16": 2}
+LOGIT_DTYPES = {"f32": 0, "bf16": 1, "f16": 2}
 ORDERS = {"chain": 0, "block": 1, "tree": 2}
 MASKS = {"none": 0, "u8": 1, "bits": 2}
 ALLOW_NONCONVEX = 1
@@ -77,6 +78,47 @@ class Attention(ctypes.Structure):
     ]
 
 
+class Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_t", ctypes.c_int64)]
+
+
+_SIZES = [("dtype", ctypes.c_int), *((n, ctypes.c_int32) for n in ("B", "T", "V"))]
+
+
+class Adjust(ctypes.Structure):
+    _fields_ = _SIZES + [
+        ("logits", Rows), ("out", Rows),
+        *((n, ctypes.c_void_p) for n in ("count", "history", "history_len")),
+        ("H", ctypes.c_int32),
+        *((n, ctypes.c_void_p) for n in ("repetition", "presence", "frequency", "bias_ids", "bias")),
+        ("n_bias", ctypes.c_int32),
+        ("allowed", ctypes.c_void_p), ("allowed_stride_b", ctypes.c_int64), ("allowed_stride_t", ctypes.c_int64),
+        *((n, ctypes.c_void_p) for n in ("token_ids", "parent")),
+        ("fill", ctypes.c_float),
+    ]
+
+
+class Verify(ctypes.Structure):
+    _fields_ = _SIZES + [
+        ("logits", Rows),
+        *((n, ctypes.c_void_p) for n in ("chosen", "token_ids", "parent", "count")),
+        ("M", ctypes.c_int32),
+        *((n, ctypes.c_void_p) for n in ("accepted", "index", "tokens", "weight")),
+    ]
+
+
+class Distill(ctypes.Structure):
+    _fields_ = _SIZES + [
+        ("logits", Rows),
+        ("K", ctypes.c_int32),
+        *((n, ctypes.c_void_p) for n in ("ids", "target", "weight")),
+        ("temperature", ctypes.c_float),
+        ("tail", ctypes.c_int32),
+        *((n, ctypes.c_void_p) for n in ("loss", "stats")),
+        ("grad", Rows),
+    ]
+
+
 EXPORTS = [
     "caddtree_plan_create", "caddtree_plan_destroy", "caddtree_workspace_bytes", "caddtree_build",
     "caddtree_build_noalloc",
@@ -85,6 +127,8 @@ EXPORTS = [
     "caddtree_attention_workspace_bytes", "caddtree_window_attention", "caddtree_cache_attention",
     "caddtree_cache_write", "caddtree_cache_read", "caddtree_cache_score", "caddtree_cache_evict",
     "caddtree_evict_workspace_bytes",
+    "caddtree_adjust_logits", "caddtree_verify_tree", "caddtree_verify_workspace_bytes",
+    "caddtree_distill", "caddtree_distill_grad", "caddtree_distill_workspace_bytes",
 ]
 
 
@@ -137,6 +181,19 @@ def load(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.caddtree_cache_evict.restype = ctypes.c_int
     lib.caddtree_evict_workspace_bytes.argtypes = [cp, i32, i32, i64]
     lib.caddtree_evict_workspace_bytes.restype = sz
+    xp, tp, dp = ctypes.POINTER(Adjust), ctypes.POINTER(Verify), ctypes.POINTER(Distill)
+    lib.caddtree_adjust_logits.argtypes = [xp, vp]
+    lib.caddtree_adjust_logits.restype = ctypes.c_int
+    lib.caddtree_verify_tree.argtypes = [tp, vp, sz, vp]
+    lib.caddtree_verify_tree.restype = ctypes.c_int
+    lib.caddtree_verify_workspace_bytes.argtypes = [tp]
+    lib.caddtree_verify_workspace_bytes.restype = sz
+    lib.caddtree_distill.argtypes = [dp, vp, sz, vp]
+    lib.caddtree_distill.restype = ctypes.c_int
+    lib.caddtree_distill_grad.argtypes = [dp, vp]
+    lib.caddtree_distill_grad.restype = ctypes.c_int
+    lib.caddtree_distill_workspace_bytes.argtypes = [dp]
+    lib.caddtree_distill_workspace_bytes.restype = sz
     lib.caddtree_status_string.argtypes = [ctypes.c_int]
     lib.caddtree_status_string.restype = ctypes.c_char_p
     lib.caddtree_last_error.argtypes = []
@@ -198,3 +255,16 @@ def attention_ops():
                l.caddtree_cache_score, l.caddtree_cache_evict)
         _OPS = binding(), binding().ops(0, *(ctypes.cast(f, ctypes.c_void_p).value for f in fns))
     return _OPS
+
+
+_LOGITS_OPS = None
+
+
+def logits_ops():
+    """The native calls on logits, as attention_ops: the library's functions for the binding, or None."""
+    global _LOGITS_OPS
+    if _LOGITS_OPS is None and binding() is not None:
+        l = lib()
+        fns = (l.caddtree_adjust_logits, l.caddtree_verify_tree, l.caddtree_distill, l.caddtree_distill_grad)
+        _LOGITS_OPS = binding().logits_ops(0, *(ctypes.cast(f, ctypes.c_void_p).value for f in fns))
+    return _LOGITS_OPS

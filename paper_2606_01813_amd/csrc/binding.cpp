@@ -413,11 +413,11 @@ constexpr int64_t kAny = -1;
 
 // One call's view of its arguments, as Call above: ok falls at the first one that is not as it should be.
 struct Attn {
-  const Ops& s;
+  const bool host;
   int device;
   bool ok = true;
 
-  Attn(const Ops& ops, PyObject* dev) : s(ops) { device = (int)integer(dev, 0, 1 << 20); }
+  Attn(bool on_host, PyObject* dev) : host(on_host) { device = (int)integer(dev, 0, 1 << 20); }
 
   c10::TensorImpl* tensor(PyObject* o) {
     if (!ok || !THPVariable_CheckExact(o)) {
@@ -426,7 +426,7 @@ struct Attn {
     }
     c10::TensorImpl* t = THPVariable_Unpack(o).unsafeGetTensorImpl();
     const c10::Device d = t->device();
-    const bool here = s.host ? d.is_cpu() : d.is_cuda() && d.index() == device;
+    const bool here = host ? d.is_cpu() : d.is_cuda() && d.index() == device;
     if (!here || t->layout() != c10::kStrided || !t->has_storage() || t->has_symbolic_sizes_strides() || t->numel() == 0) {
       ok = false;
       return nullptr;
@@ -499,7 +499,45 @@ struct Attn {
     return v;
   }
 
-  // attention has no backward pass: an input that wants one is the Python path's to refuse
+  // [B, T, V] rows with a unit last stride
+  caddtree_rows_t rows(PyObject* o, c10::ScalarType type, const int64_t (&dims)[3], bool output = false) {
+    caddtree_rows_t v = {nullptr, 0, 0};
+    c10::TensorImpl* t = tensor(o);
+    if (t == nullptr) return v;
+    const auto sz = t->sizes();
+    const auto st = t->strides();
+    bool good = c10::typeMetaToScalarType(t->dtype()) == type && sz.size() == 3;
+    for (int i = 0; good && i < 3; ++i) good = (dims[i] == kAny || sz[i] == dims[i]) && sz[i] <= INT32_MAX;
+    if (!good || (sz[2] > 1 && st[2] != 1)) {
+      ok = false;
+      return v;
+    }
+    v.stride_b = sz[0] > 1 ? st[0] : 0;
+    v.stride_t = sz[1] > 1 ? st[1] : 0;
+    v.data = output ? t->mutable_data() : const_cast<void*>(t->data());
+    return v;
+  }
+  // ... of logits, whose sizes and type they give the call
+  template <typename A>
+  c10::ScalarType logits(PyObject* o, A* a) {
+    c10::TensorImpl* t = tensor(o);
+    if (t == nullptr || t->sizes().size() != 3) {
+      ok = false;
+      return c10::kFloat;
+    }
+    const c10::ScalarType type = c10::typeMetaToScalarType(t->dtype());
+    if (type != c10::kBFloat16 && type != c10::kHalf && type != c10::kFloat) ok = false;
+    a->logits = rows(o, type, {kAny, kAny, kAny});
+    no_gradient(o);
+    if (!ok) return type;
+    a->dtype = type == c10::kBFloat16 ? CADDTREE_BF16 : type == c10::kHalf ? CADDTREE_F16 : CADDTREE_F32;
+    a->B = (int32_t)t->sizes()[0];
+    a->T = (int32_t)t->sizes()[1];
+    a->V = (int32_t)t->sizes()[2];
+    return type;
+  }
+
+  // no call here has a backward pass: an input that wants one is the Python path's to refuse
   void no_gradient(PyObject* o) {
     if (!c10::GradMode::is_enabled()) return;
     const c10::TensorImpl* t = tensor(o);
@@ -592,13 +630,13 @@ struct Attn {
   }
 };
 
-template <typename F>
-PyObject* guarded_ops(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t want, F&& body) {
+template <typename S = Ops, typename F>
+PyObject* guarded_ops(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t want, F&& body, const char* name = kOpsName) {
   if (nargs != want) {
     PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", want, nargs);
     return nullptr;
   }
-  const Ops* s = static_cast<const Ops*>(PyCapsule_GetPointer(args[0], kOpsName));
+  const S* s = static_cast<const S*>(PyCapsule_GetPointer(args[0], name));
   if (s == nullptr) return nullptr;
   int status = -1;
   try {
@@ -616,7 +654,7 @@ PyObject* guarded_ops(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t want, 
 // ops, device, stream, q, k, v, window, sinks, causal, scale, q_len, k_len, out, lse, workspace
 PyObject* py_window_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded_ops(p, n, 15, [&](const Ops& s) -> int {
-    Attn c(s, p[1]);
+    Attn c(s.host, p[1]);
     const hipStream_t st = c.stream(p[2]);
     caddtree_attention_t a = {};
     const c10::ScalarType t = c.queries(p[3], &a);
@@ -646,7 +684,7 @@ PyObject* py_window_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
 // workspace
 PyObject* py_cache_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded_ops(p, n, 19, [&](const Ops& s) -> int {
-    Attn c(s, p[1]);
+    Attn c(s.host, p[1]);
     const hipStream_t st = c.stream(p[2]);
     const caddtree_cache_t* cache = c.cache(p[3]);
     if (!c.ok) return -1;
@@ -691,7 +729,7 @@ PyObject* py_cache_attention(PyObject*, PyObject* const* p, Py_ssize_t n) {
 // ops, device, stream, cache, k, v, page_table, start, count, index
 PyObject* py_cache_write(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded_ops(p, n, 10, [&](const Ops& s) -> int {
-    Attn c(s, p[1]);
+    Attn c(s.host, p[1]);
     const hipStream_t st = c.stream(p[2]);
     const caddtree_cache_t* cache = c.cache(p[3]);
     if (!c.ok) return -1;
@@ -715,7 +753,7 @@ PyObject* py_cache_write(PyObject*, PyObject* const* p, Py_ssize_t n) {
 // ops, device, stream, cache, k, v, page_table, start, end
 PyObject* py_cache_read(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded_ops(p, n, 9, [&](const Ops& s) -> int {
-    Attn c(s, p[1]);
+    Attn c(s.host, p[1]);
     const hipStream_t st = c.stream(p[2]);
     const caddtree_cache_t* cache = c.cache(p[3]);
     if (!c.ok) return -1;
@@ -737,7 +775,7 @@ PyObject* py_cache_read(PyObject*, PyObject* const* p, Py_ssize_t n) {
 // ops, device, stream, cache, q, page_table, ctx_len, lse, scores, new_scores, weight, count, depth, window, sinks, scale
 PyObject* py_cache_score(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded_ops(p, n, 16, [&](const Ops& s) -> int {
-    Attn c(s, p[1]);
+    Attn c(s.host, p[1]);
     const hipStream_t st = c.stream(p[2]);
     const caddtree_cache_t* cache = c.cache(p[3]);
     if (!c.ok) return -1;
@@ -759,7 +797,7 @@ PyObject* py_cache_score(PyObject*, PyObject* const* p, Py_ssize_t n) {
 // workspace
 PyObject* py_cache_evict(PyObject*, PyObject* const* p, Py_ssize_t n) {
   return guarded_ops(p, n, 15, [&](const Ops& s) -> int {
-    Attn c(s, p[1]);
+    Attn c(s.host, p[1]);
     const hipStream_t st = c.stream(p[2]);
     const caddtree_cache_t* cache = c.cache(p[3]);
     if (!c.ok) return -1;
@@ -806,10 +844,166 @@ PyObject* py_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return cap;
 }
 
+// ---------------------------------------------------------------- logits
+
+struct LogitsOps {
+  bool host;
+  decltype(&caddtree_adjust_logits) adjust;
+  decltype(&caddtree_verify_tree) verify;
+  decltype(&caddtree_distill) distill;
+  decltype(&caddtree_distill_grad) grad;
+};
+const char* const kLogitsName = "caddtree.logits_ops";
+
+template <typename F>
+PyObject* guarded_logits(PyObject* const* args, Py_ssize_t nargs, Py_ssize_t want, F&& body) {
+  return guarded_ops<LogitsOps>(args, nargs, want, body, kLogitsName);
+}
+
+// ops, device, stream, logits, out, history, history_len, repetition, presence, frequency, bias_ids, bias, allowed, token_ids,
+// parent, count, fill
+PyObject* py_adjust_logits(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_logits(p, n, 17, [&](const LogitsOps& s) -> int {
+    Attn c(s.host, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    caddtree_adjust_t a = {};
+    const c10::ScalarType t = c.logits(p[3], &a);
+    if (!c.ok) return -1;
+    a.out = c.rows(p[4], t, {a.B, a.T, a.V}, true);
+    if ((p[5] == Py_None && p[6] != Py_None) || (p[10] == Py_None) != (p[11] == Py_None) || (p[13] == Py_None) != (p[14] == Py_None))
+      return -1;
+    a.history = as<int32_t>(c.array(p[5], c10::kInt, {a.B, kAny}, false));
+    if (c.ok && a.history) a.H = (int32_t)c.size(p[5], 1);
+    a.history_len = as<int32_t>(c.array(p[6], c10::kInt, {a.B}, false));
+    a.repetition = as<float>(c.array(p[7], c10::kFloat, {a.B}, false));
+    a.presence = as<float>(c.array(p[8], c10::kFloat, {a.B}, false));
+    a.frequency = as<float>(c.array(p[9], c10::kFloat, {a.B}, false));
+    a.bias_ids = as<int32_t>(c.array(p[10], c10::kInt, {a.B, kAny}, false));
+    if (c.ok && a.bias_ids) a.n_bias = (int32_t)c.size(p[10], 1);
+    a.bias = as<float>(c.array(p[11], c10::kFloat, {a.B, a.n_bias}, false));
+    if (!c.ok) return -1;
+    if (p[12] != Py_None) {
+      c10::TensorImpl* m = c.tensor(p[12]);
+      if (m == nullptr) return -1;
+      const c10::ScalarType mt = c10::typeMetaToScalarType(m->dtype());
+      if (mt != c10::kInt && mt != c10::kUInt32) return -1;
+      const caddtree_rows_t w = c.rows(p[12], mt, {a.B, a.T, (a.V + 31) / 32});
+      a.allowed = w.data;
+      a.allowed_stride_b = w.stride_b;
+      a.allowed_stride_t = w.stride_t;
+    }
+    a.token_ids = as<int32_t>(c.array(p[13], c10::kInt, {a.B, a.T - 1}, false));
+    a.parent = as<int32_t>(c.array(p[14], c10::kInt, {a.B, a.T - 1}, false));
+    a.count = as<int32_t>(c.array(p[15], c10::kInt, {a.B}, false));
+    if (p[16] == Py_None) return -1;
+    a.fill = c.scale(p[16], 1);
+    if (!c.ok) return -1;
+    return unlocked([&] { return s.adjust(&a, st); });
+  });
+}
+
+// ops, device, stream, logits, token_ids, parent, count, accepted, index, tokens, chosen, weight, workspace
+PyObject* py_verify_tree(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_logits(p, n, 13, [&](const LogitsOps& s) -> int {
+    Attn c(s.host, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    caddtree_verify_t a = {};
+    if ((p[3] == Py_None) == (p[10] == Py_None)) return -1;
+    if (p[3] != Py_None) {
+      c.logits(p[3], &a);
+    } else {
+      a.chosen = as<int32_t>(c.array(p[10], c10::kInt, {kAny, kAny}));
+      if (!c.ok) return -1;
+      a.B = (int32_t)c.size(p[10], 0);
+      a.T = (int32_t)c.size(p[10], 1);
+      a.V = 1;
+    }
+    if (!c.ok) return -1;
+    a.token_ids = as<int32_t>(c.array(p[4], c10::kInt, {a.B, a.T - 1}));
+    a.parent = as<int32_t>(c.array(p[5], c10::kInt, {a.B, a.T - 1}));
+    a.count = as<int32_t>(c.array(p[6], c10::kInt, {a.B}));
+    a.accepted = as<int32_t>(c.array(p[7], c10::kInt, {a.B}));
+    a.index = as<int32_t>(c.array(p[8], c10::kInt, {a.B, kAny}));
+    if (!c.ok) return -1;
+    a.M = (int32_t)c.size(p[8], 1);
+    a.tokens = as<int32_t>(c.array(p[9], c10::kInt, {a.B, a.M}));
+    a.weight = as<float>(c.array(p[11], c10::kFloat, {a.B, a.T}, false));
+    size_t bytes;
+    void* ws = c.workspace(p[12], &bytes);
+    if (!c.ok) return -1;
+    return unlocked([&] { return s.verify(&a, ws, bytes, st); });
+  });
+}
+
+// what both distillation calls take
+bool distill_tensors(Attn& c, PyObject* logits, PyObject* ids, PyObject* target, PyObject* grad, PyObject* stats, PyObject* weight,
+                     PyObject* temperature, PyObject* tail, caddtree_distill_t* a) {
+  const c10::ScalarType t = c.logits(logits, a);
+  if (!c.ok) return false;
+  a->ids = as<int32_t>(c.array(ids, c10::kInt, {a->B, a->T, kAny}));
+  if (!c.ok) return false;
+  a->K = (int32_t)c.size(ids, 2);
+  a->target = as<float>(c.array(target, c10::kFloat, {a->B, a->T, a->K}));
+  if (grad != Py_None) a->grad = c.rows(grad, t, {a->B, a->T, a->V}, true);
+  a->stats = as<float>(c.array(stats, c10::kFloat, {a->B, a->T, 3}, false));
+  a->weight = as<float>(c.array(weight, c10::kFloat, {a->B, a->T}, false));
+  a->temperature = c.scale(temperature, 1);
+  a->tail = c.truth(tail);
+  if (temperature == Py_None) c.ok = false;
+  return c.ok;
+}
+
+// ops, device, stream, logits, ids, target, loss, grad, stats, weight, temperature, tail, workspace
+PyObject* py_distill(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_logits(p, n, 13, [&](const LogitsOps& s) -> int {
+    Attn c(s.host, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    caddtree_distill_t a = {};
+    if (!distill_tensors(c, p[3], p[4], p[5], p[7], p[8], p[9], p[10], p[11], &a)) return -1;
+    a.loss = as<float>(c.array(p[6], c10::kFloat, {a.B, a.T}));
+    size_t bytes;
+    void* ws = c.workspace(p[12], &bytes);
+    if (!c.ok) return -1;
+    return unlocked([&] { return s.distill(&a, ws, bytes, st); });
+  });
+}
+
+// ops, device, stream, logits, ids, target, stats, grad, weight, temperature, tail
+PyObject* py_distill_grad(PyObject*, PyObject* const* p, Py_ssize_t n) {
+  return guarded_logits(p, n, 11, [&](const LogitsOps& s) -> int {
+    Attn c(s.host, p[1]);
+    const hipStream_t st = c.stream(p[2]);
+    caddtree_distill_t a = {};
+    if (p[6] == Py_None || p[7] == Py_None || !distill_tensors(c, p[3], p[4], p[5], p[7], p[6], p[8], p[9], p[10], &a)) return -1;
+    return unlocked([&] { return s.grad(&a, st); });
+  });
+}
+
+// host, the addresses of adjust_logits, verify_tree, distill, distill_grad
+PyObject* py_logits_ops(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  if (n != 5) {
+    PyErr_Format(PyExc_TypeError, "5 arguments expected, got %zd", n);
+    return nullptr;
+  }
+  uint64_t v[5];
+  for (int i = 0; i < 5; ++i) {
+    v[i] = PyLong_AsUnsignedLongLongMask(a[i]);
+    if (PyErr_Occurred()) return nullptr;
+  }
+  LogitsOps* s = new LogitsOps{v[0] != 0, reinterpret_cast<decltype(LogitsOps::adjust)>(v[1]),
+                               reinterpret_cast<decltype(LogitsOps::verify)>(v[2]),
+                               reinterpret_cast<decltype(LogitsOps::distill)>(v[3]),
+                               reinterpret_cast<decltype(LogitsOps::grad)>(v[4])};
+  PyObject* cap = PyCapsule_New(s, kLogitsName, [](PyObject* o) { delete static_cast<LogitsOps*>(PyCapsule_GetPointer(o, kLogitsName)); });
+  if (cap == nullptr) delete s;
+  return cap;
+}
+
 #define CALL(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(py_##name)), METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {CALL(spec), CALL(build), CALL(reduce_topk), CALL(expand), CALL(emit), CALL(accept),
                            CALL(ops), CALL(window_attention), CALL(cache_attention), CALL(cache_write), CALL(cache_read),
-                           CALL(cache_score), CALL(cache_evict),
+                           CALL(cache_score), CALL(cache_evict), CALL(logits_ops), CALL(adjust_logits), CALL(verify_tree),
+                           CALL(distill), CALL(distill_grad),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
