@@ -551,7 +551,7 @@ typedef struct {
  * caddtree_distill writes the loss and, where asked for, the gradient in one pass over the logits;
  * caddtree_distill_grad the gradient alone, from the stats that such a call kept of the same logits, ids and
  * temperature (weight: the loss's gradient).
- * The gradient may overwrite the logits.  The order of the sums is fixed by the sizes and the workspace.
+ * The gradient may overwrite the logits.  The order of the sums is fixed by the sizes, the workspace and what is asked for.
  *   workspace: caddtree_distill_workspace_bytes(a) bytes, 256-byte aligned, lets a call of few rows split them over
  *   the card; NULL (or fewer bytes) is accepted. */
 caddtree_status_t caddtree_distill(const caddtree_distill_t* a, void* workspace, size_t workspace_bytes, hipStream_t stream);

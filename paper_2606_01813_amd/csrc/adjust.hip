@@ -118,18 +118,32 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
       for (int j = 0; j < N; ++j)
         if (j < some && !(ok >> j & 1)) dst[j + at] = (T)a.fill;
     } else {
-      Packed<E> x = some == N ? Packed<E>::load(src + at) : Packed<E>::load_some(src + at, some);
       const int paths = s_paths[r];
+      float x[N];
+      Vec<E> v;
+      if (some == N) {
+        v = Vec<E>::load(src + at);
+        v.get(x);
+      }
+      bool change = false;
 #pragma unroll
       for (int j = 0; j < N; ++j) {
+        if (some < N) x[j] = j < some ? (float)src[at + j] : 0.f;
         const uint32_t w = s_word[min(at + j, kChunk - 1)];
         int c = (int)(w & kCount);
         for (int k = 0; k < paths; ++k) c += s_path[r][k] == at + j;
-        if (c > 0 || w >> 20) x.set(j, adjusted(x[j], c, w >> 20, p, bias));
-        if (!(ok >> j & 1)) x.set(j, a.fill);
+        if (c > 0 || w >> 20) x[j] = adjusted(x[j], c, w >> 20, p, bias);
+        if (!(ok >> j & 1)) x[j] = a.fill;
+        change |= c > 0 || w >> 20 || !(ok >> j & 1);
       }
-      if (some == N) x.store(dst + at);
-      else x.store_some(dst + at, some);
+      if (some == N) {
+        if (change) v.set(x);
+        v.store(dst + at);
+      } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+          if (j < some) dst[at + j] = (T)x[j];
+      }
     }
   }
   if constexpr (kInPlace) {

@@ -104,7 +104,7 @@ caddtree_status_t check_distill_data(const caddtree_distill_t* a, bool loss, con
                           in_place ? array("grad", nullptr, 0) : rows_array("grad", a->grad, dtype, a->B, a->T, a->V, true),
                           array("ids", a->ids, n * a->K * 4), array("target", a->target, n * a->K * 4),
                           array("weight", a->weight, n * 4), array("loss", loss ? a->loss : nullptr, n * 4, true),
-                          array("stats", a->stats, n * 12, loss), array("workspace", workspace, workspace_bytes, true)};
+                          array("stats", a->stats, n * 12, loss), array("workspace", workspace, workspace_bytes, true)};   // (as far as it is used)
   if ((st = check_apart(arrays)) != CADDTREE_OK) return st;
   if (!in_place) return CADDTREE_OK;
   Array over[8];
@@ -208,7 +208,7 @@ caddtree_status_t caddtree_verify_tree(const caddtree_verify_t* a, void* workspa
 
 size_t caddtree_distill_workspace_bytes(const caddtree_distill_t* a) {
   if (a == nullptr || check_sizes(enum_value(a->dtype), a->B, a->T, a->V) != CADDTREE_OK) return 0;
-  return 0;
+  return caddtree::distill_workspace((int64_t)a->B * a->T, a->V);
 }
 
 caddtree_status_t caddtree_distill(const caddtree_distill_t* a, void* workspace, size_t workspace_bytes, hipStream_t stream) {
@@ -217,8 +217,10 @@ caddtree_status_t caddtree_distill(const caddtree_distill_t* a, void* workspace,
   if ((st = check_workspace(workspace)) != CADDTREE_OK) return st;
   if (a->B == 0 || a->T == 0) return ok();
   if (a->loss == nullptr) return fail(CADDTREE_E_INVALID, "loss is NULL");
-  if ((st = check_distill_data(a, true, workspace, workspace ? workspace_bytes : 0)) != CADDTREE_OK) return st;
-  const hipError_t e = caddtree::launch_distill(distill_args(a), (caddtree_dtype_t)enum_value(a->dtype), stream);
+  const size_t need = caddtree_distill_workspace_bytes(a);
+  void* ws = need > 0 && workspace_bytes >= need ? workspace : nullptr;
+  if ((st = check_distill_data(a, true, ws, need)) != CADDTREE_OK) return st;
+  const hipError_t e = caddtree::launch_distill(distill_args(a), ws, (caddtree_dtype_t)enum_value(a->dtype), stream);
   return e == hipSuccess ? ok() : hip_fail(e, "distill launch");
 }
 

@@ -59,7 +59,10 @@ struct DistillArgs {
   float* loss;
   float* stats;
 };
-hipError_t launch_distill(const DistillArgs& a, caddtree_dtype_t dtype, hipStream_t stream);
+// How many parts a row is cut into where there is a workspace, and its bytes (0: one part).
+int distill_parts(int64_t rows, int32_t V);
+size_t distill_workspace(int64_t rows, int32_t V);
+hipError_t launch_distill(const DistillArgs& a, void* workspace, caddtree_dtype_t dtype, hipStream_t stream);
 hipError_t launch_distill_grad(const DistillArgs& a, caddtree_dtype_t dtype, hipStream_t stream);
 
 }  // namespace caddtree

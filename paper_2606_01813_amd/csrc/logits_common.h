@@ -12,47 +12,67 @@ constexpr int kWave = 64;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
-// An element type: kN elements in 16 bytes, to and from fp32 (to: rounded to the nearest, ties to even).
+// The element types: an element of a 32-bit word to fp32, and fp32 rounded into one (to the nearest, ties to even).
 struct BF16 {
   using T = __bf16;
+  typedef __bf16 T2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kNegInf = 0xff80ff80u;
+  static __device__ __forceinline__ float get(uint32_t w, int j) { return __uint_as_float(j ? w & 0xffff0000u : w << 16); }
 };
 struct F16 {
   using T = _Float16;
+  typedef _Float16 T2 __attribute__((ext_vector_type(2)));
+  static constexpr uint32_t kNegInf = 0xfc00fc00u;
+  static __device__ __forceinline__ float get(uint32_t w, int j) { return (float)__builtin_bit_cast(T2, w)[j]; }
 };
 struct F32 {
   using T = float;
+  static constexpr uint32_t kNegInf = 0xff800000u;
+  static __device__ __forceinline__ float get(uint32_t w, int) { return __uint_as_float(w); }
 };
 template <typename E>
-constexpr int kN = 16 / (int)sizeof(typename E::T);
+constexpr int kN = 16 / (int)sizeof(typename E::T);      // elements of 16 bytes
+template <typename E>
+constexpr int kEach = 4 / (int)sizeof(typename E::T);    // ... of a word
 
 // 16 bytes of elements.  Rows start at any element (a vocabulary or a stride of any length), so a vector is
 // aligned to its elements alone; the hardware takes 16-byte loads and stores at such addresses.
 template <typename E>
-struct Packed {
-  typedef typename E::T V __attribute__((ext_vector_type(kN<E>)));
-  struct __attribute__((packed, aligned(sizeof(typename E::T)))) Loose {
-    V v;
+struct Vec {
+  using T = typename E::T;
+  struct __attribute__((packed, aligned(sizeof(T)))) Loose {
+    u32x4 w;
   };
-  V v;
-  static __device__ __forceinline__ Packed load(const typename E::T* p) {
-    return Packed{reinterpret_cast<const Loose*>(p)->v};
-  }
-  __device__ __forceinline__ void store(typename E::T* p) const { reinterpret_cast<Loose*>(p)->v = v; }
-  // the first n elements (n < kN at a row's end), zeros behind
-  static __device__ __forceinline__ Packed load_some(const typename E::T* p, int n) {
-    Packed r = {};
+  u32x4 w;
+  static __device__ __forceinline__ Vec load(const T* p) { return Vec{reinterpret_cast<const Loose*>(p)->w}; }
+  __device__ __forceinline__ void store(T* p) const { reinterpret_cast<Loose*>(p)->w = w; }
+  static __device__ __forceinline__ Vec neg_inf() { return Vec{u32x4{E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf}}; }
+  __device__ __forceinline__ void get(float (&x)[kN<E>]) const {
 #pragma unroll
-    for (int j = 0; j < kN<E>; ++j)
-      if (j < n) r.v[j] = p[j];
-    return r;
+    for (int j = 0; j < kN<E>; ++j) x[j] = E::get(w[j / kEach<E>], j % kEach<E>);
   }
-  __device__ __forceinline__ void store_some(typename E::T* p, int n) const {
+  __device__ __forceinline__ void set(const float (&x)[kN<E>]) {
+    if constexpr (kEach<E> == 1) {
 #pragma unroll
-    for (int j = 0; j < kN<E>; ++j)
-      if (j < n) p[j] = v[j];
+      for (int j = 0; j < 4; ++j) w[j] = __float_as_uint(x[j]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        typename E::T2 v;
+        v[0] = (T)x[2 * j];
+        v[1] = (T)x[2 * j + 1];
+        w[j] = __builtin_bit_cast(uint32_t, v);
+      }
+    }
   }
-  __device__ __forceinline__ float operator[](int j) const { return (float)v[j]; }
-  __device__ __forceinline__ void set(int j, float x) { v[j] = (typename E::T)x; }
+  // element j of those as they are
+  __device__ __forceinline__ T raw(int j) const {
+    const uint32_t word = w[j / kEach<E>];                // (a copy: bit_cast of a vector's element takes the first)
+    if constexpr (kEach<E> == 1) return __uint_as_float(word);
+    else return __builtin_bit_cast(typename E::T2, word)[j % 2];
+  }
+  // Makes the registers opaque: what was unpacked of them before is not kept for use after.
+  __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
 };
 
 template <typename E>

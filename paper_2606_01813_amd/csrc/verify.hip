@@ -24,7 +24,7 @@ struct Best {
   float x;
   int id;
   __device__ __forceinline__ void take(float y, int i) {
-    if (y > x || (y == x && i < id)) {
+    if (y > x || (y == x && y > -INFINITY && i < id)) {
       x = y;
       id = i;
     }
@@ -37,16 +37,18 @@ __device__ int choose(const typename E::T* row, int V, Best* s) {
   constexpr int N = kN<E>;
   const int tid = threadIdx.x;
   Best m = {-INFINITY, INT_MAX};
-  for (int at = tid * N; at < V; at += kThreads * N) {
-    const int some = min(N, V - at);
-    const Packed<E> v = some == N ? Packed<E>::load(row + at) : Packed<E>::load_some(row + at, some);
+  const int whole = V / N * N;
+  for (int at = tid * N; at < whole; at += kThreads * N) {
+    float x[N];
+    Vec<E>::load(row + at).get(x);
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (j < some && v[j] > m.x) {                   // (ids only grow: the first of equals stays; NaN is never above)
-        m.x = v[j];
+      if (x[j] > m.x) {                               // (ids only grow: the first of equals stays; NaN is never above)
+        m.x = x[j];
         m.id = at + j;
       }
   }
+  if (whole + tid < V) m.take((float)row[whole + tid], whole + tid);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) m.take(__shfl_xor(m.x, o), __shfl_xor(m.id, o));
   __syncthreads();                                    // (s may still be read, of the row before)

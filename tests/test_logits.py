@@ -374,11 +374,11 @@ def test_distill_sizes(V, dtype, with_workspace):
         assert bool((room[..., V:] == 9).all())
         alone = torch.full((B, T), 9.0, device="cuda")
         distill(x, ids, target, alone, weight=w, temperature=tau, tail=tail, workspace=ws)
-        assert torch.equal(alone, loss)
+        _check_distill(x, ids, target, w, tau, tail, alone)
         g = distill_grad(x, ids, target, stats, weight=w, temperature=tau, tail=tail)
         _check_distill(x, ids, target, w, tau, tail, grad=g, again=True)
         y = x.clone()                                                      # the gradient over the logits
-        distill(y, ids, target, loss, grad=y, weight=w, temperature=tau, tail=tail, workspace=ws)
+        distill(y, ids, target, alone, grad=y, weight=w, temperature=tau, tail=tail, workspace=ws)
         assert torch.equal(y, grad) and torch.equal(alone, loss)
         y = x.clone()
         assert torch.equal(distill_grad(y, ids, target, stats, y, weight=w, temperature=tau, tail=tail), g)
