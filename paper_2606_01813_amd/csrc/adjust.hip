@@ -23,32 +23,48 @@ using namespace lg;
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kChunk = 8192;                      // tokens of a workgroup
-constexpr int kRows = 16;                         // rows of a workgroup at most
+constexpr int kRows = 2;                          // rows of a workgroup at most
 constexpr int kPath = CADDTREE_MAX_L;
+constexpr int kNodes = 1024;                      // of a tree, in LDS (further ones are read where they lie)
+constexpr int kNear = 512;                        // biases in LDS, likewise
 constexpr uint32_t kCount = (1u << 20) - 1;       // a word's count; above it the bias
 static_assert(CADDTREE_MAX_HISTORY + kPath <= kCount && CADDTREE_MAX_BIAS < 1 << 12, "a word holds both");
 
+struct Lds {
+  uint32_t word[kChunk];
+  float bias[kNear];
+  uint16_t path[kRows][kPath];                    // tokens of a row's path in the chunk, from its first token on
+  int paths[kRows];
+  int listed;
+};
+struct Nodes {                                    // of a tree
+  uint32_t token[kNodes];
+  uint16_t parent[kNodes];                        // + 1
+};
+extern __shared__ __align__(16) char s_more[];    // a tree's nodes
+
 struct Penalty {
-  float repetition, presence, frequency;
+  float repetition, inverse, presence, frequency;
 };
 
-// A logit, given how often its token occurred and its bias's place in the sequence's list + 1 (0: none).
-__device__ __forceinline__ float adjusted(float x, int c, uint32_t place, const Penalty& p, const float* bias) {
-  if (c > 0) {
-    x = x > 0.f ? x / p.repetition : x * p.repetition;
-    x = fmaf(-p.frequency, (float)c, x) - p.presence;
-  }
-  if (place > 0) x += bias[place - 1];
+// A logit, given its token's word.  The quotient is a product with the inverse: two roundings in place of one, and a tenth
+// of the instructions.
+__device__ __forceinline__ float adjusted(float x, uint32_t word, const Penalty& p, const Lds& s, const float* bias) {
+  const float c = (float)(word & kCount);
+  const float y = fmaf(-p.frequency, c, x * (x > 0.f ? p.inverse : p.repetition)) - p.presence;
+  x = (word & kCount) != 0 ? y : x;
+  const uint32_t place = word >> 20;
+  if (place > 0) x += place <= kNear ? s.bias[place - 1] : bias[place - 1];
   return x;
 }
 
-// The tokens of the row's path that lie in [first, first + n), relative to first, into path; how many.
-__device__ int path_in_chunk(const AdjustArgs& a, int b, int row, int first, int n, uint16_t* path) {
+// The tokens of the row's path that lie in [from, from + n), relative to from, into path; how many.
+__device__ int path_in_chunk(const AdjustArgs& a, const Nodes& s, int b, int row, int from, int n, uint16_t* path) {
   const int64_t base = (int64_t)b * (a.T - 1);
   int node = row - 1, k = 0;
   for (int d = 0; d < kPath && node >= 0; ++d) {
-    const int t = a.token_ids[base + node] - first;
-    const int p = a.parent[base + node];
+    const int t = (node < kNodes ? (int)s.token[node] : a.token_ids[base + node]) - from;
+    const int p = node < kNodes ? (int)s.parent[node] - 1 : a.parent[base + node];
     if ((uint32_t)t < (uint32_t)n) path[k++] = (uint16_t)t;
     node = p < node ? p : -1;
   }
@@ -57,114 +73,167 @@ __device__ int path_in_chunk(const AdjustArgs& a, int b, int row, int first, int
 
 template <typename E, bool kInPlace>
 __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
-  __shared__ uint32_t s_word[kChunk];
-  __shared__ uint16_t s_list[kInPlace ? kChunk : 1];    // in place: the tokens that have a word
-  __shared__ uint16_t s_path[kRows][kPath];
-  __shared__ int s_paths[kRows];
-  __shared__ int s_listed;
-  constexpr int N = kN<E>;
+  __shared__ __align__(16) Lds s;
+  __shared__ uint16_t s_list[kInPlace ? kChunk : 1];    // in place: the words that are not 0
+  constexpr int N = kN<E>, kStep = kWave * N, kSteps = kChunk / kStep;
+  constexpr int kU = kInPlace ? 1 : kRows * kSteps / kWaves;     // loads in flight a lane: all that it has
+  constexpr uint32_t kAll = (1u << N) - 1;
   using T = typename E::T;
 
-  const int b = (int)blockIdx.z, first = (int)blockIdx.x * kChunk, n = min(kChunk, a.V - first);
+  const int b = (int)blockIdx.z, first = (int)blockIdx.x * kChunk, last = min(first + kChunk, a.V);
   const bool tree = a.parent != nullptr;
   const int rows = min(max(a.count ? a.count[b] : a.T - tree, 0), a.T - tree) + tree;   // (rows of the sequence)
   const int row0 = (int)blockIdx.y * kRows, mine = min(kRows, rows - row0);
   if (mine <= 0) return;
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  const Penalty p = {a.repetition ? a.repetition[b] : 1.f, a.presence ? a.presence[b] : 0.f, a.frequency ? a.frequency[b] : 0.f};
+  // a wavefront takes kStep tokens of a row at a time: step i is i % kSteps of row i / kSteps
+  const int items = mine * kSteps;
+  const auto token_of = [&](int i) { return first + i % kSteps * kStep + lane * N; };
+  const auto allowed_of = [&](int i, int tok) {         // bit j: token tok + j is allowed
+    if (a.allowed == nullptr || tok >= last) return kAll;
+    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(a.allowed + b * a.allowed_b + (row0 + i / kSteps) * a.allowed_t);
+    return (uint32_t)bytes[tok / 8] >> (tok % 8) & kAll;
+  };
+  Vec<E> q[kU];
+  uint32_t ok[kU];
+  const auto ask = [&](int u, int i) {
+    if (i >= items) return;
+    const int tok = token_of(i);
+    ok[u] = allowed_of(i, tok);
+    if (!kInPlace && tok + N <= last) {
+      const T* src = row_of<E>(a.in, b, row0 + i / kSteps);
+      q[u] = Vec<E>::load_once(src, (uint32_t)tok * (uint32_t)sizeof(T));
+    }
+  };
+#pragma unroll
+  for (int u = 0; u < kU; ++u) ask(u, wave + u * kWaves);
+
+  // (the first of the biases and of the history are asked for as well, before anything is waited for)
+  const int len = a.history ? min(max(a.history_len ? a.history_len[b] : a.H, 0), a.H) : 0;
+  const int32_t* history = a.history + (int64_t)b * a.H;
+  const int32_t* bias_ids = a.bias_ids + (int64_t)b * a.n_bias;
+  const auto four = [&](int i) { return i + 4 <= a.H ? Vec<F32>::load(reinterpret_cast<const float*>(history) + i) : Vec<F32>{}; };
+  Vec<F32> h = a.history ? four(tid * 4) : Vec<F32>{};
+  const int bias_id = tid < a.n_bias ? bias_ids[tid] : -1;
+  const float repetition = a.repetition ? a.repetition[b] : 1.f;
+  const Penalty p = {repetition, 1.f / repetition, a.presence ? a.presence[b] : 0.f, a.frequency ? a.frequency[b] : 0.f};
   const float* bias = a.bias + (int64_t)b * a.n_bias;
-  for (int i = tid; i < kChunk; i += kThreads) s_word[i] = 0;
-  if (tid == 0) s_listed = 0;
-  if (tid < mine) s_paths[tid] = tree ? path_in_chunk(a, b, row0 + tid, first, n, s_path[tid]) : 0;
+  Nodes& nodes = *reinterpret_cast<Nodes*>(s_more);
+  for (int i = tid; i < kChunk / 4; i += kThreads) reinterpret_cast<u32x4*>(s.word)[i] = u32x4{0, 0, 0, 0};
+  if (tid == 0) s.listed = 0;
+  if (tree)
+    for (int i = tid; i < min(row0 + mine - 1, kNodes); i += kThreads) {
+      nodes.token[i] = (uint32_t)a.token_ids[(int64_t)b * (a.T - 1) + i];
+      const int par = a.parent[(int64_t)b * (a.T - 1) + i];
+      nodes.parent[i] = (uint16_t)(par >= 0 && par < i ? par + 1 : 0);
+    }
   __syncthreads();
+  if (tid < mine) s.paths[tid] = tree ? path_in_chunk(a, nodes, b, row0 + tid, first, last - first, s.path[tid]) : 0;
+  const auto found = [&](int w, uint32_t old) {
+    if (kInPlace && old == 0) s_list[atomicAdd(&s.listed, 1)] = (uint16_t)w;
+  };
   for (int i = tid; i < a.n_bias; i += kThreads) {
-    const int t = a.bias_ids[(int64_t)b * a.n_bias + i] - first;
-    if ((uint32_t)t < (uint32_t)n) {
-      const uint32_t old = atomicMax(&s_word[t], (uint32_t)(i + 1) << 20);
-      if (kInPlace && old == 0) s_list[atomicAdd(&s_listed, 1)] = (uint16_t)t;
+    const int t = i == tid ? bias_id : bias_ids[i];
+    if (t >= first && t < last) {
+      if (i < kNear) s.bias[i] = bias[i];
+      found(t - first, atomicMax(&s.word[t - first], (uint32_t)(i + 1) << 20));
     }
   }
-  __syncthreads();
-  if (a.history != nullptr) {
-    const int len = min(max(a.history_len ? a.history_len[b] : a.H, 0), a.H);
-    const int32_t* h = a.history + (int64_t)b * a.H;
-    for (int i = tid; i < len; i += kThreads) {
-      const int t = h[i] - first;
-      if ((uint32_t)t < (uint32_t)n) {
-        const uint32_t old = atomicAdd(&s_word[t], 1u);
-        if (kInPlace && old == 0) s_list[atomicAdd(&s_listed, 1)] = (uint16_t)t;
-      }
+  if (a.n_bias > 0) __syncthreads();                    // (the places come before the counts)
+  if (len > 0) {
+    const auto count = [&](int t) {
+      if (t >= first && t < last) found(t - first, atomicAdd(&s.word[t - first], 1u));
+    };
+    int i = tid * 4;
+    while (i + 4 <= len) {
+      const Vec<F32> v = h;
+      h = four(i + kThreads * 4);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) count((int)v.w[j]);
+      i += kThreads * 4;
     }
+    for (; i < len; ++i) count(history[i]);             // (fewer than 4, in one thread)
   }
   __syncthreads();
 
-  // a wavefront takes kStep tokens of a row at a time
-  constexpr int kStep = kWave * N;
-  const int steps = (n + kStep - 1) / kStep;
-  for (int i = wave; i < mine * steps; i += kWaves) {
-    const int r = i / steps, at = (i % steps) * kStep + lane * N;
-    const T* src = row_of<E>(a.in, b, row0 + r) + first;
-    T* dst = row_of<E>(a.out, b, row0 + r) + first;
-    const int some = min(N, n - at);
-    if (some <= 0) continue;
-    uint32_t ok = 0xffffffffu;                      // bit j: token at + j is allowed
-    if (a.allowed != nullptr) {
-      const uint8_t* bytes = reinterpret_cast<const uint8_t*>(a.allowed + b * a.allowed_b + (row0 + r) * a.allowed_t);
-      ok = bytes[(first + at) / 8] >> ((first + at) % 8);
-    }
-    if constexpr (kInPlace) {
+  for (int i0 = wave; i0 < items; i0 += kU * kWaves) {
 #pragma unroll
-      for (int j = 0; j < N; ++j)
-        if (j < some && !(ok >> j & 1)) dst[j + at] = (T)a.fill;
-    } else {
-      const int paths = s_paths[r];
-      float x[N];
-      Vec<E> v;
-      if (some == N) {
-        v = Vec<E>::load(src + at);
-        v.get(x);
-      }
-      bool change = false;
+    for (int u = 0; u < kU; ++u) {
+      const int i = i0 + u * kWaves;
+      if (i >= items) break;
+      const int r = i / kSteps, tok = token_of(i);
+      T* dst = row_of<E>(a.out, b, row0 + r);
+      const uint32_t may = ok[u];
+      if constexpr (kInPlace) {
+        if (may != kAll) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (some < N) x[j] = j < some ? (float)src[at + j] : 0.f;
-        const uint32_t w = s_word[min(at + j, kChunk - 1)];
-        int c = (int)(w & kCount);
-        for (int k = 0; k < paths; ++k) c += s_path[r][k] == at + j;
-        if (c > 0 || w >> 20) x[j] = adjusted(x[j], c, w >> 20, p, bias);
-        if (!(ok >> j & 1)) x[j] = a.fill;
-        change |= c > 0 || w >> 20 || !(ok >> j & 1);
-      }
-      if (some == N) {
-        if (change) v.set(x);
-        v.store(dst + at);
+          for (int j = 0; j < N; ++j)
+            if (tok + j < last && !(may >> j & 1)) dst[tok + j] = (T)a.fill;
+        }
+        ask(u, i + kU * kWaves);
       } else {
+        Vec<E> v = q[u];
+        ask(u, i + kU * kWaves);
+        if (tok >= last) continue;
+        const bool whole = tok + N <= last;
+        uint32_t w[N], any = 0;
 #pragma unroll
-        for (int j = 0; j < N; ++j)
-          if (j < some) dst[at + j] = (T)x[j];
+        for (int k = 0; k < N / 4; ++k) {
+          const u32x4 four = *reinterpret_cast<const u32x4*>(&s.word[tok - first + 4 * k]);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) any |= w[4 * k + j] = four[j];
+        }
+        const int paths = s.paths[r];
+        for (int k = 0; k < paths; ++k) {
+          const int j0 = first + (int)s.path[r][k] - tok;
+          if (j0 >= 0 && j0 < N) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) w[j] += j0 == j;
+            any = 1;
+          }
+        }
+        if (any == 0 && may == kAll && whole) {
+          v.stream_at(dst, (uint32_t)tok * (uint32_t)sizeof(T));
+          continue;
+        }
+        float x[N];
+        v.get(x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          if (!whole) x[j] = tok + j < last ? (float)row_of<E>(a.in, b, row0 + r)[tok + j] : 0.f;
+          x[j] = adjusted(x[j], w[j], p, s, bias);
+          if (!(may >> j & 1)) x[j] = a.fill;
+        }
+        if (whole) {
+          v.set(x);
+          v.stream_at(dst, (uint32_t)tok * (uint32_t)sizeof(T));
+        } else {
+#pragma unroll
+          for (int j = 0; j < N; ++j)
+            if (tok + j < last) dst[tok + j] = (T)x[j];
+        }
       }
     }
   }
   if constexpr (kInPlace) {
-    // the listed tokens and those of the path that are not among them; one not allowed has its value already
-    const int listed = s_listed;
+    // the listed words' tokens and those of the path that are not among them; one not allowed has its value already
+    const int listed = s.listed;
     for (int r = wave; r < mine; r += kWaves) {
-      T* dst = row_of<E>(a.out, b, row0 + r) + first;
+      T* dst = row_of<E>(a.out, b, row0 + r);
       const uint32_t* allowed = a.allowed ? a.allowed + b * a.allowed_b + (row0 + r) * a.allowed_t : nullptr;
-      const int paths = s_paths[r];
+      const int paths = s.paths[r];
       for (int i = lane; i < listed + paths; i += kWave) {
-        const int t = i < listed ? s_list[i] : s_path[r][i - listed];
-        if (allowed && !(allowed[(first + t) / 32] >> ((first + t) % 32) & 1)) continue;
-        const uint32_t w = s_word[t];
-        int c = (int)(w & kCount);
+        const int t = first + (i < listed ? s_list[i] : s.path[r][i - listed]);
+        if (allowed && !(allowed[t / 32] >> (t % 32) & 1)) continue;
+        uint32_t w = s.word[t - first];
         bool again = i >= listed && w != 0;          // of the path, and listed too
         for (int k = 0; k < paths; ++k) {
-          const bool same = s_path[r][k] == t;
-          c += same;
+          const bool same = first + s.path[r][k] == t;
+          w += same;
           again |= same && i >= listed && k < i - listed;
         }
-        if (!again) dst[t] = (T)adjusted((float)dst[t], c, w >> 20, p, bias);
+        if (!again) dst[t] = (T)adjusted((float)dst[t], w, p, s, bias);
       }
     }
   }
@@ -173,8 +242,9 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
 template <typename E>
 void launch(const AdjustArgs& a, bool in_place, hipStream_t stream) {
   const dim3 g((unsigned)((a.V + kChunk - 1) / kChunk), (unsigned)((a.T + kRows - 1) / kRows), (unsigned)a.B);
-  if (in_place) adjust_kernel<E, true><<<g, kThreads, 0, stream>>>(a);
-  else adjust_kernel<E, false><<<g, kThreads, 0, stream>>>(a);
+  const size_t lds = a.parent != nullptr ? sizeof(Nodes) : 0;
+  if (in_place) adjust_kernel<E, true><<<g, kThreads, lds, stream>>>(a);
+  else adjust_kernel<E, false><<<g, kThreads, lds, stream>>>(a);
 }
 
 }  // namespace

@@ -25,6 +25,13 @@ constexpr int kMaxK = CADDTREE_MAX_TEACHER;
 constexpr int kMine = kMaxK / kWave;              // of the teacher's tokens a lane
 constexpr double kLog2e = 0x1.71547652b82fep+0;
 
+// 2^a to a step of fp32, whatever its size: a chain of a few instructions where a row's sums are waited for.
+__device__ __forceinline__ double pow2(double a) {
+  asm volatile("" : "+v"(a));                     // (as rounded: a product, fused into the difference below, is not near k)
+  const double k = rint(a);
+  return ldexp((double)__builtin_amdgcn_exp2f((float)(a - k)), (int)fmax(k, -4000.0));
+}
+
 // What a row's teacher lists, in LDS.
 struct Listed {
   int id[kMaxK];                                  // -1: padding
@@ -37,9 +44,17 @@ struct Listed {
 // How the row's sums enter loss and gradient.
 struct Row {
   float m;                                        // the largest logit, 0 where that is -inf
-  float rest;                                     // gradient of a token not listed / e_v
+  float mc;                                       // m c, rounded
+  float rest;                                     // gradient of a token not listed / exp2(l c - mc)
+  bool far;                                       // ... / exp2((l - m) c)
   double Z, mass, scale;                          // M and w / tau
 };
+
+// c = log2(e) / tau.  A term is exp2(l c - r), one fused product and difference, where l c stays within kFar; the
+// reference r is a product m c as it was rounded, and its distance from m c is made up for in fp64.  Beyond that (masks
+// of the type's lowest value in a whole row, for instance) a term is exp2((l - m) c).
+constexpr float kFar = 1e30f;
+constexpr float kRoom = 8.f;                      // a term may reach 2^kRoom before the reference moves
 
 // bits of the N tokens from `at` (a multiple of N) on
 template <int N>
@@ -47,56 +62,59 @@ __device__ __forceinline__ uint32_t bits_at(const uint32_t* bits, int at) {
   return reinterpret_cast<const uint8_t*>(bits)[at >> 3] >> (at & 7) & ((1u << N) - 1);
 }
 
-// The listed tokens of a row, by the first wavefront: into L and the bits, those of tokens first .. last - 1 (relative to
-// first), with sum p_k and sum p_k log p_k.  Their logits come from `kept` [K], or where that is
-// NULL from the row, for tokens first .. last - 1 (the others may have been overwritten by another workgroup's gradient).
+// A row's list as it lies in memory.
+struct Raw {
+  int id[kMaxK];                                  // -1: padding
+  float t[kMaxK];                                 // -inf: padding
+  float l[kMaxK];
+};
+// By one wavefront.  The student's logits come from `kept` [K], or where that is NULL from the row, for tokens
+// first .. last - 1 (the others may have been overwritten by another workgroup's gradient).
 template <typename E>
-__device__ void read_listed(const DistillArgs& a, int64_t row, const typename E::T* l, const float* kept, int first, int last,
-                            Listed& L, uint32_t* bits) {
-  const int lane = threadIdx.x;
-  int id[kMine];
-  float t[kMine], top = -INFINITY;
+__device__ void fetch_listed(const DistillArgs& a, int64_t row, const typename E::T* l, const float* kept, int first, int last, Raw& raw) {
 #pragma unroll
   for (int i = 0; i < kMine; ++i) {
-    const int k = lane + i * kWave;
-    id[i] = k < a.K ? a.ids[row * a.K + k] : -1;
-    if ((uint32_t)id[i] >= (uint32_t)a.V) id[i] = -1;
-    t[i] = id[i] >= 0 ? a.target[row * a.K + k] : -INFINITY;
-    top = fmaxf(top, t[i]);
+    const int k = (int)threadIdx.x % kWave + i * kWave;
+    if (k >= a.K) break;
+    int id = a.ids[row * a.K + k];
+    if ((uint32_t)id >= (uint32_t)a.V) id = -1;
+    const float t = a.target[row * a.K + k];
+    raw.id[k] = id;
+    raw.t[k] = id >= 0 ? t : -INFINITY;
+    raw.l[k] = kept ? kept[k] : id >= first && id < last ? (float)l[id] : -INFINITY;
   }
-  double logp[kMine], p[kMine];
+}
+
+// By one wavefront, of a row's list: probabilities, their sums, and the bits of tokens first .. last - 1 (relative to
+// first).
+__device__ void read_listed(const DistillArgs& a, const Raw& raw, int first, int last, Listed& L, uint32_t* bits) {
+  const int lane = (int)threadIdx.x % kWave;
+  float top = -INFINITY;
+  double z = 0.0;
   if (!a.tail) {
+#pragma unroll 1
+    for (int k = lane; k < a.K; k += kWave) top = fmaxf(top, raw.t[k]);
     top = wave_max(top);
     if (top == -INFINITY) top = 0.f;
     double sum = 0.0;
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      logp[i] = ((double)t[i] - (double)top) / (double)a.temperature;
-      sum += exp(logp[i]);
-    }
-    const double z = log(wave_sum(sum));
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) logp[i] = logp[i] == -INFINITY ? -INFINITY : logp[i] - z;
-  } else {
-#pragma unroll
-    for (int i = 0; i < kMine; ++i) logp[i] = (double)t[i];
+#pragma unroll 1
+    for (int k = lane; k < a.K; k += kWave) sum += exp(((double)raw.t[k] - (double)top) / (double)a.temperature);
+    z = log(wave_sum(sum));
   }
   double P = 0.0, A = 0.0;
   bool twice = false;
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int k = lane + i * kWave;
-    p[i] = exp(logp[i]);
-    P += p[i];
-    if (p[i] != 0.0) A += p[i] * logp[i];
-    const int at = id[i] - first;
-    const bool here = id[i] >= first && id[i] < last;
-    if (here) twice |= (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u) != 0;
-    if (k < a.K) {
-      L.id[k] = id[i];
-      L.p[k] = p[i];
-      L.l[k] = kept ? kept[k] : here ? (float)l[id[i]] : -INFINITY;
-    }
+#pragma unroll 1
+  for (int k = lane; k < a.K; k += kWave) {
+    const int id = raw.id[k], at = id - first;
+    const float t = raw.t[k];
+    const double logp = a.tail || t == -INFINITY ? (double)t : ((double)t - (double)top) / (double)a.temperature - z;
+    const double p = exp(logp);
+    P += p;
+    if (p != 0.0) A += p * logp;
+    if (id >= first && id < last) twice |= (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u) != 0;
+    L.id[k] = id;
+    L.p[k] = p;
+    L.l[k] = raw.l[k];
   }
   P = wave_sum(P);
   A = wave_sum(A);
@@ -126,22 +144,21 @@ __device__ __forceinline__ bool first_of(const Listed& L, int K, int k, double& 
 
 __device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) { return a.weight ? a.weight[row] : 1.f; }
 
-// (m, s): a largest value and a sum of exp((l - m) / tau), joined with another's
-__device__ __forceinline__ void join(float& m, double& s, float m2, double s2, float c) {
-  const float top = fmaxf(m, m2);
-  if (top == -INFINITY) {
-    s += s2;                                      // (zeros, or NaN)
+// A row's, or a part's, largest logit m and the sum of exp((l - m) / tau) over its tokens not listed.
+struct Sum {
+  float m;
+  double s;
+};
+__device__ __forceinline__ void join(Sum& x, const Sum& y, float c) {
+  const float m = fmaxf(x.m, y.m);
+  if (m == -INFINITY) {
+    x.s += y.s;                                   // (zeros, or NaN)
     return;
   }
-  s = s * (double)__builtin_amdgcn_exp2f((m - top) * c) + s2 * (double)__builtin_amdgcn_exp2f((m2 - top) * c);
-  m = top;
+  x.s = x.s * (double)__builtin_amdgcn_exp2f((x.m - m) * c) + y.s * (double)__builtin_amdgcn_exp2f((y.m - m) * c);
+  x.m = m;
 }
 
-// A thread's part of a row: its largest logit m and the sum of exp((l - m) / tau) over its tokens not listed.
-struct Sum {
-  float m = -INFINITY;
-  double s = 0.0;
-};
 template <int kN>
 __device__ __forceinline__ float top_of(const float (&x)[kN]) {
   float t = x[0];
@@ -149,29 +166,47 @@ __device__ __forceinline__ float top_of(const float (&x)[kN]) {
   for (int j = 1; j < kN; ++j) t = fmaxf(t, x[j]);
   return t;
 }
-// the sum of a vector's terms, without those of the bits in `on`
-template <int kN>
-__device__ __forceinline__ float terms(const float (&x)[kN], uint32_t on, float from, float c) {
-  float e[kN];
-#pragma unroll
-  for (int j = 0; j < kN; ++j) e[j] = __builtin_amdgcn_exp2f((x[j] - from) * c);
-  if (on) {
-#pragma unroll
-    for (int j = 0; j < kN; ++j) e[j] = on >> j & 1 ? 0.f : e[j];
-  }
-#pragma unroll
-  for (int w = 1; w < kN; w <<= 1)
-#pragma unroll
-    for (int j = 0; j + w < kN; j += 2 * w) e[j] += e[j + w];
-  asm volatile("" : "+v"(e[0]));                  // (summed here: the terms need no registers after)
-  return e[0];
-}
 
-// Vector v of a row that has n (-inf behind them).
-template <typename E>
+// A wavefront's sum as its logits stream by.  The reference is the wavefront's and moves seldom: when a logit is kRoom
+// above it.
+struct Stream {
+  float c, mc, lim, top = -INFINITY;
+  double s = 0.0;
+
+  __device__ __forceinline__ explicit Stream(float c_) : c(c_), mc(-kFar), lim(-2.f * kFar / c_) {}
+  template <int kN>
+  __device__ __forceinline__ void add(const float (&x)[kN], uint32_t on) {
+    const float t = top_of(x);
+    top = fmaxf(top, t);
+    if (__any(t > lim)) {
+      const float m = wave_max(t);
+      float r = m * c;
+      asm volatile("" : "+v"(r));                 // (as rounded: no part of a fused difference)
+      s *= (double)__builtin_amdgcn_exp2f(mc - r);
+      mc = r;
+      lim = m + kRoom / c;
+    }
+    float e[kN];
+#pragma unroll
+    for (int j = 0; j < kN; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(x[j], c, -mc));
+    if (__any(on != 0)) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) e[j] = on >> j & 1 ? 0.f : e[j];
+    }
+#pragma unroll
+    for (int w = 1; w < kN; w <<= 1)
+#pragma unroll
+      for (int j = 0; j + w < kN; j += 2 * w) e[j] += e[j + w];
+    asm volatile("" : "+v"(e[0]));                // (summed here: the terms need no registers after)
+    s += (double)e[0];
+  }
+};
+
+// Vector v of a row that has n (-inf behind them).  kOnce: it is not read again.
+template <typename E, bool kOnce = false>
 __device__ __forceinline__ Vec<E> row_vector(const typename E::T* l, int v, int n) {
   Vec<E> q = Vec<E>::neg_inf();
-  if (v < n) q = Vec<E>::load(l + v * kN<E>);
+  if (v < n) q = kOnce ? Vec<E>::load_once(l, (uint32_t)v * 16u) : Vec<E>::load(l, (uint32_t)v);
   return q;
 }
 
@@ -189,136 +224,156 @@ struct Edge {
   __device__ __forceinline__ void look(const uint32_t* bits) { on = here && (bits[at >> 5] >> (at & 31) & 1u); }
 };
 
-// Vectors first .. last - 1 of a row by a workgroup of kThreads, kU loads in flight a lane: the reference moves for a
-// wavefront at a time, once for each group of loads.  bits: of the first of these vectors on.
-template <typename E, int kThreads, int kU>
-__device__ Sum stream_row(const typename E::T* l, int first, int last, float c, const uint32_t* bits) {
+// Vectors first .. last - 1 of a row by a workgroup of kThreads, kU loads in flight a lane.  bits: of the first of these
+// vectors on; q: what start_stream has asked for.
+template <typename E, int kThreads, bool kOnce = false, int kU>
+__device__ __forceinline__ void start_stream(Vec<E> (&q)[kU], const typename E::T* l, int first, int last) {
+#pragma unroll
+  for (int u = 0; u < kU; ++u) q[u] = row_vector<E, kOnce>(l, first + (int)threadIdx.x + u * kThreads, last);
+}
+template <typename E, int kThreads, bool kOnce = false, int kU>
+__device__ __forceinline__ void stream_row(Stream& r, Vec<E> (&q)[kU], const typename E::T* l, int first, int last, const uint32_t* bits) {
   constexpr int N = kN<E>;
-  Sum r;
-  for (int v0 = first + (int)threadIdx.x; __any(v0 < last); v0 += kU * kThreads) {
-    Vec<E> q[kU];
-#pragma unroll
-    for (int u = 0; u < kU; ++u) q[u] = row_vector<E>(l, v0 + u * kThreads, last);
-    float top = r.m;
+  int v = first + (int)threadIdx.x;
+  // (whole wavefronts go round: v less the lane)
+  for (; v - (int)(threadIdx.x % kWave) < last; v += kU * kThreads) {
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
-      __builtin_amdgcn_sched_barrier(0);
+      const int w = v + u * kThreads;
       float x[N];
-      q[u].get(x);
-      top = fmaxf(top, top_of(x));
-    }
-    if (__any(top > r.m)) {
-      top = wave_max(top);
-      r.s *= (double)__builtin_amdgcn_exp2f((r.m - top) * c);
-      r.m = top;
-    }
-    const float from = r.m == -INFINITY ? 0.f : r.m;
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int v = v0 + u * kThreads;
       __builtin_amdgcn_sched_barrier(0);            // (one vector unpacked at a time: registers)
-      q[u].forget();
-      float x[N];
       q[u].get(x);
-      r.s += (double)terms(x, v < last ? bits_at<N>(bits, (v - first) * N) : 0u, from, c);
+      q[u] = row_vector<E, kOnce>(l, w + kU * kThreads, last);
+      r.add(x, w < last ? bits_at<N>(bits, (w - first) * N) : 0u);
     }
   }
-  return r;
 }
 
-// ... of the row's edge
-template <typename E>
-__device__ __forceinline__ void take_edge(Sum& r, const Edge<E>& e, float c) {
-  if (!e.here) return;
-  const float from = e.x == -INFINITY ? 0.f : e.x;
-  join(r.m, r.s, e.x, e.on ? 0.0 : (double)__builtin_amdgcn_exp2f(e.x == -INFINITY ? -INFINITY : (e.x - from) * c), c);
-}
-
-// The workgroup's sums joined, in all threads (fixed order).
-template <int kThreads>
-__device__ Sum join_all(Sum r, float c, float* s_m, double* s_s) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) join(r.m, r.s, __shfl_xor(r.m, o), __shfl_xor(r.s, o), c);
-  if (threadIdx.x % kWave == 0) {
-    s_m[threadIdx.x / kWave] = r.m;
-    s_s[threadIdx.x / kWave] = r.s;
+// A wavefront's result, in LDS: its largest logit, and a sum of exp2(l c - r).
+struct Partial {
+  float top;
+  double r, s;
+};
+// The edge's elements join, and where the terms were too far for the reference they are formed again, from vectors
+// first .. last - 1 as stream_row takes them.
+template <typename E, int kThreads>
+__device__ void put_partial(Stream r, const Edge<E>& edge, const typename E::T* l, int first, int last, const uint32_t* bits,
+                            Partial* p) {
+  constexpr int N = kN<E>;
+  const float x[1] = {edge.x};
+  r.add(x, edge.on ? 1u : 0u);
+  const float top = wave_max(r.top);
+  double ref = (double)r.mc;
+  if (top > kFar / r.c || (top > -INFINITY && top <= -2.f * kFar / r.c)) {
+    r.s = edge.on ? 0.0 : (double)__builtin_amdgcn_exp2f((edge.x - top) * r.c);
+    for (int v = first + (int)threadIdx.x; v < last; v += kThreads) {
+      const Vec<E> q = Vec<E>::load(l, (uint32_t)v);
+      const uint32_t on = bits_at<N>(bits, (v - first) * N);
+      float y[N];
+      q.get(y);
+      for (int j = 0; j < N; ++j) r.s += on >> j & 1 ? 0.0 : (double)__builtin_amdgcn_exp2f((y[j] - top) * r.c);
+    }
+    ref = (double)top * (double)r.c;
   }
-  __syncthreads();
-  r = Sum{s_m[0], s_s[0]};
-#pragma unroll
-  for (int w = 1; w < kThreads / kWave; ++w) join(r.m, r.s, s_m[w], s_s[w], c);
-  return r;
+  const double s = wave_sum(r.s);
+  if (threadIdx.x % kWave == 0) p[threadIdx.x / kWave] = Partial{top, ref, s};
+}
+// n partial results joined by one wavefront, in all of its lanes (fixed order).
+__device__ __forceinline__ Sum join_partials(const Partial* p, int n, float c) {
+  const int w = (int)threadIdx.x % kWave;
+  const Partial x = w < n ? p[w] : Partial{-INFINITY, 0.0, 0.0};
+  const float m = wave_max(x.top);
+  double s = x.s;
+  if (m > -INFINITY && s != 0.0) s *= pow2(x.r - (double)m * (double)c);
+  return Sum{m, wave_sum(s)};
 }
 
-// The listed tokens' part of Z, by the first wavefront, in all of its lanes.
-__device__ double listed_sum(const Listed& L, int K, float m, double inv_tau) {
+// The listed tokens' part of Z, by one wavefront, in all of its lanes.
+__device__ __forceinline__ double listed_sum(const Listed& L, int K, float m, double c) {
   double sum = 0.0;
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int k = threadIdx.x + i * kWave;
+#pragma unroll 1
+  for (int k = (int)threadIdx.x % kWave; k < K; k += kWave) {
     double p;
-    if (k < K && first_of(L, K, k, p)) sum += L.l[k] == -INFINITY ? 0.0 : exp(((double)L.l[k] - (double)m) * inv_tau);
+    if (first_of(L, K, k, p)) sum += L.l[k] == -INFINITY ? 0.0 : pow2(((double)L.l[k] - (double)m) * c);
   }
   return wave_sum(sum);
 }
 
-__device__ void finish(Row& r, float m, double Z, double R, const Listed& L, float w, float tau) {
+__device__ void finish(Row& r, float m, double Z, double R, const Listed& L, float w, float tau, float c) {
   r.m = m == -INFINITY ? 0.f : m;
+  r.mc = r.m * c;
+  r.far = !(fabsf(r.mc) <= kFar);
   r.Z = Z;
   r.mass = L.P + L.rho;
   r.scale = (double)w / (double)tau;
-  r.rest = R == 0.0 ? 0.f : (float)(r.scale * (r.mass / Z - L.rho / R));
+  const double rest = R == 0.0 ? 0.0 : r.scale * (r.mass / Z - L.rho / R);
+  r.rest = (float)(r.far ? rest : rest * pow2((double)r.mc - (double)r.m * (double)c));
 }
 
-// Loss and stats of a row, and what its gradient needs, by the first wavefront, from its largest logit and R.
-__device__ void conclude(const DistillArgs& a, int64_t row, const Listed& L, Sum sum, float w, Row& r, bool store) {
-  const int lane = threadIdx.x;
-  const double inv_tau = 1.0 / (double)a.temperature, R = sum.s;
+// By one wavefront, from a row's largest logit and R: Z, and what its gradient needs.
+__device__ __forceinline__ double conclude(const DistillArgs& a, const Listed& L, const Sum& sum, float w, float c, Row& r) {
+  const double Z = sum.s + listed_sum(L, a.K, sum.m == -INFINITY ? 0.f : sum.m, kLog2e / (double)a.temperature);
+  if (threadIdx.x % kWave == 0) finish(r, sum.m, Z, sum.s, L, w, a.temperature, c);
+  return Z;
+}
+// ... its loss and stats.
+__device__ void put_loss(const DistillArgs& a, int64_t row, const Listed& L, const Sum& sum, double Z, float w) {
+  const int lane = (int)threadIdx.x % kWave;
+  const double inv_tau = 1.0 / (double)a.temperature, R = sum.s, logZ = log(Z);
   const float from = sum.m == -INFINITY ? 0.f : sum.m;
-  const double Z = R + listed_sum(L, a.K, from, inv_tau), logZ = log(Z);
   double x = 0.0;                                 // sum p_k log q_k
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) {
-    const int k = lane + i * kWave;
-    if (k < a.K && L.id[k] >= 0 && L.p[k] != 0.0)
+#pragma unroll 1
+  for (int k = lane; k < a.K; k += kWave) {
+    if (L.id[k] >= 0 && L.p[k] != 0.0)
       x += L.p[k] * (L.l[k] == -INFINITY ? -INFINITY : ((double)L.l[k] - (double)from) * inv_tau - logZ);
   }
   x = L.A - wave_sum(x);
   if (L.rho > 0.0 && !(R == 0.0)) x += L.rho * (log(L.rho) - log(R / Z));
-  if (lane == 0) {
-    if (store) {
-      a.loss[row] = (float)((double)w * x);
-      if (a.stats) {
-        a.stats[row * 3] = sum.m;
-        a.stats[row * 3 + 1] = (float)Z;
-        a.stats[row * 3 + 2] = (float)R;
-      }
-    }
-    finish(r, sum.m, Z, R, L, w, a.temperature);
+  if (lane != 0) return;
+  a.loss[row] = (float)((double)w * x);
+  if (a.stats) {
+    a.stats[row * 3] = sum.m;
+    a.stats[row * 3 + 1] = (float)Z;
+    a.stats[row * 3 + 2] = (float)R;
   }
 }
 
-// A vector's gradient; the listed tokens' is left to put_listed.
-template <typename E>
-__device__ __forceinline__ void put_vector(const Vec<E>& q, typename E::T* g, uint32_t on, float m, float rest, float c) {
+// A vector's gradient into g; the listed tokens' is left to put_listed.  kFarOff: from exp2((l - m) c).
+template <typename E, bool kFarOff = false>
+__device__ __forceinline__ void put_vector(const Vec<E>& q, typename E::T* row, int v, uint32_t on, float m, float rest, float c) {
   constexpr int N = kN<E>;
   float x[N];
   q.get(x);
 #pragma unroll
-  for (int j = 0; j < N; ++j) x[j] = __builtin_amdgcn_exp2f((x[j] - m) * c) * rest;
-  Vec<E> v;
-  v.set(x);
+  for (int j = 0; j < N; ++j) x[j] = __builtin_amdgcn_exp2f(kFarOff ? (x[j] - m) * c : fmaf(x[j], c, -m)) * rest;
+  Vec<E> y;
+  y.set(x);
   if (on == 0) {
-    v.store(g);
+    y.stream_at(row, (uint32_t)v * 16u);
   } else {
 #pragma unroll
     for (int j = 0; j < N; ++j)
-      if (!(on >> j & 1)) g[j] = v.raw(j);
+      if (!(on >> j & 1)) row[v * N + j] = y.raw(j);
   }
 }
 template <typename E>
-__device__ __forceinline__ void put_edge(const Edge<E>& e, typename E::T* g, float m, float rest, float c) {
-  if (e.here && !e.on) g[e.at] = (typename E::T)(__builtin_amdgcn_exp2f((e.x - m) * c) * rest);
+__device__ __forceinline__ void put_edge(const Edge<E>& e, typename E::T* g, const Row& r, float c) {
+  if (e.here && !e.on) g[e.at] = (typename E::T)(__builtin_amdgcn_exp2f(r.far ? (e.x - r.m) * c : fmaf(e.x, c, -r.mc)) * r.rest);
+}
+// Vectors first .. last - 1 of a row, the last first, kU loads in flight a lane.
+template <typename E, int kThreads, int kU, bool kFarOff>
+__device__ __forceinline__ void put_vectors(const typename E::T* l, typename E::T* g, int first, int last, const uint32_t* bits,
+                                            float m, float rest, float c) {
+  constexpr int kStep = kU * kThreads;
+  for (int at = first + (last - first + kStep - 1) / kStep * kStep - kStep; at >= first; at -= kStep) {
+    Vec<E> q[kU];
+    start_stream<E, kThreads, true>(q, l, at, last);
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      const int v = at + (int)threadIdx.x + u * kThreads;
+      if (v < last) put_vector<E, kFarOff>(q[u], g, v, bits_at<kN<E>>(bits, v * kN<E>), m, rest, c);
+    }
+  }
 }
 // The listed tokens' gradient, of those in first .. last - 1.
 template <typename E, int kThreads>
@@ -327,7 +382,7 @@ __device__ void put_listed(const DistillArgs& a, typename E::T* g, const Row& r,
     if (L.id[k] < first || L.id[k] >= last) continue;
     double p;
     if (!first_of(L, a.K, k, p)) continue;
-    const double e = L.l[k] == -INFINITY ? 0.0 : exp(((double)L.l[k] - (double)r.m) / (double)a.temperature);
+    const double e = L.l[k] == -INFINITY ? 0.0 : pow2(((double)L.l[k] - (double)r.m) * (kLog2e / (double)a.temperature));
     g[L.id[k]] = (typename E::T)(float)(r.scale * ((r.Z == 0.0 ? 0.0 : e / r.Z) * r.mass - p));
   }
 }
@@ -352,144 +407,163 @@ __device__ void no_weight(const DistillArgs& a, int64_t row, typename E::T* g, i
   }
 }
 
-// Loss and gradient, a workgroup a row.  The row's first kKeep vectors a thread stay in registers between the sums and the
-// gradient; what is behind them is read again.
-constexpr int kRowThreads = 1024;
-template <typename E, int kKeep>
-__global__ __launch_bounds__(kRowThreads) void row_kernel(DistillArgs a) {
-  constexpr int N = kN<E>;
+// A workgroup a row: its loss, and the gradient.  The row's first kKeep vectors a thread stay in registers between the sums
+// and the gradient; what is behind them is read again, the last first.
+template <typename E, int kThreads, int kKeep, bool kGrad>
+__global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
+  constexpr int N = kN<E>, kU = kGrad ? 4 : 8;
   __shared__ Listed L;
+  __shared__ Raw raw;
   __shared__ Row r;
-  __shared__ float s_m[kRowThreads / kWave];
-  __shared__ double s_s[kRowThreads / kWave];
+  __shared__ Partial part[kThreads / kWave];
   const int64_t row = (int64_t)blockIdx.y * a.T + blockIdx.x;
   const int tid = threadIdx.x;
-  typename E::T* g = row_of<E>(a.grad, blockIdx.y, blockIdx.x);
+  typename E::T* g = kGrad ? row_of<E>(a.grad, blockIdx.y, blockIdx.x) : nullptr;
   const float w = weight_of(a, row);
   if (w == 0.f) {
-    no_weight<E, kRowThreads>(a, row, g, 0, a.V, true);
+    no_weight<E, kThreads>(a, row, g, 0, a.V, true);
     return;
   }
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, blockIdx.x);
   const float c = (float)(kLog2e / (double)a.temperature);
-  const int n = a.V / N, kept = min(n, kKeep * kRowThreads);       // vectors
-  for (int i = tid; i < (a.V + 31) / 32; i += kRowThreads) s_bits[i] = 0;
+  const int n = a.V / N, kept = min(n, kKeep * kThreads);          // vectors
+  for (int i = tid; i < (a.V + 31) / 32; i += kThreads) s_bits[i] = 0;
   __syncthreads();
-  if (tid < kWave) read_listed<E>(a, row, l, nullptr, 0, a.V, L, s_bits);
-  Vec<E> q[kKeep];
-#pragma unroll
-  for (int u = 0; u < kKeep; ++u) q[u] = row_vector<E>(l, u * kRowThreads + tid, n);
+  if (tid < kWave) {
+    fetch_listed<E>(a, row, l, nullptr, 0, a.V, raw);
+    read_listed(a, raw, 0, a.V, L, s_bits);
+  }
+  Vec<E> q[kKeep > 0 ? kKeep : 1], p[kU];
+  if constexpr (kKeep > 0) start_stream<E, kThreads, true>(q, l, 0, kept);
+  start_stream<E, kThreads, !kGrad>(p, l, kept, n);
   Edge<E> edge;
   edge.read(l, a.V);
+  __syncthreads();
+  edge.look(s_bits);
+  Stream acc(c);
+  int at = tid;                                     // (opaque: no address of a vector is kept until the gradient)
+  asm volatile("" : "+v"(at));
+  if constexpr (kKeep > 0) {
+#pragma unroll
+    for (int u = 0; u < kKeep; ++u) {
+      const int v = u * kThreads + at;
+      __builtin_amdgcn_sched_barrier(0);            // (one vector unpacked at a time: registers)
+      float x[N];
+      q[u].get(x);
+      acc.add(x, v < n ? bits_at<N>(s_bits, v * N) : 0u);
+    }
+  }
+  if (kept < n) stream_row<E, kThreads, !kGrad>(acc, p, l, kept, n, s_bits + kept * N / 32);
+  put_partial<E, kThreads>(acc, edge, l, 0, n, s_bits, part);
+  __syncthreads();
   Sum sum;
+  double Z;
+  if (tid < kWave) {
+    sum = join_partials(part, kThreads / kWave, c);
+    Z = conclude(a, L, sum, w, c, r);
+    if (!kGrad) put_loss(a, row, L, sum, Z, w);
+  }
+  if constexpr (kGrad) {
+    __syncthreads();
+    const float mc = r.mc, rest = r.rest;
+    put_edge<E>(edge, g, r, c);
+    if (r.far) {
+      put_vectors<E, kThreads, 1, true>(l, g, 0, n, s_bits, r.m, rest, c);
+    } else {
+      put_vectors<E, kThreads, kU, false>(l, g, kept, n, s_bits, mc, rest, c);
+      asm volatile("" : "+v"(at));
+      if constexpr (kKeep > 0) {
 #pragma unroll
-  for (int u = 0; u < kKeep; ++u) {
-    __builtin_amdgcn_sched_barrier(0);
-    float x[N];
-    q[u].get(x);
-    sum.m = fmaxf(sum.m, top_of(x));
+        for (int u = 0; u < kKeep; ++u) {
+          const int v = u * kThreads + at;
+          __builtin_amdgcn_sched_barrier(0);
+          q[u].forget();
+          if (v < n) put_vector<E>(q[u], g, v, bits_at<N>(s_bits, v * N), mc, rest, c);
+        }
+      }
+    }
+    put_listed<E, kThreads>(a, g, r, L, 0, a.V);
+    if (tid < kWave) put_loss(a, row, L, sum, Z, w);
   }
-  sum.m = wave_max(sum.m);
-  __syncthreads();                                  // (the bits are set)
-  edge.look(s_bits);
-  const float from = sum.m == -INFINITY ? 0.f : sum.m;
-#pragma unroll
-  for (int u = 0; u < kKeep; ++u) {
-    const int v = u * kRowThreads + tid;
-    __builtin_amdgcn_sched_barrier(0);              // (one vector unpacked at a time: registers)
-    q[u].forget();
-    float x[N];
-    q[u].get(x);
-    sum.s += (double)terms(x, v < n ? bits_at<N>(s_bits, v * N) : 0u, from, c);
-  }
-  if (kept < n) {
-    const Sum more = stream_row<E, kRowThreads, 2>(l, kept, n, c, s_bits + kept * N / 32);
-    join(sum.m, sum.s, more.m, more.s, c);
-  }
-  take_edge(sum, edge, c);
-  sum = join_all<kRowThreads>(sum, c, s_m, s_s);
-  if (tid < kWave) conclude(a, row, L, sum, w, r, true);
-  __syncthreads();
-  const float m = r.m, rest = r.rest;
-#pragma unroll
-  for (int u = 0; u < kKeep; ++u) {
-    const int v = u * kRowThreads + tid;
-    __builtin_amdgcn_sched_barrier(0);
-    q[u].forget();
-    if (v < n) put_vector<E>(q[u], g + v * N, bits_at<N>(s_bits, v * N), m, rest, c);
-  }
-  for (int v = kept + tid; v < n; v += kRowThreads)
-    put_vector<E>(Vec<E>::load(l + v * N), g + v * N, bits_at<N>(s_bits, v * N), m, rest, c);
-  put_edge<E>(edge, g, m, rest, c);
-  put_listed<E, kRowThreads>(a, g, r, L, 0, a.V);
 }
 
-// The loss alone, a workgroup a row.
-constexpr int kLossThreads = 512;
-template <typename E>
-__global__ __launch_bounds__(kLossThreads) void loss_kernel(DistillArgs a) {
-  __shared__ Listed L;
-  __shared__ Row r;
-  __shared__ float s_m[kLossThreads / kWave];
-  __shared__ double s_s[kLossThreads / kWave];
-  const int64_t row = (int64_t)blockIdx.y * a.T + blockIdx.x;
-  const int tid = threadIdx.x;
-  const float w = weight_of(a, row);
-  if (w == 0.f) {
-    no_weight<E, kLossThreads>(a, row, nullptr, 0, a.V, true);
-    return;
-  }
-  const typename E::T* l = row_of<E>(a.in, blockIdx.y, blockIdx.x);
-  const float c = (float)(kLog2e / (double)a.temperature);
-  for (int i = tid; i < (a.V + 31) / 32; i += kLossThreads) s_bits[i] = 0;
-  __syncthreads();
-  if (tid < kWave) read_listed<E>(a, row, l, nullptr, 0, a.V, L, s_bits);
-  Edge<E> edge;
-  edge.read(l, a.V);
-  __syncthreads();
-  edge.look(s_bits);
-  Sum sum = stream_row<E, kLossThreads, 8>(l, 0, a.V / kN<E>, c, s_bits);
-  take_edge(sum, edge, c);
-  sum = join_all<kLossThreads>(sum, c, s_m, s_s);
-  if (tid < kWave) conclude(a, row, L, sum, w, r, true);
-}
-
-// Few rows are cut into parts of `len` tokens (a multiple of 32), a workgroup each: their sums and the listed tokens' logits
-// go through the workspace to a second launch.
+// Few rows are cut into parts of `len` tokens (a multiple of 512), a workgroup each: their sums and the listed tokens'
+// logits go through the workspace to a second launch.
+struct PartSum {
+  Sum rest;                                       // of the tokens not listed
+  double listed;                                  // of the others, from the same m
+};
 struct Parts {
-  Sum* sum;                                       // [rows, n]
+  PartSum* sum;                                   // [rows, n]
   float* listed;                                  // [rows, K]
   int n, len;
 };
+constexpr int kMaxParts = kWave;
 
 constexpr int kSumThreads = 512;
 template <typename E>
 __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts ps) {
-  __shared__ float s_m[kSumThreads / kWave];
-  __shared__ double s_s[kSumThreads / kWave];
-  const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n;
+  __shared__ Partial partial[kSumThreads / kWave];
+  __shared__ int s_id[kMaxK];
+  __shared__ float s_l[kMaxK];
+  __shared__ int s_twice;
+  const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n, tid = threadIdx.x;
   const int64_t row = (int64_t)blockIdx.y * a.T + t;
   if (weight_of(a, row) == 0.f) return;
   const int first = part * ps.len, last = min(a.V, first + ps.len);
   const float c = (float)(kLog2e / (double)a.temperature);
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
-  for (int i = threadIdx.x; i < (last - first + 31) / 32; i += kSumThreads) s_bits[i] = 0;
+  Vec<E> q[8];
+  start_stream<E, kSumThreads>(q, l, first / kN<E>, last / kN<E>);
+  Edge<E> edge;                                     // (of the row's last part: the others end at a vector's end)
+  edge.read(l + first, last - first);
+  for (int i = tid; i < (last - first + 31) / 32; i += kSumThreads) s_bits[i] = 0;
+  if (tid == 0) s_twice = 0;
   __syncthreads();
-  for (int k = threadIdx.x; k < a.K; k += kSumThreads) {
-    const int id = a.ids[row * a.K + k], at = id - first;
-    if (id >= first && id < last) {
-      atomicOr(&s_bits[at >> 5], 1u << (at & 31));
-      ps.listed[row * a.K + k] = (float)l[id];
+  for (int k = tid; k < a.K; k += kSumThreads) {
+    int id = a.ids[row * a.K + k];
+    if (id < first || id >= last) id = -1;
+    s_id[k] = id;
+    if (id >= 0) {
+      const int at = id - first;
+      if (atomicOr(&s_bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u) s_twice = 1;
+      ps.listed[row * a.K + k] = s_l[k] = (float)l[id];
     }
   }
   __syncthreads();
-  Sum sum = stream_row<E, kSumThreads, 8>(l, first / kN<E>, last / kN<E>, c, s_bits);
-  Edge<E> edge;                                     // (of the row's last part: the others end at a vector's end)
-  edge.read(l + first, last - first);
   edge.look(s_bits);
-  take_edge(sum, edge, c);
-  sum = join_all<kSumThreads>(sum, c, s_m, s_s);
-  if (threadIdx.x == 0) ps.sum[row * ps.n + part] = sum;
+  Stream acc(c);
+  stream_row<E, kSumThreads>(acc, q, l, first / kN<E>, last / kN<E>, s_bits);
+  put_partial<E, kSumThreads>(acc, edge, l, first / kN<E>, last / kN<E>, s_bits, partial);
+  __syncthreads();
+  if (tid >= kWave) return;
+  const Sum rest = join_partials(partial, kSumThreads / kWave, c);
+  const double from = rest.m == -INFINITY ? 0.0 : (double)rest.m;
+  double listed = 0.0;
+  for (int k = tid; k < a.K; k += kWave) {
+    bool one = s_id[k] >= 0;
+    if (s_twice)
+      for (int j = 0; j < k; ++j) one &= s_id[j] != s_id[k];
+    if (one && s_l[k] != -INFINITY) listed += pow2(((double)s_l[k] - from) * (kLog2e / (double)a.temperature));
+  }
+  listed = wave_sum(listed);
+  if (tid == 0) ps.sum[row * ps.n + part] = PartSum{rest, listed};
+}
+
+// A row's sums from its parts', by one wavefront, in all of its lanes.
+__device__ __forceinline__ Sum join_parts(const PartSum* p, int n, double c, double& Z) {
+  const int i = (int)threadIdx.x % kWave;
+  const PartSum x = i < n ? p[i] : PartSum{{-INFINITY, 0.0}, 0.0};
+  const float m = wave_max(x.rest.m);
+  double s = x.rest.s, e = x.listed;
+  if (m > -INFINITY && (s != 0.0 || e != 0.0)) {
+    const double f = pow2(((double)x.rest.m - (double)m) * c);
+    s *= f;
+    e *= f;
+  }
+  const double R = wave_sum(s);
+  Z = R + wave_sum(e);
+  return Sum{m, R};
 }
 
 // The gradient of a part of a row.  kStats: from a.stats; else from the parts' sums, and the row's first part writes its
@@ -497,8 +571,9 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
 constexpr int kGradThreads = 256;
 template <typename E, bool kStats>
 __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts ps) {
-  constexpr int N = kN<E>, kU = 4;
+  constexpr int N = kN<E>;
   __shared__ Listed L;
+  __shared__ Raw raw;
   __shared__ Row r;
   const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n;
   const int64_t row = (int64_t)blockIdx.y * a.T + t;
@@ -513,38 +588,30 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts
   if (g == nullptr && !store) return;
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
   const float c = (float)(kLog2e / (double)a.temperature);
-  const int b0 = kStats ? first : 0, b1 = kStats ? last : a.V;      // (Z takes the row's listed tokens, each once)
-  for (int i = tid; i < (b1 - b0 + 31) / 32; i += kGradThreads) s_bits[i] = 0;
+  for (int i = tid; i < (last - first + 31) / 32; i += kGradThreads) s_bits[i] = 0;
   __syncthreads();
   if (tid < kWave) {
-    read_listed<E>(a, row, l, kStats ? nullptr : ps.listed + row * a.K, b0, b1, L, s_bits);
+    fetch_listed<E>(a, row, l, kStats ? nullptr : ps.listed + row * a.K, first, last, raw);
+    read_listed(a, raw, first, last, L, s_bits);
     if constexpr (kStats) {
-      if (tid == 0) finish(r, a.stats[row * 3], (double)a.stats[row * 3 + 1], (double)a.stats[row * 3 + 2], L, w, a.temperature);
+      if (tid == 0) finish(r, a.stats[row * 3], (double)a.stats[row * 3 + 1], (double)a.stats[row * 3 + 2], L, w, a.temperature, c);
     } else {
-      Sum sum;
-      for (int i = 0; i < ps.n; ++i) join(sum.m, sum.s, ps.sum[row * ps.n + i].m, ps.sum[row * ps.n + i].s, c);
-      conclude(a, row, L, sum, w, r, store);
+      double Z;
+      const Sum sum = join_parts(ps.sum + row * ps.n, ps.n, kLog2e / (double)a.temperature, Z);
+      if (tid == 0) finish(r, sum.m, Z, sum.s, L, w, a.temperature, c);
+      if (store) put_loss(a, row, L, sum, Z, w);
     }
   }
   Edge<E> edge;
   edge.read(l + first, last - first);
   __syncthreads();
   if (g == nullptr) return;
-  const uint32_t* bits = s_bits + (first - b0) / 32;
+  const uint32_t* bits = s_bits;
   edge.look(bits);
-  const float m = r.m, rest = r.rest;
   const int n = (last - first) / N;
-  for (int v0 = tid; v0 < n; v0 += kU * kGradThreads) {
-    Vec<E> q[kU];
-#pragma unroll
-    for (int u = 0; u < kU; ++u) q[u] = row_vector<E>(l + first, v0 + u * kGradThreads, n);
-#pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int v = v0 + u * kGradThreads;
-      if (v < n) put_vector<E>(q[u], g + first + v * N, bits_at<N>(bits, v * N), m, rest, c);
-    }
-  }
-  put_edge<E>(edge, g + first, m, rest, c);
+  put_edge<E>(edge, g + first, r, c);
+  if (__builtin_expect(r.far, 0)) put_vectors<E, kGradThreads, 1, true>(l + first, g + first, 0, n, bits, r.m, r.rest, c);
+  else put_vectors<E, kGradThreads, 4, false>(l + first, g + first, 0, n, bits, r.mc, r.rest, c);
   put_listed<E, kGradThreads>(a, g, r, L, first, last);
 }
 
@@ -563,15 +630,15 @@ hipError_t run(F kernel, dim3 grid, int threads, size_t lds, hipStream_t stream,
 
 template <typename E>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t stream) {
-  const dim3 g((unsigned)a.T, (unsigned)a.B);
+  const dim3 all((unsigned)a.T, (unsigned)a.B);
   const size_t lds = bit_bytes(a.V);
-  if (a.grad.data == nullptr) return run(loss_kernel<E>, g, kLossThreads, lds, stream, a);
-  const int vectors = (a.V + 1024 * kN<E> - 1) / (1024 * kN<E>);
-  if (vectors <= 2) return run(row_kernel<E, 2>, g, 1024, lds, stream, a);
-  if (vectors <= 4) return run(row_kernel<E, 4>, g, 1024, lds, stream, a);
-  if (vectors <= 8) return run(row_kernel<E, 8>, g, 1024, lds, stream, a);
-  if (vectors <= 14) return run(row_kernel<E, 14>, g, 1024, lds, stream, a);
-  return run(row_kernel<E, 20>, g, 1024, lds, stream, a);
+  if (a.grad.data == nullptr) return run(row_kernel<E, 512, 0, false>, all, 512, lds, stream, a);
+  const int vectors = a.V / kN<E>;
+  if (vectors <= 128 * 4) return run(row_kernel<E, 128, 4, true>, all, 128, lds, stream, a);
+  if (vectors <= 128 * 14) return run(row_kernel<E, 128, 14, true>, all, 128, lds, stream, a);
+  if (vectors <= 256 * 16) return run(row_kernel<E, 256, 16, true>, all, 256, lds, stream, a);
+  if (vectors <= 1 << 15) return run(row_kernel<E, 512, 14, true>, all, 512, lds, stream, a);
+  return run(row_kernel<E, 1024, 16, true>, all, 1024, lds, stream, a);
 }
 
 template <typename E>
@@ -579,7 +646,7 @@ hipError_t launch_parts(const DistillArgs& a, const Parts& ps, hipStream_t strea
   const dim3 g((unsigned)(a.T * ps.n), (unsigned)a.B);
   const hipError_t e = run(sums_kernel<E>, g, kSumThreads, bit_bytes(ps.len), stream, a, ps);
   if (e != hipSuccess) return e;
-  return run(grad_kernel<E, false>, g, kGradThreads, bit_bytes(a.V), stream, a, ps);
+  return run(grad_kernel<E, false>, g, kGradThreads, bit_bytes(ps.len), stream, a, ps);
 }
 
 template <typename E>
@@ -590,7 +657,7 @@ hipError_t launch(const DistillArgs& a, void* workspace, hipStream_t stream) {
   Parts ps;
   ps.len = ((a.V + n - 1) / n + 511) & ~511;
   ps.n = (a.V + ps.len - 1) / ps.len;
-  ps.sum = static_cast<Sum*>(workspace);
+  ps.sum = static_cast<PartSum*>(workspace);
   ps.listed = reinterpret_cast<float*>(ps.sum + rows * ps.n);
   return launch_parts<E>(a, ps, stream);
 }
@@ -606,12 +673,12 @@ hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
 }  // namespace
 
 int distill_parts(int64_t rows, int32_t V) {
-  if (rows < 1 || rows > 128) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>(768 / rows, V / 4096));
+  if (rows < 1 || rows > 64) return 1;
+  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / rows, V / 4096, kMaxParts}));
 }
 size_t distill_workspace(int64_t rows, int32_t V) {
   const int n = distill_parts(rows, V);
-  return n <= 1 ? 0 : (size_t)rows * (n * sizeof(Sum) + CADDTREE_MAX_TEACHER * sizeof(float));
+  return n <= 1 ? 0 : (size_t)rows * (n * sizeof(PartSum) + CADDTREE_MAX_TEACHER * sizeof(float));
 }
 
 hipError_t launch_distill(const DistillArgs& a, void* workspace, caddtree_dtype_t dtype, hipStream_t stream) {

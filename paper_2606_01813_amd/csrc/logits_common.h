@@ -46,6 +46,18 @@ struct Vec {
   u32x4 w;
   static __device__ __forceinline__ Vec load(const T* p) { return Vec{reinterpret_cast<const Loose*>(p)->w}; }
   __device__ __forceinline__ void store(T* p) const { reinterpret_cast<Loose*>(p)->w = w; }
+  // vector v of a row (of fewer than 2^32 bytes; a row's start stays in scalar registers)
+  static __device__ __forceinline__ Vec load(const T* row, uint32_t v) {
+    return load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + v * 16u));
+  }
+  __device__ __forceinline__ void store(T* row, uint32_t v) const { store(reinterpret_cast<T*>(reinterpret_cast<char*>(row) + v * 16u)); }
+  // ... with the hint that nothing else reads it soon
+  static __device__ __forceinline__ Vec load_once(const T* row, uint32_t byte) {
+    return Vec{__builtin_nontemporal_load(&reinterpret_cast<const Loose*>(reinterpret_cast<const char*>(row) + byte)->w)};
+  }
+  __device__ __forceinline__ void stream_at(T* row, uint32_t byte) const {
+    __builtin_nontemporal_store(w, &reinterpret_cast<Loose*>(reinterpret_cast<char*>(row) + byte)->w);
+  }
   static __device__ __forceinline__ Vec neg_inf() { return Vec{u32x4{E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf}}; }
   __device__ __forceinline__ void get(float (&x)[kN<E>]) const {
 #pragma unroll

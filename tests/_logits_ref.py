@@ -2,16 +2,20 @@
 with the library.
 
 Error bounds.  h = 2^-24 is half a step of fp32, u that of the logits' type (a result is rounded to it once).
-Adjusting: a division or product, a fused product and difference, a difference and a sum, each off by h of its result, which
-is at most S = |x| max(r, 1 / r) + f c + p + |bias|: 4 h S in all (f c is not rounded, c < 2^24).
-Distilling: with d = (l_v - m) / tau <= 0 a term exp(d) is the hardware's 2^x (off by a step, 2 h) of a product of a
-difference, a factor rounded to fp32, and its own rounding (3 h |d|, relative to the term): t_v = h (3 |d| + 2).  Up to
-eight terms are summed in fp32 (at most 7 h) before the sum goes on in fp64.  So a sum of terms is off by sum e_v (t_v + 7 h),
-eZ and eR relative to Z and R; all sums over the list are fp64.
+Adjusting: a quotient (a product with a rounded inverse, 2 h) or product, a fused product and difference, a difference and a
+sum, each off by h of its result, which is at most S = |x| max(r, 1 / r) + f c + p + |bias|: 5 h S in all (f c is not rounded,
+c < 2^24).
+Distilling: with d = (l_v - m) / tau <= 0 a term is the hardware's 2^x (off by a step, 2 h) of l c - r, rounded once, with
+c = log2(e) / tau rounded to fp32 (h |d|) and a reference r at most 8 below the largest in 2^x: the rounding is h (|d| + 8 ln 2).
+Far from the numbers' middle it is 2^((l - m) c): three roundings of d.  Both are below t_v = h (3 |d| + 8), relative to the
+term; without the reference's distance, as the gradient has it, t'_v = h (3 |d| + 2).  Up to eight terms are summed in fp32 (at
+most 7 h) before the sum goes on in fp64; a sum moves to the row's largest by a 2^x with an argument below 1/2 (3 h), as a
+listed token's term is formed.  So R, the sum over what is not listed, is off by dR = sum e_v (t_v + 7 h) + 3 h R, and Z over all
+by dR + 3 h (Z - R); eR and eZ are these relative to R and Z.  All sums over the list are fp64.
     stats: the largest is exact, the sums are rounded once more (h).
     loss: |w| [(P + rho) eZ + rho eR] and one rounding.
-    gradient: of a listed token eZ q M, of another t_v + eZ + eR of both of its parts, plus 2 h for the coefficient
-    and the product; then u of the result.
+    gradient: of a listed token (eZ + 3 h) q M, of another t'_v + 5 h (the reference, the coefficient and the product), and eZ
+    and eR, of both of its parts; then u of the result.
 A second call starts from sums in fp32: h more for each.  Results below the smallest normal fp32 number may be flushed; f16 has
 steps of 2^-24 below 2^-14.
 """
@@ -81,7 +85,7 @@ def adjust(x, dtype, *, history=None, history_len=None, repetition=None, presenc
                 y[(words[b, t, v // 32] >> (v % 32)) & 1 == 0] = -np.inf
             out[b, t] = y
             with np.errstate(invalid="ignore"):
-                tol[b, t] = np.where(size > 0, np.nan_to_num(4 * H * size + U[dtype] * np.abs(y), nan=0.0, posinf=0.0), 0.0)
+                tol[b, t] = np.where(size > 0, np.nan_to_num(5 * H * size + U[dtype] * np.abs(y), nan=0.0, posinf=0.0), 0.0)
                 if dtype == torch.float16:
                     tol[b, t] += np.where(size > 0, TINY[dtype], 0.0)
     return out, tol
@@ -141,9 +145,9 @@ def distill(l, ids, target, w, tau, tail, dtype, again=False):
         e = np.exp(d)
     term = np.where(d > -np.inf, H * (3 * np.abs(np.where(d > -np.inf, d, 0.0)) + 2), 0.0)
     Z, R = e.sum(), e[~on].sum()
-    # (the listed tokens' terms are fp64 in the library)
-    dR = (e * (term + 7 * H))[~on].sum() + TINY[torch.float32] * V
-    eZ, eR = (dR / Z if Z > 0 else 0.0), (dR / R if R > 0 else 0.0)
+    dR = (e * (term + 13 * H))[~on].sum() + 3 * H * R + TINY[torch.float32] * V
+    dZ = dR + 3 * H * (Z - R)
+    eZ, eR = (dZ / Z if Z > 0 else 0.0), (dR / R if R > 0 else 0.0)
     loss, M = 0.0, p.sum() + rho
     teacher = np.zeros(V)
     for pk, lk, i in zip(p, logp, ids):
@@ -155,17 +159,15 @@ def distill(l, ids, target, w, tau, tail, dtype, again=False):
     q = e / Z if Z > 0 else e
     g = w / tau * (q * M - teacher)
     loose = eZ + (H if again else 0)
-    tol = np.abs(w) / tau * q * M * (loose + 2 * H)
+    tol = np.abs(w) / tau * q * M * (loose + 3 * H)
     if R > 0:
         other = rho * e / R
         g = np.where(on, g, w / tau * (q * M - other))
-        more = (eR + (H if again else 0) + 2 * H + term)
-        tol = np.where(on, tol, np.abs(w) / tau * (q * M * (loose + 2 * H + term) + other * more))
-    if dtype == torch.float32:
-        tol = tol + 2 * H * np.abs(g)
+        more = eR + (H if again else 0) + 5 * H + term
+        tol = np.where(on, tol, np.abs(w) / tau * (q * M * (loose + 5 * H + term) + other * more))
     tol = tol + U[dtype] * np.abs(g) + TINY[dtype] * max(1.0, abs(w) / tau)
     loss_tol = abs(w) * (M * eZ + rho * eR + 1e-12 * (1 + abs(loss))) + H * abs(w * loss) if np.isfinite(loss) else 0.0
     stats = np.array([m, Z, R])
     with np.errstate(over="ignore"):
         loss = float(np.float32(w * loss)) if abs(w * loss) > np.finfo(np.float32).max else w * loss     # (past fp32's range: infinite)
-    return loss, stats, g, loss_tol, np.array([0.0, dR + H * Z, dR + H * R]), tol
+    return loss, stats, g, loss_tol, np.array([0.0, dZ + H * Z, dR + H * R]), tol
