@@ -28,6 +28,7 @@ constexpr int kPath = CADDTREE_MAX_L;
 constexpr int kNodes = 1024;                      // of a tree, in LDS (further ones are read where they lie)
 constexpr int kNear = 512;                        // biases in LDS, likewise
 constexpr uint32_t kCount = (1u << 20) - 1;       // a word's count; above it the bias
+static_assert(kNear == kThreads, "each thread keeps a bias");
 static_assert(CADDTREE_MAX_HISTORY + kPath <= kCount && CADDTREE_MAX_BIAS < 1 << 12, "a word holds both");
 
 struct Lds {
@@ -113,12 +114,13 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
   const int len = a.history ? min(max(a.history_len ? a.history_len[b] : a.H, 0), a.H) : 0;
   const int32_t* history = a.history + (int64_t)b * a.H;
   const int32_t* bias_ids = a.bias_ids + (int64_t)b * a.n_bias;
+  const float* bias = a.bias + (int64_t)b * a.n_bias;
   const auto four = [&](int i) { return i + 4 <= a.H ? Vec<F32>::load(reinterpret_cast<const float*>(history) + i) : Vec<F32>{}; };
   Vec<F32> h = a.history ? four(tid * 4) : Vec<F32>{};
   const int bias_id = tid < a.n_bias ? bias_ids[tid] : -1;
+  const float bias_value = tid < a.n_bias ? bias[tid] : 0.f;
   const float repetition = a.repetition ? a.repetition[b] : 1.f;
   const Penalty p = {repetition, 1.f / repetition, a.presence ? a.presence[b] : 0.f, a.frequency ? a.frequency[b] : 0.f};
-  const float* bias = a.bias + (int64_t)b * a.n_bias;
   Nodes& nodes = *reinterpret_cast<Nodes*>(s_more);
   for (int i = tid; i < kChunk / 4; i += kThreads) reinterpret_cast<u32x4*>(s.word)[i] = u32x4{0, 0, 0, 0};
   if (tid == 0) s.listed = 0;
@@ -136,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
   for (int i = tid; i < a.n_bias; i += kThreads) {
     const int t = i == tid ? bias_id : bias_ids[i];
     if (t >= first && t < last) {
-      if (i < kNear) s.bias[i] = bias[i];
+      if (i < kNear) s.bias[i] = bias_value;            // (kNear threads: i is this one's)
       found(t - first, atomicMax(&s.word[t - first], (uint32_t)(i + 1) << 20));
     }
   }

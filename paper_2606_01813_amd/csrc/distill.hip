@@ -58,6 +58,8 @@ constexpr float kRoom = 8.f;                      // a term may reach 2^kRoom be
 
 // bits of the N tokens from `at` (a multiple of N) on
 template <int N>
+constexpr uint32_t kNone = (1u << N) - 1;         // a lane past the row's end adds none of its vector's
+template <int N>
 __device__ __forceinline__ uint32_t bits_at(const uint32_t* bits, int at) {
   return reinterpret_cast<const uint8_t*>(bits)[at >> 3] >> (at & 7) & ((1u << N) - 1);
 }
@@ -202,14 +204,6 @@ struct Stream {
   }
 };
 
-// Vector v of a row that has n (-inf behind them).  kOnce: it is not read again.
-template <typename E, bool kOnce = false>
-__device__ __forceinline__ Vec<E> row_vector(const typename E::T* l, int v, int n) {
-  Vec<E> q = Vec<E>::neg_inf();
-  if (v < n) q = kOnce ? Vec<E>::load_once(l, (uint32_t)v * 16u) : Vec<E>::load(l, (uint32_t)v);
-  return q;
-}
-
 // A row's last elements, fewer than a vector: one in each of the first threads.
 template <typename E>
 struct Edge {
@@ -244,7 +238,7 @@ __device__ __forceinline__ void stream_row(Stream& r, Vec<E> (&q)[kU], const typ
       __builtin_amdgcn_sched_barrier(0);            // (one vector unpacked at a time: registers)
       q[u].get(x);
       q[u] = row_vector<E, kOnce>(l, w + kU * kThreads, last);
-      r.add(x, w < last ? bits_at<N>(bits, (w - first) * N) : 0u);
+      r.add(x, w < last ? bits_at<N>(bits, (w - first) * N) : kNone<N>);
     }
   }
 }
@@ -434,8 +428,8 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
     read_listed(a, raw, 0, a.V, L, s_bits);
   }
   Vec<E> q[kKeep > 0 ? kKeep : 1], p[kU];
-  if constexpr (kKeep > 0) start_stream<E, kThreads, true>(q, l, 0, kept);
-  start_stream<E, kThreads, !kGrad>(p, l, kept, n);
+  if (kKeep > 0 && n > 0) start_stream<E, kThreads, true>(q, l, 0, kept);
+  if (kept < n) start_stream<E, kThreads, !kGrad>(p, l, kept, n);
   Edge<E> edge;
   edge.read(l, a.V);
   __syncthreads();
@@ -443,14 +437,14 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
   Stream acc(c);
   int at = tid;                                     // (opaque: no address of a vector is kept until the gradient)
   asm volatile("" : "+v"(at));
-  if constexpr (kKeep > 0) {
+  if (kKeep > 0 && n > 0) {
 #pragma unroll
     for (int u = 0; u < kKeep; ++u) {
       const int v = u * kThreads + at;
       __builtin_amdgcn_sched_barrier(0);            // (one vector unpacked at a time: registers)
       float x[N];
       q[u].get(x);
-      acc.add(x, v < n ? bits_at<N>(s_bits, v * N) : 0u);
+      acc.add(x, v < n ? bits_at<N>(s_bits, v * N) : kNone<N>);
     }
   }
   if (kept < n) stream_row<E, kThreads, !kGrad>(acc, p, l, kept, n, s_bits + kept * N / 32);
@@ -514,7 +508,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
   const float c = (float)(kLog2e / (double)a.temperature);
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
   Vec<E> q[8];
-  start_stream<E, kSumThreads>(q, l, first / kN<E>, last / kN<E>);
+  if (first / kN<E> < last / kN<E>) start_stream<E, kSumThreads>(q, l, first / kN<E>, last / kN<E>);
   Edge<E> edge;                                     // (of the row's last part: the others end at a vector's end)
   edge.read(l + first, last - first);
   for (int i = tid; i < (last - first + 31) / 32; i += kSumThreads) s_bits[i] = 0;

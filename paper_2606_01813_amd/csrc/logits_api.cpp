@@ -164,8 +164,8 @@ caddtree_status_t caddtree_adjust_logits(const caddtree_adjust_t* a, hipStream_t
 }
 
 size_t caddtree_verify_workspace_bytes(const caddtree_verify_t* a) {
-  if (a == nullptr || check_sizes(enum_value(a->dtype), a->B, a->T, a->V) != CADDTREE_OK) return 0;
-  return 0;
+  if (a == nullptr || check_sizes(enum_value(a->dtype), a->B, a->T, a->V) != CADDTREE_OK || a->T > CADDTREE_MAX_CAP + 1) return 0;
+  return caddtree::verify_workspace(a->B, a->T, a->V, size_of(enum_value(a->dtype)));
 }
 
 caddtree_status_t caddtree_verify_tree(const caddtree_verify_t* a, void* workspace, size_t workspace_bytes, hipStream_t stream) {
@@ -202,7 +202,7 @@ caddtree_status_t caddtree_verify_tree(const caddtree_verify_t* a, void* workspa
   if ((st = check_apart(arrays)) != CADDTREE_OK) return st;
   const caddtree::VerifyArgs k = {rows(a->logits), a->B, a->T, a->V, a->chosen, a->token_ids, a->parent, a->count, a->M,
                                   a->accepted, a->index, a->tokens, a->weight};
-  const hipError_t e = caddtree::launch_verify(k, all ? static_cast<int32_t*>(workspace) : nullptr, (caddtree_dtype_t)dtype, stream);
+  const hipError_t e = caddtree::launch_verify(k, all ? workspace : nullptr, (caddtree_dtype_t)dtype, stream);
   return e == hipSuccess ? ok() : hip_fail(e, "verify launch");
 }
 

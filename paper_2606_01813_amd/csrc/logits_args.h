@@ -45,8 +45,11 @@ struct VerifyArgs {
   int32_t* tokens;
   float* weight;
 };
-// all: [B, T] tokens of every row, chosen before the walk (NULL: the walk reads the rows of its path)
-hipError_t launch_verify(const VerifyArgs& a, int32_t* all, caddtree_dtype_t dtype, hipStream_t stream);
+// How many parts each row is cut into where all rows are read at once (0: the walk reads those of its path), and the
+// workspace for that; elem: bytes of a logit.
+int verify_parts(int64_t B, int64_t T, int32_t V, size_t elem);
+size_t verify_workspace(int64_t B, int64_t T, int32_t V, size_t elem);
+hipError_t launch_verify(const VerifyArgs& a, void* workspace, caddtree_dtype_t dtype, hipStream_t stream);
 
 struct DistillArgs {
   Rows in, grad;             // grad.data NULL: none

@@ -92,6 +92,14 @@ __device__ __forceinline__ typename E::T* row_of(const Rows& r, int64_t b, int64
   return reinterpret_cast<typename E::T*>(r.data) + b * r.b + t * r.t;
 }
 
+// Vector v of a row that has n >= 1, or the last where there are fewer: no load waits behind a branch, and a lane past the
+// row's end leaves out what it gets.  kOnce: it is not read again.
+template <typename E, bool kOnce = false>
+__device__ __forceinline__ Vec<E> row_vector(const typename E::T* l, int v, int n) {
+  const uint32_t at = (uint32_t)min(v, n - 1);
+  return kOnce ? Vec<E>::load_once(l, at * 16u) : Vec<E>::load(l, at);
+}
+
 // over the lanes of a wavefront, the result in all of them (fixed order)
 __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
