@@ -3,8 +3,8 @@
     python examples/speculative_decoding.py --rounds 24
 
 Prompt: ``window_attention`` and ``KVCache.write``.  Each round: a draft tree (``Plan.build``), the target's
-attention over cache and tree (``KVCache.attention``), the longest path of the tree that the target agrees with,
-its tokens into the cache (``KVCache.write`` with an index) and the cached tokens' attention weight
+attention over cache and tree (``KVCache.attention``), the longest path of the tree that the target agrees with
+(``verify_tree``), its tokens into the cache (``KVCache.write`` with an index) and the cached tokens' attention weight
 (``KVCache.score``).  A sequence near its cache's end is cut to the tokens that were attended to most
 (``KVCache.evict``).  Everything between two rounds stays on the device.
 
@@ -21,7 +21,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 
 import torch
 
-from paper_2606_01813_amd import KVCache, Plan, attention_workspace, window_attention
+from paper_2606_01813_amd import KVCache, Plan, attention_workspace, verify_tree, verify_workspace, window_attention
 
 PAGE = 64
 
@@ -43,10 +43,9 @@ class Target:
         cut = lambda y, n: y.view(*tokens.shape, n, self.head_dim)
         return cut(x @ self.wq, self.heads), cut(x @ self.wk, self.kv_heads), cut(x @ self.wv, self.kv_heads)
 
-    def choose(self, tokens, attended):
+    def logits(self, tokens, attended):
         logits = (attended.flatten(-2) @ self.head).float()
-        logits.scatter_add_(-1, self.after[tokens].unsqueeze(-1), torch.full((*tokens.shape, 1), 12.0, device="cuda"))
-        return logits.argmax(-1)
+        return logits.scatter_add_(-1, self.after[tokens].unsqueeze(-1), torch.full((*tokens.shape, 1), 12.0, device="cuda"))
 
 
 def draft(target, last, L, gen):
@@ -62,22 +61,6 @@ def draft(target, last, L, gen):
         at = logits[:, i].gather(1, wrong)
         logits[:, i].scatter_(1, wrong, torch.where(slip & (wrong != token[:, None]), 10.0, at))
     return logits.to(torch.bfloat16)
-
-
-def accepted(tree, tokens, chosen, L):
-    """Per sequence: which rows (root and nodes) are on the path that the target agrees with, in order and how many."""
-    B, cap = tree.parent.shape
-    nodes = torch.arange(cap, device="cuda") < tree.n_star[:, None]
-    parent = torch.where(nodes, tree.parent, -1).to(torch.int64) + 1          # as rows
-    agrees = nodes & (tokens[:, 1:] == chosen.gather(1, parent))
-    on = torch.zeros((B, cap + 1), dtype=torch.bool, device="cuda")
-    on[:, 0] = True
-    for _ in range(L):
-        on[:, 1:] = agrees & on.gather(1, parent)
-    rows = torch.arange(cap + 1, device="cuda")
-    depth = torch.cat([torch.zeros((B, 1), dtype=torch.int32, device="cuda"), tree.depth], 1)
-    order = torch.where(on, depth.to(torch.int64) * (cap + 1) + rows, 1 << 40).argsort(1)[:, :L + 1]
-    return on, order, on.sum(1).to(torch.int32)
 
 
 @dataclass
@@ -113,14 +96,15 @@ def run(B=4, prompt=300, rounds=24, L=8, cap=24, slots=512, budget=320, window=0
     ctx_len = torch.zeros(B, dtype=torch.int64, device="cuda")
     cache.write(k, v, table, ctx_len)
     ctx_len += prompt
-    last = target.choose(text[:, prompt - 1:prompt], out[:, -1:])[:, 0]       # (the bonus token: chosen, not yet cached)
+    last = target.logits(text[:, prompt - 1:prompt], out[:, -1:]).argmax(-1)[:, 0]       # (the bonus token: chosen, not yet cached)
     text[:, prompt] = last
     length = ctx_len + 1
 
     T = cap + 1
     lse = torch.zeros((B, T, target.heads), device="cuda")
     attended = torch.zeros((B, T, target.heads, target.head_dim), dtype=torch.bfloat16, device="cuda")
-    attn_ws, most, evictions, took, cached = None, prompt, 0, [], []
+    on = torch.zeros((B, T), device="cuda")
+    attn_ws, verify_ws, most, evictions, took, cached = None, None, prompt, 0, [], []
     for _ in range(rounds):
         if most + L + 1 > slots:                                              # (an upper bound, known without asking the device)
             new_len = torch.empty_like(ctx_len)
@@ -136,12 +120,16 @@ def run(B=4, prompt=300, rounds=24, L=8, cap=24, slots=512, budget=320, window=0
             attn_ws = attention_workspace(q, cache=cache, page_table=table)
         cache.attention(q, table, ctx_len, k, v, mask=tree.mask, depth=tree.depth, count=tree.n_star, window=window, sinks=4,
                         out=attended, lse=lse, workspace=attn_ws)
-        chosen = target.choose(tokens, attended)
-        on, order, count = accepted(tree, tokens, chosen, L)
-        cache.score(q, table, ctx_len, lse, scores, weight=on.float(), count=tree.n_star, depth=tree.depth, window=window, sinks=4)
-        cache.write(k, v, table, ctx_len, count=count, index=order.to(torch.int32))
+        logits = target.logits(tokens, attended)
+        if verify_ws is None:
+            verify_ws = verify_workspace(logits)
+        count = torch.empty(B, dtype=torch.int32, device="cuda")
+        index, chosen = torch.empty((2, B, L + 1), dtype=torch.int32, device="cuda").unbind(0)
+        verify_tree(logits, tree.token_ids, tree.parent, tree.n_star, count, index, chosen, weight=on, workspace=verify_ws)
+        cache.score(q, table, ctx_len, lse, scores, weight=on, count=tree.n_star, depth=tree.depth, window=window, sinks=4)
+        cache.write(k, v, table, ctx_len, count=count, index=index)
         ctx_len = ctx_len + count
-        new = chosen.gather(1, order)                                         # each accepted row's choice: the next row, or the bonus
+        new = chosen.to(torch.int64)                                          # each accepted row's choice: the next row, or the bonus
         at = torch.arange(L + 1, device="cuda")
         text.scatter_(1, torch.where(at < count[:, None], length[:, None] + at, text.shape[1] - 1), new)
         length = length + count

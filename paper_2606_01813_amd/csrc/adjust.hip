@@ -81,10 +81,11 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
   constexpr uint32_t kAll = (1u << N) - 1;
   using T = typename E::T;
 
-  const int b = (int)blockIdx.z, first = (int)blockIdx.x * kChunk, last = min(first + kChunk, a.V);
+  const int chunks = (a.V + kChunk - 1) / kChunk;
+  const int b = (int)blockIdx.y, first = (int)(blockIdx.x % chunks) * kChunk, last = min(first + kChunk, a.V);
   const bool tree = a.parent != nullptr;
   const int rows = min(max(a.count ? a.count[b] : a.T - tree, 0), a.T - tree) + tree;   // (rows of the sequence)
-  const int row0 = (int)blockIdx.y * kRows, mine = min(kRows, rows - row0);
+  const int row0 = (int)(blockIdx.x / chunks) * kRows, mine = min(kRows, rows - row0);
   if (mine <= 0) return;
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
@@ -243,7 +244,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
 
 template <typename E>
 void launch(const AdjustArgs& a, bool in_place, hipStream_t stream) {
-  const dim3 g((unsigned)((a.V + kChunk - 1) / kChunk), (unsigned)((a.T + kRows - 1) / kRows), (unsigned)a.B);
+  const dim3 g((unsigned)((a.V + kChunk - 1) / kChunk) * (unsigned)((a.T + kRows - 1) / kRows), (unsigned)a.B);
   const size_t lds = a.parent != nullptr ? sizeof(Nodes) : 0;
   if (in_place) adjust_kernel<E, true><<<g, kThreads, lds, stream>>>(a);
   else adjust_kernel<E, false><<<g, kThreads, lds, stream>>>(a);

@@ -17,7 +17,7 @@ using caddtree::ok;
 namespace {
 
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
-constexpr int32_t kMaxRows = 1 << 19;              // of a sequence: workgroups of 16 rows are numbered in 16 bits
+constexpr int32_t kMaxRows = 1 << 19;              // of a sequence
 
 size_t size_of(int dtype) { return dtype == CADDTREE_F32 ? 4 : 2; }
 
@@ -125,6 +125,9 @@ caddtree_status_t caddtree_adjust_logits(const caddtree_adjust_t* a, hipStream_t
   if (a->H < 0 || a->n_bias < 0) return fail(CADDTREE_E_INVALID, "H = %d and n_bias = %d must not be negative", a->H, a->n_bias);
   if (a->H > CADDTREE_MAX_HISTORY) return fail(CADDTREE_E_UNSUPPORTED, "H = %d exceeds %d", a->H, CADDTREE_MAX_HISTORY);
   if (a->n_bias > CADDTREE_MAX_BIAS) return fail(CADDTREE_E_UNSUPPORTED, "n_bias = %d exceeds %d", a->n_bias, CADDTREE_MAX_BIAS);
+  // (workgroups of 512 threads, for 2 rows of 8192 tokens each, are numbered in 32 bits by their threads)
+  if (((int64_t)a->T / 2 + 1) * ((int64_t)a->V / 8192 + 1) >= 1 << 23)
+    return fail(CADDTREE_E_UNSUPPORTED, "T = %d rows of V = %d: more than 2^23 workgroups", a->T, a->V);
   if (std::isnan(a->fill)) return fail(CADDTREE_E_INVALID, "fill is NaN");
   if (a->B == 0 || a->T == 0) return ok();
   if (a->n_bias > 0 && (a->bias_ids == nullptr || a->bias == nullptr))

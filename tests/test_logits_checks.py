@@ -268,7 +268,8 @@ GRAD = [(dict(grad=(AT["grad"], 350, 69)), INVALID), (dict(grad=(AT["grad"], 70,
     (dict(allowed_stride_b=-1), INVALID), (dict(allowed_stride_t=-1), INVALID), (dict(out=(AT["out"], 350, 69)), INVALID),
     (dict(out=(AT["out"], 349, 70)), INVALID), (dict(out=(AT["out"], 0, 70)), INVALID), (dict(out=(AT["logits"] + 2, 350, 70)), INVALID),
     (dict(out=(AT["logits"], 700, 70)), INVALID), (dict(out=(AT["history"], 350, 70)), INVALID), (dict(out=(AT["allowed"] + 8, 350, 70)), INVALID),
-    (dict(out=(AT["parent"], 350, 70)), INVALID), (dict(fill=float("nan")), INVALID)])
+    (dict(out=(AT["parent"], 350, 70)), INVALID), (dict(fill=float("nan")), INVALID),
+    (dict(T=2 ** 19, V=2 ** 20, parent=None, token_ids=None), UNSUPPORTED)])
 def test_adjust_validation(kw, status):
     a = _args(_lib.Adjust, **kw)
     assert _lib.lib().caddtree_adjust_logits(ctypes.byref(a), None) == status, _lib.lib().caddtree_last_error()
