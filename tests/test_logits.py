@@ -181,6 +181,34 @@ def test_adjust_paths():
     _check_adjust(x, adjust_logits(y, y, **kw), x, kw, "path, in place")
 
 
+def test_adjust_the_largest_tree():
+    """4096 nodes, more than are kept near, with paths that go through all parts of the tree."""
+    V, cap = 300, 4096
+    i = torch.arange(cap)
+    par = torch.maximum(i - 170, torch.tensor(-1)).to(I32).view(1, -1).cuda()
+    tok = torch.randint(V, (1, cap), generator=_gen(12), device="cuda", dtype=I32)
+    kw = dict(repetition=torch.tensor([1.2], device="cuda"), frequency=torch.tensor([0.25], device="cuda"), token_ids=tok, parent=par,
+              count=torch.tensor([4090], dtype=I32, device="cuda"))
+    x = _rows(_gen(13), 1, cap + 1, V, BF)
+    out = torch.full_like(x, 3.0)
+    _check_adjust(x, adjust_logits(x, out, **kw), torch.full_like(x, 3.0), kw, "largest tree")
+    y = x.clone()
+    _check_adjust(x, adjust_logits(y, y, **kw), x, kw, "largest tree, in place")
+
+
+@pytest.mark.parametrize("H", [3, 4, 2047, 2048, 2049, 4096, 6145])
+def test_adjust_history_lengths(H):
+    """Around what the workgroup takes at a time; every token from the same few."""
+    V = 9000
+    hist = (torch.arange(3 * H, device="cuda") * 7919 % 12 * 800).to(I32).view(3, H)
+    kw = dict(history=hist, history_len=torch.tensor([H, H - 1, H - 3], dtype=I32, device="cuda"),
+              frequency=torch.tensor([2.0 ** -6, 2.0 ** -5, 1.0], device="cuda"))
+    x = _rows(_gen(14), 3, 3, V, F32)
+    _check_adjust(x, adjust_logits(x, **kw), x, kw, "history")
+    y = x.clone()
+    _check_adjust(x, adjust_logits(y, y, **kw), x, kw, "history, in place")
+
+
 def test_adjust_shared_masks_and_repeated_logits():
     """One mask for all rows (strides of 0), and rows of logits that are one row."""
     gen = _gen(9)
@@ -292,6 +320,29 @@ def test_verify_reads_only_its_path():
     verify_tree(x, tok, par, count, *got[:3], weight=got[3])
     assert got[0].tolist() == [2, 1] and got[1][0, :2].tolist() == [0, 2]
     _check_verify(got, ref.verify(tok.cpu().numpy(), par.cpu().numpy(), count.cpu().numpy(), 5, logits=ref.f64(x)))
+
+
+@pytest.mark.parametrize("with_workspace", [False, True])
+@pytest.mark.parametrize("V", [64, 4200])
+def test_verify_the_largest_tree(V, with_workspace):
+    """A path to the last of 4096 nodes, most of them further than those kept near (of few tokens: siblings share them, and
+    the first of them ends the path early)."""
+    cap = 4096
+    i = torch.arange(cap)
+    par = torch.maximum(i - 500, torch.tensor(-1)).to(I32).view(1, -1).cuda()
+    tok = (i * 31 % V).to(I32).view(1, -1).cuda()
+    x = torch.randn((1, cap + 1, V), generator=_gen(4), device="cuda")
+    row, path = cap, []
+    while row > 0:
+        path.append(row)
+        row = int(par[0, row - 1]) + 1
+    for r, after in zip([0] + path[::-1], path[::-1]):
+        x[0, r, int(tok[0, after - 1])] = 50.0
+    count = torch.tensor([cap], dtype=I32, device="cuda")
+    got = _outputs(1, cap + 1, 12)
+    verify_tree(x, tok, par, count, *got[:3], weight=got[3], workspace=verify_workspace(x) if with_workspace else None)
+    _check_verify(got, ref.verify(tok.cpu().numpy(), par.cpu().numpy(), count.cpu().numpy(), 12, logits=ref.f64(x)))
+    assert V < cap or got[1][0, :len(path) + 1].tolist() == [0] + path[::-1]
 
 
 def test_verify_chosen_tokens():
@@ -510,6 +561,22 @@ def test_offsets_past_32_bits():
     none = torch.zeros((2, 0), dtype=I32, device="cuda")
     verify_tree(x, none, none, torch.zeros(2, dtype=I32, device="cuda"), *got[:3], weight=got[3])
     assert got[2][:, 0].tolist() == x[:, 0].float().argmax(-1).tolist()
+
+
+def test_more_rows_than_a_grid_has_places_in_its_second_dimension():
+    T, V = 70001, 9
+    x = _rows(_gen(19), 1, T, V, BF)
+    ok = torch.rand((1, T, V), generator=_gen(20), device="cuda") < 0.5
+    want = torch.where(ok, x, torch.tensor(-INF, dtype=BF, device="cuda"))
+    assert torch.equal(adjust_logits(x, allowed=_words(ok)), want)
+    y = x.clone()
+    assert torch.equal(adjust_logits(y, y, allowed=_words(ok)), want)
+    ids, target = torch.zeros((1, T, 1), dtype=I32, device="cuda"), torch.zeros((1, T, 1), device="cuda")
+    loss, stats, grad = torch.zeros((1, T), device="cuda"), torch.zeros((1, T, 3), device="cuda"), torch.zeros_like(x)
+    distill(x, ids, target, loss, grad=grad, stats=stats)
+    cut = lambda t: t[:, -3:].contiguous()
+    _check_distill(cut(x), cut(ids), cut(target), None, 1.0, False, cut(loss), cut(stats), cut(grad))
+    _check_distill(cut(x), cut(ids), cut(target), None, 1.0, False, grad=cut(distill_grad(x, ids, target, stats)), again=True)
 
 
 def test_empty_calls():
