@@ -563,6 +563,7 @@ __device__ __forceinline__ Sum join_parts(const PartSum* p, int n, double c, dou
 // The gradient of a part of a row.  kStats: from a.stats; else from the parts' sums, and the row's first part writes its
 // loss and stats (grad NULL: these alone).
 constexpr int kGradThreads = 256;
+constexpr int kGradLoads = 4;                     // vectors a lane has in flight while the list is gone over
 template <typename E, bool kStats>
 __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts ps) {
   constexpr int N = kN<E>;
@@ -582,31 +583,44 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts
   if (g == nullptr && !store) return;
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
   const float c = (float)(kLog2e / (double)a.temperature);
+  const int n = (last - first) / N;
+  Vec<E> q[kGradLoads];
+  if (g && n > 0) start_stream<E, kGradThreads, true>(q, l + first, 0, n);
+  Edge<E> edge;
+  edge.read(l + first, last - first);
   for (int i = tid; i < (last - first + 31) / 32; i += kGradThreads) s_bits[i] = 0;
   __syncthreads();
+  double Z = 0.0;
+  Sum sum = {};
   if (tid < kWave) {
     fetch_listed<E>(a, row, l, kStats ? nullptr : ps.listed + row * a.K, first, last, raw);
     read_listed(a, raw, first, last, L, s_bits);
     if constexpr (kStats) {
       if (tid == 0) finish(r, a.stats[row * 3], (double)a.stats[row * 3 + 1], (double)a.stats[row * 3 + 2], L, w, a.temperature, c);
     } else {
-      double Z;
-      const Sum sum = join_parts(ps.sum + row * ps.n, ps.n, kLog2e / (double)a.temperature, Z);
+      sum = join_parts(ps.sum + row * ps.n, ps.n, kLog2e / (double)a.temperature, Z);
       if (tid == 0) finish(r, sum.m, Z, sum.s, L, w, a.temperature, c);
-      if (store) put_loss(a, row, L, sum, Z, w);
     }
   }
-  Edge<E> edge;
-  edge.read(l + first, last - first);
   __syncthreads();
-  if (g == nullptr) return;
-  const uint32_t* bits = s_bits;
-  edge.look(bits);
-  const int n = (last - first) / N;
-  put_edge<E>(edge, g + first, r, c);
-  if (__builtin_expect(r.far, 0)) put_vectors<E, kGradThreads, 1, true>(l + first, g + first, 0, n, bits, r.m, r.rest, c);
-  else put_vectors<E, kGradThreads, 4, false>(l + first, g + first, 0, n, bits, r.mc, r.rest, c);
-  put_listed<E, kGradThreads>(a, g, r, L, first, last);
+  if (g) {
+    edge.look(s_bits);
+    put_edge<E>(edge, g + first, r, c);
+    const float mc = r.mc, rest = r.rest;
+    if (__builtin_expect(r.far, 0)) {
+      put_vectors<E, kGradThreads, 1, true>(l + first, g + first, 0, n, s_bits, r.m, rest, c);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kGradLoads; ++u) {
+        const int v = u * kGradThreads + tid;
+        __builtin_amdgcn_sched_barrier(0);
+        if (v < n) put_vector<E>(q[u], g + first, v, bits_at<N>(s_bits, v * N), mc, rest, c);
+      }
+      put_vectors<E, kGradThreads, 4, false>(l + first, g + first, min(n, kGradLoads * kGradThreads), n, s_bits, mc, rest, c);
+    }
+    put_listed<E, kGradThreads>(a, g, r, L, first, last);
+  }
+  if (store && tid < kWave) put_loss(a, row, L, sum, Z, w);
 }
 
 size_t bit_bytes(int n) { return (size_t)((n + 31) / 32) * 4; }
@@ -659,7 +673,7 @@ hipError_t launch(const DistillArgs& a, void* workspace, hipStream_t stream) {
 template <typename E>
 hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
   Parts ps = {};
-  ps.len = 8 * kGradThreads * kN<E>;
+  ps.len = kGradLoads * kGradThreads * kN<E>;
   ps.n = (a.V + ps.len - 1) / ps.len;
   return run(grad_kernel<E, true>, dim3((unsigned)(a.T * ps.n), (unsigned)a.B), kGradThreads, bit_bytes(ps.len), stream, a, ps);
 }
