@@ -8,6 +8,10 @@
 //
 // A bit for each token says whether it is listed (in LDS): its term is left out of R as the row streams by, and its
 // gradient is written by a lane of its own.
+//
+// Least traffic: each logit read once and each gradient written once.  The gradient needs the row's sums, so a row has to be
+// kept or read again; row_kernel does some of both, sums_kernel and grad_kernel do the latter with parts of a few rows.
+// Terms are fp32 exponentials of fp32 differences, added in fp64 (one addition a vector of 16 bytes) and joined in fp64.
 
 #include <hip/hip_runtime.h>
 
@@ -56,9 +60,9 @@ struct Row {
 constexpr float kFar = 1e30f;
 constexpr float kRoom = 8.f;                      // a term may reach 2^kRoom before the reference moves
 
-// bits of the N tokens from `at` (a multiple of N) on
 template <int N>
 constexpr uint32_t kNone = (1u << N) - 1;         // a lane past the row's end adds none of its vector's
+// bits of the N tokens from `at` (a multiple of N) on
 template <int N>
 __device__ __forceinline__ uint32_t bits_at(const uint32_t* bits, int at) {
   return reinterpret_cast<const uint8_t*>(bits)[at >> 3] >> (at & 7) & ((1u << N) - 1);
@@ -151,15 +155,6 @@ struct Sum {
   float m;
   double s;
 };
-__device__ __forceinline__ void join(Sum& x, const Sum& y, float c) {
-  const float m = fmaxf(x.m, y.m);
-  if (m == -INFINITY) {
-    x.s += y.s;                                   // (zeros, or NaN)
-    return;
-  }
-  x.s = x.s * (double)__builtin_amdgcn_exp2f((x.m - m) * c) + y.s * (double)__builtin_amdgcn_exp2f((y.m - m) * c);
-  x.m = m;
-}
 
 template <int kN>
 __device__ __forceinline__ float top_of(const float (&x)[kN]) {
@@ -402,7 +397,14 @@ __device__ void no_weight(const DistillArgs& a, int64_t row, typename E::T* g, i
 }
 
 // A workgroup a row: its loss, and the gradient.  The row's first kKeep vectors a thread stay in registers between the sums
-// and the gradient; what is behind them is read again, the last first.
+// and the gradient; what is behind them is read again, the last first, while it may still be in a cache.
+//
+// Bound by memory: 1024 rows of 151936 bf16 (a tenth of weight 0) in 126 us, 594 MB that have to move at 4.7 TB/s, where a
+// copy reaches 5.0.  Of 512 threads 0 / 8 / 14 / 18 vectors kept: 169 / 147 / 136 / 141 us; the whole
+// row in 1024 threads' registers: 151 (one workgroup a compute unit: nothing loads while it joins).
+// Streaming stores took 154 to 136, streaming loads of the second pass 133 to 123.
+// The loss alone: 2048 such rows in 103 us, 5.7 TB/s of the row's one read; bound by the exponentials' instructions (VALU
+// 80% active).  512 threads 108 us, 256 108, 1024 136 when it was chosen.
 template <typename E, int kThreads, int kKeep, bool kGrad>
 __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
   constexpr int N = kN<E>, kU = kGrad ? 4 : 8;
@@ -494,6 +496,8 @@ struct Parts {
 };
 constexpr int kMaxParts = kWave;
 
+// The parts' sums.  Bound by latency: 64 rows of 151936 bf16, 19 MB, in 11.7 us of which the read at the card's rate is 3;
+// the rest is a launch, the list's bits, and two barriers.  Read with the cache's hint, so that the second launch finds the row there.
 constexpr int kSumThreads = 512;
 template <typename E>
 __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts ps) {
@@ -562,6 +566,11 @@ __device__ __forceinline__ Sum join_parts(const PartSum* p, int n, double c, dou
 
 // The gradient of a part of a row.  kStats: from a.stats; else from the parts' sums, and the row's first part writes its
 // loss and stats (grad NULL: these alone).
+//
+// Each workgroup works the list out again, 8 K bytes and K exponentials: that costs less than another launch to do it once.
+// A part is what its lanes ask for at once, before the list is gone over.  520 rows of 65537 f16 with K = 128 (three tenths
+// of weight 0): 30.5 us, 116 MB at 3.8 TB/s; 1024 rows of 151936 bf16: 103 us with 4 loads a lane, 112 with 8.  Bound by
+// the wait for the list (waits 61% of the wavefronts' cycles), then by memory.
 constexpr int kGradThreads = 256;
 constexpr int kGradLoads = 4;                     // vectors a lane has in flight while the list is gone over
 template <typename E, bool kStats>
@@ -636,6 +645,10 @@ hipError_t run(F kernel, dim3 grid, int threads, size_t lds, hipStream_t stream,
   return hipGetLastError();
 }
 
+// By a row's vectors: as few threads as hold the row, so that many rows are under way, and none where a row does not fit.
+// Measured, us: 8192 rows of 8192 bf16 128 threads x 14 72 - 80, 512 x 0 171; 4096 rows of 32000 bf16 256 x 16 104, 512 x 8
+// 119, 512 x 14 134; 512 rows of 25000 vectors 512 x 14 64, 1024 x 16 68; 512 rows of 151936 f32 (37984 vectors) 512 x 14
+// 148, 1024 x 16 131.
 template <typename E>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t stream) {
   const dim3 all((unsigned)a.T, (unsigned)a.B);
@@ -674,12 +687,15 @@ template <typename E>
 hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
   Parts ps = {};
   ps.len = kGradLoads * kGradThreads * kN<E>;
-  ps.n = (a.V + ps.len - 1) / ps.len;
+  ps.n = distill_grad_parts(a.V, sizeof(typename E::T));
   return run(grad_kernel<E, true>, dim3((unsigned)(a.T * ps.n), (unsigned)a.B), kGradThreads, bit_bytes(ps.len), stream, a, ps);
 }
 
 }  // namespace
 
+// Two workgroups a compute unit where the rows are fewer than that, a part no shorter than what a workgroup asks for at
+// once.  Parts or whole rows, us, of 151936 bf16: 1 row 13.4 / 27.1, 16 rows 16.1 / 28, 64 rows 20.7 / 28.5, 128 rows
+// 32.5 / 29.6; 64 rows of 32000 16.8 / 15.0.  512 / 768 / 1024 workgroups: 20.7 / 23.6 / 24.9.
 int distill_parts(int64_t rows, int32_t V) {
   if (rows < 1 || rows > 64) return 1;
   return (int)std::max<int64_t>(1, std::min<int64_t>({512 / rows, V / 4096, kMaxParts}));
@@ -687,6 +703,11 @@ int distill_parts(int64_t rows, int32_t V) {
 size_t distill_workspace(int64_t rows, int32_t V) {
   const int n = distill_parts(rows, V);
   return n <= 1 ? 0 : (size_t)rows * (n * sizeof(PartSum) + CADDTREE_MAX_TEACHER * sizeof(float));
+}
+
+int distill_grad_parts(int32_t V, size_t elem) {
+  const int len = kGradLoads * kGradThreads * 16 / (int)elem;
+  return (V + len - 1) / len;
 }
 
 hipError_t launch_distill(const DistillArgs& a, void* workspace, caddtree_dtype_t dtype, hipStream_t stream) {

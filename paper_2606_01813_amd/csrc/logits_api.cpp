@@ -230,6 +230,9 @@ caddtree_status_t caddtree_distill(const caddtree_distill_t* a, void* workspace,
 caddtree_status_t caddtree_distill_grad(const caddtree_distill_t* a, hipStream_t stream) {
   caddtree_status_t st = check_distill(a);
   if (st != CADDTREE_OK) return st;
+  // (workgroups of 256 threads are numbered in 32 bits by their threads)
+  if ((int64_t)a->T * caddtree::distill_grad_parts(a->V, size_of(enum_value(a->dtype))) >= 1 << 24)
+    return fail(CADDTREE_E_UNSUPPORTED, "T = %d rows of V = %d: more than 2^24 workgroups", a->T, a->V);
   if (a->B == 0 || a->T == 0) return ok();
   if (a->stats == nullptr) return fail(CADDTREE_E_INVALID, "stats is NULL");
   if ((st = check_distill_data(a, false, nullptr, 0)) != CADDTREE_OK) return st;

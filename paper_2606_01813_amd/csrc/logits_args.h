@@ -65,6 +65,8 @@ struct DistillArgs {
 // How many parts a row is cut into where there is a workspace, and its bytes (0: one part).
 int distill_parts(int64_t rows, int32_t V);
 size_t distill_workspace(int64_t rows, int32_t V);
+// ... where its gradient is written by itself; elem: bytes of a logit.
+int distill_grad_parts(int32_t V, size_t elem);
 hipError_t launch_distill(const DistillArgs& a, void* workspace, caddtree_dtype_t dtype, hipStream_t stream);
 hipError_t launch_distill_grad(const DistillArgs& a, caddtree_dtype_t dtype, hipStream_t stream);
 

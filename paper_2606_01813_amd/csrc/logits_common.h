@@ -50,8 +50,7 @@ struct Vec {
   static __device__ __forceinline__ Vec load(const T* row, uint32_t v) {
     return load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + v * 16u));
   }
-  __device__ __forceinline__ void store(T* row, uint32_t v) const { store(reinterpret_cast<T*>(reinterpret_cast<char*>(row) + v * 16u)); }
-  // ... with the hint that nothing else reads it soon
+  // ... at a byte of the row, with the hint that nothing else reads it soon
   static __device__ __forceinline__ Vec load_once(const T* row, uint32_t byte) {
     return Vec{__builtin_nontemporal_load(&reinterpret_cast<const Loose*>(reinterpret_cast<const char*>(row) + byte)->w)};
   }

@@ -4,6 +4,9 @@
 // Only the rows on the path decide, a handful of a tree's hundreds, and which they are is known one row at a time: a
 // workgroup walks a tree and reads a row whenever it gets there.  Where all rows of the call are few, that chain is
 // longer than reading them all at once: choose_kernel does so, a part of a row a workgroup, and the walk joins the parts.
+//
+// 32 trees of up to 256 nodes, 151936 bf16 logits a row, take 55 us: the longest path's rows one after the other, each at what
+// a compute unit reads of its 304 KB.  One tree of 64 nodes: 12 us, all rows at once in 6.5 and the walk over the parts in 6.
 
 #include <hip/hip_runtime.h>
 
@@ -42,6 +45,7 @@ struct Best {
 // The best of a row's tokens first .. last - 1 (first a multiple of 8) by a workgroup, kU loads in flight a lane; in each
 // wavefront its own.  A lane keeps the vector with the largest logit, the first of equals; which of its elements that is
 // is looked for once, at the end.
+// The walk with 5 / 10 / 20 loads a lane: 55.2 / 56.4 / 92 us (20 leave room for too few wavefronts).
 template <typename E, int kThreads, int kU>
 __device__ Best best_of(const typename E::T* row, int first, int last) {
   constexpr int N = kN<E>;
@@ -177,6 +181,8 @@ void launch(const VerifyArgs& a, void* workspace, size_t elem, hipStream_t strea
 
 }  // namespace
 
+// All rows at once where their logits are no more than the card reads in a walk's time, 96 MiB.  Both ways, us, 151936 bf16:
+// 2 trees of 65 rows (40 MB) 15 / 25, 4 of 65 (79 MB) 23 - 26 / 42, 1 of 257 (78 MB) 20 - 23 / 24.4.
 int verify_parts(int64_t B, int64_t T, int32_t V, size_t elem) {
   const int64_t rows = B * T;
   if (rows < 1 || rows * V * (int64_t)elem > 96 << 20) return 0;

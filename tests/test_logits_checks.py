@@ -311,6 +311,7 @@ def test_other_refusals_and_calls_of_nothing():
     assert lib.caddtree_distill(r(_args(_lib.Distill, grad=(AT["loss"], 350, 70))), None, 0, None) == INVALID
     assert lib.caddtree_distill_grad(r(_args(_lib.Distill, stats=None)), None) == INVALID
     assert lib.caddtree_distill_grad(r(_args(_lib.Distill, grad=(None, 0, 0))), None) == INVALID
+    assert lib.caddtree_distill_grad(r(_args(_lib.Distill, T=2 ** 19, V=2 ** 18, dtype=0)), None) == UNSUPPORTED   # 2^25 workgroups
     for kw in (dict(B=0), dict(T=0)):
         assert lib.caddtree_adjust_logits(r(_args(_lib.Adjust, parent=None, token_ids=None, **kw)), None) == _lib.OK
         assert lib.caddtree_distill(r(_args(_lib.Distill, **kw)), None, 0, None) == _lib.OK
