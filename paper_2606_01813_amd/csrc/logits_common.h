@@ -16,18 +16,15 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 struct BF16 {
   using T = __bf16;
   typedef __bf16 T2 __attribute__((ext_vector_type(2)));
-  static constexpr uint32_t kNegInf = 0xff80ff80u;
   static __device__ __forceinline__ float get(uint32_t w, int j) { return __uint_as_float(j ? w & 0xffff0000u : w << 16); }
 };
 struct F16 {
   using T = _Float16;
   typedef _Float16 T2 __attribute__((ext_vector_type(2)));
-  static constexpr uint32_t kNegInf = 0xfc00fc00u;
   static __device__ __forceinline__ float get(uint32_t w, int j) { return (float)__builtin_bit_cast(T2, w)[j]; }
 };
 struct F32 {
   using T = float;
-  static constexpr uint32_t kNegInf = 0xff800000u;
   static __device__ __forceinline__ float get(uint32_t w, int) { return __uint_as_float(w); }
 };
 template <typename E>
@@ -50,6 +47,9 @@ struct Vec {
   static __device__ __forceinline__ Vec load(const T* row, uint32_t v) {
     return load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + v * 16u));
   }
+  static __device__ __forceinline__ Vec load_at(const T* row, uint32_t byte) {
+    return load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(row) + byte));
+  }
   // ... at a byte of the row, with the hint that nothing else reads it soon
   static __device__ __forceinline__ Vec load_once(const T* row, uint32_t byte) {
     return Vec{__builtin_nontemporal_load(&reinterpret_cast<const Loose*>(reinterpret_cast<const char*>(row) + byte)->w)};
@@ -57,7 +57,6 @@ struct Vec {
   __device__ __forceinline__ void stream_at(T* row, uint32_t byte) const {
     __builtin_nontemporal_store(w, &reinterpret_cast<Loose*>(reinterpret_cast<char*>(row) + byte)->w);
   }
-  static __device__ __forceinline__ Vec neg_inf() { return Vec{u32x4{E::kNegInf, E::kNegInf, E::kNegInf, E::kNegInf}}; }
   __device__ __forceinline__ void get(float (&x)[kN<E>]) const {
 #pragma unroll
     for (int j = 0; j < kN<E>; ++j) x[j] = E::get(w[j / kEach<E>], j % kEach<E>);

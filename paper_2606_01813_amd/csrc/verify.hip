@@ -42,72 +42,88 @@ struct Best {
   __device__ __forceinline__ int token() const { return x > -INFINITY ? id : -1; }
 };
 
-// The best of a row's tokens first .. last - 1 (first a multiple of 8) by a workgroup, kU loads in flight a lane; in each
-// wavefront its own.  A lane keeps the vector with the largest logit, the first of equals; which of its elements that is
-// is looked for once, at the end.
+// The best of a row's tokens first .. last - 1 (first a multiple of 8) by a workgroup, kU loads in flight a lane.  A lane
+// keeps its largest logit and which kU vectors it was among, the first of equals; the lanes that have the workgroup's
+// largest read theirs again and look for its token: 13 instructions a vector of 8 logits, of which unpacking is 8.
+// s_top and s_id: in LDS, not read any more by a thread that another's call may overtake.
 // The walk with 5 / 10 / 20 loads a lane: 55.2 / 56.4 / 92 us (20 leave room for too few wavefronts).
 template <typename E, int kThreads, int kU>
-__device__ Best best_of(const typename E::T* row, int first, int last) {
-  constexpr int N = kN<E>;
-  const int n = last / N, lane = (int)(threadIdx.x % kWave);
-  const int edge = n * N + (int)threadIdx.x;
-  const float rest = edge < last && threadIdx.x < N ? (float)row[edge] : -INFINITY;
-  int v = first / N + (int)threadIdx.x;
-  Vec<E> q[kU], best = Vec<E>::neg_inf();
-  if (v - lane < n) {
-#pragma unroll
-    for (int u = 0; u < kU; ++u) q[u] = row_vector<E>(row, v + u * kThreads, n);
-  }
+__device__ Best best_of(const typename E::T* row, int first, int last, float* s_top, int* s_id) {
+  constexpr int N = kN<E>, kWaves = kThreads / kWave;
+  const int n = last / N, tid = (int)threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+  const int edge = n * N + tid;
+  const float rest = edge < last && tid < N ? (float)row[edge] : -INFINITY;
+  int at = first / N + wave * kWave, got = -1;          // (at: of the wavefront's first lane)
   float top = -INFINITY;
-  int at = 0;
-  for (; v - lane < n; v += kU * kThreads) {          // (past the end a lane sees the last vector again)
+  if (at < n) {
+    const uint32_t end = (uint32_t)(n - 1) * 16u;       // (past it a lane sees the last vector again)
+    uint32_t byte = (uint32_t)(first / N + tid) * 16u;
+    Vec<E> q[kU];
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      float x[N];
-      __builtin_amdgcn_sched_barrier(0);              // (one vector unpacked at a time: registers)
-      q[u].get(x);
-      float t = x[0];
+    for (int u = 0; u < kU; ++u) q[u] = Vec<E>::load_at(row, min(byte + u * kThreads * 16u, end));
+    for (; at < n; at += kU * kThreads) {
+      byte += kU * kThreads * 16u;
+      float t = -INFINITY;
 #pragma unroll
-      for (int j = 1; j < N; ++j) t = fmaxf(t, x[j]);
-      const bool up = t > top;                        // (vectors only grow: the first of equals stays; NaN is never above)
+      for (int u = 0; u < kU; ++u) {
+        float x[N];
+        __builtin_amdgcn_sched_barrier(0);              // (one vector unpacked at a time: registers)
+        q[u].get(x);
+#pragma unroll
+        for (int j = 0; j < N; ++j) t = fmaxf(t, x[j]);
+        q[u] = Vec<E>::load_at(row, min(byte + u * kThreads * 16u, end));
+      }
+      const bool up = t > top;
       top = up ? t : top;
-      at = up ? min(v + u * kThreads, n - 1) : at;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) best.w[j] = up ? q[u].w[j] : best.w[j];
-      q[u] = row_vector<E>(row, v + (u + kU) * kThreads, n);
+      got = up ? at : got;
     }
   }
-  float x[N];
-  best.get(x);
-  int place = N - 1;
+  const float most = wave_max(fmaxf(top, rest));
+  if (tid % kWave == 0) s_top[wave] = most;
+  if (tid == 0) *s_id = INT_MAX;
+  __syncthreads();
+  float x = s_top[0];
 #pragma unroll
-  for (int j = N - 2; j >= 0; --j) place = x[j] == top ? j : place;
-  Best m = {top, top > -INFINITY ? at * N + place : INT_MAX};
-  if (rest > -INFINITY) m.take(rest, edge);
-  m.join();
-  return m;
+  for (int w = 1; w < kWaves; ++w) x = fmaxf(x, s_top[w]);
+  if (x > -INFINITY && (top == x || rest == x)) {
+    int id = edge;
+    if (top == x) {
+      const int v = got + tid % kWave;
+      Vec<E> q[kU];
+      int place = 0;
+#pragma unroll
+      for (int u = 0; u < kU; ++u) q[u] = row_vector<E>(row, v + u * kThreads, n);
+#pragma unroll
+      for (int u = kU - 1; u >= 0; --u) {               // (the last first: the lowest of equals stays)
+        float y[N];
+        q[u].get(y);
+#pragma unroll
+        for (int j = N - 1; j >= 0; --j) place = y[j] == x ? u * N + j : place;
+      }
+      id = min(v + place / N * kThreads, n - 1) * N + place % N;
+    }
+    atomicMin(s_id, id);
+  }
+  __syncthreads();
+  return Best{x, *s_id};
 }
 
 // Part blockIdx.x of row blockIdx.y of tree blockIdx.z: parts [B, T, n], of len tokens (a multiple of 8)
 template <typename E>
 __global__ __launch_bounds__(kChooseThreads) void choose_kernel(VerifyArgs a, Best* parts, int len) {
-  __shared__ Best s[kChooseThreads / kWave];
+  __shared__ float s_top[kChooseThreads / kWave];
+  __shared__ int s_id;
   const int b = (int)blockIdx.z, t = (int)blockIdx.y, first = (int)blockIdx.x * len;
   if (t > min(max(a.count[b], 0), a.T - 1)) return;
-  const Best m = best_of<E, kChooseThreads, 4>(row_of<E>(a.in, b, t), first, min(first + len, a.V));
-  if (threadIdx.x % kWave == 0) s[threadIdx.x / kWave] = m;
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  Best all = s[0];
-#pragma unroll
-  for (int w = 1; w < kChooseThreads / kWave; ++w) all.take(s[w].x, s[w].id);
-  parts[((int64_t)b * a.T + t) * gridDim.x + blockIdx.x] = all;
+  const Best m = best_of<E, kChooseThreads, 4>(row_of<E>(a.in, b, t), first, min(first + len, a.V), s_top, &s_id);
+  if (threadIdx.x == 0) parts[((int64_t)b * a.T + t) * gridDim.x + blockIdx.x] = m;
 }
 
 enum Source { kRead, kParts, kChosen };               // where a row's token comes from: its logits, their parts, the caller
 template <typename E, Source kFrom, int kThreads>
 __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best* parts, int n_parts) {
-  __shared__ Best s[kThreads / kWave];
+  __shared__ float s_top[kThreads / kWave];
+  __shared__ int s_id;
   __shared__ uint32_t s_token[kNodes];
   __shared__ uint16_t s_parent[kNodes];               // + 1
   __shared__ int s_child;
@@ -124,24 +140,20 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best
     for (int i = tid; i < a.T; i += kThreads) a.weight[(int64_t)b * a.T + i] = 0.f;
   int row = 0, steps = 0;
   while (true) {
-    Best m;
+    int t;
     if constexpr (kFrom == kRead) {
-      m = best_of<E, kThreads, 5>(row_of<E>(a.in, b, row), 0, a.V);
-      if (tid % kWave == 0) s[tid / kWave] = m;
+      const Best m = best_of<E, kThreads, 5>(row_of<E>(a.in, b, row), 0, a.V, s_top, &s_id);
+      t = m.token();
     } else if constexpr (kFrom == kParts) {
       const int i = tid % kWave;
-      m = i < n_parts ? parts[((int64_t)b * a.T + row) * n_parts + i] : Best{-INFINITY, INT_MAX};
+      Best m = i < n_parts ? parts[((int64_t)b * a.T + row) * n_parts + i] : Best{-INFINITY, INT_MAX};
       m.join();
+      t = m.token();
+    } else {
+      t = a.chosen[(int64_t)b * a.T + row];
     }
     if (tid == 0) s_child = INT_MAX;
     __syncthreads();                                  // (the weights are cleared too, and the nodes are there)
-    int t;
-    if constexpr (kFrom == kRead) {
-      m = tid % kWave < kThreads / kWave ? s[tid % kWave] : Best{-INFINITY, INT_MAX};
-      m.join();
-    }
-    if constexpr (kFrom == kChosen) t = a.chosen[(int64_t)b * a.T + row];
-    else t = m.token();
     if (tid == 0) {
       a.index[(int64_t)b * a.M + steps] = row;
       a.tokens[(int64_t)b * a.M + steps] = t;
@@ -152,7 +164,7 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best
     for (int i = row + tid; i < n; i += kThreads)
       if (i < kNodes ? s_parent[i] == row && (int)s_token[i] == t : par[i] == row - 1 && tok[i] == t) atomicMin(&s_child, i);
     __syncthreads();
-    const int child = s_child;
+    const int child = __builtin_amdgcn_readfirstlane(s_child);
     if (child == INT_MAX) break;
     row = child + 1;
     __syncthreads();                                  // (s and s_child have been read)
