@@ -40,13 +40,20 @@ struct Best {
     for (int o = 32; o > 0; o >>= 1) take(__shfl_xor(x, o), __shfl_xor(id, o));
   }
   __device__ __forceinline__ int token() const { return x > -INFINITY ? id : -1; }
+  // as a number that is larger for the better (-0 and 0 are equals)
+  __device__ __forceinline__ uint64_t key() const {
+    const uint32_t w = __float_as_uint(x + 0.f);
+    return (uint64_t)(w >> 31 ? ~w : w | 1u << 31) << 32 | ~(uint32_t)id;
+  }
 };
+constexpr uint64_t kNoKey = (uint64_t)0x00800000u << 32;      // (keys of -inf are below)
 
 // The best of a row's tokens first .. last - 1 (first a multiple of 8) by a workgroup, kU loads in flight a lane.  A lane
 // keeps its largest logit and which kU vectors it was among, the first of equals; the lanes that have the workgroup's
 // largest read theirs again and look for its token: 13 instructions a vector of 8 logits, of which unpacking is 8.
 // s_top and s_id: in LDS, not read any more by a thread that another's call may overtake.
-// The walk with 5 / 10 / 20 loads a lane: 55.2 / 56.4 / 92 us (20 leave room for too few wavefronts).
+// The walk over 32 trees with 2 / 3 / 4 / 5 loads a lane: 43.4 / 42.1 / 45.2 / 46.3 us (a wavefront's last ones reach past
+// the row); 512 threads with 6 45.2.
 template <typename E, int kThreads, int kU>
 __device__ Best best_of(const typename E::T* row, int first, int last, float* s_top, int* s_id) {
   constexpr int N = kN<E>, kWaves = kThreads / kWave;
@@ -61,8 +68,7 @@ __device__ Best best_of(const typename E::T* row, int first, int last, float* s_
     Vec<E> q[kU];
 #pragma unroll
     for (int u = 0; u < kU; ++u) q[u] = Vec<E>::load_at(row, min(byte + u * kThreads * 16u, end));
-    for (; at < n; at += kU * kThreads) {
-      byte += kU * kThreads * 16u;
+    const auto look = [&](bool more) {                  // (inlined for each)
       float t = -INFINITY;
 #pragma unroll
       for (int u = 0; u < kU; ++u) {
@@ -71,12 +77,17 @@ __device__ Best best_of(const typename E::T* row, int first, int last, float* s_
         q[u].get(x);
 #pragma unroll
         for (int j = 0; j < N; ++j) t = fmaxf(t, x[j]);
-        q[u] = Vec<E>::load_at(row, min(byte + u * kThreads * 16u, end));
+        if (more) q[u] = Vec<E>::load_at(row, min(byte + u * kThreads * 16u, end));
       }
       const bool up = t > top;
       top = up ? t : top;
       got = up ? at : got;
+    };
+    for (; at + kU * kThreads < n; at += kU * kThreads) {
+      byte += kU * kThreads * 16u;
+      look(true);
     }
+    look(false);
   }
   const float most = wave_max(fmaxf(top, rest));
   if (tid % kWave == 0) s_top[wave] = most;
@@ -127,11 +138,22 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best
   __shared__ uint32_t s_token[kNodes];
   __shared__ uint16_t s_parent[kNodes];               // + 1
   __shared__ int s_child;
+  __shared__ uint64_t s_key[kFrom == kParts ? kNodes : 1];   // of the first rows
+  __shared__ int s_chosen[kFrom == kChosen ? kNodes : 1];
   const int b = (int)blockIdx.x, tid = threadIdx.x;
   const int n = min(max(a.count[b], 0), a.T - 1);
   const int32_t* tok = a.token_ids + (int64_t)b * (a.T - 1);
   const int32_t* par = a.parent + (int64_t)b * (a.T - 1);
-  for (int i = tid; i < min(n, kNodes); i += kThreads) {
+  const int near = min(a.T, kNodes);
+  if constexpr (kFrom == kParts) {
+    for (int i = tid; i < near; i += kThreads) s_key[i] = 0;
+    __syncthreads();
+    for (int i = tid; i < near * n_parts; i += kThreads)
+      atomicMax(reinterpret_cast<unsigned long long*>(&s_key[i / n_parts]), (unsigned long long)parts[(int64_t)b * a.T * n_parts + i].key());
+  }
+  if constexpr (kFrom == kChosen)
+    for (int i = tid; i < near; i += kThreads) s_chosen[i] = a.chosen[(int64_t)b * a.T + i];
+  for (int i = tid; i < min(a.T - 1, kNodes); i += kThreads) {    // (those past n are not looked at)
     const int p = par[i];
     s_token[i] = (uint32_t)tok[i];
     s_parent[i] = (uint16_t)(p >= -1 && p < i ? p + 1 : 0xffff);     // (no child of any row: children come after their parent)
@@ -141,19 +163,20 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best
   int row = 0, steps = 0;
   while (true) {
     int t;
-    if constexpr (kFrom == kRead) {
-      const Best m = best_of<E, kThreads, 5>(row_of<E>(a.in, b, row), 0, a.V, s_top, &s_id);
-      t = m.token();
-    } else if constexpr (kFrom == kParts) {
-      const int i = tid % kWave;
-      Best m = i < n_parts ? parts[((int64_t)b * a.T + row) * n_parts + i] : Best{-INFINITY, INT_MAX};
-      m.join();
-      t = m.token();
-    } else {
-      t = a.chosen[(int64_t)b * a.T + row];
-    }
+    if constexpr (kFrom == kRead) t = best_of<E, kThreads, 3>(row_of<E>(a.in, b, row), 0, a.V, s_top, &s_id).token();
     if (tid == 0) s_child = INT_MAX;
-    __syncthreads();                                  // (the weights are cleared too, and the nodes are there)
+    __syncthreads();                                  // (the weights are cleared too, and what is in LDS is there)
+    if constexpr (kFrom == kParts) {
+      if (row < kNodes) {
+        t = s_key[row] >= kNoKey ? (int)~(uint32_t)s_key[row] : -1;
+      } else {
+        const int i = tid % kWave;
+        Best m = i < n_parts ? parts[((int64_t)b * a.T + row) * n_parts + i] : Best{-INFINITY, INT_MAX};
+        m.join();
+        t = m.token();
+      }
+    }
+    if constexpr (kFrom == kChosen) t = row < kNodes ? s_chosen[row] : a.chosen[(int64_t)b * a.T + row];
     if (tid == 0) {
       a.index[(int64_t)b * a.M + steps] = row;
       a.tokens[(int64_t)b * a.M + steps] = t;
