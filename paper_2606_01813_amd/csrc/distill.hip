@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
   __shared__ int s_twice;
   const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n, tid = threadIdx.x;
   const int64_t row = (int64_t)blockIdx.y * a.T + t;
-  if (weight_of(a, row) == 0.f) return;
+  if (weight_of(a, row) == 0.f) return;             // (asking for the logits before that gains nothing)
   const int first = part * ps.len, last = min(a.V, first + ps.len);
   const float c = (float)(kLog2e / (double)a.temperature);
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
@@ -568,6 +568,7 @@ __device__ __forceinline__ Sum join_parts(const PartSum* p, int n, double c, dou
 // loss and stats (grad NULL: these alone).
 //
 // Each workgroup works the list out again, 8 K bytes and K exponentials: that costs less than another launch to do it once.
+// One wavefront does, while another joins the parts (one after the other: 64 rows of 151936 19.5 us in both launches, so 18.5).
 // A part is what its lanes ask for at once, before the list is gone over.  520 rows of 65537 f16 with K = 128 (three tenths
 // of weight 0): 30.5 us, 116 MB at 3.8 TB/s; 1024 rows of 151936 bf16: 103 us with 4 loads a lane, 112 with 8.  Bound by
 // the wait for the list (waits 61% of the wavefronts' cycles), then by memory.
@@ -578,7 +579,8 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts
   constexpr int N = kN<E>;
   __shared__ Listed L;
   __shared__ Raw raw;
-  __shared__ Row r;
+  __shared__ Sum s_sum;
+  __shared__ double s_Z;
   const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n;
   const int64_t row = (int64_t)blockIdx.y * a.T + t;
   const int tid = threadIdx.x, first = part * ps.len, last = min(a.V, first + ps.len);
@@ -599,19 +601,28 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts
   edge.read(l + first, last - first);
   for (int i = tid; i < (last - first + 31) / 32; i += kGradThreads) s_bits[i] = 0;
   __syncthreads();
-  double Z = 0.0;
-  Sum sum = {};
   if (tid < kWave) {
     fetch_listed<E>(a, row, l, kStats ? nullptr : ps.listed + row * a.K, first, last, raw);
     read_listed(a, raw, first, last, L, s_bits);
+  } else if (tid < 2 * kWave) {                     // (meanwhile)
+    Sum sum;
+    double Z;
     if constexpr (kStats) {
-      if (tid == 0) finish(r, a.stats[row * 3], (double)a.stats[row * 3 + 1], (double)a.stats[row * 3 + 2], L, w, a.temperature, c);
+      sum = Sum{a.stats[row * 3], (double)a.stats[row * 3 + 2]};
+      Z = (double)a.stats[row * 3 + 1];
     } else {
       sum = join_parts(ps.sum + row * ps.n, ps.n, kLog2e / (double)a.temperature, Z);
-      if (tid == 0) finish(r, sum.m, Z, sum.s, L, w, a.temperature, c);
+    }
+    if (tid == kWave) {
+      s_sum = sum;
+      s_Z = Z;
     }
   }
   __syncthreads();
+  const Sum sum = s_sum;
+  const double Z = s_Z;
+  Row r;                                            // (each for itself)
+  finish(r, sum.m, Z, sum.s, L, w, a.temperature, c);
   if (g) {
     edge.look(s_bits);
     put_edge<E>(edge, g + first, r, c);

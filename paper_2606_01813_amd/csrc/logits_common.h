@@ -98,16 +98,60 @@ __device__ __forceinline__ Vec<E> row_vector(const typename E::T* l, int v, int 
   return kOnce ? Vec<E>::load_once(l, at * 16u) : Vec<E>::load(l, at);
 }
 
-// over the lanes of a wavefront, the result in all of them (fixed order)
+// Over the lanes of a wavefront, the result in all of them, in a fixed order: pairs, fours, eights (a mirrored eight holds
+// the other four's), sixteens, then rows of 16 and halves swapped between two registers.  No trip through LDS: with
+// shuffles, which go through it, 64 rows' loss and gradient took 21.2 us instead of 19.5, one row's 13.4 instead of 11.7.
+template <int kControl>
+__device__ __forceinline__ uint32_t moved(uint32_t w) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)w, kControl, 0xf, 0xf, true);
+}
+template <int kControl>
+__device__ __forceinline__ float moved(float v) { return __uint_as_float(moved<kControl>(__float_as_uint(v))); }
+template <int kControl>
+__device__ __forceinline__ double moved(double v) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  return __builtin_bit_cast(double, (uint64_t)moved<kControl>((uint32_t)(w >> 32)) << 32 | moved<kControl>((uint32_t)w));
+}
+constexpr int kPairs = 0xb1, kFours = 0x4e, kEights = 0x141, kSixteens = 0x140;
+template <bool kHalves>
+__device__ __forceinline__ void split(uint32_t w, uint32_t& even, uint32_t& odd) {
+  const auto r = kHalves ? __builtin_amdgcn_permlane32_swap(w, w, false, false) : __builtin_amdgcn_permlane16_swap(w, w, false, false);
+  even = r[0];
+  odd = r[1];
+}
+template <bool kHalves>
+__device__ __forceinline__ void split(float v, float& even, float& odd) {
+  uint32_t a, b;
+  split<kHalves>(__float_as_uint(v), a, b);
+  even = __uint_as_float(a);
+  odd = __uint_as_float(b);
+}
+template <bool kHalves>
+__device__ __forceinline__ void split(double v, double& even, double& odd) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, v);
+  uint32_t a0, b0, a1, b1;
+  split<kHalves>((uint32_t)w, a0, b0);
+  split<kHalves>((uint32_t)(w >> 32), a1, b1);
+  even = __builtin_bit_cast(double, (uint64_t)a1 << 32 | a0);
+  odd = __builtin_bit_cast(double, (uint64_t)b1 << 32 | b0);
+}
+template <typename T, typename F>
+__device__ __forceinline__ T over_wave(T v, F join) {
+  v = join(v, moved<kPairs>(v));
+  v = join(v, moved<kFours>(v));
+  v = join(v, moved<kEights>(v));
+  v = join(v, moved<kSixteens>(v));
+  T a, b;
+  split<false>(v, a, b);
+  v = join(a, b);
+  split<true>(v, a, b);
+  return join(a, b);
+}
 __device__ __forceinline__ float wave_max(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
-  return v;
+  return over_wave(v, [](float a, float b) { return fmaxf(a, b); });
 }
 __device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  return over_wave(v, [](double a, double b) { return a + b; });
 }
 
 }  // namespace lg
