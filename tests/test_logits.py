@@ -345,6 +345,51 @@ def test_verify_the_largest_tree(V, with_workspace):
     assert V < cap or got[1][0, :len(path) + 1].tolist() == [0] + path[::-1]
 
 
+@pytest.mark.parametrize("V", [4099, 40011, 151936])
+@pytest.mark.parametrize("dtype", [BF, F16, F32])
+@pytest.mark.parametrize("with_workspace", [False, True])
+def test_verify_ties_anywhere(V, dtype, with_workspace):
+    """Of equals the lowest id, whichever lanes, vectors and parts of the row they stand in; -0 and 0 are equals."""
+    gen = _gen(V)
+    B = 40
+    x = torch.full((B, 1, V), -5.0, dtype=dtype, device="cuda")
+    first = []
+    for b in range(B):
+        n = [1, 2, 3, 50][b % 4]
+        at = torch.randint(V * (b % 3) // 3, V, (n,), generator=gen, device="cuda")
+        x[b, 0, at] = [2.5, 0.0, -0.0][b % 3]
+        if b % 5 == 0:
+            x[b, 0, at[0]] = -0.0 if b % 3 else 2.5
+        if b % 7 == 3:
+            at = torch.tensor([V - 1], device="cuda")                      # alone, past the last whole vector
+            x[b, 0] = float("nan")
+            x[b, 0, V - 1] = -7.0
+        first.append(int(at.min()))
+    none = torch.zeros((B, 0), dtype=I32, device="cuda")
+    got = _outputs(B, 1, 1)
+    verify_tree(x, none, none, torch.zeros(B, dtype=I32, device="cuda"), *got[:3], weight=got[3],
+                workspace=verify_workspace(x) if with_workspace else None)
+    assert got[2][:, 0].tolist() == first
+
+
+def test_verify_chosen_tokens_of_the_largest_tree():
+    cap = 4096
+    i = torch.arange(cap)
+    par = torch.maximum(i - 500, torch.tensor(-1)).to(I32).view(1, -1).cuda()
+    tok = i.to(I32).view(1, -1).cuda()
+    chosen = torch.full((1, cap + 1), -1, dtype=I32, device="cuda")
+    row, path = cap, [cap]
+    while row > 0:
+        row, after = int(par[0, row - 1]) + 1, row
+        chosen[0, row] = after - 1
+        path.append(row)
+    got = _outputs(1, cap + 1, 12)
+    verify_tree(None, tok, par, torch.tensor([cap], dtype=I32, device="cuda"), *got[:3], chosen=chosen, weight=got[3])
+    path = path[::-1]
+    assert got[0].tolist() == [len(path)] and got[1][0, :len(path)].tolist() == path
+    assert got[3].nonzero()[:, 1].tolist() == path
+
+
 def test_verify_chosen_tokens():
     B, cap, V = 5, 100, 6
     gen = _gen(3)
