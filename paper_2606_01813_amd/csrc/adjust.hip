@@ -12,7 +12,7 @@
 // changes: the tokens with a word (listed as they are found), those on the row's path, and those not allowed.
 //
 // Bound by memory where there are many rows: 1024 rows of 151936 bf16 (histories of up to 2048, 32 biases) in 110 us, 622 MB
-// at 5.6 TB/s, 1032 rows of 100003 f32 in a tree with a mask in 118 us.  64 rows with a mask and histories of up to 8192 in
+// at 5.7 TB/s, 1032 rows of 100003 f32 in a tree with a mask in 118 us.  64 rows with a mask and histories of up to 8192 in
 // 17 us: a workgroup has to have gone over the history before its first logit, and VALU is 65% active meanwhile.
 
 #include <hip/hip_runtime.h>
@@ -27,8 +27,9 @@ using namespace lg;
 constexpr int kThreads = 512;
 constexpr int kWaves = kThreads / kWave;
 constexpr int kChunk = 8192;                      // tokens of a workgroup
-// Rows of a workgroup at most: each goes over the history for itself.  2 / 4 / 8 / 16 rows: 114 / 122 / 143 / 159 us for the
-// 1024 rows, 120 / 131 / 150 / 152 for the tree's; with histories of 16384 2 rows take 147 and 8 rows 165.
+// Rows of a workgroup at most: it goes over the history for them all.  1 / 2 / 4 rows: 123 / 110 / 117 us for the 1024 rows,
+// 125 / 119 / 147 for the tree's, with histories of 16384 182 / 147 / 161.  256 threads or chunks of 4096 are slower (120 and
+// 114 for the 1024 rows).
 constexpr int kRows = 2;
 constexpr int kPath = CADDTREE_MAX_L;
 constexpr int kNodes = 1024;                      // of a tree, in LDS (further ones are read where they lie)

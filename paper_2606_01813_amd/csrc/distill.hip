@@ -223,19 +223,23 @@ __device__ __forceinline__ void start_stream(Vec<E> (&q)[kU], const typename E::
 template <typename E, int kThreads, bool kOnce = false, int kU>
 __device__ __forceinline__ void stream_row(Stream& r, Vec<E> (&q)[kU], const typename E::T* l, int first, int last, const uint32_t* bits) {
   constexpr int N = kN<E>;
-  int v = first + (int)threadIdx.x;
-  // (whole wavefronts go round: v less the lane)
-  for (; v - (int)(threadIdx.x % kWave) < last; v += kU * kThreads) {
+  const int lane = (int)threadIdx.x % kWave;
+  int at = first + __builtin_amdgcn_readfirstlane((int)threadIdx.x / kWave) * kWave;   // (of the wavefront's first lane)
+  const auto add = [&](int u) {
+    const int w = at + lane + u * kThreads;
+    float x[N];
+    __builtin_amdgcn_sched_barrier(0);              // (one vector unpacked at a time: registers)
+    q[u].get(x);
+    if (at + kU * kThreads < last) q[u] = row_vector<E, kOnce>(l, w + kU * kThreads, last);
+    r.add(x, w < last ? bits_at<N>(bits, (w - first) * N) : kNone<N>);
+  };
+  for (; at + kU * kThreads < last; at += kU * kThreads) {
 #pragma unroll
-    for (int u = 0; u < kU; ++u) {
-      const int w = v + u * kThreads;
-      float x[N];
-      __builtin_amdgcn_sched_barrier(0);            // (one vector unpacked at a time: registers)
-      q[u].get(x);
-      q[u] = row_vector<E, kOnce>(l, w + kU * kThreads, last);
-      r.add(x, w < last ? bits_at<N>(bits, (w - first) * N) : kNone<N>);
-    }
+    for (int u = 0; u < kU; ++u) add(u);
   }
+#pragma unroll
+  for (int u = 0; u < kU; ++u)                      // the last ones, of which there may be fewer
+    if (at + u * kThreads < last) add(u);
 }
 
 // A wavefront's result, in LDS: its largest logit, and a sum of exp2(l c - r).
@@ -399,12 +403,13 @@ __device__ void no_weight(const DistillArgs& a, int64_t row, typename E::T* g, i
 // A workgroup a row: its loss, and the gradient.  The row's first kKeep vectors a thread stay in registers between the sums
 // and the gradient; what is behind them is read again, the last first, while it may still be in a cache.
 //
-// Bound by memory: 1024 rows of 151936 bf16 (a tenth of weight 0) in 126 us, 594 MB that have to move at 4.7 TB/s, where a
-// copy reaches 5.0.  Of 512 threads 0 / 8 / 14 / 18 vectors kept: 169 / 147 / 136 / 141 us; the whole
-// row in 1024 threads' registers: 151 (one workgroup a compute unit: nothing loads while it joins).
+// Bound by memory: 1024 rows of 151936 bf16 (a tenth of weight 0) in 121 us, 594 MB that have to move at 4.9 TB/s, where a
+// copy reaches 5.0.  Of 512 threads 0 / 8 / 14 vectors kept: 157 / 129 / 121 us, and 18 were slower than 14; the whole row in
+// 1024 threads' registers: 151 when 14 took 136 (one workgroup a compute unit: nothing loads while it joins).
 // Streaming stores took 154 to 136, streaming loads of the second pass 133 to 123.
-// The loss alone: 2048 such rows in 103 us, 5.7 TB/s of the row's one read; bound by the exponentials' instructions (VALU
-// 80% active).  512 threads 108 us, 256 108, 1024 136 when it was chosen.
+// The loss alone: 2048 such rows in 96 us, 6.2 TB/s of the row's one read; bound by the exponentials' instructions (VALU
+// 80% active).  512 threads with 4 / 6 / 8 / 12 loads a lane 94 / 95 / 96 / 99 us, and for 128 rows 17.7 / 16.9 / 16.4 / 16.6;
+// 256 threads 97 and 22.
 template <typename E, int kThreads, int kKeep, bool kGrad>
 __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
   constexpr int N = kN<E>, kU = kGrad ? 4 : 8;
@@ -444,6 +449,7 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
     for (int u = 0; u < kKeep; ++u) {
       const int v = u * kThreads + at;
       __builtin_amdgcn_sched_barrier(0);            // (one vector unpacked at a time: registers)
+      if (kThreads == 128 && v - tid % kWave >= n) break;   // (8192 rows of 8192: 71 -> 63 us; with more threads 1% slower)
       float x[N];
       q[u].get(x);
       acc.add(x, v < n ? bits_at<N>(s_bits, v * N) : kNone<N>);
@@ -496,9 +502,10 @@ struct Parts {
 };
 constexpr int kMaxParts = kWave;
 
-// The parts' sums.  Bound by latency: 64 rows of 151936 bf16, 19 MB, in 11.7 us of which the read at the card's rate is 3;
-// the rest is a launch, the list's bits, and two barriers.  Read with the cache's hint, so that the second launch finds the row there.
-constexpr int kSumThreads = 512;
+// The parts' sums.  Bound by latency: 64 rows of 151936 bf16, 19 MB, in 8 us of which the read at the card's rate is 3; the
+// rest is a launch, the list's bits, and two barriers.  Read with the cache's hint, so that the second launch finds the row
+// there.  Few wavefronts are sooner under way: 256 / 512 threads 17.6 / 18.0 us in both launches, 16 rows 11.2 / 12.3.
+constexpr int kSumThreads = 256;
 template <typename E>
 __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts ps) {
   __shared__ Partial partial[kSumThreads / kWave];
@@ -511,7 +518,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
   const int first = part * ps.len, last = min(a.V, first + ps.len);
   const float c = (float)(kLog2e / (double)a.temperature);
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
-  Vec<E> q[8];
+  Vec<E> q[6];
   if (first / kN<E> < last / kN<E>) start_stream<E, kSumThreads>(q, l, first / kN<E>, last / kN<E>);
   Edge<E> edge;                                     // (of the row's last part: the others end at a vector's end)
   edge.read(l + first, last - first);
@@ -569,14 +576,16 @@ __device__ __forceinline__ Sum join_parts(const PartSum* p, int n, double c, dou
 //
 // Each workgroup works the list out again, 8 K bytes and K exponentials: that costs less than another launch to do it once.
 // One wavefront does, while another joins the parts (one after the other: 64 rows of 151936 19.5 us in both launches, so 18.5).
-// A part is what its lanes ask for at once, before the list is gone over.  520 rows of 65537 f16 with K = 128 (three tenths
-// of weight 0): 30.5 us, 116 MB at 3.8 TB/s; 1024 rows of 151936 bf16: 103 us with 4 loads a lane, 112 with 8.  Bound by
-// the wait for the list (waits 61% of the wavefronts' cycles), then by memory.
-constexpr int kGradThreads = 256;
+// From stats a part is what its lanes ask for at once, before the list is gone over.  520 rows of 65537 f16 with K = 128
+// (three tenths of weight 0): 29.7 us, 116 MB at 3.9 TB/s; 1024 rows of 151936 bf16: 103 us with 4 loads a lane, 111 with 8.
+// Bound by the wait for the list (waits 66% of the wavefronts' cycles), then by memory.  256 / 512 / 1024 threads: from stats
+// 103 / 108 / 105 us, behind the sums (a workgroup a compute unit) 20.2 / 17.9 / 18.0.
 constexpr int kGradLoads = 4;                     // vectors a lane has in flight while the list is gone over
+template <bool kStats>
+constexpr int kGradThreads = kStats ? 256 : 512;
 template <typename E, bool kStats>
-__global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts ps) {
-  constexpr int N = kN<E>;
+__global__ __launch_bounds__(kGradThreads<kStats>) void grad_kernel(DistillArgs a, Parts ps) {
+  constexpr int N = kN<E>, kThreads = kGradThreads<kStats>;
   __shared__ Listed L;
   __shared__ Raw raw;
   __shared__ Sum s_sum;
@@ -588,7 +597,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts
   const float w = weight_of(a, row);
   const bool store = !kStats && part == 0;
   if (w == 0.f) {
-    no_weight<E, kGradThreads>(a, row, g, first, last, store);
+    no_weight<E, kThreads>(a, row, g, first, last, store);
     return;
   }
   if (g == nullptr && !store) return;
@@ -596,10 +605,10 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts
   const float c = (float)(kLog2e / (double)a.temperature);
   const int n = (last - first) / N;
   Vec<E> q[kGradLoads];
-  if (g && n > 0) start_stream<E, kGradThreads, true>(q, l + first, 0, n);
+  if (g && n > 0) start_stream<E, kThreads, true>(q, l + first, 0, n);
   Edge<E> edge;
   edge.read(l + first, last - first);
-  for (int i = tid; i < (last - first + 31) / 32; i += kGradThreads) s_bits[i] = 0;
+  for (int i = tid; i < (last - first + 31) / 32; i += kThreads) s_bits[i] = 0;
   __syncthreads();
   if (tid < kWave) {
     fetch_listed<E>(a, row, l, kStats ? nullptr : ps.listed + row * a.K, first, last, raw);
@@ -628,17 +637,17 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(DistillArgs a, Parts
     put_edge<E>(edge, g + first, r, c);
     const float mc = r.mc, rest = r.rest;
     if (__builtin_expect(r.far, 0)) {
-      put_vectors<E, kGradThreads, 1, true>(l + first, g + first, 0, n, s_bits, r.m, rest, c);
+      put_vectors<E, kThreads, 1, true>(l + first, g + first, 0, n, s_bits, r.m, rest, c);
     } else {
 #pragma unroll
       for (int u = 0; u < kGradLoads; ++u) {
-        const int v = u * kGradThreads + tid;
+        const int v = u * kThreads + tid;
         __builtin_amdgcn_sched_barrier(0);
         if (v < n) put_vector<E>(q[u], g + first, v, bits_at<N>(s_bits, v * N), mc, rest, c);
       }
-      put_vectors<E, kGradThreads, 4, false>(l + first, g + first, min(n, kGradLoads * kGradThreads), n, s_bits, mc, rest, c);
+      put_vectors<E, kThreads, 4, false>(l + first, g + first, min(n, kGradLoads * kThreads), n, s_bits, mc, rest, c);
     }
-    put_listed<E, kGradThreads>(a, g, r, L, first, last);
+    put_listed<E, kThreads>(a, g, r, L, first, last);
   }
   if (store && tid < kWave) put_loss(a, row, L, sum, Z, w);
 }
@@ -657,7 +666,7 @@ hipError_t run(F kernel, dim3 grid, int threads, size_t lds, hipStream_t stream,
 }
 
 // By a row's vectors: as few threads as hold the row, so that many rows are under way, and none where a row does not fit.
-// Measured, us: 8192 rows of 8192 bf16 128 threads x 14 72 - 80, 512 x 0 171; 4096 rows of 32000 bf16 256 x 16 104, 512 x 8
+// Measured, us: 8192 rows of 8192 bf16 128 threads x 14 63, 512 x 0 171; 4096 rows of 32000 bf16 256 x 16 104, 512 x 8
 // 119, 512 x 14 134; 512 rows of 25000 vectors 512 x 14 64, 1024 x 16 68; 512 rows of 151936 f32 (37984 vectors) 512 x 14
 // 148, 1024 x 16 131.
 template <typename E>
@@ -678,7 +687,7 @@ hipError_t launch_parts(const DistillArgs& a, const Parts& ps, hipStream_t strea
   const dim3 g((unsigned)(a.T * ps.n), (unsigned)a.B);
   const hipError_t e = run(sums_kernel<E>, g, kSumThreads, bit_bytes(ps.len), stream, a, ps);
   if (e != hipSuccess) return e;
-  return run(grad_kernel<E, false>, g, kGradThreads, bit_bytes(ps.len), stream, a, ps);
+  return run(grad_kernel<E, false>, g, kGradThreads<false>, bit_bytes(ps.len), stream, a, ps);
 }
 
 template <typename E>
@@ -697,19 +706,20 @@ hipError_t launch(const DistillArgs& a, void* workspace, hipStream_t stream) {
 template <typename E>
 hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
   Parts ps = {};
-  ps.len = kGradLoads * kGradThreads * kN<E>;
+  ps.len = kGradLoads * kGradThreads<true> * kN<E>;
   ps.n = distill_grad_parts(a.V, sizeof(typename E::T));
-  return run(grad_kernel<E, true>, dim3((unsigned)(a.T * ps.n), (unsigned)a.B), kGradThreads, bit_bytes(ps.len), stream, a, ps);
+  return run(grad_kernel<E, true>, dim3((unsigned)(a.T * ps.n), (unsigned)a.B), kGradThreads<true>, bit_bytes(ps.len), stream, a, ps);
 }
 
 }  // namespace
 
-// Two workgroups a compute unit where the rows are fewer than that, a part no shorter than what a workgroup asks for at
-// once.  Parts or whole rows, us, of 151936 bf16: 1 row 13.4 / 27.1, 16 rows 16.1 / 28, 64 rows 20.7 / 28.5, 128 rows
-// 32.5 / 29.6; 64 rows of 32000 16.8 / 15.0.  512 / 768 / 1024 workgroups: 20.7 / 23.6 / 24.9.
+// A workgroup a compute unit where the rows are fewer than that, a part no shorter than what a workgroup asks for at once.
+// Parts or whole rows, us, of 151936 bf16: 1 row 8.9 / 24.0, 16 rows 10.4 / 25.3, 64 rows 16.1 / 25.6, 128 rows 25.5 / 26.9
+// (their loss alone 17.3 / 16.4); 64 rows of 32000 11.2 / 13.1.  256 or 512 workgroups: 16 rows 11.2 / 12.8, 64 rows
+// 17.6 / 18.1, 64 rows of 40000 11.6 / 13.4.
 int distill_parts(int64_t rows, int32_t V) {
   if (rows < 1 || rows > 64) return 1;
-  return (int)std::max<int64_t>(1, std::min<int64_t>({512 / rows, V / 4096, kMaxParts}));
+  return (int)std::max<int64_t>(1, std::min<int64_t>({256 / rows, V / 4096, kMaxParts}));
 }
 size_t distill_workspace(int64_t rows, int32_t V) {
   const int n = distill_parts(rows, V);
@@ -717,7 +727,7 @@ size_t distill_workspace(int64_t rows, int32_t V) {
 }
 
 int distill_grad_parts(int32_t V, size_t elem) {
-  const int len = kGradLoads * kGradThreads * 16 / (int)elem;
+  const int len = kGradLoads * kGradThreads<true> * 16 / (int)elem;
   return (V + len - 1) / len;
 }
 

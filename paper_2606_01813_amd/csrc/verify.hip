@@ -5,8 +5,9 @@
 // workgroup walks a tree and reads a row whenever it gets there.  Where all rows of the call are few, that chain is
 // longer than reading them all at once: choose_kernel does so, a part of a row a workgroup, and the walk joins the parts.
 //
-// 32 trees of up to 256 nodes, 151936 bf16 logits a row, take 55 us: the longest path's rows one after the other, each at what
-// a compute unit reads of its 304 KB.  One tree of 64 nodes: 12 us, all rows at once in 6.5 and the walk over the parts in 6.
+// 32 trees of up to 256 nodes, 151936 bf16 logits a row, take 41 us: the longest path's 9 rows one after the other, 4.4 us each,
+// of which a compute unit at 64 bytes a clock needs 2 for the 304 KB and the first loads' latency, the joins and the search for
+// the child the rest.  One tree of 64 nodes: 10 us, all rows at once in 6.0 and the walk over the parts in 4.0.
 
 #include <hip/hip_runtime.h>
 
@@ -217,7 +218,8 @@ void launch(const VerifyArgs& a, void* workspace, size_t elem, hipStream_t strea
 }  // namespace
 
 // All rows at once where their logits are no more than the card reads in a walk's time, 96 MiB.  Both ways, us, 151936 bf16:
-// 2 trees of 65 rows (40 MB) 15 / 25, 4 of 65 (79 MB) 23 - 26 / 42, 1 of 257 (78 MB) 20 - 23 / 24.4.
+// 1 tree of 65 rows (20 MB) 9.5 / 17.4, 2 (40 MB) 12.8 / 17.6, 4 (79 MB) 19.1 / 31.5, 8 (158 MB) 37.2 / 31.5; 1 of 257 (78 MB)
+// 18.0 / 17.3, 3 of 100 (91 MB) 20.6 / 26.9: it is the longest path that decides, which is not known before.
 int verify_parts(int64_t B, int64_t T, int32_t V, size_t elem) {
   const int64_t rows = B * T;
   if (rows < 1 || rows * V * (int64_t)elem > 96 << 20) return 0;
