@@ -27,7 +27,6 @@ using namespace lg;
 
 constexpr int kMaxK = CADDTREE_MAX_TEACHER;
 constexpr int kMine = kMaxK / kWave;              // of the teacher's tokens a lane
-constexpr double kLog2e = 0x1.71547652b82fep+0;
 
 // 2^a to a step of fp32, whatever its size: a chain of a few instructions where a row's sums are waited for.
 __device__ __forceinline__ double pow2(double a) {
@@ -96,7 +95,7 @@ __device__ void fetch_listed(const DistillArgs& a, int64_t row, const typename E
 __device__ void read_listed(const DistillArgs& a, const Raw& raw, int first, int last, Listed& L, uint32_t* bits) {
   const int lane = (int)threadIdx.x % kWave;
   float top = -INFINITY;
-  double z = 0.0;
+  double z = 0.0, of = 0.0;
   if (!a.tail) {
 #pragma unroll 1
     for (int k = lane; k < a.K; k += kWave) top = fmaxf(top, raw.t[k]);
@@ -104,8 +103,10 @@ __device__ void read_listed(const DistillArgs& a, const Raw& raw, int first, int
     if (top == -INFINITY) top = 0.f;
     double sum = 0.0;
 #pragma unroll 1
-    for (int k = lane; k < a.K; k += kWave) sum += exp(((double)raw.t[k] - (double)top) / (double)a.temperature);
-    z = log(wave_sum(sum));
+    for (int k = lane; k < a.K; k += kWave) sum += L.p[k] = exp(((double)raw.t[k] - (double)top) * a.inverse);
+    sum = wave_sum(sum);
+    z = log(sum);
+    of = 1.0 / sum;
   }
   double P = 0.0, A = 0.0;
   bool twice = false;
@@ -113,8 +114,8 @@ __device__ void read_listed(const DistillArgs& a, const Raw& raw, int first, int
   for (int k = lane; k < a.K; k += kWave) {
     const int id = raw.id[k], at = id - first;
     const float t = raw.t[k];
-    const double logp = a.tail || t == -INFINITY ? (double)t : ((double)t - (double)top) / (double)a.temperature - z;
-    const double p = exp(logp);
+    const double logp = a.tail ? (double)t : ((double)t - (double)top) * a.inverse - z;
+    const double p = t == -INFINITY ? 0.0 : a.tail ? exp((double)t) : L.p[k] * of;
     P += p;
     if (p != 0.0) A += p * logp;
     if (id >= first && id < last) twice |= (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u) != 0;
@@ -292,33 +293,33 @@ __device__ __forceinline__ double listed_sum(const Listed& L, int K, float m, do
   return wave_sum(sum);
 }
 
-__device__ void finish(Row& r, float m, double Z, double R, const Listed& L, float w, float tau, float c) {
+__device__ void finish(Row& r, float m, double Z, double R, const Listed& L, float w, double inverse, float c) {
   r.m = m == -INFINITY ? 0.f : m;
   r.mc = r.m * c;
   r.far = !(fabsf(r.mc) <= kFar);
   r.Z = Z;
   r.mass = L.P + L.rho;
-  r.scale = (double)w / (double)tau;
-  const double rest = R == 0.0 ? 0.0 : r.scale * (r.mass / Z - L.rho / R);
+  r.scale = (double)w * inverse;
+  const double rest = R == 0.0 ? 0.0 : r.scale * (r.mass / Z - (L.rho == 0.0 ? 0.0 : L.rho / R));
   r.rest = (float)(r.far ? rest : rest * pow2((double)r.mc - (double)r.m * (double)c));
 }
 
 // By one wavefront, from a row's largest logit and R: Z, and what its gradient needs.
 __device__ __forceinline__ double conclude(const DistillArgs& a, const Listed& L, const Sum& sum, float w, float c, Row& r) {
-  const double Z = sum.s + listed_sum(L, a.K, sum.m == -INFINITY ? 0.f : sum.m, kLog2e / (double)a.temperature);
-  if (threadIdx.x % kWave == 0) finish(r, sum.m, Z, sum.s, L, w, a.temperature, c);
+  const double Z = sum.s + listed_sum(L, a.K, sum.m == -INFINITY ? 0.f : sum.m, a.c);
+  if (threadIdx.x % kWave == 0) finish(r, sum.m, Z, sum.s, L, w, a.inverse, c);
   return Z;
 }
 // ... its loss and stats.
 __device__ void put_loss(const DistillArgs& a, int64_t row, const Listed& L, const Sum& sum, double Z, float w) {
   const int lane = (int)threadIdx.x % kWave;
-  const double inv_tau = 1.0 / (double)a.temperature, R = sum.s, logZ = log(Z);
+  const double R = sum.s, logZ = log(Z);
   const float from = sum.m == -INFINITY ? 0.f : sum.m;
   double x = 0.0;                                 // sum p_k log q_k
 #pragma unroll 1
   for (int k = lane; k < a.K; k += kWave) {
     if (L.id[k] >= 0 && L.p[k] != 0.0)
-      x += L.p[k] * (L.l[k] == -INFINITY ? -INFINITY : ((double)L.l[k] - (double)from) * inv_tau - logZ);
+      x += L.p[k] * (L.l[k] == -INFINITY ? -INFINITY : ((double)L.l[k] - (double)from) * a.inverse - logZ);
   }
   x = L.A - wave_sum(x);
   if (L.rho > 0.0 && !(R == 0.0)) x += L.rho * (log(L.rho) - log(R / Z));
@@ -375,7 +376,7 @@ __device__ void put_listed(const DistillArgs& a, typename E::T* g, const Row& r,
     if (L.id[k] < first || L.id[k] >= last) continue;
     double p;
     if (!first_of(L, a.K, k, p)) continue;
-    const double e = L.l[k] == -INFINITY ? 0.0 : pow2(((double)L.l[k] - (double)r.m) * (kLog2e / (double)a.temperature));
+    const double e = L.l[k] == -INFINITY ? 0.0 : pow2(((double)L.l[k] - (double)r.m) * a.c);
     g[L.id[k]] = (typename E::T)(float)(r.scale * ((r.Z == 0.0 ? 0.0 : e / r.Z) * r.mass - p));
   }
 }
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
     return;
   }
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, blockIdx.x);
-  const float c = (float)(kLog2e / (double)a.temperature);
+  const float c = a.c32;
   const int n = a.V / N, kept = min(n, kKeep * kThreads);          // vectors
   for (int i = tid; i < (a.V + 31) / 32; i += kThreads) s_bits[i] = 0;
   __syncthreads();
@@ -449,7 +450,7 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
     for (int u = 0; u < kKeep; ++u) {
       const int v = u * kThreads + at;
       __builtin_amdgcn_sched_barrier(0);            // (one vector unpacked at a time: registers)
-      if (kThreads == 128 && v - tid % kWave >= n) break;   // (8192 rows of 8192: 71 -> 63 us; with more threads 1% slower)
+      if (kThreads <= 128 && v - tid % kWave >= n) break;   // (with more threads 1% slower)
       float x[N];
       q[u].get(x);
       acc.add(x, v < n ? bits_at<N>(s_bits, v * N) : kNone<N>);
@@ -516,7 +517,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
   const int64_t row = (int64_t)blockIdx.y * a.T + t;
   if (weight_of(a, row) == 0.f) return;             // (asking for the logits before that gains nothing)
   const int first = part * ps.len, last = min(a.V, first + ps.len);
-  const float c = (float)(kLog2e / (double)a.temperature);
+  const float c = a.c32;
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
   Vec<E> q[6];
   if (first / kN<E> < last / kN<E>) start_stream<E, kSumThreads>(q, l, first / kN<E>, last / kN<E>);
@@ -549,7 +550,7 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
     bool one = s_id[k] >= 0;
     if (s_twice)
       for (int j = 0; j < k; ++j) one &= s_id[j] != s_id[k];
-    if (one && s_l[k] != -INFINITY) listed += pow2(((double)s_l[k] - from) * (kLog2e / (double)a.temperature));
+    if (one && s_l[k] != -INFINITY) listed += pow2(((double)s_l[k] - from) * a.c);
   }
   listed = wave_sum(listed);
   if (tid == 0) ps.sum[row * ps.n + part] = PartSum{rest, listed};
@@ -602,7 +603,7 @@ __global__ __launch_bounds__(kGradThreads<kStats>) void grad_kernel(DistillArgs 
   }
   if (g == nullptr && !store) return;
   const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
-  const float c = (float)(kLog2e / (double)a.temperature);
+  const float c = a.c32;
   const int n = (last - first) / N;
   Vec<E> q[kGradLoads];
   if (g && n > 0) start_stream<E, kThreads, true>(q, l + first, 0, n);
@@ -620,7 +621,7 @@ __global__ __launch_bounds__(kGradThreads<kStats>) void grad_kernel(DistillArgs 
       sum = Sum{a.stats[row * 3], (double)a.stats[row * 3 + 2]};
       Z = (double)a.stats[row * 3 + 1];
     } else {
-      sum = join_parts(ps.sum + row * ps.n, ps.n, kLog2e / (double)a.temperature, Z);
+      sum = join_parts(ps.sum + row * ps.n, ps.n, a.c, Z);
     }
     if (tid == kWave) {
       s_sum = sum;
@@ -631,7 +632,7 @@ __global__ __launch_bounds__(kGradThreads<kStats>) void grad_kernel(DistillArgs 
   const Sum sum = s_sum;
   const double Z = s_Z;
   Row r;                                            // (each for itself)
-  finish(r, sum.m, Z, sum.s, L, w, a.temperature, c);
+  finish(r, sum.m, Z, sum.s, L, w, a.inverse, c);
   if (g) {
     edge.look(s_bits);
     put_edge<E>(edge, g + first, r, c);
@@ -673,9 +674,14 @@ template <typename E>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t stream) {
   const dim3 all((unsigned)a.T, (unsigned)a.B);
   const size_t lds = bit_bytes(a.V);
-  if (a.grad.data == nullptr) return run(row_kernel<E, 512, 0, false>, all, 512, lds, stream, a);
   const int vectors = a.V / kN<E>;
-  if (vectors <= 128 * 4) return run(row_kernel<E, 128, 4, true>, all, 128, lds, stream, a);
+  if (a.grad.data == nullptr) {
+    if (vectors <= 64 * 16) return run(row_kernel<E, 64, 0, false>, all, 64, lds, stream, a);
+    if (vectors <= 256 * 16) return run(row_kernel<E, 256, 0, false>, all, 256, lds, stream, a);
+    return run(row_kernel<E, 512, 0, false>, all, 512, lds, stream, a);
+  }
+  if (vectors <= 64 * 4) return run(row_kernel<E, 64, 4, true>, all, 64, lds, stream, a);
+  if (vectors <= 64 * 16) return run(row_kernel<E, 64, 16, true>, all, 64, lds, stream, a);
   if (vectors <= 128 * 14) return run(row_kernel<E, 128, 14, true>, all, 128, lds, stream, a);
   if (vectors <= 256 * 16) return run(row_kernel<E, 256, 16, true>, all, 256, lds, stream, a);
   if (vectors <= 1 << 15) return run(row_kernel<E, 512, 14, true>, all, 512, lds, stream, a);

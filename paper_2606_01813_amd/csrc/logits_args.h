@@ -57,7 +57,8 @@ struct DistillArgs {
   const int32_t* ids;
   const float* target;
   const float* weight;
-  float temperature;
+  float c32;                 // log2(e) / temperature, rounded
+  double c, inverse;         // ... and 1 / temperature
   int32_t tail;
   float* loss;
   float* stats;
