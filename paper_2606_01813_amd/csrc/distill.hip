@@ -582,13 +582,12 @@ __device__ __forceinline__ Sum join_parts(const PartSum* p, int n, double c, dou
 // Bound by the wait for the list (waits 66% of the wavefronts' cycles), then by memory.  256 / 512 / 1024 threads: from stats
 // 103 / 108 / 105 us, behind the sums (a workgroup a compute unit) 20.2 / 17.9 / 18.0.
 constexpr int kGradLoads = 4;                     // vectors a lane has in flight while the list is gone over
-template <bool kStats>
-constexpr int kGradThreads = kStats ? 256 : 512;
-template <typename E, bool kStats>
-__global__ __launch_bounds__(kGradThreads<kStats>) void grad_kernel(DistillArgs a, Parts ps) {
-  constexpr int N = kN<E>, kThreads = kGradThreads<kStats>;
+template <typename E, bool kStats, int kThreads>
+__global__ __launch_bounds__(kThreads) void grad_kernel(DistillArgs a, Parts ps) {
+  constexpr int N = kN<E>;
   __shared__ Listed L;
   __shared__ Raw raw;
+  static_assert(kStats || kThreads >= 2 * kWave, "a wavefront for the list, one for the parts");
   __shared__ Sum s_sum;
   __shared__ double s_Z;
   const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n;
@@ -614,23 +613,25 @@ __global__ __launch_bounds__(kGradThreads<kStats>) void grad_kernel(DistillArgs 
   if (tid < kWave) {
     fetch_listed<E>(a, row, l, kStats ? nullptr : ps.listed + row * a.K, first, last, raw);
     read_listed(a, raw, first, last, L, s_bits);
-  } else if (tid < 2 * kWave) {                     // (meanwhile)
-    Sum sum;
+  } else if (!kStats && tid < 2 * kWave) {          // (meanwhile)
     double Z;
-    if constexpr (kStats) {
-      sum = Sum{a.stats[row * 3], (double)a.stats[row * 3 + 2]};
-      Z = (double)a.stats[row * 3 + 1];
-    } else {
-      sum = join_parts(ps.sum + row * ps.n, ps.n, a.c, Z);
-    }
+    const Sum sum = join_parts(ps.sum + row * ps.n, ps.n, a.c, Z);
     if (tid == kWave) {
       s_sum = sum;
       s_Z = Z;
     }
   }
+  Sum sum;
+  double Z;
+  if constexpr (kStats) {
+    sum = Sum{a.stats[row * 3], (double)a.stats[row * 3 + 2]};
+    Z = (double)a.stats[row * 3 + 1];
+  }
   __syncthreads();
-  const Sum sum = s_sum;
-  const double Z = s_Z;
+  if constexpr (!kStats) {
+    sum = s_sum;
+    Z = s_Z;
+  }
   Row r;                                            // (each for itself)
   finish(r, sum.m, Z, sum.s, L, w, a.inverse, c);
   if (g) {
@@ -682,7 +683,7 @@ hipError_t launch_rows(const DistillArgs& a, hipStream_t stream) {
   }
   if (vectors <= 64 * 4) return run(row_kernel<E, 64, 4, true>, all, 64, lds, stream, a);
   if (vectors <= 64 * 16) return run(row_kernel<E, 64, 16, true>, all, 64, lds, stream, a);
-  if (vectors <= 128 * 14) return run(row_kernel<E, 128, 14, true>, all, 128, lds, stream, a);
+  if (vectors <= 128 * 16) return run(row_kernel<E, 128, 16, true>, all, 128, lds, stream, a);
   if (vectors <= 256 * 16) return run(row_kernel<E, 256, 16, true>, all, 256, lds, stream, a);
   if (vectors <= 1 << 15) return run(row_kernel<E, 512, 14, true>, all, 512, lds, stream, a);
   return run(row_kernel<E, 1024, 16, true>, all, 1024, lds, stream, a);
@@ -693,7 +694,7 @@ hipError_t launch_parts(const DistillArgs& a, const Parts& ps, hipStream_t strea
   const dim3 g((unsigned)(a.T * ps.n), (unsigned)a.B);
   const hipError_t e = run(sums_kernel<E>, g, kSumThreads, bit_bytes(ps.len), stream, a, ps);
   if (e != hipSuccess) return e;
-  return run(grad_kernel<E, false>, g, kGradThreads<false>, bit_bytes(ps.len), stream, a, ps);
+  return run(grad_kernel<E, false, 512>, g, 512, bit_bytes(ps.len), stream, a, ps);
 }
 
 template <typename E>
@@ -712,9 +713,14 @@ hipError_t launch(const DistillArgs& a, void* workspace, hipStream_t stream) {
 template <typename E>
 hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
   Parts ps = {};
-  ps.len = kGradLoads * kGradThreads<true> * kN<E>;
+  ps.len = kGradLoads * 256 * kN<E>;
   ps.n = distill_grad_parts(a.V, sizeof(typename E::T));
-  return run(grad_kernel<E, true>, dim3((unsigned)(a.T * ps.n), (unsigned)a.B), kGradThreads<true>, bit_bytes(ps.len), stream, a, ps);
+  const dim3 g((unsigned)(a.T * ps.n), (unsigned)a.B);
+  // (rows shorter than a part: us with 64 / 128 / 256 threads, 65536 rows of 1024 bf16 99 / 104 / 155, 16384 of 4096 56 / 53 / 59)
+  const int vectors = a.V / kN<E>;
+  if (vectors <= 64 * 4) return run(grad_kernel<E, true, 64>, g, 64, bit_bytes(ps.len), stream, a, ps);
+  if (vectors <= 128 * 4) return run(grad_kernel<E, true, 128>, g, 128, bit_bytes(ps.len), stream, a, ps);
+  return run(grad_kernel<E, true, 256>, g, 256, bit_bytes(ps.len), stream, a, ps);
 }
 
 }  // namespace
@@ -733,7 +739,7 @@ size_t distill_workspace(int64_t rows, int32_t V) {
 }
 
 int distill_grad_parts(int32_t V, size_t elem) {
-  const int len = kGradLoads * kGradThreads<true> * 16 / (int)elem;
+  const int len = kGradLoads * 256 * 16 / (int)elem;
   return (V + len - 1) / len;
 }
 
