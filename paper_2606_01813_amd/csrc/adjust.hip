@@ -17,6 +17,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 #include "logits_common.h"
 
 namespace caddtree {
@@ -31,6 +33,7 @@ constexpr int kChunk = 8192;                      // tokens of a workgroup
 // 125 / 119 / 147 for the tree's, with histories of 16384 182 / 147 / 161.  256 threads or chunks of 4096 are slower (120 and
 // 114 for the 1024 rows).
 constexpr int kRows = 2;
+constexpr int kMost = 16;                         // ... of a short vocabulary
 constexpr int kPath = CADDTREE_MAX_L;
 constexpr int kNodes = 1024;                      // of a tree, in LDS (further ones are read where they lie)
 constexpr int kNear = 512;                        // biases in LDS, likewise
@@ -41,8 +44,8 @@ static_assert(CADDTREE_MAX_HISTORY + kPath <= kCount && CADDTREE_MAX_BIAS < 1 <<
 struct Lds {
   uint32_t word[kChunk];
   float bias[kNear];
-  uint16_t path[kRows][kPath];                    // tokens of a row's path in the chunk, from its first token on
-  int paths[kRows];
+  uint16_t path[kMost][kPath];                    // tokens of a row's path in the chunk, from its first token on
+  int paths[kMost];
   int listed;
 };
 struct Nodes {                                    // of a tree
@@ -80,11 +83,13 @@ __device__ int path_in_chunk(const AdjustArgs& a, const Nodes& s, int b, int row
 }
 
 template <typename E, bool kInPlace>
-__global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
+__global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int shift) {
   __shared__ __align__(16) Lds s;
   __shared__ uint16_t s_list[kInPlace ? kChunk : 1];    // in place: the words that are not 0
   constexpr int N = kN<E>, kStep = kWave * N, kSteps = kChunk / kStep;
   constexpr int kU = kInPlace ? 1 : kRows * kSteps / kWaves;     // loads in flight a lane: all that it has
+  // a workgroup takes 2^shift steps of each of its rows
+  const int most = min(kRows * kSteps >> shift, kMost);
   constexpr uint32_t kAll = (1u << N) - 1;
   using T = typename E::T;
 
@@ -92,16 +97,16 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
   const int b = (int)blockIdx.y, first = (int)(blockIdx.x % chunks) * kChunk, last = min(first + kChunk, a.V);
   const bool tree = a.parent != nullptr;
   const int rows = min(max(a.count ? a.count[b] : a.T - tree, 0), a.T - tree) + tree;   // (rows of the sequence)
-  const int row0 = (int)(blockIdx.x / chunks) * kRows, mine = min(kRows, rows - row0);
+  const int row0 = (int)(blockIdx.x / chunks) * most, mine = min(most, rows - row0);
   if (mine <= 0) return;
 
   const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-  // a wavefront takes kStep tokens of a row at a time: step i is i % kSteps of row i / kSteps
-  const int items = mine * kSteps;
-  const auto token_of = [&](int i) { return first + i % kSteps * kStep + lane * N; };
+  // a wavefront takes kStep tokens of a row at a time: step i is i % 2^shift of row i / 2^shift
+  const int items = mine << shift;
+  const auto token_of = [&](int i) { return first + (i & ((1 << shift) - 1)) * kStep + lane * N; };
   const auto allowed_of = [&](int i, int tok) {         // bit j: token tok + j is allowed
     if (a.allowed == nullptr || tok >= last) return kAll;
-    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(a.allowed + b * a.allowed_b + (row0 + i / kSteps) * a.allowed_t);
+    const uint8_t* bytes = reinterpret_cast<const uint8_t*>(a.allowed + b * a.allowed_b + (row0 + (i >> shift)) * a.allowed_t);
     return (uint32_t)bytes[tok / 8] >> (tok % 8) & kAll;
   };
   Vec<E> q[kU];
@@ -111,7 +116,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
     const int tok = token_of(i);
     ok[u] = allowed_of(i, tok);
     if (!kInPlace && tok + N <= last) {
-      const T* src = row_of<E>(a.in, b, row0 + i / kSteps);
+      const T* src = row_of<E>(a.in, b, row0 + (i >> shift));
       q[u] = Vec<E>::load_once(src, (uint32_t)tok * (uint32_t)sizeof(T));
     }
   };
@@ -130,7 +135,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
   const float repetition = a.repetition ? a.repetition[b] : 1.f;
   const Penalty p = {repetition, 1.f / repetition, a.presence ? a.presence[b] : 0.f, a.frequency ? a.frequency[b] : 0.f};
   Nodes& nodes = *reinterpret_cast<Nodes*>(s_more);
-  for (int i = tid; i < kChunk / 4; i += kThreads) reinterpret_cast<u32x4*>(s.word)[i] = u32x4{0, 0, 0, 0};
+  for (int i = tid; i < kStep / 4 << shift; i += kThreads) reinterpret_cast<u32x4*>(s.word)[i] = u32x4{0, 0, 0, 0};
   if (tid == 0) s.listed = 0;
   if (tree)
     for (int i = tid; i < min(row0 + mine - 1, kNodes); i += kThreads) {
@@ -172,7 +177,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
     for (int u = 0; u < kU; ++u) {
       const int i = i0 + u * kWaves;
       if (i >= items) break;
-      const int r = i / kSteps, tok = token_of(i);
+      const int r = i >> shift, tok = token_of(i);
       T* dst = row_of<E>(a.out, b, row0 + r);
       const uint32_t may = ok[u];
       if constexpr (kInPlace) {
@@ -251,10 +256,14 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
 
 template <typename E>
 void launch(const AdjustArgs& a, bool in_place, hipStream_t stream) {
-  const dim3 g((unsigned)((a.V + kChunk - 1) / kChunk) * (unsigned)((a.T + kRows - 1) / kRows), (unsigned)a.B);
+  constexpr int kStep = kWave * kN<E>, kSteps = kChunk / kStep;
+  int shift = 0;
+  while (1 << shift < kSteps && a.V > kStep << shift) ++shift;
+  const int most = std::min(kRows * kSteps >> shift, kMost);
+  const dim3 g((unsigned)((a.V + kChunk - 1) / kChunk) * (unsigned)((a.T + most - 1) / most), (unsigned)a.B);
   const size_t lds = a.parent != nullptr ? sizeof(Nodes) : 0;
-  if (in_place) adjust_kernel<E, true><<<g, kThreads, lds, stream>>>(a);
-  else adjust_kernel<E, false><<<g, kThreads, lds, stream>>>(a);
+  if (in_place) adjust_kernel<E, true><<<g, kThreads, lds, stream>>>(a, shift);
+  else adjust_kernel<E, false><<<g, kThreads, lds, stream>>>(a, shift);
 }
 
 }  // namespace
