@@ -119,6 +119,23 @@ def test_adjust_rows_past_count(tree, in_place):
     _check_adjust(x, out, before, kw, "count")
 
 
+@pytest.mark.parametrize("V", [5, 256, 257, 512, 513, 1024, 1025, 2048, 2049, 4096, 4097])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("tree", [False, True])
+def test_adjust_many_rows_of_a_short_vocabulary(V, dtype, tree):
+    gen = _gen(V + 7)
+    B, T = 5, 37
+    kw = _adjust_inputs(gen, B, T, V, 90, 9, "most", tree)
+    kw["count"] = torch.tensor([36, 17, 0, 100, 31], dtype=I32, device="cuda")
+    x = _rows(gen, B, T, V, dtype, pad=1, shift=1)
+    out = torch.full_like(x, 77.0)
+    adjust_logits(x, out, **kw)
+    _check_adjust(x, out, torch.full_like(x, 77.0), kw, "out of place")
+    y = _rows(gen, B, T, V, dtype, pad=1, shift=1).copy_(x)
+    adjust_logits(y, y, **kw)
+    _check_adjust(x, y, x, kw, "in place")
+
+
 def test_adjust_pad_between_rows_stays():
     gen = _gen(6)
     full = torch.randn((2, 3, 1030), generator=gen, device="cuda").to(BF)
@@ -478,6 +495,28 @@ def test_distill_sizes(V, dtype, with_workspace):
         assert torch.equal(y, grad) and torch.equal(alone, loss)
         y = x.clone()
         assert torch.equal(distill_grad(y, ids, target, stats, y, weight=w, temperature=tau, tail=tail), g)
+
+
+@pytest.mark.parametrize("vectors", [64, 128, 256, 512, 1024, 2048, 4096, 32768])
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("more", [0, 1, 9])
+def test_distill_rows_around_the_launches_limits(vectors, dtype, more):
+    """Rows of just so many vectors of 16 bytes, and of a few elements more."""
+    gen = _gen(vectors + more)
+    V = vectors * (16 // dtype.itemsize) + more
+    B, T, K, tau = (1, 2, 5, 0.7) if vectors > 4096 else (2, 3, 5, 0.7)
+    used = float(np.float32(tau))                                          # (a call's temperature is a float: 0.7 (1 - 1.7e-8))
+    x = _rows(gen, B, T, V, dtype, 1, 1)
+    ids, target = _teacher(gen, B, T, V, K, False)
+    ids[0, 0, 0] = V - 1
+    loss, stats = torch.full((B, T), 9.0, device="cuda"), torch.full((B, T, 3), 9.0, device="cuda")
+    grad = torch.full_like(x, 9.0)
+    distill(x, ids, target, loss, grad=grad, stats=stats, temperature=tau)
+    _check_distill(x, ids, target, None, used, False, loss, stats, grad)
+    alone = torch.full((B, T), 9.0, device="cuda")
+    distill(x, ids, target, alone, temperature=tau)
+    _check_distill(x, ids, target, None, used, False, alone)
+    _check_distill(x, ids, target, None, used, False, grad=distill_grad(x, ids, target, stats, temperature=tau), again=True)
 
 
 @pytest.mark.parametrize("tail", [False, True])
