@@ -513,7 +513,7 @@ typedef struct {
  *   weight[b, row]: 1 on the path, else 0.
  * accepted and index are caddtree_cache_write's count and index, weight is caddtree_cache_score's.  The outputs
  * overlap nothing else.  workspace: caddtree_verify_workspace_bytes(a) bytes, 256-byte aligned, lets a call on few
- * logits read all of their rows at once; NULL (or fewer bytes) is accepted, and the rows are read one after the other. */
+ * rows read them all at once; NULL (or fewer bytes) is accepted, and the rows are read one after the other. */
 caddtree_status_t caddtree_verify_tree(const caddtree_verify_t* a, void* workspace, size_t workspace_bytes, hipStream_t stream);
 /* HOST only (0 where none is of use, or for sizes that the call refuses). */
 size_t caddtree_verify_workspace_bytes(const caddtree_verify_t* a);

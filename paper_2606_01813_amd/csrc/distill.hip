@@ -667,10 +667,12 @@ hipError_t run(F kernel, dim3 grid, int threads, size_t lds, hipStream_t stream,
   return hipGetLastError();
 }
 
-// By a row's vectors: as few threads as hold the row, so that many rows are under way, and none where a row does not fit.
-// Measured, us: 8192 rows of 8192 bf16 128 threads x 14 63, 512 x 0 171; 4096 rows of 32000 bf16 256 x 16 104, 512 x 8
+// By a row's vectors: as few threads as hold the row, so that many rows are under way, a wavefront alone where that does.
+// Measured, us (threads x vectors kept): 65536 rows of 1024 bf16 64 x 4 135, 128 x 4 180; 8192 rows of 8192 64 x 16 57,
+// 128 x 14 63, 512 x 0 171; 8192 of 16000 128 x 16 97, 256 x 16 130; 4096 of 32000 256 x 16 96, and when that took 104 512 x 8
 // 119, 512 x 14 134; 512 rows of 25000 vectors 512 x 14 64, 1024 x 16 68; 512 rows of 151936 f32 (37984 vectors) 512 x 14
-// 148, 1024 x 16 131.
+// 148, 1024 x 16 131.  The loss alone: 65536 rows of 1024 64 threads 102, 128 132, 512 496; 16384 of 8192 64 60, 128 63, 512
+// 150; 4096 of 32000 64 60, 256 48, 512 58.
 template <typename E>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t stream) {
   const dim3 all((unsigned)a.T, (unsigned)a.B);

@@ -21,25 +21,14 @@ namespace {
 
 using namespace lg;
 
-constexpr int kWalkThreads = 1024;
 constexpr int kChooseThreads = 256;
 constexpr int kNodes = 2048;                      // of a tree, in LDS (further ones are read where they lie)
+constexpr int kAllRows = 520;                     // of a call that reads them all at once, at most
 
-// (x, id) of the larger x, of equals the lower id; nothing yet: (-inf, INT_MAX)
+// A row's or a part's choice: the largest logit and the lowest token that has it; none: (-inf, INT_MAX)
 struct Best {
   float x;
   int id;
-  __device__ __forceinline__ void take(float y, int i) {
-    if (y > x || (y == x && i < id)) {
-      x = y;
-      id = i;
-    }
-  }
-  // over a wavefront, in all of its lanes
-  __device__ __forceinline__ void join() {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) take(__shfl_xor(x, o), __shfl_xor(id, o));
-  }
   __device__ __forceinline__ int token() const { return x > -INFINITY ? id : -1; }
   // as a number that is larger for the better (-0 and 0 are equals)
   __device__ __forceinline__ uint64_t key() const {
@@ -139,21 +128,20 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best
   __shared__ uint32_t s_token[kNodes];
   __shared__ uint16_t s_parent[kNodes];               // + 1
   __shared__ int s_child;
-  __shared__ uint64_t s_key[kFrom == kParts ? kNodes : 1];   // of the first rows
+  __shared__ uint64_t s_key[kFrom == kParts ? kAllRows : 1]; // of each row
   __shared__ int s_chosen[kFrom == kChosen ? kNodes : 1];
   const int b = (int)blockIdx.x, tid = threadIdx.x;
   const int n = min(max(a.count[b], 0), a.T - 1);
   const int32_t* tok = a.token_ids + (int64_t)b * (a.T - 1);
   const int32_t* par = a.parent + (int64_t)b * (a.T - 1);
-  const int near = min(a.T, kNodes);
   if constexpr (kFrom == kParts) {
-    for (int i = tid; i < near; i += kThreads) s_key[i] = 0;
+    for (int i = tid; i < a.T; i += kThreads) s_key[i] = 0;
     __syncthreads();
-    for (int i = tid; i < near * n_parts; i += kThreads)
+    for (int i = tid; i < a.T * n_parts; i += kThreads)
       atomicMax(reinterpret_cast<unsigned long long*>(&s_key[i / n_parts]), (unsigned long long)parts[(int64_t)b * a.T * n_parts + i].key());
   }
   if constexpr (kFrom == kChosen)
-    for (int i = tid; i < near; i += kThreads) s_chosen[i] = a.chosen[(int64_t)b * a.T + i];
+    for (int i = tid; i < min(a.T, kNodes); i += kThreads) s_chosen[i] = a.chosen[(int64_t)b * a.T + i];
   for (int i = tid; i < min(a.T - 1, kNodes); i += kThreads) {    // (those past n are not looked at)
     const int p = par[i];
     s_token[i] = (uint32_t)tok[i];
@@ -167,16 +155,7 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best
     if constexpr (kFrom == kRead) t = best_of<E, kThreads, 3>(row_of<E>(a.in, b, row), 0, a.V, s_top, &s_id).token();
     if (tid == 0) s_child = INT_MAX;
     __syncthreads();                                  // (the weights are cleared too, and what is in LDS is there)
-    if constexpr (kFrom == kParts) {
-      if (row < kNodes) {
-        t = s_key[row] >= kNoKey ? (int)~(uint32_t)s_key[row] : -1;
-      } else {
-        const int i = tid % kWave;
-        Best m = i < n_parts ? parts[((int64_t)b * a.T + row) * n_parts + i] : Best{-INFINITY, INT_MAX};
-        m.join();
-        t = m.token();
-      }
-    }
+    if constexpr (kFrom == kParts) t = s_key[row] >= kNoKey ? (int)~(uint32_t)s_key[row] : -1;
     if constexpr (kFrom == kChosen) t = row < kNodes ? s_chosen[row] : a.chosen[(int64_t)b * a.T + row];
     if (tid == 0) {
       a.index[(int64_t)b * a.M + steps] = row;
@@ -205,7 +184,10 @@ void launch(const VerifyArgs& a, void* workspace, size_t elem, hipStream_t strea
   }
   const int n = workspace ? verify_parts(a.B, a.T, a.V, elem) : 0;
   if (n == 0) {
-    walk_kernel<E, kRead, kWalkThreads><<<(unsigned)a.B, kWalkThreads, 0, stream>>>(a, nullptr, 0);
+    // (512 or 1024 threads, us: 64 x 65 rows of 8192 bf16 11.5 / 13.7, 16 x 65 of 32000 14.5 / 17.5, 4 x 65 of 65536 19.0 / 19.7,
+    // 32 x 257 of 151936 52.5 / 41.3)
+    if ((int64_t)a.V * (int64_t)elem <= 128 << 10) walk_kernel<E, kRead, 512><<<(unsigned)a.B, 512, 0, stream>>>(a, nullptr, 0);
+    else walk_kernel<E, kRead, 1024><<<(unsigned)a.B, 1024, 0, stream>>>(a, nullptr, 0);
     return;
   }
   const int len = ((a.V + n - 1) / n + 7) & ~7;
@@ -217,12 +199,14 @@ void launch(const VerifyArgs& a, void* workspace, size_t elem, hipStream_t strea
 
 }  // namespace
 
-// All rows at once where their logits are no more than the card reads in a walk's time, 96 MiB.  Both ways, us, 151936 bf16:
-// 1 tree of 65 rows (20 MB) 9.5 / 17.4, 2 (40 MB) 12.8 / 17.6, 4 (79 MB) 19.1 / 31.5, 8 (158 MB) 37.2 / 31.5; 1 of 257 (78 MB)
-// 18.0 / 17.3, 3 of 100 (91 MB) 20.6 / 26.9: it is the longest path that decides, which is not known before.
+// All rows at once where they are few: it reads them all, and a walk those of its longest path one after the other, which is not
+// known before.  Walk or all, us, bf16, trees x rows of tokens:
+//     1 x 65 of 151936 17.4 / 9.5    4 x 65 of 151936 31.5 / 19.1    1 x 257 of 151936 17.3 / 18.0   8 x 65 of 151936 31.5 / 37.2
+//     1 x 65 of 32000 9.0 / 8.2      4 x 65 of 65536 19.0 / 13.1     8 x 65 of 65536 19.1 / 18.4
+//     1 x 513 of 32000 9.2 / 13.5    1 x 513 of 1024 6.8 / 9.7       64 x 65 of 8192 11.5 / 18.0     64 x 513 of 1024 15.4 / 45.0
 int verify_parts(int64_t B, int64_t T, int32_t V, size_t elem) {
   const int64_t rows = B * T;
-  if (rows < 1 || rows * V * (int64_t)elem > 96 << 20) return 0;
+  if (rows < 1 || rows > kAllRows || rows * V * (int64_t)elem > 96 << 20) return 0;
   return (int)std::max<int64_t>(1, std::min<int64_t>({512 / rows, V / 4096, kWave}));
 }
 size_t verify_workspace(int64_t B, int64_t T, int32_t V, size_t elem) {
