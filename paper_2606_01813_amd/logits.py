@@ -235,7 +235,7 @@ def distill_grad(logits, ids, target, stats, grad=None, *, weight=None, temperat
                  workspace=None, stream=None):
     """The gradient of ``distill`` by itself, from the ``stats`` that it wrote of the same logits, ids and temperature
     (weight: the gradient of its losses times their weights).  Into ``grad`` (made of zeros if not given; it may be the
-    logits).  Returns grad."""
+    logits).  Returns grad.  A workspace is taken, as ``distill``'s arguments are, and not used."""
     grad = _at._made(logits, grad, stream)
     native = _at._native(stream)
     if native is not None and _lib.logits_ops() is not None:
