@@ -452,7 +452,7 @@ typedef struct {
 /* One call of caddtree_adjust_logits. */
 typedef struct {
   caddtree_dtype_t dtype;
-  int32_t B;                    /* sequences, 0 .. 65535 */
+  int32_t B;                    /* sequences, 0 .. 2^19 */
   int32_t T;                    /* rows of a sequence at most; with a tree: cap + 1 */
   int32_t V;                    /* 1 .. CADDTREE_MAX_VOCAB */
   caddtree_rows_t logits, out;
@@ -489,7 +489,7 @@ caddtree_status_t caddtree_adjust_logits(const caddtree_adjust_t* a, hipStream_t
 /* One call of caddtree_verify_tree. */
 typedef struct {
   caddtree_dtype_t dtype;
-  int32_t B;                    /* trees, 0 .. 65535 */
+  int32_t B;                    /* trees, 0 .. 2^19 */
   int32_t T;                    /* rows of a tree: cap + 1, the root and the nodes */
   int32_t V;                    /* 1 .. CADDTREE_MAX_VOCAB */
   caddtree_rows_t logits;       /* [B, T, V]; data NULL where `chosen` is given */
@@ -521,7 +521,7 @@ size_t caddtree_verify_workspace_bytes(const caddtree_verify_t* a);
 /* One call of caddtree_distill or caddtree_distill_grad. */
 typedef struct {
   caddtree_dtype_t dtype;
-  int32_t B;                    /* 0 .. 65535 */
+  int32_t B;                    /* 0 .. 2^19 */
   int32_t T;
   int32_t V;                    /* 1 .. CADDTREE_MAX_VOCAB */
   caddtree_rows_t logits;       /* the student's, [B, T, V] */

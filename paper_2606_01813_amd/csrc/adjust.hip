@@ -94,7 +94,8 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a, int shif
   using T = typename E::T;
 
   const int chunks = (a.V + kChunk - 1) / kChunk;
-  const int b = (int)blockIdx.y, first = (int)(blockIdx.x % chunks) * kChunk, last = min(first + kChunk, a.V);
+  const int b = sequence(), first = (int)(blockIdx.x % chunks) * kChunk, last = min(first + kChunk, a.V);
+  if (b >= a.B) return;
   const bool tree = a.parent != nullptr;
   const int rows = min(max(a.count ? a.count[b] : a.T - tree, 0), a.T - tree) + tree;   // (rows of the sequence)
   const int row0 = (int)(blockIdx.x / chunks) * most, mine = min(most, rows - row0);
@@ -260,7 +261,7 @@ void launch(const AdjustArgs& a, bool in_place, hipStream_t stream) {
   int shift = 0;
   while (1 << shift < kSteps && a.V > kStep << shift) ++shift;
   const int most = std::min(kRows * kSteps >> shift, kMost);
-  const dim3 g((unsigned)((a.V + kChunk - 1) / kChunk) * (unsigned)((a.T + most - 1) / most), (unsigned)a.B);
+  const dim3 g = grid_of((int64_t)((a.V + kChunk - 1) / kChunk) * ((a.T + most - 1) / most), a.B);
   const size_t lds = a.parent != nullptr ? sizeof(Nodes) : 0;
   if (in_place) adjust_kernel<E, true><<<g, kThreads, lds, stream>>>(a, shift);
   else adjust_kernel<E, false><<<g, kThreads, lds, stream>>>(a, shift);

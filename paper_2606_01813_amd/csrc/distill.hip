@@ -418,15 +418,17 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
   __shared__ Raw raw;
   __shared__ Row r;
   __shared__ Partial part[kThreads / kWave];
-  const int64_t row = (int64_t)blockIdx.y * a.T + blockIdx.x;
+  const int b = sequence();
+  if (b >= a.B) return;
+  const int64_t row = (int64_t)b * a.T + blockIdx.x;
   const int tid = threadIdx.x;
-  typename E::T* g = kGrad ? row_of<E>(a.grad, blockIdx.y, blockIdx.x) : nullptr;
+  typename E::T* g = kGrad ? row_of<E>(a.grad, b, blockIdx.x) : nullptr;
   const float w = weight_of(a, row);
   if (w == 0.f) {
     no_weight<E, kThreads>(a, row, g, 0, a.V, true);
     return;
   }
-  const typename E::T* l = row_of<E>(a.in, blockIdx.y, blockIdx.x);
+  const typename E::T* l = row_of<E>(a.in, b, blockIdx.x);
   const float c = a.c32;
   const int n = a.V / N, kept = min(n, kKeep * kThreads);          // vectors
   for (int i = tid; i < (a.V + 31) / 32; i += kThreads) s_bits[i] = 0;
@@ -591,9 +593,11 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(DistillArgs a, Parts ps)
   __shared__ Sum s_sum;
   __shared__ double s_Z;
   const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n;
-  const int64_t row = (int64_t)blockIdx.y * a.T + t;
+  const int b = sequence();
+  if (b >= a.B) return;
+  const int64_t row = (int64_t)b * a.T + t;
   const int tid = threadIdx.x, first = part * ps.len, last = min(a.V, first + ps.len);
-  typename E::T* g = a.grad.data ? row_of<E>(a.grad, blockIdx.y, t) : nullptr;
+  typename E::T* g = a.grad.data ? row_of<E>(a.grad, b, t) : nullptr;
   const float w = weight_of(a, row);
   const bool store = !kStats && part == 0;
   if (w == 0.f) {
@@ -601,7 +605,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(DistillArgs a, Parts ps)
     return;
   }
   if (g == nullptr && !store) return;
-  const typename E::T* l = row_of<E>(a.in, blockIdx.y, t);
+  const typename E::T* l = row_of<E>(a.in, b, t);
   const float c = a.c32;
   const int n = (last - first) / N;
   Vec<E> q[kGradLoads];
@@ -675,7 +679,7 @@ hipError_t run(F kernel, dim3 grid, int threads, size_t lds, hipStream_t stream,
 // 150; 4096 of 32000 64 60, 256 48, 512 58.
 template <typename E>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t stream) {
-  const dim3 all((unsigned)a.T, (unsigned)a.B);
+  const dim3 all = grid_of(a.T, a.B);
   const size_t lds = bit_bytes(a.V);
   const int vectors = a.V / kN<E>;
   if (a.grad.data == nullptr) {
@@ -717,7 +721,7 @@ hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
   Parts ps = {};
   ps.len = kGradLoads * 256 * kN<E>;
   ps.n = distill_grad_parts(a.V, sizeof(typename E::T));
-  const dim3 g((unsigned)(a.T * ps.n), (unsigned)a.B);
+  const dim3 g = grid_of((int64_t)a.T * ps.n, a.B);
   // (rows shorter than a part: us with 64 / 128 / 256 threads, 65536 rows of 1024 bf16 99 / 104 / 155, 16384 of 4096 56 / 53 / 59)
   const int vectors = a.V / kN<E>;
   if (vectors <= 64 * 4) return run(grad_kernel<E, true, 64>, g, 64, bit_bytes(ps.len), stream, a, ps);

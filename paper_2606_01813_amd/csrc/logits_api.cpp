@@ -17,7 +17,7 @@ using caddtree::ok;
 namespace {
 
 constexpr int64_t kMaxStride = (int64_t)1 << 40;
-constexpr int32_t kMaxRows = 1 << 19;              // of a sequence
+constexpr int32_t kMaxRows = 1 << 19;              // of a sequence; and sequences
 
 size_t size_of(int dtype) { return dtype == CADDTREE_F32 ? 4 : 2; }
 
@@ -25,7 +25,7 @@ caddtree_status_t check_sizes(int dtype, int32_t B, int32_t T, int32_t V) {
   if (dtype != CADDTREE_F32 && dtype != CADDTREE_BF16 && dtype != CADDTREE_F16)
     return fail(CADDTREE_E_INVALID, "unknown dtype %d", dtype);
   if (B < 0 || T < 0) return fail(CADDTREE_E_INVALID, "B = %d and T = %d must not be negative", B, T);
-  if (B > 65535) return fail(CADDTREE_E_UNSUPPORTED, "B = %d exceeds 65535", B);
+  if (B > kMaxRows) return fail(CADDTREE_E_UNSUPPORTED, "B = %d exceeds 2^19 sequences", B);
   if (T > kMaxRows) return fail(CADDTREE_E_UNSUPPORTED, "T = %d exceeds 2^19 rows", T);
   if (V < 1) return fail(CADDTREE_E_INVALID, "V = %d must be >= 1", V);
   if (V > CADDTREE_MAX_VOCAB) return fail(CADDTREE_E_UNSUPPORTED, "V = %d exceeds %d", V, CADDTREE_MAX_VOCAB);

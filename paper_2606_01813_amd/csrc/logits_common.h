@@ -85,6 +85,13 @@ struct Vec {
   __device__ __forceinline__ void forget() { asm volatile("" : "+v"(w)); }
 };
 
+// Sequences are numbered in a grid's second and third dimension, which hold 65535 each; the last workgroups may have none.
+inline dim3 grid_of(int64_t x, int32_t B) {
+  const unsigned y = B < 32768 ? (unsigned)B : 32768u;
+  return dim3((unsigned)x, y, ((unsigned)B + y - 1) / y);
+}
+__device__ __forceinline__ int sequence() { return (int)(blockIdx.z * gridDim.y + blockIdx.y); }
+
 template <typename E>
 __device__ __forceinline__ typename E::T* row_of(const Rows& r, int64_t b, int64_t t) {
   return reinterpret_cast<typename E::T*>(r.data) + b * r.b + t * r.t;

@@ -663,6 +663,31 @@ def test_more_rows_than_a_grid_has_places_in_its_second_dimension():
     _check_distill(cut(x), cut(ids), cut(target), None, 1.0, False, grad=cut(distill_grad(x, ids, target, stats)), again=True)
 
 
+def test_more_sequences_than_a_grid_has_places_in_its_second_dimension():
+    B, V = 70001, 9
+    x = _rows(_gen(19), B, 1, V, BF)
+    ok = torch.rand((B, 1, V), generator=_gen(20), device="cuda") < 0.5
+    want = torch.where(ok, x, torch.tensor(-INF, dtype=BF, device="cuda"))
+    assert torch.equal(adjust_logits(x, allowed=_words(ok)), want)
+    y = x.clone()
+    assert torch.equal(adjust_logits(y, y, allowed=_words(ok)), want)
+    y[:, 0, 4] = 70.0
+    tok, par = torch.full((B, 0), 4, dtype=I32, device="cuda"), torch.full((B, 0), -1, dtype=I32, device="cuda")
+    acc, index, tokens, weight = _outputs(B, 1, 2)
+    verify_tree(y, tok, par, torch.zeros(B, dtype=I32, device="cuda"), acc, index, tokens, weight=weight)
+    assert bool((acc == 1).all()) and bool((tokens == torch.tensor([4, -1], device="cuda")).all())
+    ids, target = torch.zeros((B, 1, 1), dtype=I32, device="cuda"), torch.zeros((B, 1, 1), device="cuda")
+    loss, stats, grad = torch.zeros((B, 1), device="cuda"), torch.zeros((B, 1, 3), device="cuda"), torch.zeros_like(x)
+    distill(x, ids, target, loss, grad=grad, stats=stats)
+    again = distill_grad(x, ids, target, stats)
+    alone = torch.zeros((B, 1), device="cuda")
+    distill(x, ids, target, alone)
+    for cut in (lambda t: t[:2], lambda t: t[32767:32770], lambda t: t[-3:]):
+        _check_distill(cut(x), cut(ids), cut(target), None, 1.0, False, cut(loss), cut(stats), cut(grad))
+        _check_distill(cut(x), cut(ids), cut(target), None, 1.0, False, cut(alone))
+        _check_distill(cut(x), cut(ids), cut(target), None, 1.0, False, grad=cut(again), again=True)
+
+
 def test_empty_calls():
     z = lambda *s, t=F32: torch.zeros(s, dtype=t, device="cuda")
     assert adjust_logits(z(0, 3, 8)).shape == (0, 3, 8) and adjust_logits(z(2, 0, 8)).shape == (2, 0, 8)

@@ -251,7 +251,7 @@ def _args(cls, **kw):
     return a
 
 
-SIZES = [(dict(dtype=7), INVALID), (dict(dtype=-1), INVALID), (dict(B=-1), INVALID), (dict(T=-1), INVALID), (dict(B=65536), UNSUPPORTED),
+SIZES = [(dict(dtype=7), INVALID), (dict(dtype=-1), INVALID), (dict(B=-1), INVALID), (dict(T=-1), INVALID), (dict(B=2 ** 19 + 1), UNSUPPORTED),
          (dict(T=2 ** 19 + 1), UNSUPPORTED), (dict(V=0), INVALID), (dict(V=-5), INVALID), (dict(V=2 ** 20 + 1), UNSUPPORTED),
          (dict(logits=(AT["logits"] + 1, 350, 70)), INVALID), (dict(logits=(AT["logits"], -350, 70)), INVALID),
          (dict(logits=(AT["logits"], 350, -70)), INVALID), (dict(logits=(AT["logits"], 2 ** 41, 70)), UNSUPPORTED)]
