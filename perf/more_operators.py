@@ -254,7 +254,7 @@ def _plain_teacher(c, s):
 
 def _plain_student(c, s):
     """The student's log-probabilities [B, T, V], which tokens are listed, log(1 - Q) [B, T], and the largest logit of a
-    row with the sums of the exponentials of the distances to it, over all and over the tokens not listed [B, T, 3]."""
+    row with the sum of the exponentials of the distances to it [B, T, 2]."""
     x = s["logits"].float()
     top = x.amax(-1, keepdim=True)
     x = (x - top) / c["tau"]
@@ -262,7 +262,7 @@ def _plain_student(c, s):
     total = e.sum(-1, keepdim=True)
     on = torch.zeros(x.shape, dtype=torch.bool, device="cuda").scatter_(2, s["ids"].to(torch.int64), True)
     rest = torch.where(on, 0.0, e).sum(-1)
-    return x - total.log(), on, rest.log() - total.log()[..., 0], torch.cat((top, total, rest[..., None]), -1)
+    return x - total.log(), on, rest.log() - total.log()[..., 0], torch.cat((top, total), -1)
 
 
 def _plain_distill(c, s):
@@ -378,15 +378,13 @@ def prepare(c, seed):
     w.view(-1)[off] = 0.0
     s["weight"] = w
     s["loss"] = torch.zeros((B, T), device="cuda")
-    s["stats"] = torch.zeros((B, T, 3), device="cuda")
+    s["stats"] = torch.zeros((B, T, 2), device="cuda")
     if c["op"] == "grad":
         for b in range(0, B, 8):
             x = s["logits"][b:b + 8].double()
             m = x.amax(-1)
             s["stats"][b:b + 8, :, 0] = m
-            x = ((x - m[..., None]) / c["tau"]).exp()
-            s["stats"][b:b + 8, :, 1] = x.sum(-1)
-            s["stats"][b:b + 8, :, 2] = x.scatter(2, ids[b:b + 8].to(torch.int64), 0.0).sum(-1)
+            s["stats"][b:b + 8, :, 1] = ((x - m[..., None]) / c["tau"]).exp().sum(-1)
     if c["op"] != "loss":
         s["grad"] = torch.zeros((B, T, V + c["pad"]), dtype=TYPES[c["dtype"]], device="cuda")[..., :V]
     if own:
@@ -475,7 +473,7 @@ def _exact_verify(c, s):
 def _exact_distill(c, s):
     B, T = c["B"], c["T"]
     loss = torch.zeros((B, T), dtype=torch.float64, device="cuda")
-    norm = torch.zeros((B, T, 3), dtype=torch.float64, device="cuda")
+    norm = torch.zeros((B, T, 2), dtype=torch.float64, device="cuda")
     grad = torch.zeros((B, T, c["V"]), dtype=torch.float64, device="cuda") if c["op"] != "loss" else None
     for b in range(B):
         x = s["logits"][b].double() / c["tau"]
@@ -494,7 +492,7 @@ def _exact_distill(c, s):
         some = rho > 0
         one[some] += rho[some] * (torch.log(rho[some]) - (top[some, 0] + torch.log(rest[some]) - lse[some]))
         loss[b] = torch.where(w != 0, w * one, 0.0)
-        norm[b] = torch.where(w[:, None] != 0, torch.stack((s["logits"][b].double().max(1).values, e.sum(1), rest), 1), 0.0)
+        norm[b] = torch.where(w[:, None] != 0, torch.stack((top[:, 0] * c["tau"], e.sum(1)), 1), 0.0)
         if grad is not None:
             q = torch.exp(x - lse[:, None])
             teacher = full + torch.where(some[:, None], rho[:, None] * (1.0 - on) * e / rest[:, None], 0.0)
