@@ -388,8 +388,12 @@ def prepare(c, seed):
     if c["op"] != "loss":
         s["grad"] = torch.zeros((B, T, V + c["pad"]), dtype=TYPES[c["dtype"]], device="cuda")[..., :V]
     if own:
-        from paper_2606_01813_amd import distill_workspace
+        from paper_2606_01813_amd import distill, distill_workspace
         s["workspace"] = distill_workspace(s["logits"])
+        s["kept"] = torch.zeros((B, T, 3), device="cuda")                          # as the calls have them: with the rest's sum
+        if c["op"] == "grad":
+            distill(s["logits"], s["ids"], s["target"], s["loss"], stats=s["kept"], weight=w, temperature=c["tau"], tail=c["tail"],
+                    workspace=s["workspace"])
     return s
 
 
@@ -409,9 +413,10 @@ def run(s):
         return s["accepted"], s["index"], s["tokens"], s["weight"]
     how = dict(weight=s["weight"], temperature=c["tau"], tail=c["tail"], workspace=s["workspace"])
     if c["op"] == "grad":
-        return (distill_grad(s["logits"], s["ids"], s["target"], s["stats"], s["grad"], **how),)
-    distill(s["logits"], s["ids"], s["target"], s["loss"], stats=s["stats"], grad=s.get("grad"), **how)
-    return (s["loss"], s["stats"]) if c["op"] == "loss" else (s["loss"], s["stats"], s["grad"])
+        return (distill_grad(s["logits"], s["ids"], s["target"], s["kept"], s["grad"], **how),)
+    distill(s["logits"], s["ids"], s["target"], s["loss"], stats=s["kept"], grad=s.get("grad"), **how)
+    stats = s["kept"][..., :2]
+    return (s["loss"], stats) if c["op"] == "loss" else (s["loss"], stats, s["grad"])
 
 
 # ---------------------------------------------------------------- the definition in 64 bits
