@@ -53,10 +53,11 @@ struct Row {
   double Z, mass, scale;                          // M and w / tau
 };
 
-// c = log2(e) / tau.  A term is exp2(l c - r), one fused product and difference, where l c stays within kFar; the
-// reference r is a product m c as it was rounded, and its distance from m c is made up for in fp64.  Beyond that (masks
-// of the type's lowest value in a whole row, for instance) a term is exp2((l - m) c).
-constexpr float kFar = 1e30f;
+// c = log2(e) / tau.  A term is exp2(l c - r), one fused product and difference, where l c stays within kFar: the reference r
+// is a product m c as it was rounded, by a half at most, and its distance from m c is made up for in fp64.  Beyond that (masks of
+// -1e10 or of the type's lowest value in a whole row, for instance), where the rounding alone would make a term infinite or 0, a
+// term is exp2((l - m) c).
+constexpr float kFar = 0x1p24f;
 constexpr float kRoom = 8.f;                      // a term may reach 2^kRoom before the reference moves
 
 template <int N>
@@ -171,7 +172,12 @@ struct Stream {
   float c, mc, lim, top = -INFINITY;
   double s = 0.0;
 
-  __device__ __forceinline__ explicit Stream(float c_) : c(c_), mc(-kFar), lim(-2.f * kFar / c_) {}
+  // The first reference is the lowest there is: what is below has no part in s (and where all is, far() says so), what is above
+  // moves it up.  So it only rises, and s never grows where it does.
+  __device__ __forceinline__ explicit Stream(float c_) : c(c_), mc(-kFar), lim(lowest(c_)) {}
+  static __device__ __forceinline__ float lowest(float c) { return (kRoom - kFar) / c; }
+  // whether the sum has to be formed again, from differences to its largest logit t
+  __device__ __forceinline__ bool far(float t) const { return t > kFar / c || (t > -INFINITY && t <= lowest(c)); }
   template <int kN>
   __device__ __forceinline__ void add(const float (&x)[kN], uint32_t on) {
     const float t = top_of(x);
@@ -258,7 +264,7 @@ __device__ void put_partial(Stream r, const Edge<E>& edge, const typename E::T* 
   r.add(x, edge.on ? 1u : 0u);
   const float top = wave_max(r.top);
   double ref = (double)r.mc;
-  if (top > kFar / r.c || (top > -INFINITY && top <= -2.f * kFar / r.c)) {
+  if (r.far(top)) {
     r.s = edge.on ? 0.0 : (double)__builtin_amdgcn_exp2f((edge.x - top) * r.c);
     for (int v = first + (int)threadIdx.x; v < last; v += kThreads) {
       const Vec<E> q = Vec<E>::load(l, (uint32_t)v);
