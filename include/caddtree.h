@@ -542,12 +542,14 @@ typedef struct {
  *     loss = weight [ sum_k p_k (log p_k - log q_k) + rho (log rho - log(1 - Q)) ],  Q = sum of q over the listed
  *     grad_v = weight / temperature [ q_v M - (v is listed: the sum of its p_k; else: rho q_v / (1 - Q)) ]
  * with M = sum_k p_k + rho.  A term with p_k = 0 (t_k = -inf) is 0.  Where all t_k are -inf and tail = 0
- * nothing counts as listed.  The rest's term is left out where the student
- * gives the rest nothing.  Padding is in no sum: with nothing listed, loss and gradient are 0.  A token listed twice
+ * nothing counts as listed.  The rest's mass 1 - Q is a sum of its own, at any distance from the listed tokens; its term is left
+ * out where the student gives the rest nothing: where that sum, of exp((logit - largest) / temperature), is less than
+ * fp64 has (2^-1074).  Padding is in no sum: with nothing listed, loss and gradient are 0.  A token listed twice
  * is two terms.  Where weight is 0 the row is not read: loss, gradient and stats are 0.  A student's logit of -inf
- * (a mask) has q = 0; in a row of nothing else every q is 0.  NaN and +inf spread over their row.
+ * (a mask) has q = 0; in a row of nothing else every q is 0; a finite one is a logit of that value, whatever its size.  NaN and
+ * +inf spread over their row.  weight / temperature has to be a number of fp32.
  *   stats[b, t]: the row's largest logit, the sum of exp((logit - largest) / temperature) (0 if all are -inf), and
- *   the same sum without the listed tokens.
+ *   the same sum without the listed tokens; where that is above 0 and below 2^-126, its logarithm to base 2, a negative number.
  * caddtree_distill writes the loss and, where asked for, the gradient in one pass over the logits;
  * caddtree_distill_grad the gradient alone, from the stats that such a call kept of the same logits, ids and
  * temperature (weight: the loss's gradient).

@@ -2,11 +2,12 @@
 // q = softmax(l / tau); the teacher lists K tokens with probabilities p_k, and may leave rho to all others:
 //     loss = w [ sum_k p_k (log p_k - log q_k) + rho (log rho - log(1 - Q)) ],  Q = sum of q over the listed tokens
 //     dloss/dl_v = w / tau [ q_v M - (listed: sum of its p_k; else: rho q_v / (1 - Q)) ],  M = sum_k p_k + rho
-// With m the row's largest logit, e_v = exp((l_v - m) / tau), R the sum of e_v over the tokens not listed and Z over
-// all: q_v = e_v / Z and 1 - Q = R / Z, formed without a difference.  A token not listed has the gradient
-// e_v (M / Z - rho / R) w / tau: one exponential and one product.
+// With m the row's largest logit and r the largest of the tokens not listed, e_v = exp((l_v - r) / tau), S the sum of e_v over the
+// tokens not listed, f = exp((r - m) / tau) and Z = S f + the listed tokens' exp((l_k - m) / tau): 1 - Q = S f / Z, formed without
+// a difference, and its logarithm without f.  A token not listed has the gradient e_v (M f / Z - rho / S) w / tau: one exponential
+// and one product, of numbers that are near 1 where the gradient is, however far below the listed tokens the others lie.
 //
-// A bit for each token says whether it is listed (in LDS): its term is left out of R as the row streams by, and its
+// A bit for each token says whether it is listed (in LDS): its term is left out of S as the row streams by, and its
 // gradient is written by a lane of its own.
 //
 // Least traffic: each logit read once and each gradient written once.  The gradient needs the row's sums, so a row has to be
@@ -41,15 +42,16 @@ struct Listed {
   double p[kMaxK];
   float l[kMaxK];                                 // the student's logit
   int twice;                                      // a token is listed twice
+  float top;                                      // the student's largest logit of them
   double P, A, rho;                               // sum p_k, sum p_k log p_k
 };
 
-// How the row's sums enter loss and gradient.
+// How the row's sums enter the gradient.
 struct Row {
-  float m;                                        // the largest logit, 0 where that is -inf
-  float mc;                                       // m c, rounded
+  float top;                                      // the largest logit, 0 where that is -inf
+  float m, k, mc;                                 // terms are exp2((l - m) c - k); m c + k, rounded
   float rest;                                     // gradient of a token not listed / exp2(l c - mc)
-  bool far;                                       // ... / exp2((l - m) c)
+  bool far;                                       // ... / exp2((l - m) c - k)
   double Z, mass, scale;                          // M and w / tau
 };
 
@@ -95,7 +97,7 @@ __device__ void fetch_listed(const DistillArgs& a, int64_t row, const typename E
 // first).
 __device__ void read_listed(const DistillArgs& a, const Raw& raw, int first, int last, Listed& L, uint32_t* bits) {
   const int lane = (int)threadIdx.x % kWave;
-  float top = -INFINITY;
+  float top = -INFINITY, most = -INFINITY;
   double z = 0.0, of = 0.0;
   if (!a.tail) {
 #pragma unroll 1
@@ -120,15 +122,18 @@ __device__ void read_listed(const DistillArgs& a, const Raw& raw, int first, int
     P += p;
     if (p != 0.0) A += p * logp;
     if (id >= first && id < last) twice |= (atomicOr(&bits[at >> 5], 1u << (at & 31)) >> (at & 31) & 1u) != 0;
+    if (id >= 0) most = fmaxf(most, raw.l[k]);
     L.id[k] = id;
     L.p[k] = p;
     L.l[k] = raw.l[k];
   }
+  most = wave_max(most);
   P = wave_sum(P);
   A = wave_sum(A);
   const bool any = __any(twice);
   if (lane == 0) {
     L.twice = any;
+    L.top = most;
     L.P = P;
     L.A = A;
     L.rho = a.tail && 1.0 - P > 0.0 ? 1.0 - P : 0.0;
@@ -152,10 +157,20 @@ __device__ __forceinline__ bool first_of(const Listed& L, int K, int k, double& 
 
 __device__ __forceinline__ float weight_of(const DistillArgs& a, int64_t row) { return a.weight ? a.weight[row] : 1.f; }
 
-// A row's, or a part's, largest logit m and the sum of exp((l - m) / tau) over its tokens not listed.
+// Of the tokens not listed of a row, or of a part: the largest logit m and the sum of exp((l - m) / tau).
 struct Sum {
   float m;
   double s;
+};
+// A row's sums.  The tokens not listed have exp2((l - rest.m) c - k) as their terms, and f is the size of such a term beside
+// the largest logit's.
+struct Whole {
+  float m;                                        // the largest logit
+  double Z;                                       // the sum of exp((l - m) / tau)
+  Sum rest;
+  int k;
+  double f;
+  __device__ __forceinline__ double R() const { return rest.s == 0.0 ? 0.0 : rest.s * f; }     // (0: nothing, or less than fp64 has)
 };
 
 template <int kN>
@@ -166,8 +181,8 @@ __device__ __forceinline__ float top_of(const float (&x)[kN]) {
   return t;
 }
 
-// A wavefront's sum as its logits stream by.  The reference is the wavefront's and moves seldom: when a logit is kRoom
-// above it.
+// A wavefront's sum as its logits stream by, of those not listed: a listed one may be so far above the others that beside it they
+// were nothing.  The reference is the wavefront's and moves seldom: when a logit is kRoom above it.
 struct Stream {
   float c, mc, lim, top = -INFINITY;
   double s = 0.0;
@@ -179,7 +194,11 @@ struct Stream {
   // whether the sum has to be formed again, from differences to its largest logit t
   __device__ __forceinline__ bool far(float t) const { return t > kFar / c || (t > -INFINITY && t <= lowest(c)); }
   template <int kN>
-  __device__ __forceinline__ void add(const float (&x)[kN], uint32_t on) {
+  __device__ __forceinline__ void add(float (&x)[kN], uint32_t on) {
+    if (__any(on != 0)) {
+#pragma unroll
+      for (int j = 0; j < kN; ++j) x[j] = on >> j & 1 ? -INFINITY : x[j];
+    }
     const float t = top_of(x);
     top = fmaxf(top, t);
     if (__any(t > lim)) {
@@ -193,10 +212,6 @@ struct Stream {
     float e[kN];
 #pragma unroll
     for (int j = 0; j < kN; ++j) e[j] = __builtin_amdgcn_exp2f(fmaf(x[j], c, -mc));
-    if (__any(on != 0)) {
-#pragma unroll
-      for (int j = 0; j < kN; ++j) e[j] = on >> j & 1 ? 0.f : e[j];
-    }
 #pragma unroll
     for (int w = 1; w < kN; w <<= 1)
 #pragma unroll
@@ -249,7 +264,7 @@ __device__ __forceinline__ void stream_row(Stream& r, Vec<E> (&q)[kU], const typ
     if (at + u * kThreads < last) add(u);
 }
 
-// A wavefront's result, in LDS: its largest logit, and a sum of exp2(l c - r).
+// A wavefront's result, in LDS: its largest logit not listed, and a sum of exp2(l c - r).
 struct Partial {
   float top;
   double r, s;
@@ -260,7 +275,7 @@ template <typename E, int kThreads>
 __device__ void put_partial(Stream r, const Edge<E>& edge, const typename E::T* l, int first, int last, const uint32_t* bits,
                             Partial* p) {
   constexpr int N = kN<E>;
-  const float x[1] = {edge.x};
+  float x[1] = {edge.x};
   r.add(x, edge.on ? 1u : 0u);
   const float top = wave_max(r.top);
   double ref = (double)r.mc;
@@ -299,53 +314,90 @@ __device__ __forceinline__ double listed_sum(const Listed& L, int K, float m, do
   return wave_sum(sum);
 }
 
-__device__ void finish(Row& r, float m, double Z, double R, const Listed& L, float w, double inverse, float c) {
-  r.m = m == -INFINITY ? 0.f : m;
-  r.mc = r.m * c;
-  r.far = !(fabsf(r.mc) <= kFar);
-  r.Z = Z;
-  r.mass = L.P + L.rho;
-  r.scale = (double)w * inverse;
-  const double rest = R == 0.0 ? 0.0 : r.scale * (r.mass / Z - (L.rho == 0.0 ? 0.0 : L.rho / R));
-  r.rest = (float)(r.far ? rest : rest * pow2((double)r.mc - (double)r.m * (double)c));
+// From the sums of the tokens not listed and of the listed ones, which are relative to the row's largest logit m.
+__device__ __forceinline__ Whole whole_of(float m, const Sum& rest, double listed, double c) {
+  Whole h;
+  h.m = m;
+  h.rest = rest;
+  h.k = 0;
+  h.f = rest.s == 0.0 ? 0.0 : pow2(((double)rest.m - (double)m) * c);
+  h.Z = h.R() + listed;
+  return h;
+}
+// From what put_loss kept of them: R, or its logarithm where that is below what a float holds.  The terms are taken relative to
+// the power of two next to R, where R is below 1: beside the largest logit they may be nothing.
+__device__ __forceinline__ Whole whole_of(const float* stats) {
+  Whole h;
+  h.m = stats[0];
+  h.Z = (double)stats[1];
+  const float R = stats[2];
+  h.k = 0;
+  double s = (double)R;
+  if (R < 0.f) {
+    h.k = (int)fmaxf(ceilf(R), -2000.f);
+    s = pow2((double)R - (double)h.k);
+  } else if (R < 1.f && R > 0.f) {
+    s = frexp(s, &h.k);
+  }
+  h.rest = Sum{h.m, s};
+  h.f = ldexp(1.0, h.k);
+  return h;
 }
 
-// By one wavefront, from a row's largest logit and R: Z, and what its gradient needs.
-__device__ __forceinline__ double conclude(const DistillArgs& a, const Listed& L, const Sum& sum, float w, float c, Row& r) {
-  const double Z = sum.s + listed_sum(L, a.K, sum.m == -INFINITY ? 0.f : sum.m, a.c);
-  if (threadIdx.x % kWave == 0) finish(r, sum.m, Z, sum.s, L, w, a.inverse, c);
-  return Z;
+// The distance of c from c32 grows with that of the terms from m: at k, where they lie, it is made up for.  (A NaN in Z is the
+// whole row's.)
+__device__ void finish(Row& r, const Whole& h, const Listed& L, float w, const DistillArgs& a) {
+  const double k = (double)h.k;
+  r.top = h.m == -INFINITY ? 0.f : h.m;
+  r.m = h.rest.m == -INFINITY ? 0.f : h.rest.m;
+  r.k = (float)h.k;
+  const double ref = (double)r.m * (double)a.c32 + k;
+  r.mc = (float)ref;
+  r.far = !(fabsf(r.mc) <= kFar);
+  r.Z = h.Z;
+  r.mass = L.P + L.rho;
+  r.scale = (double)w * a.inverse;
+  const double rest = h.R() == 0.0 ? 0.0 * h.Z : r.scale * (r.mass * h.f / h.Z - (L.rho == 0.0 ? 0.0 : L.rho / h.rest.s));
+  r.rest = (float)(rest * pow2((r.far ? 0.0 : (double)r.mc - ref) + k * a.off));
+}
+
+// By one wavefront, from the sum of a row's tokens not listed: all its sums, and what its gradient needs.
+__device__ __forceinline__ Whole conclude(const DistillArgs& a, const Listed& L, const Sum& rest, float w, Row& r) {
+  const float m = fmaxf(rest.m, L.top);
+  const Whole h = whole_of(m, rest, listed_sum(L, a.K, m == -INFINITY ? 0.f : m, a.c), a.c);
+  if (threadIdx.x % kWave == 0) finish(r, h, L, w, a);
+  return h;
 }
 // ... its loss and stats.
-__device__ void put_loss(const DistillArgs& a, int64_t row, const Listed& L, const Sum& sum, double Z, float w) {
+__device__ void put_loss(const DistillArgs& a, int64_t row, const Listed& L, const Whole& h, float w) {
   const int lane = (int)threadIdx.x % kWave;
-  const double R = sum.s, logZ = log(Z);
-  const float from = sum.m == -INFINITY ? 0.f : sum.m;
+  const double R = h.R(), logZ = log(h.Z);
+  const double from = h.m == -INFINITY ? 0.0 : (double)h.m;
   double x = 0.0;                                 // sum p_k log q_k
 #pragma unroll 1
   for (int k = lane; k < a.K; k += kWave) {
     if (L.id[k] >= 0 && L.p[k] != 0.0)
-      x += L.p[k] * (L.l[k] == -INFINITY ? -INFINITY : ((double)L.l[k] - (double)from) * a.inverse - logZ);
+      x += L.p[k] * (L.l[k] == -INFINITY ? -INFINITY : ((double)L.l[k] - from) * a.inverse - logZ);
   }
   x = L.A - wave_sum(x);
-  if (L.rho > 0.0 && !(R == 0.0)) x += L.rho * (log(L.rho) - log(R / Z));
+  if (L.rho > 0.0 && !(R == 0.0)) x += L.rho * (log(L.rho / h.rest.s) - ((double)h.rest.m - from) * a.inverse + logZ);
   if (lane != 0) return;
   a.loss[row] = (float)((double)w * x);
   if (a.stats) {
-    a.stats[row * 3] = sum.m;
-    a.stats[row * 3 + 1] = (float)Z;
-    a.stats[row * 3 + 2] = (float)R;
+    a.stats[row * 3] = h.m;
+    a.stats[row * 3 + 1] = (float)h.Z;
+    a.stats[row * 3 + 2] = (float)(R < 0x1p-126 && R > 0.0 ? log2(h.rest.s) + ((double)h.rest.m - from) * a.c : R);
   }
 }
 
-// A vector's gradient into g; the listed tokens' is left to put_listed.  kFarOff: from exp2((l - m) c).
+// A vector's gradient into g; the listed tokens' is left to put_listed.  kFarOff: from exp2((l - m) c - k), else m is Row::mc.
 template <typename E, bool kFarOff = false>
-__device__ __forceinline__ void put_vector(const Vec<E>& q, typename E::T* row, int v, uint32_t on, float m, float rest, float c) {
+__device__ __forceinline__ void put_vector(const Vec<E>& q, typename E::T* row, int v, uint32_t on, float m, float rest, float c, float k = 0.f) {
   constexpr int N = kN<E>;
   float x[N];
   q.get(x);
 #pragma unroll
-  for (int j = 0; j < N; ++j) x[j] = __builtin_amdgcn_exp2f(kFarOff ? (x[j] - m) * c : fmaf(x[j], c, -m)) * rest;
+  for (int j = 0; j < N; ++j) x[j] = __builtin_amdgcn_exp2f(kFarOff ? fmaf(x[j] - m, c, -k) : fmaf(x[j], c, -m)) * rest;
   Vec<E> y;
   y.set(x);
   if (on == 0) {
@@ -358,12 +410,12 @@ __device__ __forceinline__ void put_vector(const Vec<E>& q, typename E::T* row, 
 }
 template <typename E>
 __device__ __forceinline__ void put_edge(const Edge<E>& e, typename E::T* g, const Row& r, float c) {
-  if (e.here && !e.on) g[e.at] = (typename E::T)(__builtin_amdgcn_exp2f(r.far ? (e.x - r.m) * c : fmaf(e.x, c, -r.mc)) * r.rest);
+  if (e.here && !e.on) g[e.at] = (typename E::T)(__builtin_amdgcn_exp2f(r.far ? fmaf(e.x - r.m, c, -r.k) : fmaf(e.x, c, -r.mc)) * r.rest);
 }
 // Vectors first .. last - 1 of a row, the last first, kU loads in flight a lane.
 template <typename E, int kThreads, int kU, bool kFarOff>
 __device__ __forceinline__ void put_vectors(const typename E::T* l, typename E::T* g, int first, int last, const uint32_t* bits,
-                                            float m, float rest, float c) {
+                                            float m, float rest, float c, float k = 0.f) {
   constexpr int kStep = kU * kThreads;
   for (int at = first + (last - first + kStep - 1) / kStep * kStep - kStep; at >= first; at -= kStep) {
     Vec<E> q[kU];
@@ -371,7 +423,7 @@ __device__ __forceinline__ void put_vectors(const typename E::T* l, typename E::
 #pragma unroll
     for (int u = 0; u < kU; ++u) {
       const int v = at + (int)threadIdx.x + u * kThreads;
-      if (v < last) put_vector<E, kFarOff>(q[u], g, v, bits_at<kN<E>>(bits, v * kN<E>), m, rest, c);
+      if (v < last) put_vector<E, kFarOff>(q[u], g, v, bits_at<kN<E>>(bits, v * kN<E>), m, rest, c, k);
     }
   }
 }
@@ -382,7 +434,7 @@ __device__ void put_listed(const DistillArgs& a, typename E::T* g, const Row& r,
     if (L.id[k] < first || L.id[k] >= last) continue;
     double p;
     if (!first_of(L, a.K, k, p)) continue;
-    const double e = L.l[k] == -INFINITY ? 0.0 : pow2(((double)L.l[k] - (double)r.m) * a.c);
+    const double e = L.l[k] == -INFINITY ? 0.0 : pow2(((double)L.l[k] - (double)r.top) * a.c);
     g[L.id[k]] = (typename E::T)(float)(r.scale * ((r.Z == 0.0 ? 0.0 : e / r.Z) * r.mass - p));
   }
 }
@@ -467,19 +519,17 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
   if (kept < n) stream_row<E, kThreads, !kGrad>(acc, p, l, kept, n, s_bits + kept * N / 32);
   put_partial<E, kThreads>(acc, edge, l, 0, n, s_bits, part);
   __syncthreads();
-  Sum sum;
-  double Z;
+  Whole h;
   if (tid < kWave) {
-    sum = join_partials(part, kThreads / kWave, c);
-    Z = conclude(a, L, sum, w, c, r);
-    if (!kGrad) put_loss(a, row, L, sum, Z, w);
+    h = conclude(a, L, join_partials(part, kThreads / kWave, c), w, r);
+    if (!kGrad) put_loss(a, row, L, h, w);
   }
   if constexpr (kGrad) {
     __syncthreads();
     const float mc = r.mc, rest = r.rest;
     put_edge<E>(edge, g, r, c);
     if (r.far) {
-      put_vectors<E, kThreads, 1, true>(l, g, 0, n, s_bits, r.m, rest, c);
+      put_vectors<E, kThreads, 1, true>(l, g, 0, n, s_bits, r.m, rest, c, r.k);
     } else {
       put_vectors<E, kThreads, kU, false>(l, g, kept, n, s_bits, mc, rest, c);
       asm volatile("" : "+v"(at));
@@ -494,7 +544,7 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
       }
     }
     put_listed<E, kThreads>(a, g, r, L, 0, a.V);
-    if (tid < kWave) put_loss(a, row, L, sum, Z, w);
+    if (tid < kWave) put_loss(a, row, L, h, w);
   }
 }
 
@@ -502,7 +552,8 @@ __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
 // logits go through the workspace to a second launch.
 struct PartSum {
   Sum rest;                                       // of the tokens not listed
-  double listed;                                  // of the others, from the same m
+  float top;                                      // the largest logit, and from there
+  double listed;                                  // ... the sum of the others
 };
 struct Parts {
   PartSum* sum;                                   // [rows, n]
@@ -552,7 +603,11 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
   __syncthreads();
   if (tid >= kWave) return;
   const Sum rest = join_partials(partial, kSumThreads / kWave, c);
-  const double from = rest.m == -INFINITY ? 0.0 : (double)rest.m;
+  float top = -INFINITY;
+  for (int k = tid; k < a.K; k += kWave)
+    if (s_id[k] >= 0) top = fmaxf(top, s_l[k]);
+  top = fmaxf(wave_max(top), rest.m);
+  const double from = top == -INFINITY ? 0.0 : (double)top;
   double listed = 0.0;
   for (int k = tid; k < a.K; k += kWave) {
     bool one = s_id[k] >= 0;
@@ -561,23 +616,19 @@ __global__ __launch_bounds__(kSumThreads) void sums_kernel(DistillArgs a, Parts 
     if (one && s_l[k] != -INFINITY) listed += pow2(((double)s_l[k] - from) * a.c);
   }
   listed = wave_sum(listed);
-  if (tid == 0) ps.sum[row * ps.n + part] = PartSum{rest, listed};
+  if (tid == 0) ps.sum[row * ps.n + part] = PartSum{rest, top, listed};
 }
 
 // A row's sums from its parts', by one wavefront, in all of its lanes.
-__device__ __forceinline__ Sum join_parts(const PartSum* p, int n, double c, double& Z) {
+__device__ __forceinline__ Whole join_parts(const PartSum* p, int n, double c) {
   const int i = (int)threadIdx.x % kWave;
-  const PartSum x = i < n ? p[i] : PartSum{{-INFINITY, 0.0}, 0.0};
-  const float m = wave_max(x.rest.m);
+  const PartSum x = i < n ? p[i] : PartSum{{-INFINITY, 0.0}, -INFINITY, 0.0};
+  const float m = wave_max(x.rest.m), top = wave_max(x.top);
   double s = x.rest.s, e = x.listed;
-  if (m > -INFINITY && (s != 0.0 || e != 0.0)) {
-    const double f = pow2(((double)x.rest.m - (double)m) * c);
-    s *= f;
-    e *= f;
-  }
-  const double R = wave_sum(s);
-  Z = R + wave_sum(e);
-  return Sum{m, R};
+  if (m > -INFINITY && s != 0.0) s *= pow2(((double)x.rest.m - (double)m) * c);
+  if (top > -INFINITY && e != 0.0) e *= pow2(((double)x.top - (double)top) * c);
+  const Sum rest = {m, wave_sum(s)};
+  return whole_of(top, rest, wave_sum(e), c);
 }
 
 // The gradient of a part of a row.  kStats: from a.stats; else from the parts' sums, and the row's first part writes its
@@ -596,8 +647,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(DistillArgs a, Parts ps)
   __shared__ Listed L;
   __shared__ Raw raw;
   static_assert(kStats || kThreads >= 2 * kWave, "a wavefront for the list, one for the parts");
-  __shared__ Sum s_sum;
-  __shared__ double s_Z;
+  __shared__ Whole s_whole;
   const int t = (int)blockIdx.x / ps.n, part = (int)blockIdx.x % ps.n;
   const int b = sequence();
   if (b >= a.B) return;
@@ -624,32 +674,21 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(DistillArgs a, Parts ps)
     fetch_listed<E>(a, row, l, kStats ? nullptr : ps.listed + row * a.K, first, last, raw);
     read_listed(a, raw, first, last, L, s_bits);
   } else if (!kStats && tid < 2 * kWave) {          // (meanwhile)
-    double Z;
-    const Sum sum = join_parts(ps.sum + row * ps.n, ps.n, a.c, Z);
-    if (tid == kWave) {
-      s_sum = sum;
-      s_Z = Z;
-    }
+    const Whole h = join_parts(ps.sum + row * ps.n, ps.n, a.c);
+    if (tid == kWave) s_whole = h;
   }
-  Sum sum;
-  double Z;
-  if constexpr (kStats) {
-    sum = Sum{a.stats[row * 3], (double)a.stats[row * 3 + 2]};
-    Z = (double)a.stats[row * 3 + 1];
-  }
+  Whole h;
+  if constexpr (kStats) h = whole_of(a.stats + row * 3);
   __syncthreads();
-  if constexpr (!kStats) {
-    sum = s_sum;
-    Z = s_Z;
-  }
+  if constexpr (!kStats) h = s_whole;
   Row r;                                            // (each for itself)
-  finish(r, sum.m, Z, sum.s, L, w, a.inverse, c);
+  finish(r, h, L, w, a);
   if (g) {
     edge.look(s_bits);
     put_edge<E>(edge, g + first, r, c);
     const float mc = r.mc, rest = r.rest;
     if (__builtin_expect(r.far, 0)) {
-      put_vectors<E, kThreads, 1, true>(l + first, g + first, 0, n, s_bits, r.m, rest, c);
+      put_vectors<E, kThreads, 1, true>(l + first, g + first, 0, n, s_bits, r.m, rest, c, r.k);
     } else {
 #pragma unroll
       for (int u = 0; u < kGradLoads; ++u) {
@@ -661,7 +700,7 @@ __global__ __launch_bounds__(kThreads) void grad_kernel(DistillArgs a, Parts ps)
     }
     put_listed<E, kThreads>(a, g, r, L, first, last);
   }
-  if (store && tid < kWave) put_loss(a, row, L, sum, Z, w);
+  if (store && tid < kWave) put_loss(a, row, L, h, w);
 }
 
 size_t bit_bytes(int n) { return (size_t)((n + 31) / 32) * 4; }
@@ -682,7 +721,8 @@ hipError_t run(F kernel, dim3 grid, int threads, size_t lds, hipStream_t stream,
 // 128 x 14 63, 512 x 0 171; 8192 of 16000 128 x 16 97, 256 x 16 130; 4096 of 32000 256 x 16 96, and when that took 104 512 x 8
 // 119, 512 x 14 134; 512 rows of 25000 vectors 512 x 14 64, 1024 x 16 68; 512 rows of 151936 f32 (37984 vectors) 512 x 14
 // 148, 1024 x 16 131.  The loss alone: 65536 rows of 1024 64 threads 102, 128 132, 512 496; 16384 of 8192 64 60, 128 63, 512
-// 150; 4096 of 32000 64 60, 256 48, 512 58.
+// 150; 4096 of 32000 64 60, 256 48, 512 58.  (Each with the sums relative to the row's largest logit; relative to the largest of
+// the tokens not listed the 65536 rows take 141, their loss 105.)
 template <typename E>
 hipError_t launch_rows(const DistillArgs& a, hipStream_t stream) {
   const dim3 all = grid_of(a.T, a.B);

@@ -88,7 +88,7 @@ caddtree_status_t check_distill(const caddtree_distill_t* a) {
 caddtree::DistillArgs distill_args(const caddtree_distill_t* a) {
   const double c = 0x1.71547652b82fep+0 / (double)a->temperature;             // log2(e) / temperature
   return caddtree::DistillArgs{rows(a->logits), rows(a->grad), a->B, a->T, a->V, a->K, a->ids, a->target, a->weight,
-                               (float)c, c, 1.0 / (double)a->temperature, a->tail, a->loss, a->stats};
+                               (float)c, c, 1.0 / (double)a->temperature, (c - (double)(float)c) / c, a->tail, a->loss, a->stats};
 }
 
 // what both distillation calls read, and the gradient

@@ -59,6 +59,7 @@ struct DistillArgs {
   const float* weight;
   float c32;                 // log2(e) / temperature, rounded
   double c, inverse;         // ... and 1 / temperature
+  double off;                // (c - c32) / c
   int32_t tail;
   float* loss;
   float* stats;

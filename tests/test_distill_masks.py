@@ -33,6 +33,7 @@ def _close(got, want, tol, name):
 def _every_form(x, ids, target, tau, tail, names, weight=None):
     """Loss with gradient, the loss alone and the gradient from the stats, in whole rows and in parts, a call each."""
     B, T, V = x.shape
+    tau = float(np.float32(tau))                           # (a call's temperature is a float: 0.1 (1 + 1.5e-8))
     l, t, i = (a.detach().double().cpu().numpy() for a in (x, target, ids))
     w = np.ones((B, T)) if weight is None else weight.double().cpu().numpy()
     want = [[ref.distill(l[b, r], i[b, r].astype(int), t[b, r], w[b, r], tau, tail, x.dtype, again)
@@ -127,3 +128,43 @@ def test_logits_as_a_grammar_leaves_them(V):
                 target = torch.randn((B, T, K + 1), generator=gen, device="cuda")
                 target = (torch.log_softmax(target, -1) if tail else target)[..., :K].contiguous()
                 _every_form(y, ids, target, tau, tail, list(range(B)), weight=torch.rand((B, T), generator=gen, device="cuda") + 0.5)
+
+
+@pytest.mark.parametrize("tau", [0.1, 0.25, 1.0, 3.0])
+@pytest.mark.parametrize("dtype,V", [(F32, 40), (F32, 900), (F32, 4001), (F32, 16001), (F32, 70001), (F32, 140001), (BF, 1501), (BF, 8001),
+                                     (BF, 140009), (F16, 33), (F16, 16005)])
+def test_the_rest_far_below_the_listed_tokens(dtype, V, tau):
+    """The rest's mass is its own sum, wherever the listed tokens lie and however far above the others they are."""
+    gen = _gen(V + 3)
+    gaps = [9.0, 30.0, 80.0, 86.0, 87.0, 88.0, 90.0, 100.0, 104.0, 120.0, 200.0, 300.0, 500.0, 700.0, 800.0, 2000.0]
+    B, K = len(gaps), 5
+    ids, target = _teacher(gen, B, V, K, True)
+    x = torch.randn((B, 1, V), generator=gen, device="cuda") * tau          # (largest some 4 tau)
+    for b, gap in enumerate(gaps):
+        if b % 3 == 1:
+            ids[b, 0, :2] = torch.tensor([0, V - 1], dtype=I32)
+        listed = ids[b, 0].long()
+        others = x[b, 0].index_fill(0, listed, -1e9).max()
+        x[b, 0, listed] = others - torch.rand(K, generator=gen, device="cuda") * 3 * tau
+        x[b, 0, listed[K - 1 if b % 2 else 0]] = others + gap * tau           # (one of them)
+        if b % 4 == 3:
+            x[b, 0, listed[1]] = others + (gap - 1) * tau
+    weight = torch.rand((B, 1), generator=gen, device="cuda") * 64 + 0.5
+    _every_form(x.to(dtype), ids, target, tau, True, gaps, weight)
+    _every_form(x.to(dtype), ids, target, tau, False, gaps, weight)
+
+
+def test_where_the_listed_token_lies_does_not_matter():
+    """One listed token 88 above the rest, in each of a row's places: the same loss to the bound, in every form of the call."""
+    V, n = 4096, 64
+    x = torch.randn(V, generator=_gen(4), device="cuda").repeat(n, 1, 1)
+    ids = (torch.arange(n, device="cuda") * (V // n)).to(I32).view(n, 1, 1)
+    high = x[0].max() + 88
+    first = x[0, 0, 0].clone()
+    for b in range(n):                                     # (the same numbers in every row: place 0's and the listed one's change seats)
+        x[b, 0, 0] = x[b, 0, ids[b, 0, 0].long()]
+        x[b, 0, ids[b, 0, 0].long()] = high
+    x[0, 0, 0] = high
+    assert float(first) != float(high)
+    target = torch.full((n, 1, 1), float(np.log(0.9)), device="cuda")
+    _every_form(x, ids, target, 1.0, True, list(range(n)))
