@@ -543,6 +543,10 @@ struct Attn {
     const c10::TensorImpl* t = tensor(o);
     if (t != nullptr && t->requires_grad()) ok = false;
   }
+  void no_gradients(std::initializer_list<PyObject*> some) {
+    for (PyObject* o : some)
+      if (o != Py_None) no_gradient(o);
+  }
 
   int64_t integer(PyObject* o, int64_t lo, int64_t hi) {
     int over = 0;
@@ -897,6 +901,7 @@ PyObject* py_adjust_logits(PyObject*, PyObject* const* p, Py_ssize_t n) {
     a.count = as<int32_t>(c.array(p[15], c10::kInt, {a.B}, false));
     if (p[16] == Py_None) return -1;
     a.fill = c.scale(p[16], 1);
+    c.no_gradients({p[4], p[7], p[8], p[9], p[11]});
     if (!c.ok) return -1;
     return unlocked([&] { return s.adjust(&a, st); });
   });
@@ -930,6 +935,7 @@ PyObject* py_verify_tree(PyObject*, PyObject* const* p, Py_ssize_t n) {
     a.weight = as<float>(c.array(p[11], c10::kFloat, {a.B, a.T}, false));
     size_t bytes;
     void* ws = c.workspace(p[12], &bytes);
+    c.no_gradients({p[11]});
     if (!c.ok) return -1;
     return unlocked([&] { return s.verify(&a, ws, bytes, st); });
   });
@@ -949,6 +955,7 @@ bool distill_tensors(Attn& c, PyObject* logits, PyObject* ids, PyObject* target,
   a->weight = as<float>(c.array(weight, c10::kFloat, {a->B, a->T}, false));
   a->temperature = c.scale(temperature, 1);
   a->tail = c.truth(tail);
+  c.no_gradients({target, grad, stats, weight});
   if (temperature == Py_None) c.ok = false;
   return c.ok;
 }
@@ -963,6 +970,7 @@ PyObject* py_distill(PyObject*, PyObject* const* p, Py_ssize_t n) {
     a.loss = as<float>(c.array(p[6], c10::kFloat, {a.B, a.T}));
     size_t bytes;
     void* ws = c.workspace(p[12], &bytes);
+    c.no_gradients({p[6]});
     if (!c.ok) return -1;
     return unlocked([&] { return s.distill(&a, ws, bytes, st); });
   });

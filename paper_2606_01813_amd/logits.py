@@ -16,8 +16,8 @@
 
 Every call checks its tensors, then enqueues kernels on the stream (default: torch's current one) and returns.  Logits are
 bf16, f16 or f32 [B, rows, V] with a unit last stride, in any strides.  include/caddtree.h states what is computed.
-Autograd does not see these calls: ``distill`` writes the gradient itself, and logits that require one are refused while
-gradients are recorded.
+Autograd does not see these calls: ``distill`` writes the logits' gradient itself, and a tensor that requires one, be it the
+logits, a bias, a teacher's logits or a weight, is refused while gradients are recorded.
 
 As a plan's calls do, these go to the native binding first, which checks the tensors and calls the library; what it cannot
 vouch for comes back as None and takes the Python checks here, which raise what is wrong.
@@ -53,6 +53,11 @@ def _no_gradient(name: str, t, instead: str) -> None:
     torch = _torch()
     if torch.is_grad_enabled() and isinstance(t, torch.Tensor) and t.requires_grad:
         raise ValueError(f"{name} requires a gradient, which autograd does not carry through this call: {instead}")
+
+
+def _no_gradients(**others) -> None:
+    for name, t in others.items():
+        _no_gradient(name, t, f"call it under torch.no_grad(), or detach {name}")
 
 
 def _rows(name: str, t, dtype, shape, device: int) -> _lib.Rows:
@@ -94,7 +99,7 @@ def adjust_logits(logits, out=None, *, history=None, history_len=None, repetitio
         if _at._done(binding.adjust_logits(_lib.logits_ops(), device, raw, logits, out, history, history_len, repetition, presence,
                                            frequency, bias_ids, bias, allowed, token_ids, parent, count, fill)):
             return out
-    _no_gradient("logits", logits, "call it under torch.no_grad(), or detach logits")
+    _no_gradients(logits=logits, out=out, repetition=repetition, presence=presence, frequency=frequency, bias=bias)
     torch = _torch()
     device = _at._device()
     a = _lib.Adjust()
@@ -152,7 +157,7 @@ def verify_tree(logits, token_ids, parent, count, accepted, index, tokens, *, ch
         if _at._done(binding.verify_tree(_lib.logits_ops(), device, raw, logits, token_ids, parent, count, accepted, index, tokens,
                                          chosen, weight, workspace)):
             return
-    _no_gradient("logits", logits, "call it under torch.no_grad(), or detach logits")
+    _no_gradients(logits=logits, weight=weight)
     torch = _torch()
     device = _at._device()
     i32 = torch.int32
@@ -224,6 +229,7 @@ def distill(logits, ids, target, loss, *, grad=None, stats=None, weight=None, te
                                      workspace)):
             return
     _no_gradient("logits", logits, "pass logits.detach() and grad, then call logits.backward(grad)")
+    _no_gradients(target=target, loss=loss, grad=grad, stats=stats, weight=weight)
     device = _at._device()
     a = _distill(logits, ids, target, stats, grad, weight, temperature, tail, device)
     a.loss = _at._array("loss", loss, _torch().float32, (a.B, a.T), device)
@@ -243,6 +249,7 @@ def distill_grad(logits, ids, target, stats, grad=None, *, weight=None, temperat
         if _at._done(binding.distill_grad(_lib.logits_ops(), device, raw, logits, ids, target, stats, grad, weight, temperature, tail)):
             return grad
     _no_gradient("logits", logits, "pass logits.detach(), then call logits.backward(grad)")
+    _no_gradients(target=target, stats=stats, grad=grad, weight=weight)
     device = _at._device()
     if stats is None:
         raise TypeError("stats must be a torch tensor, got NoneType")
