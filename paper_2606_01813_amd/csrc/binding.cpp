@@ -543,6 +543,16 @@ struct Attn {
     const c10::TensorImpl* t = tensor(o);
     if (t != nullptr && t->requires_grad()) ok = false;
   }
+  // A call that was made wrote these (None: not given): what autograd saved of them is not what it was.
+  static int wrote(int status, std::initializer_list<PyObject*> some) {
+    if (status != 0) return status;
+    for (PyObject* o : some) {
+      if (o == Py_None) continue;
+      c10::TensorImpl* t = THPVariable_Unpack(o).unsafeGetTensorImpl();
+      if (!t->is_inference()) t->bump_version();
+    }
+    return status;
+  }
   void no_gradients(std::initializer_list<PyObject*> some) {
     for (PyObject* o : some)
       if (o != Py_None) no_gradient(o);
@@ -903,7 +913,7 @@ PyObject* py_adjust_logits(PyObject*, PyObject* const* p, Py_ssize_t n) {
     a.fill = c.scale(p[16], 1);
     c.no_gradients({p[4], p[7], p[8], p[9], p[11]});
     if (!c.ok) return -1;
-    return unlocked([&] { return s.adjust(&a, st); });
+    return c.wrote(unlocked([&] { return s.adjust(&a, st); }), {p[4]});
   });
 }
 
@@ -937,7 +947,7 @@ PyObject* py_verify_tree(PyObject*, PyObject* const* p, Py_ssize_t n) {
     void* ws = c.workspace(p[12], &bytes);
     c.no_gradients({p[11]});
     if (!c.ok) return -1;
-    return unlocked([&] { return s.verify(&a, ws, bytes, st); });
+    return c.wrote(unlocked([&] { return s.verify(&a, ws, bytes, st); }), {p[7], p[8], p[9], p[11]});
   });
 }
 
@@ -972,7 +982,7 @@ PyObject* py_distill(PyObject*, PyObject* const* p, Py_ssize_t n) {
     void* ws = c.workspace(p[12], &bytes);
     c.no_gradients({p[6]});
     if (!c.ok) return -1;
-    return unlocked([&] { return s.distill(&a, ws, bytes, st); });
+    return c.wrote(unlocked([&] { return s.distill(&a, ws, bytes, st); }), {p[6], p[7], p[8]});
   });
 }
 
@@ -983,7 +993,7 @@ PyObject* py_distill_grad(PyObject*, PyObject* const* p, Py_ssize_t n) {
     const hipStream_t st = c.stream(p[2]);
     caddtree_distill_t a = {};
     if (p[6] == Py_None || p[7] == Py_None || !distill_tensors(c, p[3], p[4], p[5], p[7], p[6], p[8], p[9], p[10], &a)) return -1;
-    return unlocked([&] { return s.grad(&a, st); });
+    return c.wrote(unlocked([&] { return s.grad(&a, st); }), {p[7]});
   });
 }
 

@@ -17,7 +17,9 @@
 Every call checks its tensors, then enqueues kernels on the stream (default: torch's current one) and returns.  Logits are
 bf16, f16 or f32 [B, rows, V] with a unit last stride, in any strides.  include/caddtree.h states what is computed.
 Autograd does not see these calls: ``distill`` writes the logits' gradient itself, and a tensor that requires one, be it the
-logits, a bias, a teacher's logits or a weight, is refused while gradients are recorded.
+logits, a bias, a teacher's logits or a weight, is refused while gradients are recorded.  What a call writes counts as changed in
+place: where a layer saved its output for its backward pass (tanh, softmax), adjusting that output's detached form in place, or
+writing the gradient over it, makes the backward pass raise an error; give the call an output of its own there.
 
 As a plan's calls do, these go to the native binding first, which checks the tensors and calls the library; what it cannot
 vouch for comes back as None and takes the Python checks here, which raise what is wrong.
@@ -53,6 +55,13 @@ def _no_gradient(name: str, t, instead: str) -> None:
     torch = _torch()
     if torch.is_grad_enabled() and isinstance(t, torch.Tensor) and t.requires_grad:
         raise ValueError(f"{name} requires a gradient, which autograd does not carry through this call: {instead}")
+
+
+def _wrote(*tensors) -> None:
+    """Tells autograd what a call wrote (None: not given): a backward pass that saved one of them is refused."""
+    for t in tensors:
+        if t is not None and not t.is_inference():
+            _torch().autograd.graph.increment_version(t)
 
 
 def _no_gradients(**others) -> None:
@@ -137,6 +146,7 @@ def adjust_logits(logits, out=None, *, history=None, history_len=None, repetitio
     if count is not None:
         a.count = _at._array("count", count, i32, (a.B,), device)
     _lib.check(_lib.lib().caddtree_adjust_logits(ctypes.byref(a), _at._stream(stream, device)))
+    _wrote(out)
     return out
 
 
@@ -183,6 +193,7 @@ def verify_tree(logits, token_ids, parent, count, accepted, index, tokens, *, ch
         a.weight = _at._array("weight", weight, torch.float32, (a.B, a.T), device)
     ws, n = _at._workspace(workspace, device)
     _lib.check(_lib.lib().caddtree_verify_tree(ctypes.byref(a), ws, n, _at._stream(stream, device)))
+    _wrote(accepted, index, tokens, weight)
 
 
 def verify_workspace(logits):
@@ -235,6 +246,7 @@ def distill(logits, ids, target, loss, *, grad=None, stats=None, weight=None, te
     a.loss = _at._array("loss", loss, _torch().float32, (a.B, a.T), device)
     ws, n = _at._workspace(workspace, device)
     _lib.check(_lib.lib().caddtree_distill(ctypes.byref(a), ws, n, _at._stream(stream, device)))
+    _wrote(loss, grad, stats)
 
 
 def distill_grad(logits, ids, target, stats, grad=None, *, weight=None, temperature: float = 1.0, tail: bool = False,
@@ -255,6 +267,7 @@ def distill_grad(logits, ids, target, stats, grad=None, *, weight=None, temperat
         raise TypeError("stats must be a torch tensor, got NoneType")
     a = _distill(logits, ids, target, stats, grad, weight, temperature, tail, device)
     _lib.check(_lib.lib().caddtree_distill_grad(ctypes.byref(a), _at._stream(stream, device)))
+    _wrote(grad)
     return grad
 
 
