@@ -469,8 +469,8 @@ typedef struct {
   const void* allowed;          /* u32 words, optional: bit (v % 32) of word v / 32 of row (b, t), which starts at word */
   int64_t allowed_stride_b;     /*   b allowed_stride_b + t allowed_stride_t (strides >= 0; 0: one mask for all) */
   int64_t allowed_stride_t;
-  const int32_t* token_ids;     /* [B, T - 1] each, with a tree (else both NULL): as written by caddtree_build */
-  const int32_t* parent;
+  const int32_t* token_ids;     /* [B, T - 1] each, with a tree (else both NULL): as written by caddtree_build.  A tree of its */
+  const int32_t* parent;        /*   root alone (T = 1) gives two that are not NULL, or no count */
   float fill;                   /* what a token that is not allowed gets, not NaN; 0 stands for -inf.  A plan's calls
                                    take finite logits: the drafter's get a finite one */
 } caddtree_adjust_t;

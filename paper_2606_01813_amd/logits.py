@@ -145,6 +145,8 @@ def adjust_logits(logits, out=None, *, history=None, history_len=None, repetitio
         a.parent = _at._array("parent", parent, i32, (a.B, a.T - 1), device)
     if count is not None:
         a.count = _at._array("count", count, i32, (a.B,), device)
+        if parent is not None and a.T == 1:                # (the root alone: no nodes to count, and no arrays that say a tree)
+            a.count = None
     _lib.check(_lib.lib().caddtree_adjust_logits(ctypes.byref(a), _at._stream(stream, device)))
     _wrote(out)
     return out

@@ -1,0 +1,43 @@
+"""Calls on logits that the other tests do not make."""
+
+import pytest
+import torch
+
+from paper_2606_01813_amd import adjust_logits, verify_tree
+from tests import _logits_ref as ref
+from tests.test_logits_checks import rec  # noqa: F401  (a fixture)
+
+BF, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+I32 = torch.int32
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype", [BF, F16, F32])
+def test_a_tree_of_its_root_alone(dtype, in_place):
+    """cap = 0: count's nodes are none, and the root's row is adjusted as every tree's is."""
+    B, V = 3, 700
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    x = (torch.randn((B, 1, V), generator=gen, device="cuda") * 3).to(dtype)
+    kw = dict(history=torch.randint(V, (B, 40), generator=gen, device="cuda", dtype=I32), repetition=torch.full((B,), 1.5, device="cuda"),
+              frequency=torch.full((B,), 0.25, device="cuda"), token_ids=torch.zeros((B, 0), dtype=I32, device="cuda"),
+              parent=torch.zeros((B, 0), dtype=I32, device="cuda"), count=torch.tensor([0, -3, 7], dtype=I32, device="cuda"))
+    want, tol = ref.adjust(ref.f64(x), dtype, **kw)
+    y = x.clone()
+    out = adjust_logits(y, y if in_place else torch.full_like(x, 9.0), **kw)
+    assert bool((abs(ref.f64(out) - want) <= tol).all())
+    acc, index, tokens = (torch.full(s, 9, dtype=I32, device="cuda") for s in ((B,), (B, 1), (B, 1)))
+    verify_tree(x, kw["token_ids"], kw["parent"], kw["count"], acc, index, tokens)
+    assert acc.tolist() == [1] * B and index.flatten().tolist() == [0] * B
+    assert tokens.flatten().tolist() == x[:, 0].float().argmax(-1).tolist()
+
+
+def test_a_tree_of_its_root_alone_has_no_count(rec):  # noqa: F811
+    """Empty arrays have no address: the library would take the call for one without a tree, whose rows are `count`."""
+    x, none, n = torch.zeros((2, 1, 70), dtype=BF), torch.zeros((2, 0), dtype=I32), torch.zeros(2, dtype=I32)
+    adjust_logits(x, x, token_ids=none, parent=none, count=n)
+    adjust_logits(x, x, count=n)
+    (_, (with_tree, _)), (_, (without, _)) = rec.calls
+    assert n.data_ptr() not in with_tree and n.data_ptr() in without
+    with pytest.raises(TypeError):
+        adjust_logits(x, x, token_ids=none, parent=none, count=n.long())
