@@ -38,6 +38,11 @@ struct Best {
 };
 constexpr uint64_t kNoKey = (uint64_t)0x00800000u << 32;      // (keys of -inf are below)
 
+// A NaN is never chosen, a signalling one neither: outside the mode that a kernel starts in (MODE.IEEE, bit 9 of register 1) the
+// maximum of a number and any NaN is the number.  In it a signalling one makes the maximum a NaN, and the next maximum drops
+// that with all before it; quieting each logit first would be 8 instructions a vector on top of 13.
+__device__ __forceinline__ void numbers_over_nan() { __builtin_amdgcn_s_setreg(1 | 9 << 6, 0); }
+
 // The best of a row's tokens first .. last - 1 (first a multiple of 8) by a workgroup, kU loads in flight a lane.  A lane
 // keeps its largest logit and which kU vectors it was among, the first of equals; the lanes that have the workgroup's
 // largest read theirs again and look for its token: 13 instructions a vector of 8 logits, of which unpacking is 8.
@@ -114,6 +119,7 @@ template <typename E>
 __global__ __launch_bounds__(kChooseThreads) void choose_kernel(VerifyArgs a, Best* parts, int len) {
   __shared__ float s_top[kChooseThreads / kWave];
   __shared__ int s_id;
+  numbers_over_nan();
   const int b = (int)blockIdx.z, t = (int)blockIdx.y, first = (int)blockIdx.x * len;
   if (t > min(max(a.count[b], 0), a.T - 1)) return;
   const Best m = best_of<E, kChooseThreads, 4>(row_of<E>(a.in, b, t), first, min(first + len, a.V), s_top, &s_id);
@@ -130,6 +136,7 @@ __global__ __launch_bounds__(kThreads) void walk_kernel(VerifyArgs a, const Best
   __shared__ int s_child;
   __shared__ uint64_t s_key[kFrom == kParts ? kAllRows : 1]; // of each row
   __shared__ int s_chosen[kFrom == kChosen ? kNodes : 1];
+  numbers_over_nan();
   const int b = (int)blockIdx.x, tid = threadIdx.x;
   const int n = min(max(a.count[b], 0), a.T - 1);
   const int32_t* tok = a.token_ids + (int64_t)b * (a.T - 1);

@@ -41,3 +41,32 @@ def test_a_tree_of_its_root_alone_has_no_count(rec):  # noqa: F811
     assert n.data_ptr() not in with_tree and n.data_ptr() in without
     with pytest.raises(TypeError):
         adjust_logits(x, x, token_ids=none, parent=none, count=n.long())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B,T,V", [(1, 3, 50), (1, 3, 20000), (70, 9, 3000), (40, 15, 70000)])
+@pytest.mark.parametrize("dtype", [BF, F16, F32])
+def test_no_nan_is_chosen_signalling_or_quiet(B, T, V, dtype):
+    """NaNs of every kind, next to the largest logit, before it and after it."""
+    from paper_2606_01813_amd import verify_workspace
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randn((B, T, V), generator=gen, device="cuda").to(dtype)
+    at = torch.randint(V - 2, (B, T), generator=gen, device="cuda") + 1
+    x.scatter_(2, at[..., None], 50.0)
+    bits = {BF: (torch.int16, [0x7f81, -0x7f, 0x7fc0, -0x40, 0x7fbf]), F16: (torch.int16, [0x7c01, -0x3ff, 0x7e00, -0x200, 0x7dff]),
+            F32: (torch.int32, [0x7f800001, -0x7fffff, 0x7fc00000, -0x400000, 0x7fbfffff])}[dtype]
+    nan = torch.tensor(bits[1], dtype=bits[0], device="cuda").view(dtype)
+    assert bool(torch.isnan(nan).all())
+    raw = x.view(bits[0])
+    for i in range(5):
+        raw[:, :, i::11] = bits[1][i]
+    raw.scatter_(2, at[..., None] + 1, bits[1][0])
+    raw.scatter_(2, at[..., None] - 1, bits[1][0])
+    x.scatter_(2, at[..., None], 50.0)
+    none = torch.full((B, T - 1), -1, dtype=I32, device="cuda")
+    tok = torch.zeros((B, T - 1), dtype=I32, device="cuda")
+    count = torch.zeros(B, dtype=I32, device="cuda")
+    for ws in (None, verify_workspace(x)):
+        acc, index, tokens = (torch.full(s, 9, dtype=I32, device="cuda") for s in ((B,), (B, 1), (B, 1)))
+        verify_tree(x, tok, none, count, acc, index, tokens, workspace=ws)
+        assert tokens[:, 0].tolist() == at[:, 0].tolist()
