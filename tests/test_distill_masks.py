@@ -168,3 +168,35 @@ def test_where_the_listed_token_lies_does_not_matter():
     assert float(first) != float(high)
     target = torch.full((n, 1, 1), float(np.log(0.9)), device="cuda")
     _every_form(x, ids, target, 1.0, True, list(range(n)))
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("tau", [2.0 ** -20, 2.0 ** -7, 2.0 ** 20])
+@pytest.mark.parametrize("dtype,V", [(F32, 900), (F32, 8003), (F32, 70001), (BF, 16005), (F16, 8001)])
+def test_the_smallest_and_largest_temperatures(dtype, V, tau, tail):
+    gen, B = _gen(V + 5), 4
+    x = (torch.randn((B, 1, V), generator=gen, device="cuda") * 3).to(dtype)
+    x[1, 0, :600] = -1e4
+    x[2, 0, ::3] = x[2, 0].max()                           # (many at the top)
+    ids, target = _teacher(gen, B, V, 4, tail)
+    x[3, 0, ids[3, 0].long()] = x[3, 0].max() + 1
+    _every_form(x, ids, target, tau, tail, list(range(B)), torch.full((B, 1), min(1.0, tau), device="cuda"))   # (f16 ends at 65504)
+
+
+@pytest.mark.parametrize("with_workspace", [False, True])
+@pytest.mark.parametrize("V", [40, 4001, 16001, 70001, 140001])
+def test_a_listed_nan_or_infinity_spreads_over_its_row(V, with_workspace):
+    gen, B, K = _gen(V + 6), 4, 3
+    x = torch.randn((B, 1, V), generator=gen, device="cuda")
+    ids, target = _teacher(gen, B, V, K, True)
+    at = ids[:, 0, 1].long()
+    x[0, 0, at[0]], x[1, 0, at[1]] = float("nan"), float("inf")
+    x[2] = -float("inf")
+    x[2, 0, at[2]] = float("nan")                          # (and nothing else)
+    x[3, 0, at[3]] = 1e30
+    loss, stats, grad = torch.zeros((B, 1), device="cuda"), torch.zeros((B, 1, 3), device="cuda"), torch.zeros_like(x)
+    for tail in (True, False):
+        distill(x, ids, target, loss, grad=grad, stats=stats, tail=tail, workspace=distill_workspace(x) if with_workspace else None)
+        for g in (grad, distill_grad(x, ids, target, stats, tail=tail)):
+            assert torch.isnan(g[:3]).flatten(1).all(1).tolist() == [True] * 3 and bool(torch.isfinite(g[3]).all())
+        assert torch.isnan(loss[:3, 0]).tolist() == [True] * 3 and bool(torch.isfinite(loss[3]))

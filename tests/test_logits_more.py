@@ -3,7 +3,7 @@
 import pytest
 import torch
 
-from paper_2606_01813_amd import adjust_logits, verify_tree
+from paper_2606_01813_amd import adjust_logits, distill, distill_grad, verify_tree
 from tests import _logits_ref as ref
 from tests.test_logits_checks import rec  # noqa: F401  (a fixture)
 
@@ -70,3 +70,35 @@ def test_no_nan_is_chosen_signalling_or_quiet(B, T, V, dtype):
         acc, index, tokens = (torch.full(s, 9, dtype=I32, device="cuda") for s in ((B,), (B, 1), (B, 1)))
         verify_tree(x, tok, none, count, acc, index, tokens, workspace=ws)
         assert tokens[:, 0].tolist() == at[:, 0].tolist()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("V", [400000, 1 << 20])
+def test_a_graph_of_rows_that_take_much_lds(V):
+    """Past some vocabulary a launch has to say how much LDS it takes, in a captured call too."""
+    B, K = 70, 4
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn((B, 1, V), generator=gen, device="cuda").to(BF)
+    ids = torch.randint(V, (B, 1, K), generator=gen, device="cuda", dtype=I32)
+    target = torch.randn((B, 1, K), generator=gen, device="cuda")
+    loss, stats, grad, grad2 = torch.zeros((B, 1), device="cuda"), torch.zeros((B, 1, 3), device="cuda"), torch.zeros_like(x), torch.zeros_like(x)
+
+    def call():
+        distill(x, ids, target, loss, grad=grad, stats=stats)
+        distill_grad(x, ids, target, stats, grad2)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for _ in range(3):
+        for t in (loss, stats, grad, grad2):
+            t.fill_(9)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in (loss, stats, grad, grad2)]
+        call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, t) for g, t in zip(got, (loss, stats, grad, grad2)))
+        assert bool(torch.isfinite(loss).all()) and bool((loss > 0).all())
