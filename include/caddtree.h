@@ -471,8 +471,9 @@ typedef struct {
   int64_t allowed_stride_t;
   const int32_t* token_ids;     /* [B, T - 1] each, with a tree (else both NULL): as written by caddtree_build.  A tree of its */
   const int32_t* parent;        /*   root alone (T = 1) gives two that are not NULL, or no count */
-  float fill;                   /* what a token that is not allowed gets, not NaN; 0 stands for -inf.  A plan's calls
-                                   take finite logits: the drafter's get a finite one */
+  float fill;                   /* what a token that is not allowed gets, rounded to the logits' type (past its range: an
+                                   infinity), not NaN; 0 stands for -inf.  A plan's calls take finite logits, in BF16 or
+                                   F32: the drafter's get a finite one */
 } caddtree_adjust_t;
 
 /* Penalties for repeated tokens, biases and a grammar's mask.  x = the logit of token v in row (b, t), in fp32:

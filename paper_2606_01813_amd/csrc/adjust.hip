@@ -13,7 +13,8 @@
 //
 // Bound by memory where there are many rows: 1024 rows of 151936 bf16 (histories of up to 2048, 32 biases) in 110 us, 622 MB
 // at 5.7 TB/s, 1032 rows of 100003 f32 in a tree with a mask in 118 us.  64 rows with a mask and histories of up to 8192 in
-// 17 us: a workgroup has to have gone over the history before its first logit, and VALU is 65% active meanwhile.
+// 17 us: a workgroup has to have gone over the history before its first logit, and VALU is 65% active meanwhile.  In place the
+// 1024 rows take 59 us, the 1032 102 and the 64, most of whose tokens are filled one by one, 25.
 
 #include <hip/hip_runtime.h>
 
@@ -59,7 +60,7 @@ struct Penalty {
 };
 
 // A logit, given its token's word.  The quotient is a product with the inverse: two roundings in place of one, and a tenth
-// of the instructions.
+// of the instructions.  (Rounded once, by its remainder: one row 6.4 us instead of 5.6, the 1024 rows 115.5 instead of 110.6.)
 __device__ __forceinline__ float adjusted(float x, uint32_t word, const Penalty& p, const Lds& s, const float* bias) {
   const float c = (float)(word & kCount);
   const float y = fmaf(-p.frequency, c, x * (x > 0.f ? p.inverse : p.repetition)) - p.presence;

@@ -462,12 +462,12 @@ __device__ void no_weight(const DistillArgs& a, int64_t row, typename E::T* g, i
 // A workgroup a row: its loss, and the gradient.  The row's first kKeep vectors a thread stay in registers between the sums
 // and the gradient; what is behind them is read again, the last first, while it may still be in a cache.
 //
-// Bound by memory: 1024 rows of 151936 bf16 (a tenth of weight 0) in 121 us, 594 MB that have to move at 4.9 TB/s, where a
-// copy reaches 5.0.  Of 512 threads 0 / 8 / 14 vectors kept: 157 / 129 / 121 us, and 18 were slower than 14; the whole row in
+// Bound by memory: 1024 rows of 151936 bf16 (a tenth of weight 0) in 121 to 126 us, 594 MB that have to move at 4.7 to 4.9
+// TB/s, where a copy reaches 5.0.  Of 512 threads 0 / 8 / 14 vectors kept: 157 / 129 / 121 us, and 18 were slower than 14; the whole row in
 // 1024 threads' registers: 151 when 14 took 136 (one workgroup a compute unit: nothing loads while it joins).
 // Streaming stores took 154 to 136, streaming loads of the second pass 133 to 123.
 // The loss alone: 2048 such rows in 96 us, 6.2 TB/s of the row's one read; bound by the exponentials' instructions (VALU
-// 80% active).  512 threads with 4 / 6 / 8 / 12 loads a lane 94 / 95 / 96 / 99 us, and for 128 rows 17.7 / 16.9 / 16.4 / 16.6;
+// 85% active).  512 threads with 4 / 6 / 8 / 12 loads a lane 94 / 95 / 96 / 99 us, and for 128 rows 17.7 / 16.9 / 16.4 / 16.6;
 // 256 threads 97 and 22.
 template <typename E, int kThreads, int kKeep, bool kGrad>
 __global__ __launch_bounds__(kThreads, 4) void row_kernel(DistillArgs a) {
@@ -768,7 +768,8 @@ hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
   ps.len = kGradLoads * 256 * kN<E>;
   ps.n = distill_grad_parts(a.V, sizeof(typename E::T));
   const dim3 g = grid_of((int64_t)a.T * ps.n, a.B);
-  // (rows shorter than a part: us with 64 / 128 / 256 threads, 65536 rows of 1024 bf16 99 / 104 / 155, 16384 of 4096 56 / 53 / 59)
+  // (rows shorter than a part: us with 64 / 128 / 256 threads, 65536 rows of 1024 bf16 99 / 104 / 155, 16384 of 4096 56 / 53 / 59;
+  // the first 103 with the sums' reference beside R)
   const int vectors = a.V / kN<E>;
   if (vectors <= 64 * 4) return run(grad_kernel<E, true, 64>, g, 64, bit_bytes(ps.len), stream, a, ps);
   if (vectors <= 128 * 4) return run(grad_kernel<E, true, 128>, g, 128, bit_bytes(ps.len), stream, a, ps);
@@ -779,7 +780,7 @@ hipError_t launch_grad(const DistillArgs& a, hipStream_t stream) {
 
 // A workgroup a compute unit where the rows are fewer than that, a part no shorter than what a workgroup asks for at once.
 // Parts or whole rows, us, of 151936 bf16: 1 row 8.9 / 24.0, 16 rows 10.4 / 25.3, 64 rows 16.1 / 25.6, 128 rows 25.5 / 26.9
-// (their loss alone 17.3 / 16.4); 64 rows of 32000 11.2 / 13.1.  256 or 512 workgroups: 16 rows 11.2 / 12.8, 64 rows
+// (their loss alone 17.3 / 16.4, so the rule ends at 64 for both; nothing between was measured); 64 rows of 32000 11.2 / 13.1.  256 or 512 workgroups: 16 rows 11.2 / 12.8, 64 rows
 // 17.6 / 18.1, 64 rows of 40000 11.6 / 13.4.
 int distill_parts(int64_t rows, int32_t V) {
   if (rows < 1 || rows > 64) return 1;

@@ -96,8 +96,8 @@ def adjust_logits(logits, out=None, *, history=None, history_len=None, repetitio
     A logit x of a token that occurred c > 0 times becomes x / repetition[b] (x repetition[b] if not positive), less
     frequency[b] c and presence[b] (float32 [B] each); bias[b, j] (float32 [B, n]) is added to token bias_ids[b, j]
     (int32); a token whose bit is not set in ``allowed`` (int32 or uint32 words [B, T, ceil(V / 32)], in any strides of
-    its first two dimensions) becomes ``fill``: -inf (0 stands for it too), or for the drafter's logits, of which a plan's
-    calls want finite ones, a finite value.  Ids outside the vocabulary are padding; of a token listed twice the last
+    its first two dimensions) becomes ``fill``: -inf (0 stands for it too, and so does what is past the logits' type, as
+    -1e30 is in f16), or for the drafter's logits, of which a plan's calls want finite ones, a finite value.  Ids outside the vocabulary are padding; of a token listed twice the last
     bias counts.  With ``token_ids`` and ``parent`` (int32 [B, T - 1]) the rows are a tree's, row 0 its root and row i
     node i - 1, and a row's path counts as its history too.  ``count`` (int32 [B]): the rows of each sequence, in a
     tree its n_star; rows past it are left as they are."""
